@@ -406,6 +406,151 @@ int32_t attncache_project(const void *h, const int32_t *seq_len,
                           int32_t normalize, void *workspace,
                           size_t workspace_bytes, void *stream);
 
+/* ---- generation after the prefill ---------------------------------------- */
+
+/*
+ * A paged K/V cache.  Reuse serves the prefill; a program that goes on
+ * generating keeps K and V of the prompt and of every further token, and each
+ * new token attends to all of them.  The cache is two arrays of pages,
+ *
+ *   k_pages, v_pages  [n_pages][heads][page_size][D], consecutive pages
+ *                     page_stride elements apart (at least heads * page_size
+ *                     * D; more where the cache holds further layers, whose
+ *                     heads lie behind these, or K and V in one array).
+ *                     Where a row of D elements is a whole number of 16-byte
+ *                     pieces, page_stride must be one, too (AC_ERR_ALIGN).
+ *
+ * Token j of request b lies in page page_table[b][j / page_size] at place
+ * j % page_size, in all heads; its slot is page * page_size + place.
+ * n_pages * page_size and max_pages * page_size must be below 2^31.  Page
+ * numbers and slots that the kernels read are checked: what is outside
+ * [0, n_pages) or [0, n_pages * page_size) is never followed.
+ *
+ * All pointers of these calls are to be memory of the current device
+ * (AC_ERR_MEMSPACE for another device's, too).
+ */
+
+/*
+ * The plan of a step: which pages the requests of a batch take and give back,
+ * and where their new tokens go, from the requests' lengths, on the device.
+ *
+ *   seq_len    DEVICE [B] int32: tokens of each request that are in the cache
+ *              (clamped to [0, max_pages * page_size]).
+ *   new_len    DEVICE [B] int32: tokens to be added now (at most S are), 0 for
+ *              none.  Negative: the request has ended and its pages go back.
+ *   free_pages DEVICE [n_pages] int32: a ring of the pages that nobody has;
+ *              free_state (DEVICE [2] int32) = index of the first, number.
+ *   page_table DEVICE [B][max_pages] int32, in and out: entries below
+ *              ceil(seq_len / page_size) are read, the new pages' entries
+ *              written, all others left as they are.
+ *   seq_len_out  DEVICE [B] int32 out: tokens after this step (0 for ended
+ *              requests): what attention_paged takes once the rows are there.
+ *   added      DEVICE [B] int32 out: tokens taken in, min(new_len, S) or 0.
+ *   free_state_out  DEVICE [2] int32 out.
+ *   slot       DEVICE [B][S] int32 out: slot of new token t, -1 from added[b]
+ *              on: what attncache_page_append takes.
+ *
+ * Requests are served in their order.  One that needs more pages than the
+ * ring has left takes nothing (added 0), and so do all after it that need a
+ * page; those whose last page has room are served.  One that would outgrow
+ * its max_pages takes nothing either.  Pages given back are the ring's for the
+ * next call; they go behind its last one in order of request and place.
+ * The outputs seq_len_out, added, free_state_out may be seq_len, new_len,
+ * free_state (a captured step then continues from where the last replay
+ * ended); other arrays must not overlap.  B <= 2^22, S <= 2^26,
+ * B * max_pages < 2^31.  One launch, or two for many slots.
+ */
+int32_t attncache_page_plan(const int32_t *seq_len, const int32_t *new_len,
+                            const int32_t *free_state, int32_t *free_pages,
+                            int32_t *page_table, int32_t *seq_len_out,
+                            int32_t *added, int32_t *free_state_out,
+                            int32_t *slot, int32_t B, int32_t S,
+                            int32_t max_pages, int32_t page_size,
+                            int32_t n_pages, void *stream);
+
+/*
+ * Rows of K and V to their places: row t of head h of item b goes to slot
+ * slot[b][t] of k_pages and v_pages; rows whose slot is outside
+ * [0, n_pages * page_size), such as -1, are not read.
+ *
+ *   K, V       DEVICE [B][H][S][D] of dtype (AC_BF16: D 64 or 128; AC_F32:
+ *              D <= 256), as attention_exact and attncache_insert take them
+ *              (layers fold into heads); S = 1 for a generated token.
+ *   slot       DEVICE [B][S] int32.  Slots of one call must be distinct
+ *              (equal slots race).
+ *   k_pages, v_pages  DEVICE, as above, with H heads.  Other places keep
+ *              what they hold.
+ * B * H * S below 2^31 - 4096.
+ */
+int32_t attncache_page_append(const void *K, const void *V,
+                              const int32_t *slot, void *k_pages,
+                              void *v_pages, int32_t B, int32_t H, int32_t S,
+                              int32_t D, int32_t n_pages, int32_t page_size,
+                              int64_t page_stride, int32_t dtype,
+                              void *stream);
+
+/*
+ * Attention of one new token of each request to all tokens of its pages:
+ * O[b][h] = softmax(scale * Q[b][h] K^T) V over the keys j < seq_len[b] of
+ * K/V head h / (Hq / Hkv).
+ *
+ *   Q, O       DEVICE [B][Hq][D] of dtype (AC_BF16: D 64 or 128; AC_F32:
+ *              D <= 256).
+ *   page_table DEVICE [B][max_pages] int32.  Keys whose page is outside
+ *              [0, n_pages) are hidden.
+ *   seq_len    DEVICE [B] int32, clamped to [0, max_pages * page_size].  The
+ *              new token's own K and V row is one of these keys if it has
+ *              been appended before.  Places behind seq_len may hold anything.
+ *              A request without a visible key gets zeros.
+ *   scale      0 selects 1/sqrt(D).
+ *   workspace  DEVICE, attention_paged_workspace_bytes(...) bytes (0 for sizes
+ *              that are not positive), 16-byte aligned; scratch, and written
+ *              by a call before it is read.  Its size depends on neither B nor
+ *              the lengths.  Calls that may overlap in time need one each.
+ *
+ * fp32 statistics and sums; bf16 weights are rounded once before the product
+ * with V and the result once.  Two launches; deterministic.
+ * B * Hkv * ceil(Hq / Hkv / 16) * ceil(max_pages * page_size / 16) below 2^31.
+ */
+size_t attention_paged_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv,
+                                       int32_t D);
+int32_t attention_paged(const void *Q, const void *k_pages,
+                        const void *v_pages, const int32_t *page_table,
+                        const int32_t *seq_len, void *O, int32_t B,
+                        int32_t Hq, int32_t Hkv, int32_t D, int32_t n_pages,
+                        int32_t page_size, int32_t max_pages,
+                        int64_t page_stride, int32_t dtype, float scale,
+                        void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Attention to another sequence's states (a decoder's to its encoder's):
+ * O = softmax(scale * Q K^T) V with Sq query rows and Sk keys, any lengths,
+ * nothing causal.
+ *
+ *   Q, O       DEVICE [B][Hq][Sq][D]; K, V DEVICE [B][Hkv][Sk][D]; all of
+ *              dtype (AC_BF16: D 64 or 128; AC_F32: D <= 256).
+ *   row_sel    NULL or DEVICE [B] int32: items with row_sel[b] >= 0 are
+ *              skipped and their rows of O not written.
+ *   key_len    NULL or DEVICE [B] int32: states of item b that are real,
+ *              clamped to [0, Sk]; the others may hold anything.  An item of
+ *              length 0 gets zeros.
+ *   scale      0 selects 1/sqrt(D).
+ *   workspace  DEVICE, attention_cross_workspace_bytes(...) bytes, as for
+ *              attention_paged; may be NULL where that is 0 (calls of many
+ *              bf16 rows, and sizes that attention_cross refuses).
+ *
+ * Arithmetic as in attention_paged.  Hq / Hkv * Sq <= 2^24, B * Hkv <= 2^28;
+ * AC_F32: B * Hkv * ceil(Hq / Hkv * Sq / 16) * ceil(Sk / 16) below 2^31.
+ */
+size_t attention_cross_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv,
+                                       int32_t Sq, int32_t Sk, int32_t D,
+                                       int32_t dtype);
+int32_t attention_cross(const void *Q, const void *K, const void *V, void *O,
+                        const int32_t *row_sel, const int32_t *key_len,
+                        int32_t B, int32_t Hq, int32_t Hkv, int32_t Sq,
+                        int32_t Sk, int32_t D, int32_t dtype, float scale,
+                        void *workspace, size_t workspace_bytes, void *stream);
+
 /*
  * Switches the per-call memory-space checks of pointers on (non-zero, the
  * default) or off for the whole process; returns the previous setting.

@@ -28,7 +28,9 @@ SYMBOLS = ["attncache_workspace_bytes", "attncache_map_entry_bytes", "attncache_
            "attncache_build_db", "attncache_destroy_db",
            "attncache_search", "attncache_search_static", "attncache_apply", "attention_exact", "attncache_insert",
            "attncache_cache_stats", "attncache_cache_reset",
-           "attncache_project_workspace_bytes", "attncache_project", "attncache_status_string",
+           "attncache_project_workspace_bytes", "attncache_project",
+           "attncache_page_plan", "attncache_page_append", "attention_paged_workspace_bytes", "attention_paged",
+           "attention_cross_workspace_bytes", "attention_cross", "attncache_status_string",
            "attncache_last_hip_error", "attncache_version", "attncache_set_pointer_checks"]
 
 
@@ -92,6 +94,19 @@ def lib():
         L.attncache_project_workspace_bytes.argtypes = [i32, i32, i32, i32]
         L.attncache_project.restype = i32
         L.attncache_project.argtypes = [vp] * 7 + [i32] * 8 + [vp, sz, vp]
+        i64 = ctypes.c_int64
+        L.attncache_page_plan.restype = i32
+        L.attncache_page_plan.argtypes = [vp] * 9 + [i32] * 5 + [vp]
+        L.attncache_page_append.restype = i32
+        L.attncache_page_append.argtypes = [vp] * 5 + [i32] * 6 + [i64, i32, vp]
+        L.attention_paged_workspace_bytes.restype = sz
+        L.attention_paged_workspace_bytes.argtypes = [i32] * 4
+        L.attention_paged.restype = i32
+        L.attention_paged.argtypes = [vp] * 6 + [i32] * 7 + [i64, i32, f32, vp, sz, vp]
+        L.attention_cross_workspace_bytes.restype = sz
+        L.attention_cross_workspace_bytes.argtypes = [i32] * 7
+        L.attention_cross.restype = i32
+        L.attention_cross.argtypes = [vp] * 6 + [i32] * 7 + [f32, vp, sz, vp]
         L.attncache_status_string.restype = ctypes.c_char_p
         L.attncache_status_string.argtypes = [i32]
         L.attncache_last_hip_error.restype = i32
@@ -397,3 +412,123 @@ def attncache_project(h: torch.Tensor, W1: torch.Tensor, b1: Optional[torch.Tens
                                    _DTYPE_CODE[h.dtype], _DTYPE_CODE[feat.dtype], int(normalize),
                                    wp, workspace.numel() * workspace.element_size(),
                                    _stream(stream)), "attncache_project")
+
+
+def attncache_page_plan(seq_len: torch.Tensor, new_len: torch.Tensor, free_state: torch.Tensor,
+                        free_pages: torch.Tensor, page_table: torch.Tensor, seq_len_out: torch.Tensor,
+                        added: torch.Tensor, free_state_out: torch.Tensor, slot: torch.Tensor, *,
+                        page_size: int, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """All int32: seq_len, new_len, seq_len_out, added [B]; free_state, free_state_out [2]; free_pages [n_pages];
+    page_table [B,max_pages]; slot [B,S].  The outputs may be the inputs of the same meaning."""
+    if page_table.dim() != 2 or slot.dim() != 2 or free_pages.dim() != 1:
+        raise ValueError("page_table must be [B,max_pages], slot [B,S] and free_pages [n_pages]")
+    i32 = torch.int32
+    (B, max_pages), S, n = page_table.shape, slot.shape[1], free_pages.shape[0]
+    lp = _dev(seq_len, "seq_len", i32, (B,))
+    np_ = _dev(new_len, "new_len", i32, (B,))
+    fs = _dev(free_state, "free_state", i32, (2,))
+    fp = _dev(free_pages, "free_pages", i32, (n,))
+    tp = _dev(page_table, "page_table", i32, (B, max_pages))
+    lo = _dev(seq_len_out, "seq_len_out", i32, (B,))
+    ap = _dev(added, "added", i32, (B,))
+    fo = _dev(free_state_out, "free_state_out", i32, (2,))
+    sp = _dev(slot, "slot", i32, (B, S))
+    _check(lib().attncache_page_plan(lp, np_, fs, fp, tp, lo, ap, fo, sp, B, S, max_pages, page_size, n,
+                                     _stream(stream)), "attncache_page_plan")
+
+
+def _pages(k_pages: torch.Tensor, v_pages: torch.Tensor, dtype, heads: int, D: int):
+    """Addresses, page count, page size and page stride of [n,heads,page,D] arrays whose pages may lie further apart."""
+    if k_pages.dim() != 4 or tuple(k_pages.shape) != tuple(v_pages.shape) or k_pages.shape[1] != heads or k_pages.shape[3] != D:
+        raise ValueError(f"k_pages and v_pages must be [n_pages,{heads},page_size,{D}], have "
+                         f"{tuple(k_pages.shape)} and {tuple(v_pages.shape)}")
+    n, _, page, _ = k_pages.shape
+    dense = heads * page * D
+    stride = dense
+    if not (k_pages.is_contiguous() and v_pages.is_contiguous()):
+        stride = k_pages.stride(0) if n > 1 else dense
+        # (the stride of a dimension of one element says nothing)
+        inner = all(t.shape[d] == 1 or t.stride(d) == w for t in (k_pages, v_pages)
+                    for d, w in ((1, page * D), (2, D), (3, 1)))
+        if not inner or stride < dense or (n > 1 and v_pages.stride(0) != stride):
+            raise ValueError("k_pages and v_pages must be contiguous within a page and have one page stride")
+    for t, name in ((k_pages, "k_pages"), (v_pages, "v_pages")):
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be a CUDA tensor")
+        if t.dtype != dtype:
+            raise ValueError(f"{name} must have dtype {dtype}, has {t.dtype}")
+    return k_pages.data_ptr(), v_pages.data_ptr(), n, page, stride
+
+
+def attncache_page_append(K: torch.Tensor, V: torch.Tensor, slot: torch.Tensor, k_pages: torch.Tensor,
+                          v_pages: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """K,V [B,H,S,D] bf16 or f32; slot [B,S] int32; k_pages,v_pages [n_pages,H,page_size,D], whose pages may lie further
+    apart than their size."""
+    if K.dim() != 4:
+        raise ValueError("K and V must be [B,H,S,D]")
+    B, H, S, D = K.shape
+    if K.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("unsupported dtype")
+    kp = _dev(K, "K")
+    vp = _dev(V, "V", K.dtype, (B, H, S, D))
+    sp = _dev(slot, "slot", torch.int32, (B, S))
+    kc, vc, n, page, stride = _pages(k_pages, v_pages, K.dtype, H, D)
+    _check(lib().attncache_page_append(kp, vp, sp, kc, vc, B, H, S, D, n, page, stride, _DTYPE_CODE[K.dtype],
+                                       _stream(stream)), "attncache_page_append")
+
+
+def attention_paged_workspace_bytes(B: int, Hq: int, Hkv: int, D: int) -> int:
+    return int(lib().attention_paged_workspace_bytes(B, Hq, Hkv, D))
+
+
+def attention_paged(Q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor,
+                    seq_len: torch.Tensor, O: torch.Tensor, workspace: torch.Tensor, *, scale: float = 0.0,
+                    stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Q,O [B,Hq,D]; k_pages,v_pages [n_pages,Hkv,page_size,D], whose pages may lie further apart than their size; bf16 or
+    f32; page_table [B,max_pages], seq_len [B] int32."""
+    if Q.dim() != 3 or k_pages.dim() != 4 or page_table.dim() != 2:
+        raise ValueError("Q must be [B,Hq,D], k_pages and v_pages [n_pages,Hkv,page_size,D], page_table [B,max_pages]")
+    B, Hq, D = Q.shape
+    Hkv, max_pages = k_pages.shape[1], page_table.shape[1]
+    if Q.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("unsupported dtype")
+    qp = _dev(Q, "Q")
+    op = _dev(O, "O", Q.dtype, (B, Hq, D))
+    tp = _dev(page_table, "page_table", torch.int32, (B, max_pages))
+    lp = _dev(seq_len, "seq_len", torch.int32, (B,))
+    kc, vc, n, page, stride = _pages(k_pages, v_pages, Q.dtype, Hkv, D)
+    wp = _dev(workspace, "workspace")
+    _check(lib().attention_paged(qp, kc, vc, tp, lp, op, B, Hq, Hkv, D, n, page, max_pages, stride,
+                                 _DTYPE_CODE[Q.dtype], float(scale), wp,
+                                 workspace.numel() * workspace.element_size(), _stream(stream)), "attention_paged")
+
+
+def attention_cross_workspace_bytes(B: int, Hq: int, Hkv: int, Sq: int, Sk: int, D: int,
+                                    dtype: Optional[torch.dtype] = None) -> int:
+    """Without ``dtype``: enough for either type."""
+    codes = (AC_BF16, AC_F32) if dtype is None else (_DTYPE_CODE[dtype],)
+    return max(int(lib().attention_cross_workspace_bytes(B, Hq, Hkv, Sq, Sk, D, c)) for c in codes)
+
+
+def attention_cross(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, O: torch.Tensor,
+                    workspace: Optional[torch.Tensor] = None, *, scale: float = 0.0,
+                    row_sel: Optional[torch.Tensor] = None, key_len: Optional[torch.Tensor] = None,
+                    stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Q,O [B,Hq,Sq,D]; K,V [B,Hkv,Sk,D]; bf16 or f32; row_sel, key_len [B] int32.  The workspace may be left out where
+    attention_cross_workspace_bytes says 0."""
+    if Q.dim() != 4 or K.dim() != 4:
+        raise ValueError("Q must be [B,Hq,Sq,D] and K,V [B,Hkv,Sk,D]")
+    B, Hq, Sq, D = Q.shape
+    Hkv, Sk = K.shape[1], K.shape[2]
+    if Q.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("unsupported dtype")
+    qp = _dev(Q, "Q")
+    kp = _dev(K, "K", Q.dtype, (B, Hkv, Sk, D))
+    vp = _dev(V, "V", Q.dtype, (B, Hkv, Sk, D))
+    op = _dev(O, "O", Q.dtype, (B, Hq, Sq, D))
+    rp = None if row_sel is None else _dev(row_sel, "row_sel", torch.int32, (B,))
+    lp = None if key_len is None else _dev(key_len, "key_len", torch.int32, (B,))
+    wp, w_bytes = (None, 0) if workspace is None else (
+        _dev(workspace, "workspace"), workspace.numel() * workspace.element_size())
+    _check(lib().attention_cross(qp, kp, vp, op, rp, lp, B, Hq, Hkv, Sq, Sk, D, _DTYPE_CODE[Q.dtype], float(scale),
+                                 wp, w_bytes, _stream(stream)), "attention_cross")

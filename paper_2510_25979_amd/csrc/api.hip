@@ -15,6 +15,7 @@
 
 #include "../../include/attncache.h"
 #include "launch.hpp"
+#include "serve.h"
 
 namespace {
 
@@ -61,6 +62,23 @@ bool may_query(hipStream_t stream) {
 int32_t all_device(std::initializer_list<const void*> ptrs) {
   for (const void* p : ptrs)
     if (p && memspace(p) != 0) return AC_ERR_MEMSPACE;
+  return AC_OK;
+}
+
+// The same, and on the device that is current: where the kernel will run.
+int32_t all_on_current_device(std::initializer_list<const void*> ptrs) {
+  int dev = -1;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return hip_fail(e);
+  for (const void* p : ptrs) {
+    if (!p) continue;
+    hipPointerAttribute_t attr;
+    if (hipPointerGetAttributes(&attr, p) != hipSuccess) {
+      (void)hipGetLastError();
+      return AC_ERR_MEMSPACE;
+    }
+    if (attr.type != hipMemoryTypeManaged && (attr.type != hipMemoryTypeDevice || attr.device != dev)) return AC_ERR_MEMSPACE;
+  }
   return AC_OK;
 }
 
@@ -114,6 +132,24 @@ int32_t check_desc(const attncache_db_desc* d) {
     return AC_ERR_DTYPE;
   }
   if (d->map_layout != AC_LAYOUT_DENSE && d->map_layout != AC_LAYOUT_PACKED) return AC_ERR_DTYPE;
+  return AC_OK;
+}
+
+// Element type and head dimension of the attention entry points.
+int32_t check_head(int32_t D, int32_t dtype) {
+  if (dtype == AC_BF16) return D == 64 || D == 128 ? AC_OK : AC_ERR_SHAPE;
+  if (dtype == AC_F32) return D >= 1 && D <= 256 ? AC_OK : AC_ERR_SHAPE;
+  return AC_ERR_DTYPE;
+}
+
+// Pages [n_pages][heads][page_size][D], page_stride elements apart.  Rows of whole 16-byte pieces are read as such.
+int32_t check_pages(int32_t heads, int32_t D, int32_t n_pages, int32_t page_size, int64_t page_stride, int32_t dtype) {
+  if (n_pages < 1 || page_size < 1 || (int64_t)n_pages * page_size > 0x7fffffffLL) return AC_ERR_SHAPE;
+  const int64_t page = (int64_t)heads * D;   // < 2^39
+  if (page > INT64_MAX / page_size / 8 || page_stride < page * page_size) return AC_ERR_SHAPE;
+  if (page_stride > INT64_MAX / n_pages / 8) return AC_ERR_SHAPE;
+  const int64_t esz = (int64_t)elt_size(dtype);
+  if (D * esz % 16 == 0 && page_stride * esz % 16 != 0) return AC_ERR_ALIGN;
   return AC_OK;
 }
 
@@ -581,6 +617,144 @@ int32_t attncache_project(const void* h, const int32_t* seq_len, const float* W1
   p.h_is_f32 = h_dtype == AC_F32; p.feat_is_f16 = feat_dtype == AC_F16;
   p.normalize = normalize != 0;
   hipError_t e = ac::launch_project(p, reinterpret_cast<hipStream_t>(stream));
+  return e == hipSuccess ? AC_OK : hip_fail(e);
+}
+
+int32_t attncache_page_plan(const int32_t* seq_len, const int32_t* new_len, const int32_t* free_state,
+                            int32_t* free_pages, int32_t* page_table, int32_t* seq_len_out,
+                            int32_t* added, int32_t* free_state_out, int32_t* slot, int32_t B,
+                            int32_t S, int32_t max_pages, int32_t page_size, int32_t n_pages,
+                            void* stream) {
+  if (B < 0 || S < 1 || max_pages < 1 || page_size < 1 || n_pages < 1) return AC_ERR_SHAPE;
+  if ((int64_t)n_pages * page_size > 0x7fffffffLL || (int64_t)max_pages * page_size > 0x7fffffffLL)
+    return AC_ERR_SHAPE;
+  // what the requests need and give back is added up in 32 bits; a workgroup's slots are numbered in 31
+  if ((int64_t)B * max_pages > 0x7fffffffLL || S > (1 << 26) || B > (1 << 22)) return AC_ERR_SHAPE;
+  if (B == 0) return AC_OK;
+  if (!seq_len || !new_len || !free_state || !free_pages || !page_table || !seq_len_out || !added ||
+      !free_state_out || !slot)
+    return AC_ERR_NULL;
+  if (may_query(reinterpret_cast<hipStream_t>(stream))) {
+    const int32_t rc = all_on_current_device({seq_len, new_len, free_state, free_pages, page_table, seq_len_out,
+                                              added, free_state_out, slot});
+    if (rc != AC_OK) return rc;
+  }
+  ac::PlanLaunch p;
+  p.seq_len = seq_len; p.new_len = new_len; p.free_state = free_state;
+  p.free_pages = free_pages; p.page_table = page_table;
+  p.seq_len_out = seq_len_out; p.added = added; p.free_state_out = free_state_out; p.slot = slot;
+  p.B = B; p.S = S; p.max_pages = max_pages; p.page_size = page_size; p.n_pages = n_pages;
+  const hipError_t e = ac::launch_plan(p, reinterpret_cast<hipStream_t>(stream));
+  return e == hipSuccess ? AC_OK : hip_fail(e);
+}
+
+int32_t attncache_page_append(const void* K, const void* V, const int32_t* slot, void* k_pages,
+                              void* v_pages, int32_t B, int32_t H, int32_t S, int32_t D,
+                              int32_t n_pages, int32_t page_size, int64_t page_stride,
+                              int32_t dtype, void* stream) {
+  if (B < 0 || H < 1 || S < 1 || D < 1) return AC_ERR_SHAPE;
+  int32_t rc = check_head(D, dtype);
+  if (rc != AC_OK) return rc;
+  rc = check_pages(H, D, n_pages, page_size, page_stride, dtype);
+  if (rc != AC_OK) return rc;
+  if ((double)B * H * S > 2147483647.0 - 4096) return AC_ERR_SHAPE;   // rows are numbered in 31 bits
+  if (B == 0) return AC_OK;
+  if (!K || !V || !slot || !k_pages || !v_pages) return AC_ERR_NULL;
+  if (!aligned16(K) || !aligned16(V) || !aligned16(k_pages) || !aligned16(v_pages)) return AC_ERR_ALIGN;
+  if (may_query(reinterpret_cast<hipStream_t>(stream))) {
+    rc = all_on_current_device({K, V, slot, k_pages, v_pages});
+    if (rc != AC_OK) return rc;
+  }
+  ac::AppendLaunch p;
+  p.K = K; p.V = V; p.slot = slot; p.k_pages = k_pages; p.v_pages = v_pages;
+  p.B = B; p.H = H; p.S = S; p.D = D; p.n_pages = n_pages; p.page_size = page_size;
+  p.elt = (int32_t)elt_size(dtype); p.page_stride = page_stride;
+  const hipError_t e = ac::launch_append(p, reinterpret_cast<hipStream_t>(stream));
+  return e == hipSuccess ? AC_OK : hip_fail(e);
+}
+
+size_t attention_paged_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t D) {
+  if (B < 1 || Hq < 1 || Hkv < 1 || D < 1 || Hq % Hkv != 0) return 0;
+  return ac::decode_workspace_bytes(Hq / Hkv, D);
+}
+
+int32_t attention_paged(const void* Q, const void* k_pages, const void* v_pages,
+                        const int32_t* page_table, const int32_t* seq_len, void* O, int32_t B,
+                        int32_t Hq, int32_t Hkv, int32_t D, int32_t n_pages, int32_t page_size,
+                        int32_t max_pages, int64_t page_stride, int32_t dtype, float scale,
+                        void* workspace, size_t workspace_bytes, void* stream) {
+  if (B < 0 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || max_pages < 1) return AC_ERR_SHAPE;
+  int32_t rc = check_head(D, dtype);
+  if (rc != AC_OK) return rc;
+  rc = check_pages(Hkv, D, n_pages, page_size, page_stride, dtype);
+  if (rc != AC_OK) return rc;
+  const int64_t most = (int64_t)max_pages * page_size;
+  if (most > 0x7fffffffLL || !ac::decode_fits(B, Hkv, Hq / Hkv, most)) return AC_ERR_SHAPE;
+  if (!(scale >= 0.f)) return AC_ERR_SHAPE;
+  if (B == 0) return AC_OK;
+  if (!Q || !k_pages || !v_pages || !page_table || !seq_len || !O || !workspace) return AC_ERR_NULL;
+  if (!aligned16(Q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(O) || !aligned16(workspace))
+    return AC_ERR_ALIGN;
+  if (workspace_bytes < ac::decode_workspace_bytes(Hq / Hkv, D)) return AC_ERR_WORKSPACE;
+  if (may_query(reinterpret_cast<hipStream_t>(stream))) {
+    rc = all_on_current_device({Q, k_pages, v_pages, page_table, seq_len, O, workspace});
+    if (rc != AC_OK) return rc;
+  }
+  ac::DecodeLaunch p;
+  p.Q = Q; p.K = k_pages; p.V = v_pages; p.O = O;
+  p.table = page_table; p.len = seq_len; p.row_sel = nullptr;
+  p.B = B; p.Hkv = Hkv; p.R = Hq / Hkv; p.D = D; p.Sk = (int32_t)most; p.is_f32 = dtype == AC_F32;
+  p.n_pages = n_pages; p.page_size = page_size; p.max_pages = max_pages; p.page_stride = page_stride;
+  p.scale = scale; p.ws = workspace;
+  const hipError_t e = ac::launch_decode(p, reinterpret_cast<hipStream_t>(stream));
+  return e == hipSuccess ? AC_OK : hip_fail(e);
+}
+
+namespace {
+// sizes of a cross attention, and its rows of one K/V head
+int32_t check_cross(int32_t B, int32_t Hq, int32_t Hkv, int32_t Sq, int32_t Sk, int32_t D, int32_t dtype, int32_t* R) {
+  if (B < 0 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || Sq < 1 || Sk < 1) return AC_ERR_SHAPE;
+  const int32_t rc = check_head(D, dtype);
+  if (rc != AC_OK) return rc;
+  const int64_t rows = (int64_t)(Hq / Hkv) * Sq;
+  if (rows > (1 << 24) || (int64_t)B * Hkv > (1 << 28)) return AC_ERR_SHAPE;
+  if (dtype == AC_F32 && !ac::decode_fits(B, Hkv, rows, Sk)) return AC_ERR_SHAPE;
+  *R = (int32_t)rows;
+  return AC_OK;
+}
+}  // namespace
+
+size_t attention_cross_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t Sq, int32_t Sk, int32_t D,
+                                       int32_t dtype) {
+  int32_t R = 0;
+  if (B < 1 || check_cross(B, Hq, Hkv, Sq, Sk, D, dtype, &R) != AC_OK) return 0;
+  return ac::cross_workspace_bytes(B, Hkv, R, Sk, D, dtype == AC_F32);
+}
+
+int32_t attention_cross(const void* Q, const void* K, const void* V, void* O, const int32_t* row_sel,
+                        const int32_t* key_len, int32_t B, int32_t Hq, int32_t Hkv, int32_t Sq,
+                        int32_t Sk, int32_t D, int32_t dtype, float scale, void* workspace,
+                        size_t workspace_bytes, void* stream) {
+  int32_t R = 0;
+  int32_t rc = check_cross(B, Hq, Hkv, Sq, Sk, D, dtype, &R);
+  if (rc != AC_OK) return rc;
+  if (!(scale >= 0.f)) return AC_ERR_SHAPE;
+  if (B == 0) return AC_OK;
+  const size_t need = ac::cross_workspace_bytes(B, Hkv, R, Sk, D, dtype == AC_F32);
+  if (!Q || !K || !V || !O || (need > 0 && !workspace)) return AC_ERR_NULL;
+  if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(O) || !aligned16(workspace))
+    return AC_ERR_ALIGN;
+  if (workspace_bytes < need) return AC_ERR_WORKSPACE;
+  if (may_query(reinterpret_cast<hipStream_t>(stream))) {
+    rc = all_on_current_device({Q, K, V, O, row_sel, key_len, need > 0 ? workspace : nullptr});
+    if (rc != AC_OK) return rc;
+  }
+  ac::DecodeLaunch p;
+  p.Q = Q; p.K = K; p.V = V; p.O = O; p.table = nullptr; p.len = key_len; p.row_sel = row_sel;
+  p.B = B; p.Hkv = Hkv; p.R = R; p.D = D; p.Sk = Sk; p.is_f32 = dtype == AC_F32;
+  p.n_pages = 1; p.page_size = 1; p.max_pages = 1; p.page_stride = 0;
+  p.scale = scale; p.ws = workspace;
+  const hipError_t e = ac::launch_cross(p, reinterpret_cast<hipStream_t>(stream));
   return e == hipSuccess ? AC_OK : hip_fail(e);
 }
 

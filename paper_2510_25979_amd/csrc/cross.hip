@@ -1,0 +1,280 @@
+// Attention of many rows to the states of another sequence: O = softmax(scale Q K^T) V with Sq rows and Sk keys, bf16.
+// Nothing is causal, so the g Sq rows of the heads that share K and V are alike: one run of R rows, which lie side by side.
+//
+// A workgroup owns 128 of these rows, a wave 32, and walks the keys in chunks of 64 that are copied from memory straight into
+// one of two LDS stages (the next chunk under way while this one is multiplied, one barrier a chunk).  Both products are
+// formed transposed (S^T = K Q^T, O^T = V^T P^T), so that a lane holds scores of one row, and the weights go from the first
+// product to the second without leaving their registers.  4 Sk D flop a row against 4 Sk D / 128 bytes: the matrix cores and, more
+// so, the exponentials bound it.  Both blocks of a chunk take a softmax step of their own, in an order that lets matrix and vector
+// work of a wave overlap.
+#include "common.hpp"
+#include "serve.h"
+
+namespace ac {
+
+constexpr int kCrossChunk = 64;
+constexpr int kCrossRows = 128;        // rows of a workgroup
+constexpr float kCrossSlack = 8.0f;    // the reference point of a row moves when a score has outgrown it by 2^8
+
+struct CrossArgs {
+  const void *Q, *K, *V;
+  void* O;
+  const int32_t *len, *row_sel;
+  int32_t Hkv, R, Sk, first, tiles, per;   // first: of the launch's (item, K/V head) tiles; per: workgroups of a tile
+  float scale_log2e;
+};
+
+template <int D>
+__global__ __launch_bounds__(kThreads, 2) void cross_bf16_kernel(const CrossArgs a) {
+  constexpr int PPR = D / 8;                              // 16-byte pieces of a row
+  constexpr int NCOPY = kCrossChunk * PPR / kWave / 4;    // copy instructions of a wave, tensor and chunk
+  __shared__ __attribute__((aligned(16))) bf16_t kb0[kCrossChunk * D];
+  __shared__ __attribute__((aligned(16))) bf16_t vb0[kCrossChunk * D];
+  __shared__ __attribute__((aligned(16))) bf16_t kb1[kCrossChunk * D];
+  __shared__ __attribute__((aligned(16))) bf16_t vb1[kCrossChunk * D];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int il = lane & 31, kh = lane >> 5;
+  // workgroups with ids equal mod 8 (one XCD) share K and V in its L2
+  const int slot = blockIdx.x >> 3, u = a.first + slot / a.per * 8 + (blockIdx.x & 7);
+  if (u >= a.tiles) return;
+  const int b = u / a.Hkv;
+  if (a.row_sel && a.row_sel[b] >= 0) return;
+  const int keys = a.len ? min(max(a.len[b], 0), a.Sk) : a.Sk;
+  const int r0 = slot % a.per * kCrossRows + kRowsPerWave * wave, rows = min(kRowsPerWave, a.R - r0);
+  bf16_t* O = reinterpret_cast<bf16_t*>(a.O) + ((size_t)u * a.R + r0) * D;
+  if (keys == 0) {   // nothing to attend to: zeros
+    for (int p = lane; p < rows * PPR; p += kWave) reinterpret_cast<u32x4*>(O)[p] = u32x4{0, 0, 0, 0};
+    return;
+  }
+  const bf16_t* Ksrc = reinterpret_cast<const bf16_t*>(a.K) + (size_t)u * a.Sk * D;
+  const bf16_t* Vsrc = reinterpret_cast<const bf16_t*>(a.V) + (size_t)u * a.Sk * D;
+  // (the scale through a vector instruction: straight from a scalar load it makes the compiler wait for all LDS reads)
+  const float scale_log2e = __builtin_bit_cast(
+      float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, a.scale_log2e) + (lane & 0)));
+
+  // Copies: instruction i of this wave fills LDS slots [64 (wave + 4 i), ...), slot = row * PPR + position; a lane picks the
+  // piece of its row that belongs there.  From one instruction to the next the row grows by 256 / PPR, which leaves the
+  // permutations as they are.
+  const int slot0 = kWave * wave + lane, crow = slot0 / PPR, cpos = slot0 % PPR;
+  const int koff0 = crow * D + 8 * (cpos ^ k_piece_swizzle<D>(crow)), voff0 = crow * D + 8 * (cpos ^ v_piece_swizzle<D>(crow));
+  auto copy = [&](bf16_t* kb, bf16_t* vb, int c) {
+    const int there = keys - c * kCrossChunk;
+    const bf16_t* ks = Ksrc + (size_t)c * kCrossChunk * D;
+    const bf16_t* vs = Vsrc + (size_t)c * kCrossChunk * D;
+    if (there >= kCrossChunk) {
+#pragma unroll
+      for (int i = 0; i < NCOPY; ++i) {
+        __builtin_amdgcn_global_load_lds(ks + koff0 + 2048 * i, kb + kWave * 8 * (wave + 4 * i), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds(vs + voff0 + 2048 * i, vb + kWave * 8 * (wave + 4 * i), 16, 0, 0);
+      }
+    } else {
+      // the last chunk: what lies behind the keys may be anything, and a weight of zero does not make a NaN vanish.  (K rows
+      // repeat the last one; their scores are replaced.)
+#pragma unroll
+      for (int i = 0; i < NCOPY; ++i) {
+        const int row = crow + 256 / PPR * i;
+        __builtin_amdgcn_global_load_lds(ks + koff0 - crow * D + min(row, there - 1) * D, kb + kWave * 8 * (wave + 4 * i), 16, 0, 0);
+        bf16_t* to = vb + kWave * 8 * (wave + 4 * i);
+        if (row < there) __builtin_amdgcn_global_load_lds(vs + voff0 + 2048 * i, to, 16, 0, 0);
+        else *reinterpret_cast<u32x4*>(to + 8 * lane) = u32x4{0, 0, 0, 0};
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  // operand addresses, as the exact kernel has them: K row il, piece 2 ks + kh; V^T by the transposing read in the key order
+  // in which the first product leaves the scores
+  int koff[D / 16], voff[2][D / 32];
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ++ks) koff[ks] = il * D + 8 * ((2 * ks + kh) ^ k_piece_swizzle<D>(il));
+#pragma unroll
+  for (int half = 0; half < 2; ++half)
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) {
+      const int t = lane & 15, j = 4 * kh + 8 * half + (t >> 2), d0 = 32 * db + 16 * (il >> 4) + 4 * (t & 3);
+      voff[half][db] = j * D + 8 * ((d0 >> 3) ^ v_piece_swizzle<D>(j)) + (d0 & 7);
+    }
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  typedef short s16x8 __attribute__((ext_vector_type(8)));
+  auto vop = [&](const bf16_t* vb, int db, int jb, int s2) {
+    const bf16_t* at = vb + (32 * jb + 16 * s2) * D;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(at + voff[0][db]));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(at + voff[1][db]));
+    const s16x8 w = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    return __builtin_bit_cast(bf16x8, w);
+  };
+
+  copy(kb0, vb0, 0);
+  u32x4 q[D / 16];
+  {   // (a wave beyond the last row works on a copy of it and stores nothing: no branch of its own in the loop)
+    const bf16_t* src = reinterpret_cast<const bf16_t*>(a.Q) + ((size_t)u * a.R + min(r0 + il, a.R - 1)) * D + 8 * kh;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) q[ks] = *reinterpret_cast<const u32x4*>(src + 16 * ks);
+  }
+  f32x16 acc[D / 32];
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[db][v] = 0.f;
+  float m_run = -INFINITY, l_run = 0.f;
+
+  auto qk = [&](const bf16_t* kb, int jb) {
+    f32x16 s;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) s[v] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks)
+      s = mfma_bf16(*reinterpret_cast<const bf16x8*>(kb + koff[ks] + 32 * jb * D), __builtin_bit_cast(bf16x8, q[ks]), s);
+    return s;
+  };
+  auto hide = [&](f32x16& s, int limit) {   // keys from `limit` on
+#pragma unroll
+    for (int v = 0; v < 16; ++v)
+      if (mfma_row(v, kh) >= limit) s[v] = -INFINITY;
+  };
+  auto row_max = [&](const f32x16& s) {
+    const float m01 = fmaxf(fmaxf(s[0], s[1]), s[2]), m02 = fmaxf(fmaxf(s[3], s[4]), s[5]);
+    const float m03 = fmaxf(fmaxf(s[6], s[7]), s[8]), m04 = fmaxf(fmaxf(s[9], s[10]), s[11]);
+    const float m05 = fmaxf(fmaxf(s[12], s[13]), s[14]);
+    return max_with_other_half(fmaxf(fmaxf(fmaxf(m01, m02), m03), fmaxf(fmaxf(m04, m05), s[15])));
+  };
+  // Weights 2^(score - m) in bf16, the second product's operand; their sum is over the rounded ones, which V is multiplied
+  // with.  (m = -inf: no finite score so far, all weights are zero.)
+  typedef bf16_t bf16x2 __attribute__((ext_vector_type(2)));
+  auto weights = [&](const f32x16& s, float m, u32x4(&pw)[2], float& sum) {
+    const bf16x2 ones = {(bf16_t)1.0f, (bf16_t)1.0f};
+    const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+      const float e0 = __builtin_amdgcn_exp2f(fmaf(s[2 * w], scale_log2e, -ref));
+      const float e1 = __builtin_amdgcn_exp2f(fmaf(s[2 * w + 1], scale_log2e, -ref));
+      const uint32_t pk = pack_bf16(e0, e1);
+      pw[w >> 2][w & 3] = pk;
+      sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pk), ones, sum, false);
+    }
+  };
+  auto pv = [&](const bf16_t* vb, int jb, const u32x4(&pw)[2]) {
+#pragma unroll
+    for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+        acc[db] = mfma_bf16(vop(vb, db, jb, s2), __builtin_bit_cast(bf16x8, pw[s2]), acc[db]);
+  };
+  auto rescale = [&](float m_new) {
+    const float alpha = m_new > m_run ? __builtin_amdgcn_exp2f(m_run - m_new) : 1.f;
+    l_run *= alpha;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[db][v] *= alpha;
+  };
+  // One chunk of two blocks: the scores of block 1 are requested before the exponentials of block 0, the second product of
+  // block 0 before the exponentials of block 1.  `there` keys of the chunk exist (TAIL; all 64 otherwise).
+  auto step = [&](const bf16_t* kb, const bf16_t* vb, int there, const bool TAIL) __attribute__((always_inline)) {
+    const bool two = !TAIL || there > 32;
+    f32x16 s0 = qk(kb, 0);
+    if (TAIL) hide(s0, there);
+    {
+      const float cand = fmaxf(m_run, row_max(s0) * scale_log2e);
+      if (__any(cand > m_run + kCrossSlack)) {
+        rescale(cand);
+        m_run = cand;
+      }
+    }
+    f32x16 s1;
+    if (two) s1 = qk(kb, 1);
+    u32x4 p0[2];
+    float sum = 0.f;
+    weights(s0, m_run, p0, sum);
+    l_run += sum;
+    if (two) {
+      if (TAIL) hide(s1, there - 32);
+      const float cand = fmaxf(m_run, row_max(s1) * scale_log2e);
+      const bool moved = __any(cand > m_run + kCrossSlack);
+      const float m1 = moved ? cand : m_run;
+      pv(vb, 0, p0);
+      u32x4 p1[2];
+      float sum1 = 0.f;
+      weights(s1, m1, p1, sum1);
+      if (moved) rescale(m1);
+      m_run = m1;
+      l_run += sum1;
+      pv(vb, 1, p1);
+    } else {
+      pv(vb, 0, p0);
+    }
+  };
+  auto publish = [&]() {   // this wave's copies have landed, then everybody's; the other stage is no longer read
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+  };
+
+  const int n_chunk = (keys + kCrossChunk - 1) / kCrossChunk, full = keys / kCrossChunk;
+  int c = 0;
+  for (; c + 1 < full; c += 2) {   // (two chunks a trip: the stages alternate without pointer arithmetic)
+    publish();
+    copy(kb1, vb1, c + 1);
+    step(kb0, vb0, 0, false);
+    publish();
+    if (c + 2 < n_chunk) copy(kb0, vb0, c + 2);
+    step(kb1, vb1, 0, false);
+  }
+  for (; c < n_chunk; ++c) {
+    publish();
+    bf16_t* kc = (c & 1) ? kb1 : kb0;
+    bf16_t* vc = (c & 1) ? vb1 : vb0;
+    if (c + 1 < n_chunk) copy((c & 1) ? kb0 : kb1, (c & 1) ? vb0 : vb1, c + 1);
+    step(kc, vc, min(kCrossChunk, keys - c * kCrossChunk), true);
+  }
+  __syncthreads();   // every wave is done with both stages: they now stage the output
+  if (rows <= 0) return;
+  const float sum = l_run + __shfl_xor(l_run, 32);
+  const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+  bf16_t* ost = wave == 0 ? kb0 : wave == 1 ? vb0 : wave == 2 ? kb1 : vb1;
+  if (rows == kRowsPerWave) {
+    store_tile_bf16<D>(acc, inv, ost, O, lane);
+  } else if (il < rows) {
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int vq = 0; vq < 4; ++vq)
+        *reinterpret_cast<u32x2*>(O + (size_t)il * D + 32 * db + 8 * vq + 4 * kh) =
+            u32x2{pack_bf16(acc[db][4 * vq] * inv, acc[db][4 * vq + 1] * inv),
+                  pack_bf16(acc[db][4 * vq + 2] * inv, acc[db][4 * vq + 3] * inv)};
+  }
+}
+
+static bool cross_by_rows(int64_t B, int64_t Hkv, int64_t R, int64_t Sk, int32_t is_f32) {
+  if (is_f32) return false;
+  if (!decode_fits(B, Hkv, R, Sk)) return true;
+  return R >= 64 && B * Hkv * ((R + kCrossRows - 1) / kCrossRows) >= 128;
+}
+size_t cross_workspace_bytes(int32_t B, int32_t Hkv, int32_t R, int32_t Sk, int32_t D, int32_t is_f32) {
+  return cross_by_rows(B, Hkv, R, Sk, is_f32) ? 0 : decode_workspace_bytes(R, D);
+}
+
+hipError_t launch_cross(const DecodeLaunch& p, hipStream_t stream) {
+  if (!cross_by_rows(p.B, p.Hkv, p.R, p.Sk, p.is_f32)) return launch_decode(p, stream);
+  CrossArgs a;
+  a.Q = p.Q; a.K = p.K; a.V = p.V; a.O = p.O; a.len = p.len; a.row_sel = p.row_sel;
+  a.Hkv = p.Hkv; a.R = p.R; a.Sk = p.Sk;
+  a.tiles = p.B * p.Hkv;
+  a.per = (p.R + kCrossRows - 1) / kCrossRows;
+  const float scale = p.scale == 0.f ? 1.0f / sqrtf((float)p.D) : p.scale;
+  a.scale_log2e = scale * 1.44269504088896340736f;
+  // tiles of a launch: a multiple of 8, at most 2^23 workgroups
+  const int64_t most = ((1 << 23) / a.per > 8 ? (1 << 23) / a.per : 8) & ~7LL;
+  for (int64_t first = 0; first < a.tiles; first += most) {
+    a.first = (int)first;
+    const int64_t n = a.tiles - first < most ? a.tiles - first : most;
+    const dim3 grid((unsigned)((n + 7) / 8 * 8 * a.per));
+    if (p.D == 64) hipLaunchKernelGGL((cross_bf16_kernel<64>), grid, dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL((cross_bf16_kernel<128>), grid, dim3(kThreads), 0, stream, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+}  // namespace ac
