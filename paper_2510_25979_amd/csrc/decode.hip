@@ -2,75 +2,80 @@
 // encoder's states.  O = softmax(scale Q K^T) V for the R rows of each (item b, K/V head), which lie side by side in Q and
 // O (the g heads that share K and V, times their rows); keys j < len[b] are seen.
 //
-// Each byte of K and V serves few products (2 R flop a byte in bf16), so memory bounds it, and the keys of all
-// requests have to be in flight on all compute units, however long or short each request is.  The work is therefore cut
-// by keys, not by requests: all blocks of 32 keys (16 in binary32) of all units (item, K/V head, 32 or 16 rows) form one row of
-// T blocks, and each of a fixed number of workgroups takes an equal run of it, which it finds from the lengths by itself.
-// A run covers the end of one unit, some whole ones and the beginning of another.  The four waves of a workgroup deal
-// out the blocks of a unit and meet in LDS; a whole unit leaves as output, the at most two others as partial results
-// (row maximum, sum, sum of weighted V, binary32), which decode_join_kernel adds up.  So the workspace does not grow with the lengths,
-// and the host need not know them.
+// Each byte of K and V serves few products (2 R flop a byte in bf16), so memory bounds it, and the keys of all requests have
+// to be in flight on all compute units, however long or short each request is.
 //
-// A wave's block: K rows go straight from memory to the lanes that multiply them (S^T = K Q^T), V rows through a
-// wave-private LDS tile where the transposing read wants them (O^T = V^T P^T; binary32: straight from memory), the next
-// block's on their way meanwhile.  A lane holds one key row of K and of V, so it needs one page number a block, asked for two
-// blocks ahead.  Pages may end anywhere inside a block.
+// decode_run_kernel cuts the work by keys, not by requests.  A unit is 16 rows of one (item, K/V head), cut into blocks of 32 keys
+// (16 in binary32); all units' blocks form one row, and each of a fixed number of waves takes an equal run of it, which it
+// finds from the lengths by itself.  Ending one unit and beginning the next counts as kUnitCost further blocks.  A run covers the end of
+// one unit, some whole ones and the beginning of another: whole units leave as output, the at most two others as partial results (row
+// maximum, sum, sum of weighted V, binary32), which decode_join_kernel adds up.  So the workspace does not grow with the lengths, and the host
+// need not know them.  Waves share nothing and never meet; the next block's rows, pages and queries are on their way over the end of
+// a unit, too.
+//
+// decode_unit_kernel gives each unit to a workgroup, whose waves deal out the blocks and meet in LDS: one launch and no workspace,
+// where no item can have many keys.
+//
+// A wave's block: K rows go straight from memory to the lanes that multiply them (S^T = K Q^T, 16 keys x 16 rows a product), V rows
+// through a wave-private LDS tile where the transposing read wants them (O^T = V^T P^T; binary32: straight from memory).  A lane
+// deals with one row of Q, so maximum and sum are in-lane but for the four lanes that share it, and the weights are where the
+// second product takes them.  Pages may end anywhere inside a block: each lane follows its own keys' pages.
 #include <type_traits>
 
 #include "common.hpp"
 #include "f32_tile.hpp"
 #include "serve.h"
-#include "split_tile.hpp"
 
 namespace ac {
 
-constexpr int kDecodeWaves = 4;
-constexpr int kDecodeMost = 1024;   // workgroups, what the workspace is sized for
+constexpr int kDecodeRows = 16;        // rows of a unit
+constexpr int kUnitCost = 2;           // what a unit costs beside its blocks, in blocks
+constexpr int kDecodeWaves = 4 * 768;  // most waves of decode_run_kernel, what the workspace is sized for
 constexpr float kDecodeSlack = 8.0f;   // as in exact attention: the reference point of a row moves when it is outgrown by 2^8
 
 struct DecodeArgs {
   const void *Q, *K, *V;
   void* O;
   const int32_t *table, *len, *row_sel;
-  float *part, *stat;   // partial results [2 workgroups][rp][D] and their (maximum, sum) [2 workgroups][rp][2]
+  float *part, *stat;   // partial results [2 waves][rp][D] and their (maximum, sum) [2 waves][rp][2]
   int32_t B, Hkv, R, rbs, rp, D, Sk;   // rbs: row blocks of a K/V head; rp: rows of a partial result
-  int32_t n_pages, ps, max_pages, groups;
+  int32_t n_pages, ps, max_pages, waves;
   int64_t page_stride, head_stride;
   Divider by_ps;
   float scale_log2e;
 };
+
+__device__ __forceinline__ int decode_keys(const DecodeArgs& a, int b) {
+  if (a.row_sel && a.row_sel[b] >= 0) return 0;
+  return a.len ? min(max(a.len[b], 0), a.Sk) : a.Sk;
+}
 
 // How the blocks of all units are numbered and dealt: item by item, in it K/V head, row block, key block.
 template <int BK>
 struct DecodeWalk {
   const DecodeArgs& a;
   int lane, per, total;
-  __device__ __forceinline__ int keys(int b) const {
-    if (a.row_sel && a.row_sel[b] >= 0) return 0;
-    return a.len ? min(max(a.len[b], 0), a.Sk) : a.Sk;
-  }
-  __device__ __forceinline__ int blocks(int b) const { return (keys(b) + BK - 1) / BK; }   // of a unit of item b
-  __device__ __forceinline__ DecodeWalk(const DecodeArgs& a, int lane) : a(a), lane(lane) {
-    int t = 0;
-    for (int b = lane; b < a.B; b += kWave) t += blocks(b);
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) t += __shfl_xor(t, off);
-    total = __builtin_amdgcn_readfirstlane(t) * (a.Hkv * a.rbs);
-    per = max(kDecodeWaves, (total + a.groups - 1) / a.groups);
+  __device__ __forceinline__ int cost(int b) const {   // of a unit of item b
+    const int keys = decode_keys(a, b);
+    return keys ? (keys + BK - 1) / BK + kUnitCost : 0;
   }
   // number of the first block of item `item`
   __device__ __forceinline__ int start(int item) const {
     int t = 0;
-    for (int b = lane; b < item; b += kWave) t += blocks(b);
+    for (int b = lane; b < item; b += kWave) t += cost(b);
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) t += __shfl_xor(t, off);
     return __builtin_amdgcn_readfirstlane(t) * (a.Hkv * a.rbs);
+  }
+  __device__ __forceinline__ DecodeWalk(const DecodeArgs& a, int lane) : a(a), lane(lane) {
+    total = start(a.B);
+    per = max(1, (total + a.waves - 1) / a.waves);
   }
   // the item that block x < total belongs to; x becomes the block's number in it
   __device__ __forceinline__ int locate(int& x) const {
     int before = 0;
     for (int b0 = 0;; b0 += kWave) {
-      int t = b0 + lane < a.B ? blocks(b0 + lane) * (a.Hkv * a.rbs) : 0;
+      int t = b0 + lane < a.B ? cost(b0 + lane) * (a.Hkv * a.rbs) : 0;
 #pragma unroll
       for (int off = 1; off < kWave; off <<= 1) {
         const int p = __shfl_up(t, off);
@@ -80,8 +85,7 @@ struct DecodeWalk {
       if (beyond || b0 + kWave >= a.B) {
         const int i = beyond ? __builtin_ctzll(beyond) : 0;
         const int prev = __shfl(t, max(i - 1, 0));
-        x -= before + (i > 0 ? prev : 0);
-        x = __builtin_amdgcn_readfirstlane(x);
+        x = __builtin_amdgcn_readfirstlane(x - before - (i > 0 ? prev : 0));
         return b0 + i;
       }
       before += __builtin_amdgcn_readlane(t, kWave - 1);
@@ -89,390 +93,516 @@ struct DecodeWalk {
   }
 };
 
-// Where the K and V row of key j < keys of item b lies, in elements from its head's first row of the first page (or of the
-// item); -1 where there is none.  Two steps, so that the page number can be asked for early.
+// Where the K and V row of key j of an item with `keys` keys lies, in elements from its head's first row of the first page (or of
+// the item); -1 where there is none.  Two steps, so that the page number can be asked for early.
 template <bool PAGED>
-struct DecodeRows {
-  const DecodeArgs& a;
-  const int32_t* pages;
-  int keys, D;
-  __device__ __forceinline__ int ask(int j) const {
-    return PAGED && j < keys ? pages[a.by_ps.div(j)] : 0;
+__device__ __forceinline__ int decode_ask(const DecodeArgs& a, int b, int keys, int j) {
+  return PAGED && j < keys ? a.table[(size_t)b * a.max_pages + a.by_ps.div(j)] : 0;
+}
+template <bool PAGED>
+__device__ __forceinline__ int64_t decode_at(const DecodeArgs& a, int keys, int j, int page, int D) {
+  if (j >= keys) return -1;
+  if (!PAGED) return (int64_t)j * D;
+  if ((unsigned)page >= (unsigned)a.n_pages) return -1;
+  return page * a.page_stride + (int64_t)(j - a.by_ps.div(j) * a.ps) * D;
+}
+
+// max over the lanes l, l ^ 16, l ^ 32, l ^ 48
+__device__ __forceinline__ float max_of_four(float x) {
+  float lo = x, hi = x;
+  asm volatile("s_nop 1\n\tv_permlane16_swap_b32 %0, %1\n\ts_nop 1" : "+v"(lo), "+v"(hi));
+  return max_with_other_half(fmaxf(lo, hi));
+}
+// LDS operations of one wave execute in order: only the compiler has to keep them so.
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+__device__ __forceinline__ float sum_of_four(float x) {
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
+
+// The work of a wave on one block.  Lane = (i, kq) = (lane % 16, lane / 16); i is its row of Q.  Results: NP pieces of four
+// consecutive columns of row i, piece n from column col(n).
+template <int D_>
+struct DecodeBf16 {
+  typedef bf16_t Elt;
+  static constexpr int BK = 32, KPL = 2, NP = D_ / 16, KS = D_ / 32, OCC = 3;   // keys of a block, of a lane; pieces
+  static constexpr int LDS = 32 * D_ * 2;                                      // bytes of the wave's V tile
+  struct Query { u32x4 r[KS]; };
+  u32x4 k[2][KS], v[2][KS];
+  f32x4 acc[NP];
+  float m, l;
+  bf16_t* vt;
+  int lane, i, kq;
+
+  __device__ __forceinline__ DecodeBf16(const DecodeArgs&, unsigned char* lds, int lane)
+      : vt(reinterpret_cast<bf16_t*>(lds)), lane(lane), i(lane & 15), kq(lane >> 4) {}
+  __device__ __forceinline__ int dim() const { return D_; }
+  __device__ __forceinline__ int col(int n) const { return 16 * n + 4 * kq; }
+  __device__ __forceinline__ int key(int t) const { return 16 * t + i; }   // the lane's keys of a block
+  __device__ __forceinline__ void reset() {
+#pragma unroll
+    for (int n = 0; n < NP; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    m = -INFINITY;
+    l = 0.f;
   }
-  __device__ __forceinline__ int64_t at(int j, int page) const {
-    if (j >= keys) return -1;
-    if (!PAGED) return (int64_t)j * D;
-    if ((unsigned)page >= (unsigned)a.n_pages) return -1;
-    return page * a.page_stride + (int64_t)(j - a.by_ps.div(j) * a.ps) * D;
+  __device__ __forceinline__ void load_q(Query& q, const Elt* rows, int n_rows) const {
+    const Elt* src = rows + (size_t)min(i, n_rows - 1) * D_ + 8 * kq;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) q.r[s] = *reinterpret_cast<const u32x4*>(src + 32 * s);
+  }
+  __device__ __forceinline__ void rows_of(u32x4 (&r)[2][KS], const Elt* base, const int64_t (&at)[2]) const {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const Elt* src = base + (at[t] < 0 ? 0 : at[t]) + 8 * kq;   // (row 0: there, and not used)
+#pragma unroll
+      for (int s = 0; s < KS; ++s) r[t][s] = *reinterpret_cast<const u32x4*>(src + 32 * s);
+    }
+  }
+  __device__ __forceinline__ void load_k(const Elt* base, const int64_t (&at)[2]) { rows_of(k, base, at); }
+  __device__ __forceinline__ void load_v(const Elt* base, const int64_t (&at)[2]) { rows_of(v, base, at); }
+  // scores^T: keys 16 t + 4 kq + x of row i
+  typedef f32x4 Scores[2];
+  __device__ __forceinline__ void scores(Scores& s, const Query& q) const {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < KS; ++c)
+        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[t][c]),
+                                                       __builtin_bit_cast(bf16x8, q.r[c]), s[t], 0, 0, 0);
+    }
+  }
+  // Position of piece p of row r in the V tile: sixteen rows of a write, and eight rows of a transposing read of two pieces
+  // each, fall on different banks.
+  static __device__ __forceinline__ int piece(int r) {
+    return D_ == 128 ? 4 * (r & 3) ^ 2 * ((r >> 2) & 1) ^ ((r >> 3) & 1) : 2 * ((r >> 1) & 3) ^ ((r >> 3) & 1);
+  }
+  // Rows that are not there: no score, and zeros in V, since a weight of zero does not make a NaN vanish.
+  __device__ __forceinline__ void hide(Scores& s, const int64_t (&at)[2]) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const uint32_t seen = (uint32_t)__ballot(at[t] >= 0);
+      if ((seen & 0xffff) != 0xffff) {
+#pragma unroll
+        for (int c = 0; c < KS; ++c)
+          if (at[t] < 0) v[t][c] = u32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          if (!((seen >> (4 * kq + x)) & 1)) s[t][x] = -INFINITY;
+      }
+    }
+  }
+  __device__ __forceinline__ void stage_v() const {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int c = 0; c < KS; ++c)
+        *reinterpret_cast<u32x4*>(vt + key(t) * D_ + 8 * ((4 * c + kq) ^ piece(i))) = v[t][c];
+  }
+  __device__ __forceinline__ void add(Scores& s, float scale_log2e) {
+    float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
+                     fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+    const float cand = fmaxf(m, max_of_four(mx) * scale_log2e);
+    if (__any(cand > m + kDecodeSlack)) {
+      const float alpha = cand > m ? __builtin_amdgcn_exp2f(m - cand) : 1.f;
+      l *= alpha;
+#pragma unroll
+      for (int n = 0; n < NP; ++n) acc[n] *= alpha;
+      m = cand;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;   // no finite score so far: all weights are zero
+    typedef bf16_t bf16x2 __attribute__((ext_vector_type(2)));
+    const bf16x2 ones = {(bf16_t)1.0f, (bf16_t)1.0f};
+    u32x4 p;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {   // the sum is over the rounded weights, which V is multiplied with
+      const float e0 = __builtin_amdgcn_exp2f(fmaf(s[w >> 1][2 * (w & 1)], scale_log2e, -ref));
+      const float e1 = __builtin_amdgcn_exp2f(fmaf(s[w >> 1][2 * (w & 1) + 1], scale_log2e, -ref));
+      const uint32_t pk = pack_bf16(e0, e1);
+      p[w] = pk;
+      l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pk), ones, l, false);
+    }
+    // contraction slot e of lane quarter kq is key 16 (e / 4) + 4 kq + e % 4, where the first product left the scores; lane i of a
+    // group of 16 names key 4 kq + i / 4 and four columns, and receives its own column of the four keys
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef short s16x8 __attribute__((ext_vector_type(8)));
+#pragma unroll
+    for (int n = 0; n < NP; ++n) {
+      s16x4 w[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int j = 4 * kq + (i >> 2), d0 = 16 * n + 4 * (i & 3);
+        w[t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(
+            vt + (16 * t + j) * D_ + 8 * ((d0 >> 3) ^ piece(j)) + (d0 & 7)));
+      }
+      const s16x8 vop = {w[0][0], w[0][1], w[0][2], w[0][3], w[1][0], w[1][1], w[1][2], w[1][3]};
+      acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vop), __builtin_bit_cast(bf16x8, p), acc[n], 0, 0, 0);
+    }
+  }
+  static __device__ __forceinline__ void store(Elt* to, const f32x4 r, float inv, int, int) {
+    *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16(r[0] * inv, r[1] * inv), pack_bf16(r[2] * inv, r[3] * inv)};
   }
 };
 
-// Position of piece p of row r in the V tile: the rows of a transposing read are spread over the banks as v_piece_swizzle does
-// it, and, since a lane writes pieces of one row here, the eight or sixteen rows of a write too.
-template <int D>
-__device__ __forceinline__ int decode_v_piece(int r) {
-  return v_piece_swizzle<D>(r) ^ ((r >> 2) & 3);
-}
+// Binary32, D <= 64 DB.  A row that is no whole number of 16-byte pieces is read in pieces of four that start at any 4-byte
+// address, its end in single floats.
+template <int DB, bool FULL>   // FULL: D == 64 DB
+struct DecodeF32 {
+  typedef float Elt;
+  static constexpr int BK = 16, KPL = 1, NP = 4 * DB, OCC = DB <= 2 ? 2 : 1;
+  static constexpr int LDS = 0;
+  struct Query { f32x4 r[4 * DB]; };
+  f32x4 k[4 * DB], v[4][DB];
+  f32x4 acc[4 * DB];   // [4 b + c][x]: column 64 b + 16 kq + 4 x + c
+  float m, l;
+  int D, lane, i, kq;
 
-// The rows of a unit, summed over the waves: out as bf16 or binary32 (a whole unit) or as a partial result.
-template <bool PAGED, int D>
-__global__ __launch_bounds__(kDecodeWaves* kWave, 2) void decode_bf16_kernel(const DecodeArgs a) {
-  constexpr int NW = kDecodeWaves, BK = 32, NP = D / 16;   // 16-byte pieces of a row that a lane half holds
-  __shared__ __attribute__((aligned(16))) f32x4 smem[NW * (D / 8) * kWave];   // V tiles, then the waves' sums
-  __shared__ float ms[NW][32], ls[NW][32];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int il = lane & 31, kh = lane >> 5;
-  const DecodeWalk<BK> walk(a, lane);
-  int x = blockIdx.x * walk.per;
-  if (x >= walk.total) return;
-  int left = min(walk.per, walk.total - x);
-  int b = walk.locate(x);
-  bf16_t* vt = reinterpret_cast<bf16_t*>(smem) + wave * 32 * D;
-  while (true) {
-    const int keys = __builtin_amdgcn_readfirstlane(walk.keys(b)), nb = (keys + BK - 1) / BK;
-    if (nb == 0) {   // (not the item that was located: there are more blocks to come behind it)
-      ++b;
-      continue;
-    }
-    const int unit = x / nb, first = x - unit * nb, n = min(nb - first, left);
-    const int hk = unit / a.rbs, row0 = 32 * (unit - hk * a.rbs), rows = min(32, a.R - row0);
-    const size_t head = (size_t)b * a.Hkv + hk;
-    const bf16_t* K = reinterpret_cast<const bf16_t*>(a.K) + (PAGED ? hk : head) * a.head_stride;
-    const bf16_t* V = reinterpret_cast<const bf16_t*>(a.V) + (PAGED ? hk : head) * a.head_stride;
-    const DecodeRows<PAGED> where{a, PAGED ? a.table + (size_t)b * a.max_pages : nullptr, keys, D};
-    u32x4 q[NP], k[NP], v[NP];
-    {
-      const bf16_t* src = reinterpret_cast<const bf16_t*>(a.Q) + (head * a.R + row0 + min(il, rows - 1)) * D + 8 * kh;
+  __device__ __forceinline__ DecodeF32(const DecodeArgs& a, unsigned char*, int lane)
+      : D(FULL ? 64 * DB : a.D), lane(lane), i(lane & 15), kq(lane >> 4) {}
+  __device__ __forceinline__ int dim() const { return FULL ? 64 * DB : D; }
+  __device__ __forceinline__ int col(int n) const { return 64 * (n >> 2) + 16 * kq + 4 * (n & 3); }
+  __device__ __forceinline__ int key(int) const { return i; }
+  __device__ __forceinline__ void reset() {
 #pragma unroll
-      for (int i = 0; i < NP; ++i) q[i] = *reinterpret_cast<const u32x4*>(src + 16 * i);
-    }
-    const int end = first + n;
-    int blk = first + wave, page = 0;
-    int64_t at = -1, next_at = -1;
-    auto load = [&](u32x4(&r)[NP], const bf16_t* base, int64_t where_at) {
-      const bf16_t* src = base + (where_at < 0 ? 0 : where_at) + 8 * kh;   // (page 0 or row 0: there, and not used)
-#pragma unroll
-      for (int i = 0; i < NP; ++i) r[i] = *reinterpret_cast<const u32x4*>(src + 16 * i);
-    };
-    if (blk < end) {
-      at = where.at(BK * blk + il, where.ask(BK * blk + il));
-      load(k, K, at);
-      load(v, V, at);
-      if (blk + NW < end) page = where.ask(BK * (blk + NW) + il);
-    }
-    f32x16 acc[D / 32];
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) acc[db][i] = 0.f;
-    float m = -INFINITY, l = 0.f;
-    for (; blk < end; blk += NW) {
-      f32x16 s;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = 0.f;
-#pragma unroll
-      for (int i = 0; i < NP; ++i) s = mfma_bf16(__builtin_bit_cast(bf16x8, k[i]), __builtin_bit_cast(bf16x8, q[i]), s);
-      const bool there = at >= 0, more = blk + NW < end;
-      if (more) {
-        next_at = where.at(BK * (blk + NW) + il, page);
-        load(k, K, next_at);
-        if (blk + 2 * NW < end) page = where.ask(BK * (blk + 2 * NW) + il);
-      }
-      const uint32_t seen = (uint32_t)__ballot(there);   // the block's 32 keys (both lane halves say the same)
-      if (seen != 0xffffffffu) {   // a weight of zero does not make a NaN vanish: rows that are not there are zero
-#pragma unroll
-        for (int i = 0; i < NP; ++i)
-          if (!there) v[i] = u32x4{0, 0, 0, 0};
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (!((seen >> mfma_row(i, kh)) & 1)) s[i] = -INFINITY;
-      }
-#pragma unroll
-      for (int i = 0; i < NP; ++i)
-        *reinterpret_cast<u32x4*>(vt + il * D + 8 * ((2 * i + kh) ^ decode_v_piece<D>(il))) = v[i];
-      if (more) load(v, V, next_at);
-      at = next_at;
-      wave_lds_fence();
-      float mx = s[0];
-#pragma unroll
-      for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
-      const float cand = fmaxf(m, max_with_other_half(mx) * a.scale_log2e);
-      if (__any(cand > m + kDecodeSlack)) {
-        const float alpha = cand > m ? __builtin_amdgcn_exp2f(m - cand) : 1.f;
-        l *= alpha;
-#pragma unroll
-        for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) acc[db][i] *= alpha;
-        m = cand;
-      }
-      const float ref = m == -INFINITY ? 0.f : m;   // no finite score so far: all weights are zero
-      typedef bf16_t bf16x2 __attribute__((ext_vector_type(2)));
-      const bf16x2 ones = {(bf16_t)1.0f, (bf16_t)1.0f};
-      u32x4 p[2];
-#pragma unroll
-      for (int w = 0; w < 8; ++w) {   // the sum is over the rounded weights, which V is multiplied with
-        const float e0 = __builtin_amdgcn_exp2f(fmaf(s[2 * w], a.scale_log2e, -ref));
-        const float e1 = __builtin_amdgcn_exp2f(fmaf(s[2 * w + 1], a.scale_log2e, -ref));
-        const uint32_t pk = pack_bf16(e0, e1);
-        p[w >> 2][w & 3] = pk;
-        l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pk), ones, l, false);
-      }
-      typedef short s16x4 __attribute__((ext_vector_type(4)));
-      typedef short s16x8 __attribute__((ext_vector_type(8)));
-#pragma unroll
-      for (int s2 = 0; s2 < 2; ++s2)
-#pragma unroll
-        for (int db = 0; db < D / 32; ++db) {
-          s16x4 w[2];
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {   // (the key order in which the scores lie in the registers)
-            const int t = lane & 15, j = 16 * s2 + 4 * kh + 8 * half + (t >> 2);
-            const int d0 = 32 * db + 16 * (il >> 4) + 4 * (t & 3);
-            w[half] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(
-                vt + j * D + 8 * ((d0 >> 3) ^ decode_v_piece<D>(j)) + (d0 & 7)));
-          }
-          const s16x8 vop = {w[0][0], w[0][1], w[0][2], w[0][3], w[1][0], w[1][1], w[1][2], w[1][3]};
-          acc[db] = mfma_bf16(__builtin_bit_cast(bf16x8, vop), __builtin_bit_cast(bf16x8, p[s2]), acc[db]);
-        }
-      wave_lds_fence();   // the tile is read before the next block's rows are written
-    }
-    l += __shfl_xor(l, 32);
-    if (kh == 0) {
-      ms[wave][il] = m;
-      ls[wave][il] = l;
-    }
-    __syncthreads();   // statistics are there, V tiles are no longer read
-    float top = -INFINITY, sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) top = fmaxf(top, ms[w][il]);
-    auto factor = [&](float mw) { return mw < top ? __builtin_amdgcn_exp2f(mw - top) : 1.f; };
-#pragma unroll
-    for (int w = 0; w < NW; ++w) sum = fmaf(ls[w][il], factor(ms[w][il]), sum);
-    const float mine = factor(m);
-    if (il < rows) {
-#pragma unroll
-      for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-        for (int vq = 0; vq < 4; ++vq)
-          smem[(wave * (D / 8) + 4 * db + vq) * kWave + lane] =
-              f32x4{acc[db][4 * vq], acc[db][4 * vq + 1], acc[db][4 * vq + 2], acc[db][4 * vq + 3]} * mine;
-    }
-    __syncthreads();
-    const bool whole = n == nb;
-    const size_t slot = (size_t)(2 * blockIdx.x + (first == 0)) * a.rp;
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;   // no key at all: zeros
-    if (il < rows) {
-#pragma unroll
-      for (int n0 = 0; n0 < D / 8; n0 += NW) {   // columns 8 i + 4 kh and three more of row il
-        const int i = n0 + wave;
-        f32x4 r = smem[i * kWave + lane];
-#pragma unroll
-        for (int w = 1; w < NW; ++w) r += smem[(w * (D / 8) + i) * kWave + lane];
-        const int d = 8 * i + 4 * kh;
-        if (whole)
-          *reinterpret_cast<u32x2*>(reinterpret_cast<bf16_t*>(a.O) + (head * a.R + row0 + il) * D + d) =
-              u32x2{pack_bf16(r[0] * inv, r[1] * inv), pack_bf16(r[2] * inv, r[3] * inv)};
-        else
-          *reinterpret_cast<f32x4*>(a.part + (slot + il) * D + d) = r;
-      }
-      if (!whole && wave == 0 && kh == 0) {
-        a.stat[2 * (slot + il)] = top;
-        a.stat[2 * (slot + il) + 1] = sum;
-      }
-    }
-    left -= n;
-    if (left == 0) break;
-    x += n;
-    if (x == nb * a.Hkv * a.rbs) {
-      ++b;
-      x = 0;
-    }
-    __syncthreads();   // the sums have been read: the next unit's V rows may be written there
+    for (int n = 0; n < 4 * DB; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    m = -INFINITY;
+    l = 0.f;
   }
-}
-
-// Binary32: blocks of 16 keys, units of 16 rows, the layout of f32_tile.hpp.  D of any size: a row that is no whole number of
-// 16-byte pieces is read in pieces of four that start at any 4-byte address, its end in single floats.
-template <bool PAGED, int DB, bool FULL>   // FULL: D == 64 DB
-__global__ __launch_bounds__(kDecodeWaves* kWave, DB <= 2 ? 2 : 1) void decode_f32_kernel(const DecodeArgs a) {
-  constexpr int NW = kDecodeWaves, BK = kF32Rows;
-  __shared__ __attribute__((aligned(16))) f32x4 part[NW][4 * DB][kWave];
-  __shared__ float ms[NW][kF32Rows], ls[NW][kF32Rows];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int i = lane & 15, kq = lane >> 4, D = FULL ? 64 * DB : a.D;
-  const DecodeWalk<BK> walk(a, lane);
-  int x = blockIdx.x * walk.per;
-  if (x >= walk.total) return;
-  int left = min(walk.per, walk.total - x);
-  int b = walk.locate(x);
-  // four columns from c on, zeros behind the row's end
-  auto four = [&](const float* row, int c) {
+  __device__ __forceinline__ f32x4 four(const float* row, int c) const {   // columns c ... c + 3, zeros behind the row's end
     if (FULL) return *reinterpret_cast<const f32x4*>(row + c);
     f32x4 r = {0.f, 0.f, 0.f, 0.f};
-    if (c + 4 <= D) r = *reinterpret_cast<const f32x4_dw*>(row + c);
-    else
+    if (c + 4 <= D) {
+      r = *reinterpret_cast<const f32x4_dw*>(row + c);
+    } else {
 #pragma unroll
       for (int t = 0; t < 3; ++t)
         if (c + t < D) r[t] = row[c + t];
+    }
     return r;
+  }
+  __device__ __forceinline__ void load_q(Query& q, const Elt* rows, int n_rows) const {
+    const float* src = rows + (size_t)min(i, n_rows - 1) * dim();
+#pragma unroll
+    for (int s = 0; s < 4 * DB; ++s) q.r[s] = four(src, 16 * s + 4 * kq);
+  }
+  __device__ __forceinline__ void load_k(const Elt* base, const int64_t (&at)[1]) {
+    const float* src = base + (at[0] < 0 ? 0 : at[0]);
+#pragma unroll
+    for (int s = 0; s < 4 * DB; ++s) k[s] = four(src, 16 * s + 4 * kq);
+  }
+  // columns 64 b + 4 i and three more of keys 4 kq ... 4 kq + 3; zeros if they are not there
+  __device__ __forceinline__ void load_v(const Elt* base, const int64_t (&at)[1]) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int64_t from = __shfl((long long)at[0], 4 * kq + t);
+      const float* src = base + (from < 0 ? 0 : from);
+#pragma unroll
+      for (int b = 0; b < DB; ++b) {
+        v[t][b] = four(src, 64 * b + 4 * i);
+        if (from < 0) v[t][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+    }
+  }
+  typedef f32x4 Scores[1];
+  __device__ __forceinline__ void scores(Scores& s, const Query& q) const {
+    s[0] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < 4 * DB; ++c)
+      if (FULL || 16 * c < D)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) s[0] = mfma_f32(k[c][t], q.r[c][t], s[0]);
+  }
+  __device__ __forceinline__ void hide(Scores& s, const int64_t (&at)[1]) {
+    const uint32_t seen = (uint32_t)__ballot(at[0] >= 0) >> (4 * kq);
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      if (!((seen >> x) & 1)) s[0][x] = -INFINITY;
+  }
+  __device__ __forceinline__ void stage_v() const {}
+  __device__ __forceinline__ void add(Scores& s, float scale_log2e) {
+    const float mx = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3]));
+    const float m_new = fmaxf(m, max_of_four(mx) * scale_log2e);
+    if (__any(m_new > m)) {
+      const float alpha = m_new > m ? __builtin_amdgcn_exp2f(m - m_new) : 1.f;
+      l *= alpha;
+#pragma unroll
+      for (int n = 0; n < 4 * DB; ++n) acc[n] *= alpha;
+      m = m_new;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+    f32x4 p;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      p[x] = __builtin_amdgcn_exp2f(fmaf(s[0][x], scale_log2e, -ref));
+      l += p[x];
+    }
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+#pragma unroll
+      for (int b = 0; b < DB; ++b)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) acc[4 * b + c] = mfma_f32(v[x][b][c], p[x], acc[4 * b + c]);
+  }
+  static __device__ __forceinline__ void store(Elt* to, f32x4 r, float inv, int d, int D) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) r[t] *= inv;
+    if (FULL || d + 4 <= D) {
+      *reinterpret_cast<f32x4_dw*>(to) = r;
+    } else {
+#pragma unroll
+      for (int t = 0; t < 3; ++t)
+        if (d + t < D) to[t] = r[t];
+    }
+  }
+};
+// piece n of a lane's results
+template <int D>
+__device__ __forceinline__ f32x4 decode_piece(const DecodeBf16<D>& c, int n) { return c.acc[n]; }
+template <int DB, bool FULL>
+__device__ __forceinline__ f32x4 decode_piece(const DecodeF32<DB, FULL>& c, int n) {
+  const int b = n >> 2, x = n & 3;
+  return f32x4{c.acc[4 * b][x], c.acc[4 * b + 1][x], c.acc[4 * b + 2][x], c.acc[4 * b + 3][x]};
+}
+__device__ __forceinline__ void store_partial(float* to, const f32x4 r, int d, int D) {
+  if (d + 4 <= D) *reinterpret_cast<f32x4_dw*>(to) = r;
+  else
+#pragma unroll
+    for (int t = 0; t < 3; ++t)
+      if (d + t < D) to[t] = r[t];
+}
+
+// A block of a run: its item, K/V head, row block and number in the unit, and what is left of the run from it on.
+struct DecodeItem {
+  int b, hk, rb, blk, keys, nb, left;
+};
+
+template <class Core, bool PAGED>
+__global__ __launch_bounds__(kThreads, Core::OCC) void decode_run_kernel(const DecodeArgs a) {
+  typedef typename Core::Elt Elt;
+  constexpr int BK = Core::BK, KPL = Core::KPL;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[Core::LDS ? 4 * Core::LDS : 16];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int run = blockIdx.x * 4 + wave;
+  const DecodeWalk<BK> walk(a, lane);
+  if (run >= a.waves) return;
+  int x = run * walk.per;
+  if (x >= walk.total) return;
+  Core core(a, lds + wave * Core::LDS, lane);
+  const int D = core.dim();
+
+  auto item = [&](DecodeItem& it, int b) {   // the first block of the first item from b on that has any
+    int keys;
+    while ((keys = __builtin_amdgcn_readfirstlane(decode_keys(a, b))) == 0) ++b;
+    it.b = b;
+    it.hk = it.rb = it.blk = 0;
+    it.keys = keys;
+    it.nb = (keys + BK - 1) / BK;
   };
+  auto next = [&](DecodeItem& it) {   // false: the run ends
+    --it.left;
+    if (++it.blk < it.nb) return it.left > 0;
+    it.left -= kUnitCost;
+    if (it.left <= 0) return false;
+    it.blk = 0;
+    if (++it.rb == a.rbs) {
+      it.rb = 0;
+      if (++it.hk == a.Hkv) item(it, it.b + 1);
+    }
+    return true;
+  };
+  DecodeItem now, then, later;
+  {
+    const int left = min(walk.per, walk.total - x);
+    item(now, walk.locate(x));
+    now.left = left;
+    const int unit = x / (now.nb + kUnitCost);
+    now.blk = x - unit * (now.nb + kUnitCost);
+    now.hk = unit / a.rbs;
+    now.rb = unit - now.hk * a.rbs;
+    if (now.blk >= now.nb) {   // behind a unit's last block
+      now.left -= now.nb + kUnitCost - now.blk - 1;
+      now.blk = now.nb - 1;
+      now.left += kUnitCost;
+      if (!next(now)) return;
+    }
+  }
+  auto ask = [&](const DecodeItem& it, int(&page)[KPL]) {
+#pragma unroll
+    for (int t = 0; t < KPL; ++t) page[t] = decode_ask<PAGED>(a, it.b, it.keys, BK * it.blk + core.key(t));
+  };
+  auto place = [&](const DecodeItem& it, const int(&page)[KPL], int64_t(&at)[KPL]) {
+#pragma unroll
+    for (int t = 0; t < KPL; ++t) at[t] = decode_at<PAGED>(a, it.keys, BK * it.blk + core.key(t), page[t], D);
+  };
+  auto head_of = [&](const DecodeItem& it) { return (size_t)it.b * a.Hkv + it.hk; };
+  auto base_of = [&](const void* p, const DecodeItem& it) {
+    return static_cast<const Elt*>(p) + (PAGED ? (size_t)it.hk : head_of(it)) * a.head_stride;
+  };
+  auto rows_of = [&](const DecodeItem& it) { return min(kDecodeRows, a.R - kDecodeRows * it.rb); };
+  auto load_q = [&](typename Core::Query& q, const DecodeItem& it) {
+    core.load_q(q, static_cast<const Elt*>(a.Q) + (head_of(it) * a.R + kDecodeRows * it.rb) * D, rows_of(it));
+  };
+
+  typename Core::Query q, q_then;
+  int page[KPL];
+  int64_t at[KPL], at_then[KPL];
+  ask(now, page);
+  load_q(q, now);
+  then = now;
+  bool more = next(then);
+  place(now, page, at);
+  core.load_k(base_of(a.K, now), at);
+  core.load_v(base_of(a.V, now), at);
+  if (more) ask(then, page);
+  core.reset();
+  int begin = now.blk;
   while (true) {
-    const int keys = __builtin_amdgcn_readfirstlane(walk.keys(b)), nb = (keys + BK - 1) / BK;
-    if (nb == 0) {
-      ++b;
-      continue;
+    typename Core::Scores s;
+    core.scores(s, q);
+    later = then;
+    bool more_later = false;
+    if (more) {
+      place(then, page, at_then);
+      core.load_k(base_of(a.K, then), at_then);
+      if (then.blk == 0) load_q(q_then, then);
+      more_later = next(later);
+      if (more_later) ask(later, page);
     }
-    const int unit = x / nb, first = x - unit * nb, n = min(nb - first, left);
-    const int hk = unit / a.rbs, row0 = kF32Rows * (unit - hk * a.rbs), rows = min(kF32Rows, a.R - row0);
-    const size_t head = (size_t)b * a.Hkv + hk;
-    const float* K = reinterpret_cast<const float*>(a.K) + (PAGED ? hk : head) * a.head_stride;
-    const float* V = reinterpret_cast<const float*>(a.V) + (PAGED ? hk : head) * a.head_stride;
-    const DecodeRows<PAGED> where{a, PAGED ? a.table + (size_t)b * a.max_pages : nullptr, keys, D};
-    f32x4 q[4 * DB], k[4 * DB], v[4][DB];
-    {
-      const float* src = reinterpret_cast<const float*>(a.Q) + (head * a.R + row0 + min(i, rows - 1)) * D;
+    core.hide(s, at);
+    core.stage_v();
+    if (Core::LDS && more) core.load_v(base_of(a.V, then), at_then);
+    if (Core::LDS) wave_fence();
+    core.add(s, a.scale_log2e);
+    if (Core::LDS) wave_fence();   // the tile is read before the next block's rows are written
+    if (!Core::LDS && more) core.load_v(base_of(a.V, then), at_then);
+    if (!more || then.blk == 0) {   // the unit's last block, or the run's
+      const float sum = sum_of_four(core.l);
+      const int rows = rows_of(now);
+      const bool whole = begin == 0 && now.blk == now.nb - 1;
+      const size_t slot = (size_t)(2 * run + (begin == 0)) * a.rp;
+      if (core.i < rows) {
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;   // no key at all: zeros
+        Elt* o = static_cast<Elt*>(a.O) + (head_of(now) * a.R + kDecodeRows * now.rb + core.i) * D;
 #pragma unroll
-      for (int kk = 0; kk < 4 * DB; ++kk) q[kk] = four(src, 16 * kk + 4 * kq);
-    }
-    auto load_k = [&](int64_t at) {   // key i's columns 16 kk + 4 kq and three more
-      const float* src = K + (at < 0 ? 0 : at);
-#pragma unroll
-      for (int kk = 0; kk < 4 * DB; ++kk) k[kk] = four(src, 16 * kk + 4 * kq);
-    };
-    auto load_v = [&](int64_t at) {   // columns 64 db + 4 i and three more of keys 4 kq ... 4 kq + 3; zeros if they are not there
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const int64_t from = __shfl((long long)at, 4 * kq + t);
-        const float* src = V + (from < 0 ? 0 : from);
-#pragma unroll
-        for (int db = 0; db < DB; ++db) {
-          v[t][db] = four(src, 64 * db + 4 * i);
-          if (from < 0) v[t][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int n = 0; n < Core::NP; ++n) {
+          const int d = core.col(n);
+          if (whole) Core::store(o + d, decode_piece(core, n), inv, d, D);
+          else store_partial(a.part + (slot + core.i) * D + d, decode_piece(core, n), d, D);
+        }
+        if (!whole && core.kq == 0) {
+          a.stat[2 * (slot + core.i)] = core.m;
+          a.stat[2 * (slot + core.i) + 1] = sum;
         }
       }
-    };
-    const int end = first + n;
-    int blk = first + wave, page = 0;
-    int64_t at = -1, next_at = -1;
-    if (blk < end) {
-      at = where.at(BK * blk + i, where.ask(BK * blk + i));
-      load_k(at);
-      load_v(at);
-      if (blk + NW < end) page = where.ask(BK * (blk + NW) + i);
+      if (!more) break;
+      core.reset();
+      q = q_then;
+      begin = 0;
     }
-    f32x4 acc[4 * DB];
+    now = then;
+    then = later;
+    more = more_later;
 #pragma unroll
-    for (int t = 0; t < 4 * DB; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, l = 0.f;
-    for (; blk < end; blk += NW) {
-      f32x4 s = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int kk = 0; kk < 4 * DB; ++kk)
-        if (FULL || 16 * kk < D)
-#pragma unroll
-          for (int t = 0; t < 4; ++t) s = mfma_f32(k[kk][t], q[kk][t], s);
-      const uint32_t seen = (uint32_t)__ballot(at >= 0) >> (4 * kq);
-      const bool more = blk + NW < end;
-      if (more) {
-        next_at = where.at(BK * (blk + NW) + i, page);
-        load_k(next_at);
-        if (blk + 2 * NW < end) page = where.ask(BK * (blk + 2 * NW) + i);
-      }
-      float mx = -INFINITY;
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        if (!((seen >> t) & 1)) s[t] = -INFINITY;
-        mx = fmaxf(mx, s[t]);
-      }
-      mx = fmaxf(mx, __shfl_xor(mx, 16));
-      mx = fmaxf(mx, __shfl_xor(mx, 32));
-      const float m_new = fmaxf(m, mx * a.scale_log2e);
-      if (__any(m_new > m)) {
-        const float alpha = m_new > m ? __builtin_amdgcn_exp2f(m - m_new) : 1.f;
-        l *= alpha;
-#pragma unroll
-        for (int t = 0; t < 4 * DB; ++t) acc[t] *= alpha;
-        m = m_new;
-      }
-      const float ref = m == -INFINITY ? 0.f : m;
-      f32x4 p;
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        p[t] = __builtin_amdgcn_exp2f(fmaf(s[t], a.scale_log2e, -ref));
-        l += p[t];
-      }
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-          for (int c = 0; c < 4; ++c) acc[4 * db + c] = mfma_f32(v[t][db][c], p[t], acc[4 * db + c]);
-      if (more) load_v(next_at);
-      at = next_at;
-    }
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
-    if (lane < kF32Rows) {
-      ms[wave][lane] = m;
-      ls[wave][lane] = l;
-    }
-    __syncthreads();
-    float top = -INFINITY, sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) top = fmaxf(top, ms[w][i]);
-    auto factor = [&](float mw) { return mw < top ? __builtin_amdgcn_exp2f(mw - top) : 1.f; };
-#pragma unroll
-    for (int w = 0; w < NW; ++w) sum = fmaf(ls[w][i], factor(ms[w][i]), sum);
-    const float mine = factor(m);
-    if (i < rows)
-#pragma unroll
-      for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-          part[wave][4 * db + t][lane] = f32x4{acc[4 * db][t], acc[4 * db + 1][t], acc[4 * db + 2][t], acc[4 * db + 3][t]} * mine;
-    __syncthreads();
-    const bool whole = n == nb;
-    const size_t slot = (size_t)(2 * blockIdx.x + (first == 0)) * a.rp;
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    if (i < rows) {
-      float* to = whole ? reinterpret_cast<float*>(a.O) + (head * a.R + row0 + i) * D : a.part + (slot + i) * D;
-#pragma unroll
-      for (int n0 = 0; n0 < 4 * DB; n0 += NW) {   // columns d and three more of row i
-        const int c = n0 + wave, d = 64 * (c >> 2) + 16 * kq + 4 * (c & 3);
-        f32x4 r = part[0][c][lane];
-#pragma unroll
-        for (int w = 1; w < NW; ++w) r += part[w][c][lane];
-        if (whole)
-#pragma unroll
-          for (int t = 0; t < 4; ++t) r[t] = sum == 0.f ? 0.f : f32_divide(r[t], sum, inv);
-        if (FULL || d + 4 <= D) *reinterpret_cast<f32x4_dw*>(to + d) = r;
-        else
-#pragma unroll
-          for (int t = 0; t < 3; ++t)
-            if (d + t < D) to[d + t] = r[t];
-      }
-      if (!whole && wave == 0 && kq == 0) {
-        a.stat[2 * (slot + i)] = top;
-        a.stat[2 * (slot + i) + 1] = sum;
-      }
-    }
-    left -= n;
-    if (left == 0) break;
-    x += n;
-    if (x == nb * a.Hkv * a.rbs) {
-      ++b;
-      x = 0;
-    }
-    __syncthreads();
+    for (int t = 0; t < KPL; ++t) at[t] = at_then[t];
   }
 }
 
-// The rows of units that several workgroups shared, and zeros for rows without a key.  NW waves add up one output row: its
-// partial results are those of the workgroups whose runs touch its unit.
+// A workgroup per unit, its waves deal out the blocks.
+template <class Core, bool PAGED, int NW>
+__global__ __launch_bounds__(NW* kWave, Core::OCC * 4 / NW > 0 ? Core::OCC * 4 / NW : 1) void decode_unit_kernel(const DecodeArgs a) {
+  typedef typename Core::Elt Elt;
+  constexpr int BK = Core::BK, KPL = Core::KPL, NP = Core::NP;
+  constexpr int TILES = NW * Core::LDS, SUMS = NW * NP * kWave * 16;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[TILES > SUMS ? TILES : SUMS];
+  __shared__ float ms[NW][kDecodeRows], ls[NW][kDecodeRows];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rb = blockIdx.x % a.rbs, head = blockIdx.x / a.rbs, b = head / a.Hkv, hk = head - b * a.Hkv;
+  if (a.row_sel && a.row_sel[b] >= 0) return;
+  const int keys = __builtin_amdgcn_readfirstlane(decode_keys(a, b)), nb = (keys + BK - 1) / BK;
+  Core core(a, lds + wave * Core::LDS, lane);
+  const int D = core.dim(), i = core.i, rows = min(kDecodeRows, a.R - kDecodeRows * rb);
+  const size_t row0 = (size_t)head * a.R + kDecodeRows * rb;
+  const Elt* K = static_cast<const Elt*>(a.K) + (PAGED ? (size_t)hk : (size_t)head) * a.head_stride;
+  const Elt* V = static_cast<const Elt*>(a.V) + (PAGED ? (size_t)hk : (size_t)head) * a.head_stride;
+  typename Core::Query q;
+  int page[KPL];
+  int64_t at[KPL], at_then[KPL];
+  auto ask = [&](int blk) {
+#pragma unroll
+    for (int t = 0; t < KPL; ++t) page[t] = decode_ask<PAGED>(a, b, keys, BK * blk + core.key(t));
+  };
+  auto place = [&](int blk, int64_t(&to)[KPL]) {
+#pragma unroll
+    for (int t = 0; t < KPL; ++t) to[t] = decode_at<PAGED>(a, keys, BK * blk + core.key(t), page[t], D);
+  };
+  core.reset();
+  int blk = wave;
+  if (blk < nb) {
+    ask(blk);
+    core.load_q(q, static_cast<const Elt*>(a.Q) + row0 * D, rows);
+    place(blk, at);
+    core.load_k(K, at);
+    core.load_v(V, at);
+    if (blk + NW < nb) ask(blk + NW);
+  }
+  for (; blk < nb; blk += NW) {
+    typename Core::Scores s;
+    core.scores(s, q);
+    const bool more = blk + NW < nb;
+    if (more) {
+      place(blk + NW, at_then);
+      core.load_k(K, at_then);
+      if (blk + 2 * NW < nb) ask(blk + 2 * NW);
+    }
+    core.hide(s, at);
+    core.stage_v();
+    if (Core::LDS && more) core.load_v(V, at_then);
+    if (Core::LDS) wave_fence();
+    core.add(s, a.scale_log2e);
+    if (Core::LDS) wave_fence();
+    if (!Core::LDS && more) core.load_v(V, at_then);
+#pragma unroll
+    for (int t = 0; t < KPL; ++t) at[t] = at_then[t];
+  }
+  const float l = sum_of_four(core.l);
+  if (core.kq == 0) {
+    ms[wave][i] = core.m;
+    ls[wave][i] = l;
+  }
+  __syncthreads();   // statistics are there, V tiles are no longer read
+  f32x4* sums = reinterpret_cast<f32x4*>(lds);
+  float top = -INFINITY, sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) top = fmaxf(top, ms[w][i]);
+  auto factor = [&](float mw) { return mw < top ? __builtin_amdgcn_exp2f(mw - top) : 1.f; };
+#pragma unroll
+  for (int w = 0; w < NW; ++w) sum = fmaf(ls[w][i], factor(ms[w][i]), sum);
+  const float mine = factor(core.m);
+  if (i < rows)
+#pragma unroll
+    for (int n = 0; n < NP; ++n) sums[(wave * NP + n) * kWave + lane] = decode_piece(core, n) * mine;
+  __syncthreads();
+  if (i < rows) {
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    for (int n = wave; n < NP; n += NW) {
+      f32x4 r = sums[n * kWave + lane];
+#pragma unroll
+      for (int w = 1; w < NW; ++w) r += sums[(w * NP + n) * kWave + lane];
+      const int d = core.col(n);
+      Core::store(static_cast<Elt*>(a.O) + (row0 + i) * D + d, r, inv, d, D);
+    }
+  }
+}
+
+// The rows of units that several waves shared, and zeros for rows without a key.  NW waves add up one output row: its partial
+// results are those of the waves whose runs touch its unit.
 template <bool F32, int NW>
 __global__ __launch_bounds__(NW == 1 ? kThreads : NW * kWave) void decode_join_kernel(const DecodeArgs a) {
-  constexpr int BK = F32 ? kF32Rows : 32, RB = BK, COLS = F32 ? 4 : 2;   // columns of a lane: D <= 256, 128
+  constexpr int BK = F32 ? 16 : 32, COLS = F32 ? 4 : 2;   // columns of a lane: D <= 256, 128
   __shared__ float sums[NW][COLS * kWave];
   __shared__ float weight[NW];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -482,16 +612,16 @@ __global__ __launch_bounds__(NW == 1 ? kThreads : NW * kWave) void decode_join_k
        row += NW == 1 ? gridDim.x * (kThreads / kWave) : gridDim.x) {
     const int head = row / a.R, r = row - head * a.R, b = head / a.Hkv, hk = head - b * a.Hkv;
     if (a.row_sel && a.row_sel[b] >= 0) continue;
-    const int nb = __builtin_amdgcn_readfirstlane(walk.blocks(b));
+    const int cost = __builtin_amdgcn_readfirstlane(walk.cost(b)), nb = cost - kUnitCost;
     float o[COLS];
 #pragma unroll
     for (int c = 0; c < COLS; ++c) o[c] = 0.f;
     float total = 0.f;
-    if (nb > 0) {
-      const int from = walk.start(b) + (hk * a.rbs + r / RB) * nb;
+    if (cost > 0) {
+      const int from = walk.start(b) + (hk * a.rbs + r / kDecodeRows) * cost;
       const int w0 = from / walk.per, w1 = (from + nb - 1) / walk.per;
-      if (w0 == w1) continue;   // one workgroup had all of it
-      auto slot = [&](int w) { return (size_t)(2 * w + (w * walk.per <= from)) * a.rp + r % RB; };
+      if (w0 == w1) continue;   // one wave had all of it
+      auto slot = [&](int w) { return (size_t)(2 * w + (w * walk.per <= from)) * a.rp + r % kDecodeRows; };
       float top = -INFINITY;
       for (int w = w0 + lane; w <= w1; w += kWave) top = fmaxf(top, a.stat[2 * slot(w)]);
 #pragma unroll
@@ -526,71 +656,70 @@ __global__ __launch_bounds__(NW == 1 ? kThreads : NW * kWave) void decode_join_k
     for (int c = 0; c < COLS; ++c) {
       const int d = c * kWave + lane;
       if (d >= a.D) continue;
-      const float r_ = total == 0.f ? 0.f : o[c] / total;
-      if (F32) reinterpret_cast<float*>(a.O)[(size_t)row * a.D + d] = r_;
-      else reinterpret_cast<bf16_t*>(a.O)[(size_t)row * a.D + d] = (bf16_t)r_;
+      const float x = total == 0.f ? 0.f : o[c] / total;
+      if (F32) reinterpret_cast<float*>(a.O)[(size_t)row * a.D + d] = x;
+      else reinterpret_cast<bf16_t*>(a.O)[(size_t)row * a.D + d] = (bf16_t)x;
     }
   }
 }
 
 size_t decode_workspace_bytes(int32_t R, int32_t D) {
-  return (size_t)2 * kDecodeMost * (R < 32 ? R : 32) * (D + 2) * sizeof(float);
+  return (size_t)2 * kDecodeWaves * (R < kDecodeRows ? R : kDecodeRows) * (D + 2) * sizeof(float);
 }
 bool decode_fits(int64_t B, int64_t Hkv, int64_t R, int64_t keys) {
-  // (row blocks of 16 and key blocks of 16: binary32, the smaller ones; and the rows themselves)
-  const double blocks = (double)B * Hkv * ((R + 15) / 16) * ((keys + 15) / 16);
-  return blocks < 2147483648.0 - 65536 && (double)B * Hkv * R < 2147483648.0 - 65536;
+  // blocks of 16 rows and 16 keys (binary32, the smaller ones), and the rows themselves
+  const double units = (double)B * Hkv * ((R + kDecodeRows - 1) / kDecodeRows);
+  return units * ((keys + 15) / 16 + kUnitCost) < 2147483648.0 - 65536 && (double)B * Hkv * R < 2147483648.0 - 65536;
+}
+
+template <class Core, bool PAGED>
+static hipError_t launch_decode_core(DecodeArgs& a, hipStream_t stream) {
+  constexpr bool F32 = Core::BK == 16;
+  constexpr int NW = Core::NP > 8 ? 4 : 8;
+  const int64_t units = (int64_t)a.B * a.Hkv * a.rbs, rows = (int64_t)a.B * a.Hkv * a.R;
+  const int blocks = (int)(((int64_t)a.Sk + Core::BK - 1) / Core::BK);   // the most of a unit
+  if (blocks <= 32 && units <= (1 << 22)) {
+    hipLaunchKernelGGL((decode_unit_kernel<Core, PAGED, NW>), dim3((unsigned)units), dim3(NW * kWave), 0, stream, a);
+    return hipGetLastError();
+  }
+  a.waves = 4 * 256 * Core::OCC;
+  hipLaunchKernelGGL((decode_run_kernel<Core, PAGED>), dim3((unsigned)(a.waves / 4)), dim3(kThreads), 0, stream, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (rows <= 1024) {
+    hipLaunchKernelGGL((decode_join_kernel<F32, 8>), dim3((unsigned)rows), dim3(8 * kWave), 0, stream, a);
+  } else {
+    const int64_t wgs = (rows + 3) / 4;
+    hipLaunchKernelGGL((decode_join_kernel<F32, 1>), dim3((unsigned)(wgs < 8192 ? wgs : 8192)), dim3(kThreads), 0, stream, a);
+  }
+  return hipGetLastError();
 }
 
 hipError_t launch_decode(const DecodeLaunch& p, hipStream_t stream) {
-  const int rb = p.is_f32 ? kF32Rows : 32;
   DecodeArgs a;
   a.Q = p.Q; a.K = p.K; a.V = p.V; a.O = p.O; a.table = p.table; a.len = p.len; a.row_sel = p.row_sel;
   a.B = p.B; a.Hkv = p.Hkv; a.R = p.R; a.D = p.D; a.Sk = p.Sk;
-  a.rbs = (p.R + rb - 1) / rb;
-  a.rp = p.R < rb ? p.R : rb;
+  a.rbs = (p.R + kDecodeRows - 1) / kDecodeRows;
+  a.rp = p.R < kDecodeRows ? p.R : kDecodeRows;
   a.n_pages = p.n_pages; a.ps = p.page_size; a.max_pages = p.max_pages; a.page_stride = p.page_stride;
   a.head_stride = (int64_t)(p.table ? p.page_size : p.Sk) * p.D;
   a.by_ps = Divider((uint32_t)(p.table ? p.page_size : 1));
   const float scale = p.scale == 0.f ? 1.0f / sqrtf((float)p.D) : p.scale;
   a.scale_log2e = scale * 1.44269504088896340736f;
-  a.groups = 512;
+  a.waves = 0;
   a.stat = static_cast<float*>(p.ws);
-  a.part = a.stat + (size_t)2 * kDecodeMost * a.rp * 2;
-  const dim3 grid((unsigned)a.groups), block(kDecodeWaves * kWave);
+  a.part = a.stat + (size_t)2 * kDecodeWaves * a.rp * 2;
   auto go = [&](auto paged) {
     constexpr bool P = decltype(paged)::value;
-    if (!p.is_f32) {
-      if (p.D == 64) hipLaunchKernelGGL((decode_bf16_kernel<P, 64>), grid, block, 0, stream, a);
-      else hipLaunchKernelGGL((decode_bf16_kernel<P, 128>), grid, block, 0, stream, a);
-    } else if (p.D == 64) {
-      hipLaunchKernelGGL((decode_f32_kernel<P, 1, true>), grid, block, 0, stream, a);
-    } else if (p.D == 128) {
-      hipLaunchKernelGGL((decode_f32_kernel<P, 2, true>), grid, block, 0, stream, a);
-    } else if (p.D < 64) {
-      hipLaunchKernelGGL((decode_f32_kernel<P, 1, false>), grid, block, 0, stream, a);
-    } else if (p.D < 128) {
-      hipLaunchKernelGGL((decode_f32_kernel<P, 2, false>), grid, block, 0, stream, a);
-    } else {
-      hipLaunchKernelGGL((decode_f32_kernel<P, 4, false>), grid, block, 0, stream, a);
-    }
+    if (!p.is_f32)
+      return p.D == 64 ? launch_decode_core<DecodeBf16<64>, P>(a, stream) : launch_decode_core<DecodeBf16<128>, P>(a, stream);
+    if (p.D == 64) return launch_decode_core<DecodeF32<1, true>, P>(a, stream);
+    if (p.D == 128) return launch_decode_core<DecodeF32<2, true>, P>(a, stream);
+    if (p.D < 64) return launch_decode_core<DecodeF32<1, false>, P>(a, stream);
+    if (p.D < 128) return launch_decode_core<DecodeF32<2, false>, P>(a, stream);
+    return launch_decode_core<DecodeF32<4, false>, P>(a, stream);
   };
-  if (p.table) go(std::true_type{});
-  else go(std::false_type{});
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  const int64_t rows = (int64_t)p.B * p.Hkv * p.R;
-  auto join = [&](auto f32) {
-    constexpr bool F = decltype(f32)::value;
-    if (rows <= 1024) hipLaunchKernelGGL((decode_join_kernel<F, 8>), dim3((unsigned)rows), dim3(8 * kWave), 0, stream, a);
-    else {
-      const int64_t wgs = (rows + 3) / 4;
-      hipLaunchKernelGGL((decode_join_kernel<F, 1>), dim3((unsigned)(wgs < 8192 ? wgs : 8192)), dim3(kThreads), 0, stream, a);
-    }
-  };
-  if (p.is_f32) join(std::true_type{});
-  else join(std::false_type{});
-  return hipGetLastError();
+  return p.table ? go(std::true_type{}) : go(std::false_type{});
 }
 
 }  // namespace ac

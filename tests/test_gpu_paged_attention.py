@@ -170,9 +170,9 @@ def test_the_same_result_every_time_on_any_stream(ac):  # noqa: F811
 
 
 def test_two_graphs_with_one_workspace(ac):  # noqa: F811
-    calls = []
-    ws = torch.full((2_000_000,), float("nan"), device="cuda")
-    for lens, Hq, Hkv, D in (([900, 3], 8, 2, 128), ([17] * 40 + [4000], 4, 4, 64)):
+    calls, sizes = [], (([900, 3, 2000], 8, 2, 128), ([17] * 40 + [4000], 4, 4, 64))
+    ws = torch.full((max(ac.attention_paged_workspace_bytes(len(x), *s) for x, *s in sizes) // 4,), float("nan"), device="cuda")
+    for lens, Hq, Hkv, D in sizes:
         c = Cache(lens, Hkv, D, "bf16", 16, D)
         Q = torch.randn(len(lens), Hq, D, generator=c.gen, device="cuda").bfloat16()
         O = torch.zeros_like(Q)
