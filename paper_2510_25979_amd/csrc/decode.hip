@@ -30,7 +30,7 @@ namespace ac {
 
 constexpr int kDecodeRows = 16;        // rows of a unit
 constexpr int kUnitCost = 2;           // what a unit costs beside its blocks, in blocks
-constexpr int kDecodeWaves = 4 * 768;  // most waves of decode_run_kernel, what the workspace is sized for
+constexpr int kDecodeWaves = 4 * 512;  // most waves of decode_run_kernel, what the workspace is sized for
 constexpr float kDecodeSlack = 8.0f;   // as in exact attention: the reference point of a row moves when it is outgrown by 2^8
 
 struct DecodeArgs {
@@ -41,13 +41,22 @@ struct DecodeArgs {
   int32_t B, Hkv, R, rbs, rp, D, Sk;   // rbs: row blocks of a K/V head; rp: rows of a partial result
   int32_t n_pages, ps, max_pages, waves;
   int64_t page_stride, head_stride;
-  Divider by_ps;
+  Divider by_ps, by_rbs;
   float scale_log2e;
 };
 
 __device__ __forceinline__ int decode_keys(const DecodeArgs& a, int b) {
   if (a.row_sel && a.row_sel[b] >= 0) return 0;
   return a.len ? min(max(a.len[b], 0), a.Sk) : a.Sk;
+}
+
+// The same for a b that all lanes share: scalar loads, which the compiler does not take by itself in a kernel that writes, and
+// which wait for no copy that is under way.
+__device__ __forceinline__ int decode_keys_of(const DecodeArgs& a, int b) {
+  typedef const int32_t __attribute__((address_space(4)))* scalar_ptr;
+  b = __builtin_amdgcn_readfirstlane(b);
+  if (a.row_sel && ((scalar_ptr)(uintptr_t)a.row_sel)[b] >= 0) return 0;
+  return a.len ? min(max(((scalar_ptr)(uintptr_t)a.len)[b], 0), a.Sk) : a.Sk;
 }
 
 // How the blocks of all units are numbered and dealt: item by item, in it K/V head, row block, key block.
@@ -69,7 +78,9 @@ struct DecodeWalk {
   }
   __device__ __forceinline__ DecodeWalk(const DecodeArgs& a, int lane) : a(a), lane(lane) {
     total = start(a.B);
-    per = max(1, (total + a.waves - 1) / a.waves);
+    // Runs of one block as long as every second wave has none: more partial results cost the join more than the runs save (one
+    // request of 8,000 tokens of 8 heads of 128, 2,016 blocks for 2,048 waves: 18.6 us, runs of two 16.9; of 2,000 tokens 11.7 / 13.2).
+    per = 2 * total <= a.waves ? 1 : max(2, (total + a.waves - 1) / a.waves);
   }
   // the item that block x < total belongs to; x becomes the block's number in it
   __device__ __forceinline__ int locate(int& x) const {
@@ -129,7 +140,7 @@ __device__ __forceinline__ float sum_of_four(float x) {
 template <int D_>
 struct DecodeBf16 {
   typedef bf16_t Elt;
-  static constexpr int BK = 32, KPL = 2, NP = D_ / 16, KS = D_ / 32, OCC = 3;   // keys of a block, of a lane; pieces
+  static constexpr int BK = 32, KPL = 2, NP = D_ / 16, KS = D_ / 32, OCC = 3, WGS = 2;   // keys of a block, of a lane; pieces
   static constexpr int LDS = 32 * D_ * 2;                                      // bytes of the wave's V tile
   struct Query { u32x4 r[KS]; };
   u32x4 k[2][KS], v[2][KS];
@@ -253,7 +264,7 @@ struct DecodeBf16 {
 template <int DB, bool FULL>   // FULL: D == 64 DB
 struct DecodeF32 {
   typedef float Elt;
-  static constexpr int BK = 16, KPL = 1, NP = 4 * DB, OCC = DB <= 2 ? 2 : 1;
+  static constexpr int BK = 16, KPL = 1, NP = 4 * DB, OCC = DB <= 2 ? 2 : 1, WGS = 1;
   static constexpr int LDS = 0;
   struct Query { f32x4 r[4 * DB]; };
   f32x4 k[4 * DB], v[4][DB];
@@ -375,9 +386,9 @@ __device__ __forceinline__ void store_partial(float* to, const f32x4 r, int d, i
       if (d + t < D) to[t] = r[t];
 }
 
-// A block of a run: its item, K/V head, row block and number in the unit, and what is left of the run from it on.
+// A block of a run: its item, unit of the item and number in the unit, and what is left of the run from it on.
 struct DecodeItem {
-  int b, hk, rb, blk, keys, nb, left;
+  int b, unit, blk, keys, nb, left;
 };
 
 template <class Core, bool PAGED>
@@ -396,33 +407,28 @@ __global__ __launch_bounds__(kThreads, Core::OCC) void decode_run_kernel(const D
 
   auto item = [&](DecodeItem& it, int b) {   // the first block of the first item from b on that has any
     int keys;
-    while ((keys = __builtin_amdgcn_readfirstlane(decode_keys(a, b))) == 0) ++b;
+    while ((keys = decode_keys_of(a, b)) == 0) ++b;
     it.b = b;
-    it.hk = it.rb = it.blk = 0;
+    it.unit = 0;
     it.keys = keys;
     it.nb = (keys + BK - 1) / BK;
   };
+  const int units = a.Hkv * a.rbs;
   auto next = [&](DecodeItem& it) {   // false: the run ends
-    --it.left;
-    if (++it.blk < it.nb) return it.left > 0;
-    it.left -= kUnitCost;
-    if (it.left <= 0) return false;
-    it.blk = 0;
-    if (++it.rb == a.rbs) {
-      it.rb = 0;
-      if (++it.hk == a.Hkv) item(it, it.b + 1);
-    }
-    return true;
+    const bool last = it.blk + 1 == it.nb;
+    it.left -= last ? 1 + kUnitCost : 1;
+    it.blk = last ? 0 : it.blk + 1;
+    it.unit += last ? 1 : 0;
+    if (it.unit == units && it.left > 0) item(it, it.b + 1);
+    return it.left > 0;
   };
   DecodeItem now, then, later;
   {
     const int left = min(walk.per, walk.total - x);
     item(now, walk.locate(x));
     now.left = left;
-    const int unit = x / (now.nb + kUnitCost);
-    now.blk = x - unit * (now.nb + kUnitCost);
-    now.hk = unit / a.rbs;
-    now.rb = unit - now.hk * a.rbs;
+    now.unit = x / (now.nb + kUnitCost);
+    now.blk = x - now.unit * (now.nb + kUnitCost);
     if (now.blk >= now.nb) {   // behind a unit's last block
       now.left -= now.nb + kUnitCost - now.blk - 1;
       now.blk = now.nb - 1;
@@ -438,13 +444,20 @@ __global__ __launch_bounds__(kThreads, Core::OCC) void decode_run_kernel(const D
 #pragma unroll
     for (int t = 0; t < KPL; ++t) at[t] = decode_at<PAGED>(a, it.keys, BK * it.blk + core.key(t), page[t], D);
   };
-  auto head_of = [&](const DecodeItem& it) { return (size_t)it.b * a.Hkv + it.hk; };
   auto base_of = [&](const void* p, const DecodeItem& it) {
-    return static_cast<const Elt*>(p) + (PAGED ? (size_t)it.hk : head_of(it)) * a.head_stride;
+    const int hk = a.by_rbs.div(it.unit);
+    return static_cast<const Elt*>(p) + (PAGED ? (size_t)hk : (size_t)it.b * a.Hkv + hk) * a.head_stride;
   };
-  auto rows_of = [&](const DecodeItem& it) { return min(kDecodeRows, a.R - kDecodeRows * it.rb); };
+  // the unit's first row in Q and O, and how many there are
+  auto rows_of = [&](const DecodeItem& it, size_t& row0) {
+    const int hk = a.by_rbs.div(it.unit), r0 = kDecodeRows * (it.unit - hk * a.rbs);
+    row0 = ((size_t)it.b * a.Hkv + hk) * a.R + r0;
+    return min(kDecodeRows, a.R - r0);
+  };
   auto load_q = [&](typename Core::Query& q, const DecodeItem& it) {
-    core.load_q(q, static_cast<const Elt*>(a.Q) + (head_of(it) * a.R + kDecodeRows * it.rb) * D, rows_of(it));
+    size_t row0;
+    const int rows = rows_of(it, row0);
+    core.load_q(q, static_cast<const Elt*>(a.Q) + row0 * D, rows);
   };
 
   typename Core::Query q, q_then;
@@ -463,12 +476,13 @@ __global__ __launch_bounds__(kThreads, Core::OCC) void decode_run_kernel(const D
   while (true) {
     typename Core::Scores s;
     core.scores(s, q);
+    const bool last = now.blk + 1 == now.nb;   // of its unit
     later = then;
     bool more_later = false;
     if (more) {
       place(then, page, at_then);
+      if (last) load_q(q_then, then);
       core.load_k(base_of(a.K, then), at_then);
-      if (then.blk == 0) load_q(q_then, then);
       more_later = next(later);
       if (more_later) ask(later, page);
     }
@@ -479,14 +493,15 @@ __global__ __launch_bounds__(kThreads, Core::OCC) void decode_run_kernel(const D
     core.add(s, a.scale_log2e);
     if (Core::LDS) wave_fence();   // the tile is read before the next block's rows are written
     if (!Core::LDS && more) core.load_v(base_of(a.V, then), at_then);
-    if (!more || then.blk == 0) {   // the unit's last block, or the run's
+    if (last || !more) {
       const float sum = sum_of_four(core.l);
-      const int rows = rows_of(now);
-      const bool whole = begin == 0 && now.blk == now.nb - 1;
+      size_t row0;
+      const int rows = rows_of(now, row0);
+      const bool whole = begin == 0 && last;
       const size_t slot = (size_t)(2 * run + (begin == 0)) * a.rp;
       if (core.i < rows) {
         const float inv = sum == 0.f ? 0.f : 1.f / sum;   // no key at all: zeros
-        Elt* o = static_cast<Elt*>(a.O) + (head_of(now) * a.R + kDecodeRows * now.rb + core.i) * D;
+        Elt* o = static_cast<Elt*>(a.O) + (row0 + core.i) * D;
 #pragma unroll
         for (int n = 0; n < Core::NP; ++n) {
           const int d = core.col(n);
@@ -522,7 +537,7 @@ __global__ __launch_bounds__(NW* kWave, Core::OCC * 4 / NW > 0 ? Core::OCC * 4 /
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int rb = blockIdx.x % a.rbs, head = blockIdx.x / a.rbs, b = head / a.Hkv, hk = head - b * a.Hkv;
   if (a.row_sel && a.row_sel[b] >= 0) return;
-  const int keys = __builtin_amdgcn_readfirstlane(decode_keys(a, b)), nb = (keys + BK - 1) / BK;
+  const int keys = decode_keys_of(a, b), nb = (keys + BK - 1) / BK;
   Core core(a, lds + wave * Core::LDS, lane);
   const int D = core.dim(), i = core.i, rows = min(kDecodeRows, a.R - kDecodeRows * rb);
   const size_t row0 = (size_t)head * a.R + kDecodeRows * rb;
@@ -599,67 +614,106 @@ __global__ __launch_bounds__(NW* kWave, Core::OCC * 4 / NW > 0 ? Core::OCC * 4 /
 }
 
 // The rows of units that several waves shared, and zeros for rows without a key.  NW waves add up one output row: its partial
-// results are those of the waves whose runs touch its unit.
-template <bool F32, int NW>
+// results are those of the waves whose runs touch its unit, dealt to the waves here in turn.  A lane holds four columns, G lanes a
+// partial result; a wave knows the weights of 64 of them at once, one a lane.  Bound by latency: lengths -> statistics -> sums.
+template <bool F32, int G, int NW>
 __global__ __launch_bounds__(NW == 1 ? kThreads : NW * kWave) void decode_join_kernel(const DecodeArgs a) {
-  constexpr int BK = F32 ? 16 : 32, COLS = F32 ? 4 : 2;   // columns of a lane: D <= 256, 128
-  __shared__ float sums[NW][COLS * kWave];
-  __shared__ float weight[NW];
+  typedef typename std::conditional<F32, float, bf16_t>::type Elt;
+  constexpr int BK = F32 ? 16 : 32, SUB = kWave / G;
+  __shared__ __attribute__((aligned(16))) f32x4 sums[NW][G];
+  __shared__ float ms[NW], ls[NW];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int sub = lane / G, d = 4 * (lane % G), D = a.D;
   const DecodeWalk<BK> walk(a, lane);
   const int n_rows = a.B * a.Hkv * a.R;   // of all items
   for (int row = NW == 1 ? blockIdx.x * (kThreads / kWave) + wave : blockIdx.x; row < n_rows;
        row += NW == 1 ? gridDim.x * (kThreads / kWave) : gridDim.x) {
     const int head = row / a.R, r = row - head * a.R, b = head / a.Hkv, hk = head - b * a.Hkv;
     if (a.row_sel && a.row_sel[b] >= 0) continue;
-    const int cost = __builtin_amdgcn_readfirstlane(walk.cost(b)), nb = cost - kUnitCost;
-    float o[COLS];
-#pragma unroll
-    for (int c = 0; c < COLS; ++c) o[c] = 0.f;
-    float total = 0.f;
-    if (cost > 0) {
-      const int from = walk.start(b) + (hk * a.rbs + r / kDecodeRows) * cost;
+    const int keys = decode_keys_of(a, b);
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    float top = -INFINITY, total = 0.f;
+    if (keys > 0) {
+      const int nb = (keys + BK - 1) / BK, from = walk.start(b) + (hk * a.rbs + r / kDecodeRows) * (nb + kUnitCost);
       const int w0 = from / walk.per, w1 = (from + nb - 1) / walk.per;
       if (w0 == w1) continue;   // one wave had all of it
-      auto slot = [&](int w) { return (size_t)(2 * w + (w * walk.per <= from)) * a.rp + r % kDecodeRows; };
-      float top = -INFINITY;
-      for (int w = w0 + lane; w <= w1; w += kWave) top = fmaxf(top, a.stat[2 * slot(w)]);
+      const int first = w0 + (NW == 1 ? 0 : wave);
+      for (int w = first; w <= w1; w += NW * kWave) {
+        const int mine = w + NW * lane;
+        const size_t slot = (size_t)(2 * mine + (mine * walk.per <= from)) * a.rp + r % kDecodeRows;
+        float m = -INFINITY, l = 0.f;
+        if (mine <= w1) {
+          m = a.stat[2 * slot];
+          l = a.stat[2 * slot + 1];
+        }
+        float t = fmaxf(top, m);
 #pragma unroll
-      for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
-#pragma unroll 4
-      for (int w = w0 + (NW == 1 ? 0 : wave); w <= w1; w += NW) {
-        const size_t at = slot(w);
-        const float m = a.stat[2 * at], f = m < top ? __builtin_amdgcn_exp2f(m - top) : 1.f;
-        total = fmaf(a.stat[2 * at + 1], f, total);
+        for (int off = 32; off > 0; off >>= 1) t = fmaxf(t, __shfl_xor(t, off));
+        const float old = top < t ? __builtin_amdgcn_exp2f(top - t) : 1.f, f = m < t ? __builtin_amdgcn_exp2f(m - t) : 1.f;
+        top = t;
+        total *= old;
+        o *= old;
+        l *= f;
 #pragma unroll
-        for (int c = 0; c < COLS; ++c)
-          if (c * kWave + lane < a.D) o[c] = fmaf(a.part[at * a.D + c * kWave + lane], f, o[c]);
-      }
-      if (NW > 1) {
+        for (int off = 32; off > 0; off >>= 1) l += __shfl_xor(l, off);
+        total += l;
+        const int n = min(kWave, (w1 - w) / NW + 1);
+        for (int k0 = 0; k0 < n; k0 += 4 * SUB) {   // four loads of a lane on their way at once
+          f32x4 x[4];
+          float weight[4];
 #pragma unroll
-        for (int c = 0; c < COLS; ++c) sums[wave][c * kWave + lane] = o[c];
-        if (lane == 0) weight[wave] = total;
-        __syncthreads();
-        if (wave == 0) {
+          for (int j = 0; j < 4; ++j) {
+            const int k = k0 + j * SUB + sub, from_lane = min(k, n - 1);
+            const float w_j = __shfl(f, from_lane);
+            weight[j] = k < n ? w_j : 0.f;
+            const float* src = a.part + (size_t)__shfl((int)slot, from_lane) * D + d;
+            x[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (k >= n || d >= D) continue;
+            if (!F32 || d + 4 <= D) {
+              x[j] = *reinterpret_cast<const f32x4_dw*>(src);
+            } else {
 #pragma unroll
-          for (int w = 1; w < NW; ++w) {
-            total += weight[w];
-#pragma unroll
-            for (int c = 0; c < COLS; ++c) o[c] += sums[w][c * kWave + lane];
+              for (int c = 0; c < 3; ++c)
+                if (d + c < D) x[j][c] = src[c];
+            }
           }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o += x[j] * weight[j];
+        }
+      }
+#pragma unroll
+      for (int off = G; off < kWave; off <<= 1)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) o[c] += __shfl_xor(o[c], off);
+      if (NW > 1) {
+        if (lane < G) sums[wave][lane] = o;
+        if (lane == 0) {
+          ms[wave] = top;
+          ls[wave] = total;
         }
         __syncthreads();
+        if (wave == 0) {
+          for (int w = 1; w < NW; ++w) top = fmaxf(top, ms[w]);
+          total = 0.f;
+          o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int w = 0; w < NW; ++w) {
+            const float f = ms[w] < top ? __builtin_amdgcn_exp2f(ms[w] - top) : 1.f;
+            total = fmaf(ls[w], f, total);
+            o += sums[w][lane % G] * f;
+          }
+        }
       }
     }
-    if (NW > 1 && wave > 0) continue;
-#pragma unroll
-    for (int c = 0; c < COLS; ++c) {
-      const int d = c * kWave + lane;
-      if (d >= a.D) continue;
-      const float x = total == 0.f ? 0.f : o[c] / total;
-      if (F32) reinterpret_cast<float*>(a.O)[(size_t)row * a.D + d] = x;
-      else reinterpret_cast<bf16_t*>(a.O)[(size_t)row * a.D + d] = (bf16_t)x;
+    if (wave == 0 || NW == 1) {
+      if (sub == 0 && d < D) {
+        const float inv = total == 0.f ? 0.f : 1.f / total;
+        Elt* to = static_cast<Elt*>(a.O) + (size_t)row * D + d;
+        if constexpr (F32) store_partial(to, o * inv, d, D);
+        else DecodeBf16<64>::store(to, o, inv, d, D);
+      }
     }
+    if (NW > 1) __syncthreads();
   }
 }
 
@@ -682,15 +736,16 @@ static hipError_t launch_decode_core(DecodeArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL((decode_unit_kernel<Core, PAGED, NW>), dim3((unsigned)units), dim3(NW * kWave), 0, stream, a);
     return hipGetLastError();
   }
-  a.waves = 4 * 256 * Core::OCC;
+  a.waves = 4 * 256 * Core::WGS;
   hipLaunchKernelGGL((decode_run_kernel<Core, PAGED>), dim3((unsigned)(a.waves / 4)), dim3(kThreads), 0, stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
+  constexpr int G = Core::NP * 4;
   if (rows <= 1024) {
-    hipLaunchKernelGGL((decode_join_kernel<F32, 8>), dim3((unsigned)rows), dim3(8 * kWave), 0, stream, a);
+    hipLaunchKernelGGL((decode_join_kernel<F32, G, 8>), dim3((unsigned)rows), dim3(8 * kWave), 0, stream, a);
   } else {
     const int64_t wgs = (rows + 3) / 4;
-    hipLaunchKernelGGL((decode_join_kernel<F32, 1>), dim3((unsigned)(wgs < 8192 ? wgs : 8192)), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((decode_join_kernel<F32, G, 1>), dim3((unsigned)(wgs < 8192 ? wgs : 8192)), dim3(kThreads), 0, stream, a);
   }
   return hipGetLastError();
 }
@@ -704,6 +759,7 @@ hipError_t launch_decode(const DecodeLaunch& p, hipStream_t stream) {
   a.n_pages = p.n_pages; a.ps = p.page_size; a.max_pages = p.max_pages; a.page_stride = p.page_stride;
   a.head_stride = (int64_t)(p.table ? p.page_size : p.Sk) * p.D;
   a.by_ps = Divider((uint32_t)(p.table ? p.page_size : 1));
+  a.by_rbs = Divider((uint32_t)a.rbs);
   const float scale = p.scale == 0.f ? 1.0f / sqrtf((float)p.D) : p.scale;
   a.scale_log2e = scale * 1.44269504088896340736f;
   a.waves = 0;
