@@ -535,7 +535,11 @@ __global__ __launch_bounds__(NW* kWave, Core::OCC * 4 / NW > 0 ? Core::OCC * 4 /
   __shared__ __attribute__((aligned(16))) unsigned char lds[TILES > SUMS ? TILES : SUMS];
   __shared__ float ms[NW][kDecodeRows], ls[NW][kDecodeRows];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int rb = blockIdx.x % a.rbs, head = blockIdx.x / a.rbs, b = head / a.Hkv, hk = head - b * a.Hkv;
+  // the row blocks of a head are workgroups with ids equal mod 8 (one XCD): K and V come from its L2 after the first
+  const int slot = blockIdx.x >> 3, group = a.by_rbs.div(slot), rb = slot - group * a.rbs;
+  const int head = a.rbs == 1 ? blockIdx.x : 8 * group + (blockIdx.x & 7);
+  if (head >= a.B * a.Hkv) return;
+  const int b = head / a.Hkv, hk = head - b * a.Hkv;
   if (a.row_sel && a.row_sel[b] >= 0) return;
   const int keys = decode_keys_of(a, b), nb = (keys + BK - 1) / BK;
   Core core(a, lds + wave * Core::LDS, lane);
@@ -729,11 +733,17 @@ bool decode_fits(int64_t B, int64_t Hkv, int64_t R, int64_t keys) {
 template <class Core, bool PAGED>
 static hipError_t launch_decode_core(DecodeArgs& a, hipStream_t stream) {
   constexpr bool F32 = Core::BK == 16;
-  constexpr int NW = Core::NP > 8 ? 4 : 8;
   const int64_t units = (int64_t)a.B * a.Hkv * a.rbs, rows = (int64_t)a.B * a.Hkv * a.R;
   const int blocks = (int)(((int64_t)a.Sk + Core::BK - 1) / Core::BK);   // the most of a unit
-  if (blocks <= 32 && units <= (1 << 22)) {
-    hipLaunchKernelGGL((decode_unit_kernel<Core, PAGED, NW>), dim3((unsigned)units), dim3(NW * kWave), 0, stream, a);
+  if (blocks <= (units >= 256 ? 64 : 32) && units <= (1 << 22)) {
+    const int64_t heads = (int64_t)a.B * a.Hkv;
+    const dim3 grid((unsigned)(a.rbs == 1 ? heads : (heads + 7) / 8 * 8 * a.rbs));
+    if constexpr (Core::NP <= 8)
+      if (units <= 128) {
+        hipLaunchKernelGGL((decode_unit_kernel<Core, PAGED, 8>), grid, dim3(8 * kWave), 0, stream, a);
+        return hipGetLastError();
+      }
+    hipLaunchKernelGGL((decode_unit_kernel<Core, PAGED, 4>), grid, dim3(4 * kWave), 0, stream, a);
     return hipGetLastError();
   }
   a.waves = 4 * 256 * Core::WGS;
@@ -741,8 +751,10 @@ static hipError_t launch_decode_core(DecodeArgs& a, hipStream_t stream) {
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   constexpr int G = Core::NP * 4;
-  if (rows <= 1024) {
+  if (rows <= 256) {
     hipLaunchKernelGGL((decode_join_kernel<F32, G, 8>), dim3((unsigned)rows), dim3(8 * kWave), 0, stream, a);
+  } else if (rows <= 1024) {
+    hipLaunchKernelGGL((decode_join_kernel<F32, G, 4>), dim3((unsigned)rows), dim3(4 * kWave), 0, stream, a);
   } else {
     const int64_t wgs = (rows + 3) / 4;
     hipLaunchKernelGGL((decode_join_kernel<F32, G, 1>), dim3((unsigned)(wgs < 8192 ? wgs : 8192)), dim3(kThreads), 0, stream, a);
