@@ -439,19 +439,22 @@ def attncache_page_plan(seq_len: torch.Tensor, new_len: torch.Tensor, free_state
 
 def _pages(k_pages: torch.Tensor, v_pages: torch.Tensor, dtype, heads: int, D: int):
     """Addresses, page count, page size and page stride of [n,heads,page,D] arrays whose pages may lie further apart."""
-    if k_pages.dim() != 4 or tuple(k_pages.shape) != tuple(v_pages.shape) or k_pages.shape[1] != heads or k_pages.shape[3] != D:
+    shape = k_pages.shape
+    if len(shape) != 4 or shape != v_pages.shape or shape[1] != heads or shape[3] != D:
         raise ValueError(f"k_pages and v_pages must be [n_pages,{heads},page_size,{D}], have "
-                         f"{tuple(k_pages.shape)} and {tuple(v_pages.shape)}")
-    n, _, page, _ = k_pages.shape
-    dense = heads * page * D
-    stride = dense
-    if not (k_pages.is_contiguous() and v_pages.is_contiguous()):
-        stride = k_pages.stride(0) if n > 1 else dense
-        # (the stride of a dimension of one element says nothing)
-        inner = all(t.shape[d] == 1 or t.stride(d) == w for t in (k_pages, v_pages)
-                    for d, w in ((1, page * D), (2, D), (3, 1)))
-        if not inner or stride < dense or (n > 1 and v_pages.stride(0) != stride):
-            raise ValueError("k_pages and v_pages must be contiguous within a page and have one page stride")
+                         f"{tuple(shape)} and {tuple(v_pages.shape)}")
+    n, page = shape[0], shape[2]
+    stride = dense = heads * page * D
+    kp, vp = _address(k_pages, dtype, None), _address(v_pages, dtype, None)
+    if kp is not None and vp is not None:
+        return kp, vp, n, page, stride
+    if n > 1:
+        stride = k_pages.stride(0)
+    # (the stride of a dimension of one element says nothing)
+    inner = all(t.shape[d] == 1 or t.stride(d) == w for t in (k_pages, v_pages)
+                for d, w in ((1, page * D), (2, D), (3, 1)))
+    if not inner or stride < dense or (n > 1 and v_pages.stride(0) != stride):
+        raise ValueError("k_pages and v_pages must be contiguous within a page and have one page stride")
     for t, name in ((k_pages, "k_pages"), (v_pages, "v_pages")):
         if not t.is_cuda:
             raise ValueError(f"{name} must be a CUDA tensor")

@@ -5,7 +5,7 @@
 // ones.  With P the running sum of d over the requests, request b takes entries [P_b - d_b, P_b) of the free pages'
 // ring if P_b does not exceed what is there.  Ended requests put their pages behind the ring's last one; these places are
 // not among those that are read, so pages go both ways in one launch and without an order among workgroups.
-// Bound by latency: some 5 us of dependent loads (lengths -> sums -> ring -> slots) against microseconds of launch.
+// Bound by latency: dependent loads (lengths -> sums -> ring -> slots), 4.8 us for 64 requests of one token.
 #include "common.hpp"
 #include "serve.h"
 
@@ -80,17 +80,22 @@ __device__ __forceinline__ int row_of(const int* start, int rows, int e) {
   return lo;
 }
 
-// ROWS: page table, ring and slots of the workgroup's rows; STATE: the new lengths and the ring's new state, by one
-// workgroup, which reads every array that may be written in place before it writes it.  Small plans do both in one
-// workgroup (64 requests of one token 4.9 us, 9.2 in two launches); larger ones spread the rows over the chip, where
-// each workgroup sums what lies before its rows for itself, and a second launch writes the state.
-template <int NT, bool ROWS, bool STATE>
+// What workgroups do: kPlanAll one alone does everything (it reads every array that may be written in place before it writes it);
+// kPlanRows page table, ring and slots of its rows, summing what lies before them for itself; kPlanState one alone the new lengths
+// and the ring's new state; kPlanBoth the last one the state, the others rows, where no output is an input.
+// us: 256 prompts of up to 1,024 tokens 10.6 in two launches, 5.3 in one; 64 requests of one token 4.8 in one workgroup.
+enum PlanWork { kPlanAll, kPlanRows, kPlanState, kPlanBoth };
+template <int NT, PlanWork WORK>
 __global__ __launch_bounds__(NT) void page_plan_kernel(const PlanArgs a) {
+  const bool state_too = WORK == kPlanBoth && blockIdx.x == gridDim.x - 1;   // uniform
+  const bool rows_too = WORK == kPlanAll || WORK == kPlanRows || (WORK == kPlanBoth && !state_too);
+  const bool writes_state = WORK == kPlanAll || WORK == kPlanState || state_too;
+  if (state_too && blockIdx.y > 0) return;
   __shared__ int s_len[NT], s_have[NT], s_add[NT], s_new[NT], s_give[NT];
   __shared__ int2 part[NT / kWave];
   __shared__ int s_taken;
   const int tid = threadIdx.x;
-  const int r0 = blockIdx.x * a.rows, r1 = min(a.B, r0 + a.rows);
+  const int r0 = state_too ? 0 : blockIdx.x * a.rows, r1 = state_too ? a.B : min(a.B, r0 + a.rows);
   const int first = (int)((a.state[0] % a.n + a.n) % a.n), count = min(max(a.state[1], 0), a.n);
   int before_new = 0, before_give = 0;   // what the requests before this chunk need and give back
   if (r0 > 0) {
@@ -119,12 +124,12 @@ __global__ __launch_bounds__(NT) void page_plan_kernel(const PlanArgs a) {
     s_new[tid] = upto - r.need;
     s_give[tid] = given - r.give;
     if (served && r.need > 0) atomicMax(&s_taken, before_new + upto);
-    if (STATE && tid < rows) {
+    if (writes_state && tid < rows) {
       a.seq_out[b] = r.ended ? 0 : r.len + add;
       a.added[b] = add;
     }
     __syncthreads();
-    if (ROWS) {
+    if (rows_too) {
       // the served requests that need pages come before all others that do: theirs are the ring's next entries
       auto ring_at = [&](int i) {   // entry i < count of the free pages
         const unsigned at = (unsigned)first + (unsigned)i;
@@ -160,7 +165,7 @@ __global__ __launch_bounds__(NT) void page_plan_kernel(const PlanArgs a) {
     before_new += all_new;
     before_give += all_give;
   }
-  if (STATE && tid == 0) {
+  if (writes_state && tid == 0) {
     const int taken = s_taken;
     a.state_out[0] = (int)(((unsigned)first + (unsigned)taken) % (unsigned)a.n);
     a.state_out[1] = min(a.n, count - taken + before_give);
@@ -168,7 +173,7 @@ __global__ __launch_bounds__(NT) void page_plan_kernel(const PlanArgs a) {
 }
 
 constexpr int kPlanSmall = 4096;   // slots that one workgroup writes
-constexpr int kPlanSlots = 2048;   // slots of a workgroup beyond that
+constexpr int kPlanSlots = 1024;   // slots of a workgroup beyond that: 256 x 1,024 slots 5.3 us, 2,048 6.2; 2,000 x 500 24.6, 512 27.0
 hipError_t launch_plan(const PlanLaunch& p, hipStream_t stream) {
   PlanArgs a;
   a.seq_len = p.seq_len; a.new_len = p.new_len; a.state = p.free_state;
@@ -180,24 +185,30 @@ hipError_t launch_plan(const PlanLaunch& p, hipStream_t stream) {
   a.rows = p.B;
   a.seg = p.S;
   if ((int64_t)p.B * p.S <= kPlanSmall) {
-    hipLaunchKernelGGL((page_plan_kernel<1024, true, true>), dim3(1), dim3(1024), 0, stream, a);
+    hipLaunchKernelGGL((page_plan_kernel<1024, kPlanAll>), dim3(1), dim3(1024), 0, stream, a);
     return hipGetLastError();
   }
   PlanArgs r = a;
   r.rows = p.S >= kPlanSlots ? 1 : kPlanSlots / p.S;
   if (r.rows > kThreads) r.rows = kThreads;
   r.seg = p.S > kPlanSlots ? kPlanSlots : p.S;
-  const dim3 grid((unsigned)((p.B + r.rows - 1) / r.rows), (unsigned)((p.S + r.seg - 1) / r.seg));
-  hipLaunchKernelGGL((page_plan_kernel<kThreads, true, false>), grid, dim3(kThreads), 0, stream, r);
+  const unsigned gx = (unsigned)((p.B + r.rows - 1) / r.rows), gy = (unsigned)((p.S + r.seg - 1) / r.seg);
+  if (p.seq_len_out != p.seq_len && p.added != p.new_len && p.free_state_out != p.free_state) {
+    hipLaunchKernelGGL((page_plan_kernel<kThreads, kPlanBoth>), dim3(gx + 1, gy), dim3(kThreads), 0, stream, r);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL((page_plan_kernel<kThreads, kPlanRows>), dim3(gx, gy), dim3(kThreads), 0, stream, r);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((page_plan_kernel<1024, false, true>), dim3(1), dim3(1024), 0, stream, a);
+  hipLaunchKernelGGL((page_plan_kernel<1024, kPlanState>), dim3(1), dim3(1024), 0, stream, a);
   return hipGetLastError();
 }
 
 // K and V rows to their pages: row (b, h, t) of the source, [B][H][S][D], to page slot / p, place (h, slot % p).  Nothing is
 // computed: bound by memory, each byte read once and written once.  Both sides are whole lines: the rows of one head and
-// neighbouring tokens lie side by side in the source and, up to the end of a page, in the cache.
+// neighbouring tokens lie side by side in the source and, up to the end of a page, in the cache.  Two pieces a thread and tensor on
+// their way at once, streaming stores: 64 prompts of up to 128 tokens, 128 heads of 64 (291 MB) 61 us = 4.8 TB/s (four pieces 60,
+// one 66; ordinary stores 65); 1,000 tokens half of which are padding 54 us (four 77, one 55); 128 tokens of 8 heads of 128 2.6 (four 3.3).
 struct AppendArgs {
   const void *K, *V;
   const int32_t* slot;
@@ -206,7 +217,7 @@ struct AppendArgs {
   int64_t stride;                                     // of a page, in pieces
   Divider by_s, by_h, by_ps, by_ppr;
 };
-constexpr int kAppendPieces = 4;   // of a thread and tensor, on their way at once
+constexpr int kAppendPieces = 2;
 
 template <typename T>   // a piece: 16 bytes, or 4 where rows are no whole number of those
 __global__ __launch_bounds__(kThreads) void page_append_kernel(const AppendArgs a) {
@@ -232,8 +243,8 @@ __global__ __launch_bounds__(kThreads) void page_append_kernel(const AppendArgs 
 #pragma unroll
   for (int n = 0; n < kAppendPieces; ++n)
     if (to[n] >= 0) {
-      static_cast<T*>(a.kp)[to[n]] = k[n];
-      static_cast<T*>(a.vp)[to[n]] = v[n];
+      __builtin_nontemporal_store(k[n], static_cast<T*>(a.kp) + to[n]);
+      __builtin_nontemporal_store(v[n], static_cast<T*>(a.vp) + to[n]);
     }
 }
 
