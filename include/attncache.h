@@ -509,7 +509,7 @@ int32_t attncache_page_append(const void *K, const void *V,
  *              the lengths.  Calls that may overlap in time need one each.
  *
  * fp32 statistics and sums; bf16 weights are rounded once before the product
- * with V and the result once.  Two launches; deterministic.
+ * with V and the result once.  One launch, or two; deterministic.
  * B * Hkv * ceil(Hq / Hkv / 16) * ceil(max_pages * page_size / 16) below 2^31.
  */
 size_t attention_paged_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv,

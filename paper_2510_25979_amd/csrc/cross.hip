@@ -1,13 +1,19 @@
-// Attention of many rows to the states of another sequence: O = softmax(scale Q K^T) V with Sq rows and Sk keys, bf16.
+// Attention of many rows to the states of another sequence: O = softmax(scale Q K^T) V with Sq rows and Sk keys.
 // Nothing is causal, so the g Sq rows of the heads that share K and V are alike: one run of R rows, which lie side by side.
 //
-// A workgroup owns 128 of these rows, a wave 32, and walks the keys in chunks of 64 that are copied from memory straight into
+// bf16: a workgroup owns 128 of these rows, a wave 32, and walks the keys in chunks of 64 that are copied from memory straight into
 // one of two LDS stages (the next chunk under way while this one is multiplied, one barrier a chunk).  Both products are
 // formed transposed (S^T = K Q^T, O^T = V^T P^T), so that a lane holds scores of one row, and the weights go from the first
 // product to the second without leaving their registers.  4 Sk D flop a row against 4 Sk D / 128 bytes: the matrix cores and, more
-// so, the exponentials bound it.  Both blocks of a chunk take a softmax step of their own, in an order that lets matrix and vector
-// work of a wave overlap.
+// so, the vector work beside them at the clock the chip grants bound it.  16 x 32 heads, 1024 x 2047 keys of 128: 590 us = 0.93 PFLOP/s (a
+// library's 16384^3 product reaches 1.36 on the card, an 8192^3 one 1.25).  Both blocks of a chunk take a softmax step of their own, in an order that
+// lets matrix and vector work of a wave overlap.  Without the running maximum (reference points from the first block, a second walk
+// where a sum leaves the range) it took 550, but 64 x 64 heads 11.0 instead of 9.3; raised wave priority in either product or
+// the exponentials 600 to 608.
+#include <type_traits>
+
 #include "common.hpp"
+#include "f32_tile.hpp"
 #include "serve.h"
 
 namespace ac {
@@ -20,7 +26,7 @@ struct CrossArgs {
   const void *Q, *K, *V;
   void* O;
   const int32_t *len, *row_sel;
-  int32_t Hkv, R, Sk, first, tiles, per;   // first: of the launch's (item, K/V head) tiles; per: workgroups of a tile
+  int32_t Hkv, R, Sk, D, first, tiles, per;   // first: of the launch's (item, K/V head) tiles; per: workgroups of a tile
   float scale_log2e;
 };
 
@@ -245,36 +251,175 @@ __global__ __launch_bounds__(kThreads, 2) void cross_bf16_kernel(const CrossArgs
   }
 }
 
-static bool cross_by_rows(int64_t B, int64_t Hkv, int64_t R, int64_t Sk, int32_t is_f32) {
-  if (is_f32) return false;
-  if (!decode_fits(B, Hkv, R, Sk)) return true;
-  return R >= 64 && B * Hkv * ((R + kCrossRows - 1) / kCrossRows) >= 128;
-}
-size_t cross_workspace_bytes(int32_t B, int32_t Hkv, int32_t R, int32_t Sk, int32_t D, int32_t is_f32) {
-  return cross_by_rows(B, Hkv, R, Sk, is_f32) ? 0 : decode_workspace_bytes(R, D);
+// Binary32 (the layout of f32_tile.hpp): a wave owns 16 rows, four waves share stages of 32 keys in LDS, the next stage's
+// rows are in registers while this one is multiplied.  Each 16-byte read of K or V feeds four products of 32 cycles, so the matrix
+// cores bound it: 8 x 24 heads on 8, 1000 x 1000 keys of 128 (lengths 100 to 1000) 341 us = 112 TFLOP/s of the 154 of a large
+// product.  32 rows a wave halve the reads, but leave one wave where two hide each other's exponentials: 360.
+template <int DB, int COLS>
+__global__ __launch_bounds__(kThreads, DB <= 2 ? 2 : 1) void cross_f32_kernel(const CrossArgs a) {
+  constexpr int KC = 32, NB = KC / kF32Rows;
+  typedef F32Stage<DB, KC, COLS> Stage;
+  const int D = COLS == kAllCols ? 64 * DB : a.D;
+  __shared__ __attribute__((aligned(16))) float kl[KC * Stage::LD];
+  __shared__ __attribute__((aligned(16))) float vl[KC * Stage::LD];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int i = lane & 15, kq = lane >> 4;
+  const int slot = blockIdx.x >> 3, u = a.first + slot / a.per * 8 + (blockIdx.x & 7);
+  if (u >= a.tiles) return;
+  const int b = u / a.Hkv;
+  if (a.row_sel && a.row_sel[b] >= 0) return;
+  const int keys = a.len ? min(max(a.len[b], 0), a.Sk) : a.Sk;
+  const int r0 = (slot % a.per * 4 + wave) * kF32Rows;   // this wave's first row
+  float* O = reinterpret_cast<float*>(a.O) + (size_t)u * a.R * D;
+  if (keys == 0) {
+    const int n = min(kF32Rows, a.R - r0) * D;
+    for (int p = lane; p < n; p += kWave) O[(size_t)r0 * D + p] = 0.f;
+    return;
+  }
+  const float* K = reinterpret_cast<const float*>(a.K) + (size_t)u * a.Sk * D;
+  const float* V = reinterpret_cast<const float*>(a.V) + (size_t)u * a.Sk * D;
+  f32x4 q[4 * DB], acc[4 * DB];
+  {   // (rows beyond the last work on a copy of it)
+    const float* src = reinterpret_cast<const float*>(a.Q) + ((size_t)u * a.R + min(r0 + i, a.R - 1)) * D;
+#pragma unroll
+    for (int kk = 0; kk < 4 * DB; ++kk) {
+      const int c = 16 * kk + 4 * kq;
+      q[kk] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (COLS == kAllCols || c + 4 <= D) {
+        q[kk] = *reinterpret_cast<const f32x4_dw*>(src + c);
+      } else {
+#pragma unroll
+        for (int x = 0; x < 3; ++x)
+          if (c + x < D) q[kk][x] = src[c + x];
+      }
+    }
+  }
+#pragma unroll
+  for (int x = 0; x < 4 * DB; ++x) acc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+  Stage ks, vs;
+  ks.load(K, 0, keys, D, tid);
+  vs.load(V, 0, keys, D, tid);
+  for (int j0 = 0; j0 < keys; j0 += KC) {
+    ks.template mask<false>(j0, keys, D, tid);   // (scores of keys that are not there are replaced)
+    vs.template mask<true>(j0, keys, D, tid);
+    __syncthreads();   // the previous stage has been read by everybody
+    ks.commit(kl, tid);
+    vs.commit(vl, tid);
+    __syncthreads();
+    if (j0 + KC < keys) {
+      ks.load(K, j0 + KC, keys, D, tid);
+      vs.load(V, j0 + KC, keys, D, tid);
+    }
+    f32x4 s[NB];
+#pragma unroll
+    for (int bk = 0; bk < NB; ++bk) {
+      s[bk] = f32x4{0.f, 0.f, 0.f, 0.f};
+      const float* row = kl + (kF32Rows * bk + i) * Stage::LD + 4 * kq;
+      f32x4 k = *reinterpret_cast<const f32x4*>(row);
+#pragma unroll
+      for (int kk = 0; kk < 4 * DB; ++kk)
+        if (COLS == kAllCols || 16 * kk < D) {   // uniform
+          const f32x4 next = *reinterpret_cast<const f32x4*>(row + 16 * ((kk + 1) & (4 * DB - 1)));
+#pragma unroll
+          for (int x = 0; x < 4; ++x) s[bk] = mfma_f32(k[x], q[kk][x], s[bk]);
+          k = next;
+          __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    if (j0 + KC > keys) {
+#pragma unroll
+      for (int bk = 0; bk < NB; ++bk)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          if (j0 + kF32Rows * bk + 4 * kq + x >= keys) s[bk][x] = -INFINITY;
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int bk = 0; bk < NB; ++bk)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) mx = fmaxf(mx, s[bk][x]);
+    mx = fmaxf(mx, __shfl_xor(mx, 16));
+    mx = fmaxf(mx, __shfl_xor(mx, 32));
+    const float m_new = fmaxf(m, mx * a.scale_log2e);
+    if (__any(m_new > m)) {
+      const float alpha = m_new > m ? __builtin_amdgcn_exp2f(m - m_new) : 1.f;
+      l *= alpha;
+#pragma unroll
+      for (int x = 0; x < 4 * DB; ++x) acc[x] *= alpha;
+      m = m_new;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;   // no finite score so far: all weights are zero
+#pragma unroll
+    for (int bk = 0; bk < NB; ++bk) {
+      f32x4 p;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        p[x] = __builtin_amdgcn_exp2f(fmaf(s[bk][x], a.scale_log2e, -ref));
+        l += p[x];
+      }
+      f32_weights_v<DB>(acc, vl + kF32Rows * bk * Stage::LD, p, i, kq);
+    }
+  }
+  float sum = l + __shfl_xor(l, 16);
+  sum += __shfl_xor(sum, 32);
+  if (r0 + i < a.R)
+    f32_store_row<DB, COLS, true>(O + (size_t)(r0 + i) * D, acc, sum == 0.f ? 1.f : sum, kq, D);
 }
 
-hipError_t launch_cross(const DecodeLaunch& p, hipStream_t stream) {
-  if (!cross_by_rows(p.B, p.Hkv, p.R, p.Sk, p.is_f32)) return launch_decode(p, stream);
-  CrossArgs a;
-  a.Q = p.Q; a.K = p.K; a.V = p.V; a.O = p.O; a.len = p.len; a.row_sel = p.row_sel;
-  a.Hkv = p.Hkv; a.R = p.R; a.Sk = p.Sk;
-  a.tiles = p.B * p.Hkv;
-  a.per = (p.R + kCrossRows - 1) / kCrossRows;
-  const float scale = p.scale == 0.f ? 1.0f / sqrtf((float)p.D) : p.scale;
-  a.scale_log2e = scale * 1.44269504088896340736f;
-  // tiles of a launch: a multiple of 8, at most 2^23 workgroups
+// Few rows leave most of these kernels' waves without any, and few workgroups most of the chip; decode.hip splits the keys instead,
+// and reads K and V again for every 16 rows.  us, there / here.  bf16, heads x rows x keys, by units of 16 rows: 128 x 32 x 1000 (256
+// units) 11.2 / 17.9 of 64, 18.4 / 25.5 of 128; 128 x 64 x 1000 (512) 18.5 / 18.0 and 32.5 / 25.9; 16 x 500 x 1500 (512) 24.2 / 22.6 and
+// 45.9 / 33.7; 512 x 32 x 100 (1,024) 7.8 / 7.7 and 12.5 / 12.3; 512 x 32 x 1000 33.9 / 27.6 and 66.4 / 53.1.  Binary32, by workgroups of 64
+// rows: 64 x 70 x 200 of 128 (128) 17.3 / 23.0; 64 x 282 x 333, ragged (320) 39.0 / 37.6, of 256 110 / 86; x 1000, ragged 64.7 / 76.6, 256 x 64 x
+// 1000, not ragged (256) 117 / 92; 512 x 40 x 300 (512) 60.9 / 54.6; 512 x 20 x 500 68.1 / 84.7.
+static bool cross_by_rows(int64_t B, int64_t Hkv, int64_t R, int64_t Sk, int32_t D, int32_t is_f32) {
+  const int64_t heads = B * Hkv;
+  if (is_f32) return D >= 4 && R > 32 && heads * ((R + 4 * kF32Rows - 1) / (4 * kF32Rows)) >= (D > 128 || Sk <= 512 ? 256 : 512);
+  return !decode_fits(B, Hkv, R, Sk) || (R > 16 && heads * ((R + 15) / 16) >= 512);
+}
+size_t cross_workspace_bytes(int32_t B, int32_t Hkv, int32_t R, int32_t Sk, int32_t D, int32_t is_f32) {
+  return cross_by_rows(B, Hkv, R, Sk, D, is_f32) ? 0 : decode_workspace_bytes(R, D);
+}
+
+// All tiles, in launches of at most 2^23 workgroups (a multiple of eight tiles each).
+template <typename Kernel>
+static hipError_t cross_tiles(Kernel kernel, CrossArgs a, hipStream_t stream) {
   const int64_t most = ((1 << 23) / a.per > 8 ? (1 << 23) / a.per : 8) & ~7LL;
   for (int64_t first = 0; first < a.tiles; first += most) {
     a.first = (int)first;
     const int64_t n = a.tiles - first < most ? a.tiles - first : most;
-    const dim3 grid((unsigned)((n + 7) / 8 * 8 * a.per));
-    if (p.D == 64) hipLaunchKernelGGL((cross_bf16_kernel<64>), grid, dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL((cross_bf16_kernel<128>), grid, dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((n + 7) / 8 * 8 * a.per)), dim3(kThreads), 0, stream, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
+}
+
+template <int DB, int COLS>
+static hipError_t launch_cross_f32(CrossArgs a, hipStream_t stream) {
+  a.per = (a.R + 4 * kF32Rows - 1) / (4 * kF32Rows);
+  return cross_tiles(&cross_f32_kernel<DB, COLS>, a, stream);
+}
+
+hipError_t launch_cross(const DecodeLaunch& p, hipStream_t stream) {
+  if (!cross_by_rows(p.B, p.Hkv, p.R, p.Sk, p.D, p.is_f32)) return launch_decode(p, stream);
+  CrossArgs a;
+  a.Q = p.Q; a.K = p.K; a.V = p.V; a.O = p.O; a.len = p.len; a.row_sel = p.row_sel;
+  a.Hkv = p.Hkv; a.R = p.R; a.Sk = p.Sk; a.D = p.D;
+  a.first = 0;
+  a.tiles = p.B * p.Hkv;
+  a.per = (p.R + kCrossRows - 1) / kCrossRows;
+  const float scale = p.scale == 0.f ? 1.0f / sqrtf((float)p.D) : p.scale;
+  a.scale_log2e = scale * 1.44269504088896340736f;
+  if (!p.is_f32)
+    return p.D == 64 ? cross_tiles(&cross_bf16_kernel<64>, a, stream) : cross_tiles(&cross_bf16_kernel<128>, a, stream);
+  if (p.D == 64) return launch_cross_f32<1, kAllCols>(a, stream);
+  if (p.D == 128) return launch_cross_f32<2, kAllCols>(a, stream);
+  if (p.D < 64) return p.D % 4 ? launch_cross_f32<1, kAnyCols>(a, stream) : launch_cross_f32<1, kVecCols>(a, stream);
+  if (p.D < 128) return p.D % 4 ? launch_cross_f32<2, kAnyCols>(a, stream) : launch_cross_f32<2, kVecCols>(a, stream);
+  return p.D % 4 ? launch_cross_f32<4, kAnyCols>(a, stream) : launch_cross_f32<4, kVecCols>(a, stream);
 }
 
 }  // namespace ac

@@ -735,6 +735,10 @@ static hipError_t launch_decode_core(DecodeArgs& a, hipStream_t stream) {
   constexpr bool F32 = Core::BK == 16;
   const int64_t units = (int64_t)a.B * a.Hkv * a.rbs, rows = (int64_t)a.B * a.Hkv * a.R;
   const int blocks = (int)(((int64_t)a.Sk + Core::BK - 1) / Core::BK);   // the most of a unit
+  // One launch where no item can have many blocks: the longest unit is then over before a second launch would be.  us, runs and join /
+  // units, bf16 on pages: 4 x 8 heads of 64, up to 1,008 tokens (32 blocks) 9.7 / 8.5, up to 2,000 (63) 9.8 / 12.3; 128 units of 128, 1,000
+  // tokens 23.7 / 19.6, 2,000 31.9 / 33.2; 256 units, 2,000 65.9 / 49.4; 1,024 units, 100 to 4,000 tokens (125) 231 / 252, 128 to 4,096 129 / 156,
+  // all 4,000 711 / 685.  Eight waves a unit / four: the first 8.5 / 9.2, 128 units 19.5 / 19.7, 512 units of 500 tokens 26.3 / 23.2.
   if (blocks <= (units >= 256 ? 64 : 32) && units <= (1 << 22)) {
     const int64_t heads = (int64_t)a.B * a.Hkv;
     const dim3 grid((unsigned)(a.rbs == 1 ? heads : (heads + 7) / 8 * 8 * a.rbs));
@@ -750,6 +754,8 @@ static hipError_t launch_decode_core(DecodeArgs& a, hipStream_t stream) {
   hipLaunchKernelGGL((decode_run_kernel<Core, PAGED>), dim3((unsigned)(a.waves / 4)), dim3(kThreads), 0, stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
+  // waves of an output row: 32 rows of 64 partial results each take eight, thousands of two or three one (1,024 rows with eight 9.3 us
+  // of launching waves, 2,048 with one 5.4)
   constexpr int G = Core::NP * 4;
   if (rows <= 256) {
     hipLaunchKernelGGL((decode_join_kernel<F32, G, 8>), dim3((unsigned)rows), dim3(8 * kWave), 0, stream, a);

@@ -46,11 +46,14 @@ def _check(O, Q, K, V, lens, items, scale=None):
 # B, Hq, Hkv, Sq, Sk: one row and many, one key and many, few and many heads on a K and V
 SIZES = [(1, 1, 1, 1, 1), (3, 4, 2, 1, 50), (2, 6, 2, 5, 1), (5, 3, 3, 33, 65), (2, 8, 1, 9, 200), (1, 40, 1, 1, 700),
          (1, 2, 2, 100, 3001), (4, 12, 12, 1, 1000), (40, 4, 4, 64, 64), (33, 8, 4, 65, 127), (9, 16, 16, 129, 31), (70, 6, 2, 23, 130),
-         (2, 64, 32, 260, 333), (130, 1, 1, 200, 97), (1, 1, 1, 1, 70001)]
+         (2, 64, 32, 260, 333), (130, 1, 1, 200, 97), (1, 1, 1, 1, 70001),
+         (70, 8, 8, 33, 40), (130, 6, 3, 40, 70), (3, 40, 2, 1, 2500), (260, 4, 4, 33, 20), (20, 12, 12, 1, 100),
+         (400, 6, 3, 1, 1100)]
+TYPES = [(64, "bf16"), (128, "bf16"), (64, "f32"), (128, "f32"), (3, "f32"), (33, "f32"), (36, "f32"), (80, "f32"), (101, "f32"), (199, "f32"), (256, "f32")]
 
 
 @pytest.mark.parametrize("padded", [False, True])
-@pytest.mark.parametrize("D,dt", [(64, "bf16"), (128, "bf16"), (64, "f32"), (128, "f32"), (3, "f32"), (80, "f32"), (199, "f32"), (256, "f32")])
+@pytest.mark.parametrize("D,dt", TYPES)
 @pytest.mark.parametrize("size", SIZES, ids=str)
 def test_sizes(ac, size, D, dt, padded):  # noqa: F811
     B, Hq, Hkv, Sq, Sk = size

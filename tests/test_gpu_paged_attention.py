@@ -19,8 +19,8 @@ class Cache:
         held = [-(-n // page) for n in lens]
         n = sum(held) + spare
         size = Hkv * page * D + more
-        room = torch.full((2, n, size), float("nan"), device="cuda", dtype=DT[dt])
-        self.k, self.v = (room[i].as_strided((n, Hkv, page, D), (size, page * D, D, 1), i * n * size) for i in range(2))
+        self.k, self.v = (torch.full((n, size), float("nan"), device="cuda", dtype=DT[dt]).as_strided(
+            (n, Hkv, page, D), (size, page * D, D, 1)) for _ in range(2))
         order = torch.randperm(n, generator=torch.Generator().manual_seed(seed)).tolist()
         width = max(max(held), 1) if width is None else width
         self.table = torch.full((len(lens), width), -1, dtype=torch.int32)
@@ -66,24 +66,76 @@ def _case(ac, lens, Hq, Hkv, D, dt, page, **kw):  # noqa: F811
 EDGES = [0, 1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 0, 127, 128, 129, 300]
 
 
-@pytest.mark.parametrize("page", [1, 7, 16, 32, 48, 128])
-@pytest.mark.parametrize("D,dt", [(64, "bf16"), (128, "bf16"), (64, "f32"), (128, "f32"), (1, "f32"), (33, "f32"), (80, "f32"),
-                                  (199, "f32"), (256, "f32")])
+PAGES = [1, 7, 16, 32, 48, 128]
+TYPES = [(64, "bf16"), (128, "bf16"), (64, "f32"), (128, "f32"), (1, "f32"), (33, "f32"), (80, "f32"), (199, "f32"), (256, "f32")]
+HEADS = [(1, 1), (5, 1), (12, 12), (32, 8), (16, 1), (17, 1), (33, 1), (40, 2), (64, 1)]
+RAGGED = [[1], [5000], [70001], [3] * 300, [40] * 700 + [9000], [9000] + [0] * 200, [0] * 130 + [77],
+          [100, 20000, 5, 5, 5, 17, 3000], [513] * 64]
+RAGGED_TYPES = [(4, 1, 128, "bf16"), (8, 8, 64, "bf16"), (3, 3, 128, "f32")]
+# tables of many pages: runs of blocks over all requests.  Rows of several blocks of 16, odd dimensions, lengths of zero between others,
+# more requests than lanes
+RUNS = [([70, 0, 4000, 31, 0, 0, 1, 2500], 40, 2, 64, "bf16", 16), ([3001, 64, 65], 17, 1, 128, "bf16", 7),
+        ([2100] * 9 + [0] * 70 + [33] * 60 + [5000], 24, 8, 128, "bf16", 48), ([40] * 701 + [9000], 8, 8, 128, "bf16", 16),
+        ([9000, 1] * 40, 2, 2, 64, "bf16", 128), ([2049], 64, 1, 64, "bf16", 1), ([1500, 0, 40, 1100], 6, 2, 80, "f32", 10),
+        ([1030, 16, 17, 0, 2000], 20, 1, 33, "f32", 16), ([1200] * 30 + [5] * 90, 2, 1, 199, "f32", 7), ([1025, 3], 33, 1, 256, "f32", 32),
+        ([30] * 200 + [1700] * 3, 4, 4, 64, "f32", 16), ([2000, 70], 3, 3, 3, "f32", 5),
+        ([1030] + [3] * 350, 4, 2, 64, "f32", 16), ([1030] + [3] * 350, 4, 2, 256, "f32", 16), ([1030] + [3] * 100, 4, 2, 256, "f32", 16), ([8000, 1, 700], 12, 4, 128, "f32", 64)]
+
+
+@pytest.mark.parametrize("page", PAGES)
+@pytest.mark.parametrize("D,dt", TYPES)
 def test_lengths_around_blocks_and_pages(ac, page, D, dt):  # noqa: F811
     _case(ac, EDGES, 6, 2, D, dt, page)
 
 
+@pytest.mark.parametrize("D,dt", TYPES)
+def test_many_short_requests(ac, D, dt):  # noqa: F811
+    _case(ac, EDGES * 5, 6, 2, D, dt, 16)
+
+
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
-@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (5, 1), (12, 12), (32, 8), (16, 1), (17, 1), (33, 1), (40, 2), (64, 1)])
+@pytest.mark.parametrize("Hq,Hkv", HEADS)
 def test_head_layouts(ac, Hq, Hkv, dt):  # noqa: F811
     _case(ac, [70, 1, 600, 33], Hq, Hkv, 64, dt, 16)
 
 
-@pytest.mark.parametrize("lens", [[1], [5000], [70001], [3] * 300, [40] * 700 + [9000], [9000] + [0] * 200, [0] * 130 + [77],
-                                  [100, 20000, 5, 5, 5, 17, 3000], [513] * 64], ids=lambda x: f"{len(x)}x{max(x)}")
-@pytest.mark.parametrize("Hq,Hkv,D,dt", [(4, 1, 128, "bf16"), (8, 8, 64, "bf16"), (3, 3, 128, "f32")])
+@pytest.mark.parametrize("lens", RAGGED, ids=lambda x: f"{len(x)}x{max(x)}")
+@pytest.mark.parametrize("Hq,Hkv,D,dt", RAGGED_TYPES)
 def test_ragged_batches(ac, lens, Hq, Hkv, D, dt):  # noqa: F811
     _case(ac, lens, Hq, Hkv, D, dt, 16)
+
+
+@pytest.mark.parametrize("case", RUNS, ids=lambda c: f"{len(c[0])}x{max(c[0])}-" + "-".join(map(str, c[1:])))
+def test_runs_over_many_units(ac, case):  # noqa: F811
+    lens, Hq, Hkv, D, dt, page = case
+    c, Q, O = _case(ac, lens, Hq, Hkv, D, dt, page)
+    # every row: a few at a time against one product in 64 bits, or that nothing was left as it was
+    assert O.isfinite().all() and (O != 7.0).any(-1).all()
+    assert (O[c.len == 0] == 0).all()
+
+
+@pytest.mark.parametrize("seed", range(16))
+def test_drawn_batches(ac, seed):  # noqa: F811
+    import random
+    rng = random.Random(seed)
+    Hkv = rng.choice([1, 2, 3, 8])
+    Hq = Hkv * rng.choice([1, 2, 4, 5, 19])
+    D, dt = rng.choice([(64, "bf16"), (128, "bf16"), (64, "f32"), (100, "f32")])
+    top = rng.choice([40, 600, 2500, 6000])
+    lens = [rng.choice([0, 1, top, rng.randint(0, top), rng.randint(0, 70)]) for _ in range(rng.choice([1, 3, 20, 150]))]
+    c = Cache(lens, Hkv, D, dt, rng.choice([1, 5, 16, 64]), seed, width=rng.choice([None, 6000]))
+    Q = torch.randn(len(lens), Hq, D, generator=c.gen, device="cuda").to(DT[dt])
+    O = c.call(ac, Q)
+    assert O.isfinite().all() and (O[c.len == 0] == 0).all()
+    c.check(O, Q)
+
+
+@pytest.mark.parametrize("Hq,D", [(1, 64), (4, 128), (16, 64)])
+def test_each_row_of_many_short_requests_and_a_long_one(ac, Hq, D):  # noqa: F811
+    """All requests alike but one: each result is compared."""
+    c = Cache([40] * 640 + [9000] + [64] * 60, 1, D, "bf16", 16, Hq)
+    Q = torch.randn(701, Hq, D, generator=c.gen, device="cuda").bfloat16()
+    c.check(c.call(ac, Q), Q)
 
 
 def test_nothing_to_attend_to(ac):  # noqa: F811
