@@ -63,43 +63,54 @@ __device__ __forceinline__ int decode_keys_of(const DecodeArgs& a, int b) {
 template <int BK>
 struct DecodeWalk {
   const DecodeArgs& a;
-  int lane, per, total;
+  int lane, units, head, per, total;   // units of an item; costs of the first 64 items up to this lane's
   __device__ __forceinline__ int cost(int b) const {   // of a unit of item b
-    const int keys = decode_keys(a, b);
+    const int keys = b < a.B ? decode_keys(a, b) : 0;
     return keys ? (keys + BK - 1) / BK + kUnitCost : 0;
   }
-  // number of the first block of item `item`
-  __device__ __forceinline__ int start(int item) const {
+  __device__ __forceinline__ int upto(int t) const {   // sum over the lanes up to this one
+#pragma unroll
+    for (int off = 1; off < kWave; off <<= 1) {
+      const int p = __shfl_up(t, off);
+      if (lane >= off) t += p;
+    }
+    return t;
+  }
+  // costs of the items from 64 to `end`
+  __device__ __forceinline__ int further(int end) const {
     int t = 0;
-    for (int b = lane; b < item; b += kWave) t += cost(b);
+    for (int b = kWave + lane; b < end; b += kWave) t += cost(b);
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) t += __shfl_xor(t, off);
-    return __builtin_amdgcn_readfirstlane(t) * (a.Hkv * a.rbs);
+    return __builtin_amdgcn_readfirstlane(t);
   }
-  __device__ __forceinline__ DecodeWalk(const DecodeArgs& a, int lane) : a(a), lane(lane) {
-    total = start(a.B);
+  __device__ __forceinline__ DecodeWalk(const DecodeArgs& a, int lane) : a(a), lane(lane), units(a.Hkv * a.rbs) {
+    head = upto(cost(lane));
+    int t = __builtin_amdgcn_readlane(head, kWave - 1);
+    if (a.B > kWave) t += further(a.B);
+    total = t * units;
     // Runs of one block as long as every second wave has none: more partial results cost the join more than the runs save (one
     // request of 8,000 tokens of 8 heads of 128, 2,016 blocks for 2,048 waves: 18.6 us, runs of two 16.9; of 2,000 tokens 11.7 / 13.2).
     per = 2 * total <= a.waves ? 1 : max(2, (total + a.waves - 1) / a.waves);
   }
+  // number of the first block of item `item`
+  __device__ __forceinline__ int start(int item) const {
+    if (item == 0) return 0;
+    if (item <= kWave) return __builtin_amdgcn_readlane(head, item - 1) * units;
+    return (__builtin_amdgcn_readlane(head, kWave - 1) + further(item)) * units;
+  }
   // the item that block x < total belongs to; x becomes the block's number in it
   __device__ __forceinline__ int locate(int& x) const {
-    int before = 0;
+    int before = 0, t = head;
     for (int b0 = 0;; b0 += kWave) {
-      int t = b0 + lane < a.B ? cost(b0 + lane) * (a.Hkv * a.rbs) : 0;
-#pragma unroll
-      for (int off = 1; off < kWave; off <<= 1) {
-        const int p = __shfl_up(t, off);
-        if (lane >= off) t += p;
-      }
-      const unsigned long long beyond = __ballot(x < before + t);
+      const unsigned long long beyond = __ballot(x < before + t * units);
       if (beyond || b0 + kWave >= a.B) {
         const int i = beyond ? __builtin_ctzll(beyond) : 0;
-        const int prev = __shfl(t, max(i - 1, 0));
-        x = __builtin_amdgcn_readfirstlane(x - before - (i > 0 ? prev : 0));
+        x = __builtin_amdgcn_readfirstlane(x) - before - (i > 0 ? __builtin_amdgcn_readlane(t, i - 1) * units : 0);
         return b0 + i;
       }
-      before += __builtin_amdgcn_readlane(t, kWave - 1);
+      before += __builtin_amdgcn_readlane(t, kWave - 1) * units;
+      t = upto(cost(b0 + kWave + lane));
     }
   }
 };
@@ -413,13 +424,12 @@ __global__ __launch_bounds__(kThreads, Core::OCC) void decode_run_kernel(const D
     it.keys = keys;
     it.nb = (keys + BK - 1) / BK;
   };
-  const int units = a.Hkv * a.rbs;
   auto next = [&](DecodeItem& it) {   // false: the run ends
     const bool last = it.blk + 1 == it.nb;
     it.left -= last ? 1 + kUnitCost : 1;
     it.blk = last ? 0 : it.blk + 1;
     it.unit += last ? 1 : 0;
-    if (it.unit == units && it.left > 0) item(it, it.b + 1);
+    if (it.unit == walk.units && it.left > 0) item(it, it.b + 1);
     return it.left > 0;
   };
   DecodeItem now, then, later;

@@ -184,6 +184,10 @@ hipError_t launch_plan(const PlanLaunch& p, hipStream_t stream) {
   a.by_ps = Divider((uint32_t)p.page_size);
   a.rows = p.B;
   a.seg = p.S;
+  if ((int64_t)p.B * p.S <= kThreads) {
+    hipLaunchKernelGGL((page_plan_kernel<kThreads, kPlanAll>), dim3(1), dim3(kThreads), 0, stream, a);
+    return hipGetLastError();
+  }
   if ((int64_t)p.B * p.S <= kPlanSmall) {
     hipLaunchKernelGGL((page_plan_kernel<1024, kPlanAll>), dim3(1), dim3(1024), 0, stream, a);
     return hipGetLastError();
