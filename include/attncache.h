@@ -454,7 +454,9 @@ int32_t attncache_project(const void *h, const int32_t *seq_len,
  * ring has left takes nothing (added 0), and so do all after it that need a
  * page; those whose last page has room are served.  One that would outgrow
  * its max_pages takes nothing either.  Pages given back are the ring's for the
- * next call; they go behind its last one in order of request and place.
+ * next call; they go behind its last one in order of request and place.  A
+ * page is free or one request's: nothing may be in the ring or the tables
+ * twice (attention_paged, which only reads, may be given shared pages).
  * The outputs seq_len_out, added, free_state_out may be seq_len, new_len,
  * free_state (a captured step then continues from where the last replay
  * ended); other arrays must not overlap.  B <= 2^22, S <= 2^26,

@@ -5,11 +5,9 @@
 // one of two LDS stages (the next chunk under way while this one is multiplied, one barrier a chunk).  Both products are
 // formed transposed (S^T = K Q^T, O^T = V^T P^T), so that a lane holds scores of one row, and the weights go from the first
 // product to the second without leaving their registers.  4 Sk D flop a row against 4 Sk D / 128 bytes: the matrix cores and, more
-// so, the vector work beside them at the clock the chip grants bound it.  16 x 32 heads, 1024 x 2047 keys of 128: 590 us = 0.93 PFLOP/s (a
-// library's 16384^3 product reaches 1.36 on the card, an 8192^3 one 1.25).  Both blocks of a chunk take a softmax step of their own, in an order that
-// lets matrix and vector work of a wave overlap.  Without the running maximum (reference points from the first block, a second walk
-// where a sum leaves the range) it took 550, but 64 x 64 heads 11.0 instead of 9.3; raised wave priority in either product or
-// the exponentials 600 to 608.
+// so, the vector work beside them at the clock the chip grants bound it.  16 x 32 heads, 1024 x 2047 keys of 128: 555 us = 0.99 PFLOP/s (a
+// library's 16384^3 product reaches 1.36 on the card, an 8192^3 one 1.25).  Both blocks of a chunk take a softmax step of their own, in an
+// order that lets matrix and vector work of a wave overlap.  Raised wave priority in either product or in the exponentials: 2 to 3 % slower.
 #include <type_traits>
 
 #include "common.hpp"
@@ -21,6 +19,8 @@ namespace ac {
 constexpr int kCrossChunk = 64;
 constexpr int kCrossRows = 128;        // rows of a workgroup
 constexpr float kCrossSlack = 8.0f;    // the reference point of a row moves when a score has outgrown it by 2^8
+constexpr float kCrossRange = 1e18f;   // the largest sum of weights against a point that does not move
+constexpr int kCrossLong = 10;         // chunks from which on it does not
 
 struct CrossArgs {
   const void *Q, *K, *V;
@@ -30,7 +30,7 @@ struct CrossArgs {
   float scale_log2e;
 };
 
-template <int D>
+template <int D, bool STAY>   // STAY: reference points may stay where the first keys put them (below)
 __global__ __launch_bounds__(kThreads, 2) void cross_bf16_kernel(const CrossArgs a) {
   constexpr int PPR = D / 8;                              // 16-byte pieces of a row
   constexpr int NCOPY = kCrossChunk * PPR / kWave / 4;    // copy instructions of a wave, tensor and chunk
@@ -119,11 +119,7 @@ __global__ __launch_bounds__(kThreads, 2) void cross_bf16_kernel(const CrossArgs
     for (int ks = 0; ks < D / 16; ++ks) q[ks] = *reinterpret_cast<const u32x4*>(src + 16 * ks);
   }
   f32x16 acc[D / 32];
-#pragma unroll
-  for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-    for (int v = 0; v < 16; ++v) acc[db][v] = 0.f;
-  float m_run = -INFINITY, l_run = 0.f;
+  float m_run, l_run;
 
   auto qk = [&](const bf16_t* kb, int jb) {
     f32x16 s;
@@ -176,12 +172,13 @@ __global__ __launch_bounds__(kThreads, 2) void cross_bf16_kernel(const CrossArgs
       for (int v = 0; v < 16; ++v) acc[db][v] *= alpha;
   };
   // One chunk of two blocks: the scores of block 1 are requested before the exponentials of block 0, the second product of
-  // block 0 before the exponentials of block 1.  `there` keys of the chunk exist (TAIL; all 64 otherwise).
-  auto step = [&](const bf16_t* kb, const bf16_t* vb, int there, const bool TAIL) __attribute__((always_inline)) {
+  // block 0 before the exponentials of block 1.  `there` keys of the chunk exist (TAIL; all 64 otherwise).  FOLLOW: the reference
+  // point of a row follows its largest score; otherwise it stays what it is.
+  auto step = [&](const bf16_t* kb, const bf16_t* vb, int there, const bool TAIL, const bool FOLLOW) __attribute__((always_inline)) {
     const bool two = !TAIL || there > 32;
     f32x16 s0 = qk(kb, 0);
     if (TAIL) hide(s0, there);
-    {
+    if (FOLLOW) {
       const float cand = fmaxf(m_run, row_max(s0) * scale_log2e);
       if (__any(cand > m_run + kCrossSlack)) {
         rescale(cand);
@@ -196,9 +193,13 @@ __global__ __launch_bounds__(kThreads, 2) void cross_bf16_kernel(const CrossArgs
     l_run += sum;
     if (two) {
       if (TAIL) hide(s1, there - 32);
-      const float cand = fmaxf(m_run, row_max(s1) * scale_log2e);
-      const bool moved = __any(cand > m_run + kCrossSlack);
-      const float m1 = moved ? cand : m_run;
+      float m1 = m_run;
+      bool moved = false;
+      if (FOLLOW) {
+        const float cand = fmaxf(m_run, row_max(s1) * scale_log2e);
+        moved = __any(cand > m_run + kCrossSlack);
+        if (moved) m1 = cand;
+      }
       pv(vb, 0, p0);
       u32x4 p1[2];
       float sum1 = 0.f;
@@ -217,22 +218,51 @@ __global__ __launch_bounds__(kThreads, 2) void cross_bf16_kernel(const CrossArgs
   };
 
   const int n_chunk = (keys + kCrossChunk - 1) / kCrossChunk, full = keys / kCrossChunk;
-  int c = 0;
-  for (; c + 1 < full; c += 2) {   // (two chunks a trip: the stages alternate without pointer arithmetic)
-    publish();
-    copy(kb1, vb1, c + 1);
-    step(kb0, vb0, 0, false);
-    publish();
-    if (c + 2 < n_chunk) copy(kb0, vb0, c + 2);
-    step(kb1, vb1, 0, false);
+  auto walk = [&](const bool FOLLOW) __attribute__((always_inline)) {
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[db][v] = 0.f;
+    m_run = -INFINITY;
+    l_run = 0.f;
+    if (!FOLLOW) {   // the reference point of each row: the largest score of the first 32 keys
+      publish();
+      m_run = row_max(qk(kb0, 0)) * scale_log2e;
+    }
+    int c = 0;
+    for (; c + 1 < full; c += 2) {   // (two chunks a trip: the stages alternate without pointer arithmetic)
+      publish();
+      copy(kb1, vb1, c + 1);
+      step(kb0, vb0, 0, false, FOLLOW);
+      publish();
+      if (c + 2 < n_chunk) copy(kb0, vb0, c + 2);
+      step(kb1, vb1, 0, false, FOLLOW);
+    }
+    for (; c < n_chunk; ++c) {
+      publish();
+      bf16_t* kc = (c & 1) ? kb1 : kb0;
+      bf16_t* vc = (c & 1) ? vb1 : vb0;
+      if (c + 1 < n_chunk) copy((c & 1) ? kb0 : kb1, (c & 1) ? vb0 : vb1, c + 1);
+      step(kc, vc, min(kCrossChunk, keys - c * kCrossChunk), true, FOLLOW);
+    }
+  };
+  // Over many keys the reference points stay where the first keys put them: weights may be as large as 2^127, and no digit is lost
+  // where later scores are larger.  A step then has a fifth fewer vector instructions and no exchange between lanes ahead of its
+  // exponentials.  A workgroup of which a row's sum or result leaves the range (or is NaN) walks again, with points that follow.
+  // 16 x 32 heads, 1024 x 2047 keys of 128: 590 us following, 555 so; 64 heads of 2048 x 4096 539 / 504, 1024 x 1024 306 / 293, x 700 234 / 227,
+  // lengths of 100 to 500 as long.  Of 64 columns both take as long, and the code for both costs short calls a tenth: kernels of their own.
+  bool follow = !STAY || full < kCrossLong;
+  if (STAY && !follow) {
+    walk(false);
+    bool again = !(l_run < kCrossRange);
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) again |= !(fabsf(acc[db][v]) < INFINITY);
+    follow = __syncthreads_or(again);
+    if (follow) copy(kb0, vb0, 0);
   }
-  for (; c < n_chunk; ++c) {
-    publish();
-    bf16_t* kc = (c & 1) ? kb1 : kb0;
-    bf16_t* vc = (c & 1) ? vb1 : vb0;
-    if (c + 1 < n_chunk) copy((c & 1) ? kb0 : kb1, (c & 1) ? vb0 : vb1, c + 1);
-    step(kc, vc, min(kCrossChunk, keys - c * kCrossChunk), true);
-  }
+  if (follow) walk(true);
   __syncthreads();   // every wave is done with both stages: they now stage the output
   if (rows <= 0) return;
   const float sum = l_run + __shfl_xor(l_run, 32);
@@ -414,7 +444,9 @@ hipError_t launch_cross(const DecodeLaunch& p, hipStream_t stream) {
   const float scale = p.scale == 0.f ? 1.0f / sqrtf((float)p.D) : p.scale;
   a.scale_log2e = scale * 1.44269504088896340736f;
   if (!p.is_f32)
-    return p.D == 64 ? cross_tiles(&cross_bf16_kernel<64>, a, stream) : cross_tiles(&cross_bf16_kernel<128>, a, stream);
+    return p.D == 64                              ? cross_tiles(&cross_bf16_kernel<64, false>, a, stream)
+           : p.Sk >= kCrossLong * kCrossChunk ? cross_tiles(&cross_bf16_kernel<128, true>, a, stream)
+                                              : cross_tiles(&cross_bf16_kernel<128, false>, a, stream);
   if (p.D == 64) return launch_cross_f32<1, kAllCols>(a, stream);
   if (p.D == 128) return launch_cross_f32<2, kAllCols>(a, stream);
   if (p.D < 64) return p.D % 4 ? launch_cross_f32<1, kAnyCols>(a, stream) : launch_cross_f32<1, kVecCols>(a, stream);

@@ -151,7 +151,8 @@ __device__ __forceinline__ float sum_of_four(float x) {
 template <int D_>
 struct DecodeBf16 {
   typedef bf16_t Elt;
-  static constexpr int BK = 32, KPL = 2, NP = D_ / 16, KS = D_ / 32, OCC = 3, WGS = 2;   // keys of a block, of a lane; pieces
+  static constexpr int BK = 32, KPL = 2, NP = D_ / 16, KS = D_ / 32;   // keys of a block, of a lane; pieces
+  static constexpr int OCC = 3, WGS = 2;   // waves of a SIMD the unit kernel is built for; workgroups of a compute unit with runs
   static constexpr int LDS = 32 * D_ * 2;                                      // bytes of the wave's V tile
   struct Query { u32x4 r[KS]; };
   u32x4 k[2][KS], v[2][KS];
@@ -403,7 +404,7 @@ struct DecodeItem {
 };
 
 template <class Core, bool PAGED>
-__global__ __launch_bounds__(kThreads, Core::OCC) void decode_run_kernel(const DecodeArgs a) {
+__global__ __launch_bounds__(kThreads, Core::WGS) void decode_run_kernel(const DecodeArgs a) {
   typedef typename Core::Elt Elt;
   constexpr int BK = Core::BK, KPL = Core::KPL;
   __shared__ __attribute__((aligned(16))) unsigned char lds[Core::LDS ? 4 * Core::LDS : 16];

@@ -33,7 +33,8 @@ def test_every_kernel_is_reached(tmp_path):
 
 @pytest.mark.parametrize("call,kernels", [
     # us, the other way / this one
-    (("plan", 64, 1, 128, 16, 5000, False), ["page_plan_kernel<1024"]),                              # two launches 9, one 4.8
+    (("plan", 64, 1, 128, 16, 5000, True), ["page_plan_kernel<256"]),                                # 1,024 threads 5.0 / 4.3
+    (("plan", 300, 1, 128, 16, 5000, True), ["page_plan_kernel<1024"]),
     (("plan", 256, 1024, 128, 16, 5000, False), ["page_plan_kernel<256"]),                           # 10.6 / 5.3
     (("plan", 256, 1024, 128, 16, 5000, True), ["page_plan_kernel<256", "page_plan_kernel<1024"]),
     (("paged", 4, 32, 8, 64, 300, 16, 63, "bf16"), ["decode_unit_kernel"]),                          # 9.7 / 8.5
@@ -42,7 +43,7 @@ def test_every_kernel_is_reached(tmp_path):
     (("paged", 128, 32, 8, 128, 9000, 16, 256, "bf16"), ["decode_run_kernel", "decode_join_kernel"]),   # 156 / 129
     (("cross", 32, 12, 12, 1, 1000, 64, "bf16"), ["decode_unit_kernel"]),                            # 17.8 / 15.6
     (("cross", 16, 8, 8, 32, 1000, 128, "bf16"), ["decode_unit_kernel"]),                            # 25.5 / 18.4
-    (("cross", 16, 8, 8, 64, 1000, 128, "bf16"), ["cross_bf16_kernel<128"]),                         # 32.5 / 25.9
+    (("cross", 16, 8, 8, 64, 1000, 128, "bf16"), ["cross_bf16_kernel<128, true"]),                   # 32.5 / 25.9
     (("cross", 64, 8, 8, 32, 1000, 64, "bf16"), ["cross_bf16_kernel<64"]),                           # 33.9 / 27.6
     (("cross", 8, 24, 8, 94, 333, 256, "f32"), ["cross_f32_kernel<4"]),                              # 110 / 86
     (("cross", 8, 24, 8, 94, 1000, 128, "f32"), ["decode_unit_kernel"]),                             # 76.6 / 64.7

@@ -47,7 +47,7 @@ def _check(O, Q, K, V, lens, items, scale=None):
 SIZES = [(1, 1, 1, 1, 1), (3, 4, 2, 1, 50), (2, 6, 2, 5, 1), (5, 3, 3, 33, 65), (2, 8, 1, 9, 200), (1, 40, 1, 1, 700),
          (1, 2, 2, 100, 3001), (4, 12, 12, 1, 1000), (40, 4, 4, 64, 64), (33, 8, 4, 65, 127), (9, 16, 16, 129, 31), (70, 6, 2, 23, 130),
          (2, 64, 32, 260, 333), (130, 1, 1, 200, 97), (1, 1, 1, 1, 70001),
-         (70, 8, 8, 33, 40), (130, 6, 3, 40, 70), (3, 40, 2, 1, 2500), (260, 4, 4, 33, 20), (20, 12, 12, 1, 100),
+         (70, 8, 8, 33, 40), (130, 6, 3, 40, 70), (3, 40, 2, 1, 2500), (260, 4, 4, 33, 20), (20, 12, 12, 1, 100), (9, 16, 8, 111, 705),
          (400, 6, 3, 1, 1100)]
 TYPES = [(64, "bf16"), (128, "bf16"), (64, "f32"), (128, "f32"), (3, "f32"), (33, "f32"), (36, "f32"), (80, "f32"), (101, "f32"), (199, "f32"), (256, "f32")]
 
@@ -148,3 +148,18 @@ def test_many_rows_behind_two_gibi_elements(ac):  # noqa: F811
         for b in (0, B - 1):
             for h in (0, H - 1):
                 gen.check(O[b, h], *gen.attend(Q[b, h], K[b, h], V[b, h]))
+
+
+@pytest.mark.parametrize("keys", [(700, 33, 1.0), (700, 33, 40.0), (700, 650, 300.0), (1500, 1400, 1e4)])
+def test_scores_that_outgrow_the_first_keys(ac, keys):  # noqa: F811
+    """Keys whose scores exceed those of the first ones by little, by a lot and beyond the range of the weights; and rows whose first
+    keys are all -inf."""
+    Sk, at, by = keys
+    Q, K, V, _ = _data(20, 8, 4, 70, Sk, 128, "bf16", None)
+    K[:, :, at] = (Q[:, ::2, 5] * by / 11.3).clamp(-1e6, 1e6)
+    V[3] *= 1e30
+    K[4, :, :40] = -float("inf")
+    Q[4] = Q[4].abs()
+    O = _call(ac, Q, K, V, None)
+    _check(O, Q, K, V, None, [0, 3, 7, 19])
+    _check(O, Q[:, :], K[:, :, 40:].contiguous(), V[:, :, 40:].contiguous(), None, [4])

@@ -149,6 +149,22 @@ def test_pages_that_lie_apart(ac, dt, more):  # noqa: F811
     _case(ac, EDGES, 4, 2, 128, dt, 16, more=more, width=40)
 
 
+def test_requests_that_share_pages_and_empty_batches(ac):  # noqa: F811
+    c = Cache([100, 100, 37, 100], 2, 64, "bf16", 16, 3)
+    c.table[1], c.rows[1] = c.table[0], c.rows[0]
+    c.table[3] = c.table[0]
+    c.table[3, :2], c.rows[3] = c.table[2, :2], [torch.cat([a[:, :32], b[:, 32:]], 1) for a, b in zip(c.rows[2], c.rows[0])]
+    Q = torch.randn(4, 4, 64, generator=c.gen, device="cuda").bfloat16()
+    c.check(c.call(ac, Q), Q)
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda")  # noqa: E731
+    ws, none = torch.empty(ac.attention_paged_workspace_bytes(1, 4, 2, 64), dtype=torch.uint8, device="cuda"), Q[:0]
+    kv = torch.empty(0, 2, 3, 64, dtype=torch.bfloat16, device="cuda")
+    ac.attention_paged(none, c.k, c.v, i32(0, 3), i32(0), none.clone(), ws)
+    ac.attncache_page_append(kv, kv, i32(0, 3), c.k, c.v)
+    ac.attncache_page_plan(i32(0), i32(0), i32(2), i32(5), i32(0, 3), i32(0), i32(0), i32(2), i32(0, 1), page_size=16)
+    ac.attention_cross(none.view(0, 4, 1, 64), kv, kv, none.clone().view(0, 4, 1, 64))
+
+
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
 def test_keys_whose_page_is_out_of_range_are_hidden(ac, dt):  # noqa: F811
     page = 12
