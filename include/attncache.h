@@ -422,8 +422,8 @@ int32_t attncache_project(const void *h, const int32_t *seq_len,
  *
  * Token j of request b lies in page page_table[b][j / page_size] at place
  * j % page_size, in all heads; its slot is page * page_size + place.
- * n_pages * page_size and max_pages * page_size must be below 2^31.  Page
- * numbers and slots that the kernels read are checked: what is outside
+ * n_pages * page_size must be below 2^31, max_pages * page_size at most 2^30.
+ * Page numbers and slots that the kernels read are checked: what is outside
  * [0, n_pages) or [0, n_pages * page_size) is never followed.
  *
  * All pointers of these calls are to be memory of the current device
@@ -459,7 +459,7 @@ int32_t attncache_project(const void *h, const int32_t *seq_len,
  * twice (attention_paged, which only reads, may be given shared pages).
  * The outputs seq_len_out, added, free_state_out may be seq_len, new_len,
  * free_state (a captured step then continues from where the last replay
- * ended); other arrays must not overlap.  B <= 2^22, S <= 2^26,
+ * ended); other arrays must not overlap.  B <= 2^22, S <= 2^25,
  * B * max_pages < 2^31.  One launch, or two for many slots.
  */
 int32_t attncache_page_plan(const int32_t *seq_len, const int32_t *new_len,
@@ -541,8 +541,8 @@ int32_t attention_paged(const void *Q, const void *k_pages,
  *              attention_paged; may be NULL where that is 0 (calls of many
  *              bf16 rows, and sizes that attention_cross refuses).
  *
- * Arithmetic as in attention_paged.  Hq / Hkv * Sq <= 2^24, B * Hkv <= 2^28;
- * AC_F32: B * Hkv * ceil(Hq / Hkv * Sq / 16) * ceil(Sk / 16) below 2^31.
+ * Arithmetic as in attention_paged.  Hq / Hkv * Sq <= 2^24, B * Hkv <= 2^28,
+ * Sk <= 2^30; AC_F32: B * Hkv * ceil(Hq / Hkv * Sq / 16) * ceil(Sk / 16) below 2^31.
  */
 size_t attention_cross_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv,
                                        int32_t Sq, int32_t Sk, int32_t D,

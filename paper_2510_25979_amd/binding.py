@@ -422,16 +422,16 @@ def attncache_page_plan(seq_len: torch.Tensor, new_len: torch.Tensor, free_state
     page_table [B,max_pages]; slot [B,S].  The outputs may be the inputs of the same meaning."""
     if page_table.dim() != 2 or slot.dim() != 2 or free_pages.dim() != 1:
         raise ValueError("page_table must be [B,max_pages], slot [B,S] and free_pages [n_pages]")
-    i32 = torch.int32
+    i32, per_request, two = torch.int32, (page_table.shape[0],), (2,)
     (B, max_pages), S, n = page_table.shape, slot.shape[1], free_pages.shape[0]
-    lp = _dev(seq_len, "seq_len", i32, (B,))
-    np_ = _dev(new_len, "new_len", i32, (B,))
-    fs = _dev(free_state, "free_state", i32, (2,))
-    fp = _dev(free_pages, "free_pages", i32, (n,))
-    tp = _dev(page_table, "page_table", i32, (B, max_pages))
-    lo = _dev(seq_len_out, "seq_len_out", i32, (B,))
-    ap = _dev(added, "added", i32, (B,))
-    fo = _dev(free_state_out, "free_state_out", i32, (2,))
+    lp = _dev(seq_len, "seq_len", i32, per_request)
+    np_ = _dev(new_len, "new_len", i32, per_request)
+    fs = _dev(free_state, "free_state", i32, two)
+    fp = _dev(free_pages, "free_pages", i32)
+    tp = _dev(page_table, "page_table", i32)
+    lo = _dev(seq_len_out, "seq_len_out", i32, per_request)
+    ap = _dev(added, "added", i32, per_request)
+    fo = _dev(free_state_out, "free_state_out", i32, two)
     sp = _dev(slot, "slot", i32, (B, S))
     _check(lib().attncache_page_plan(lp, np_, fs, fp, tp, lo, ap, fo, sp, B, S, max_pages, page_size, n,
                                      _stream(stream)), "attncache_page_plan")
@@ -439,14 +439,14 @@ def attncache_page_plan(seq_len: torch.Tensor, new_len: torch.Tensor, free_state
 
 def _pages(k_pages: torch.Tensor, v_pages: torch.Tensor, dtype, heads: int, D: int):
     """Addresses, page count, page size and page stride of [n,heads,page,D] arrays whose pages may lie further apart."""
-    shape = k_pages.shape
-    if len(shape) != 4 or shape != v_pages.shape or shape[1] != heads or shape[3] != D:
+    shape = tuple(k_pages.shape)
+    if len(shape) != 4 or shape[1] != heads or shape[3] != D or shape != tuple(v_pages.shape):
         raise ValueError(f"k_pages and v_pages must be [n_pages,{heads},page_size,{D}], have "
-                         f"{tuple(shape)} and {tuple(v_pages.shape)}")
-    n, page = shape[0], shape[2]
+                         f"{shape} and {tuple(v_pages.shape)}")
+    n, _, page, _ = shape
     stride = dense = heads * page * D
     kp, vp = _address(k_pages, dtype, None), _address(v_pages, dtype, None)
-    if kp is not None and vp is not None:
+    if kp is not None and vp is not None:   # dense, both
         return kp, vp, n, page, stride
     if n > 1:
         stride = k_pages.stride(0)
@@ -467,16 +467,17 @@ def attncache_page_append(K: torch.Tensor, V: torch.Tensor, slot: torch.Tensor, 
                           v_pages: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
     """K,V [B,H,S,D] bf16 or f32; slot [B,S] int32; k_pages,v_pages [n_pages,H,page_size,D], whose pages may lie further
     apart than their size."""
-    if K.dim() != 4:
+    shape, dtype = tuple(K.shape), K.dtype
+    if len(shape) != 4:
         raise ValueError("K and V must be [B,H,S,D]")
-    B, H, S, D = K.shape
-    if K.dtype not in (torch.bfloat16, torch.float32):
+    if dtype not in (torch.bfloat16, torch.float32):
         raise ValueError("unsupported dtype")
+    B, H, S, D = shape
     kp = _dev(K, "K")
-    vp = _dev(V, "V", K.dtype, (B, H, S, D))
+    vp = _dev(V, "V", dtype, shape)
     sp = _dev(slot, "slot", torch.int32, (B, S))
-    kc, vc, n, page, stride = _pages(k_pages, v_pages, K.dtype, H, D)
-    _check(lib().attncache_page_append(kp, vp, sp, kc, vc, B, H, S, D, n, page, stride, _DTYPE_CODE[K.dtype],
+    kc, vc, n, page, stride = _pages(k_pages, v_pages, dtype, H, D)
+    _check(lib().attncache_page_append(kp, vp, sp, kc, vc, B, H, S, D, n, page, stride, _DTYPE_CODE[dtype],
                                        _stream(stream)), "attncache_page_append")
 
 

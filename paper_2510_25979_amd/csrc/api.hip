@@ -142,6 +142,9 @@ int32_t check_head(int32_t D, int32_t dtype) {
   return AC_ERR_DTYPE;
 }
 
+// Keys of one request or sequence: a kernel rounds them up to whole blocks in 31 bits.
+constexpr int64_t kMostTokens = 1 << 30;
+
 // Pages [n_pages][heads][page_size][D], page_stride elements apart.  Rows of whole 16-byte pieces are read as such.
 int32_t check_pages(int32_t heads, int32_t D, int32_t n_pages, int32_t page_size, int64_t page_stride, int32_t dtype) {
   if (n_pages < 1 || page_size < 1 || (int64_t)n_pages * page_size > 0x7fffffffLL) return AC_ERR_SHAPE;
@@ -626,10 +629,10 @@ int32_t attncache_page_plan(const int32_t* seq_len, const int32_t* new_len, cons
                             int32_t S, int32_t max_pages, int32_t page_size, int32_t n_pages,
                             void* stream) {
   if (B < 0 || S < 1 || max_pages < 1 || page_size < 1 || n_pages < 1) return AC_ERR_SHAPE;
-  if ((int64_t)n_pages * page_size > 0x7fffffffLL || (int64_t)max_pages * page_size > 0x7fffffffLL)
+  if ((int64_t)n_pages * page_size > 0x7fffffffLL || (int64_t)max_pages * page_size > kMostTokens)
     return AC_ERR_SHAPE;
   // what the requests need and give back is added up in 32 bits; a workgroup's slots are numbered in 31
-  if ((int64_t)B * max_pages > 0x7fffffffLL || S > (1 << 26) || B > (1 << 22)) return AC_ERR_SHAPE;
+  if ((int64_t)B * max_pages > 0x7fffffffLL || S > (1 << 25) || B > (1 << 22)) return AC_ERR_SHAPE;
   if (B == 0) return AC_OK;
   if (!seq_len || !new_len || !free_state || !free_pages || !page_table || !seq_len_out || !added ||
       !free_state_out || !slot)
@@ -689,7 +692,7 @@ int32_t attention_paged(const void* Q, const void* k_pages, const void* v_pages,
   rc = check_pages(Hkv, D, n_pages, page_size, page_stride, dtype);
   if (rc != AC_OK) return rc;
   const int64_t most = (int64_t)max_pages * page_size;
-  if (most > 0x7fffffffLL || !ac::decode_fits(B, Hkv, Hq / Hkv, most)) return AC_ERR_SHAPE;
+  if (most > kMostTokens || !ac::decode_fits(B, Hkv, Hq / Hkv, most)) return AC_ERR_SHAPE;
   if (!(scale >= 0.f)) return AC_ERR_SHAPE;
   if (B == 0) return AC_OK;
   if (!Q || !k_pages || !v_pages || !page_table || !seq_len || !O || !workspace) return AC_ERR_NULL;
@@ -717,7 +720,7 @@ int32_t check_cross(int32_t B, int32_t Hq, int32_t Hkv, int32_t Sq, int32_t Sk, 
   const int32_t rc = check_head(D, dtype);
   if (rc != AC_OK) return rc;
   const int64_t rows = (int64_t)(Hq / Hkv) * Sq;
-  if (rows > (1 << 24) || (int64_t)B * Hkv > (1 << 28)) return AC_ERR_SHAPE;
+  if (Sk > kMostTokens || rows > (1 << 24) || (int64_t)B * Hkv > (1 << 28)) return AC_ERR_SHAPE;
   if (dtype == AC_F32 && !ac::decode_fits(B, Hkv, rows, Sk)) return AC_ERR_SHAPE;
   *R = (int32_t)rows;
   return AC_OK;

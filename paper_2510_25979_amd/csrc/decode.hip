@@ -417,9 +417,9 @@ __global__ __launch_bounds__(kThreads, Core::WGS) void decode_run_kernel(const D
   Core core(a, lds + wave * Core::LDS, lane);
   const int D = core.dim();
 
-  auto item = [&](DecodeItem& it, int b) {   // the first block of the first item from b on that has any
+  auto item = [&](DecodeItem& it, int b) {   // the first block of the first item from b on that has any (there is one)
     int keys;
-    while ((keys = decode_keys_of(a, b)) == 0) ++b;
+    while ((keys = decode_keys_of(a, b)) == 0 && b + 1 < a.B) ++b;
     it.b = b;
     it.unit = 0;
     it.keys = keys;
@@ -539,7 +539,7 @@ __global__ __launch_bounds__(kThreads, Core::WGS) void decode_run_kernel(const D
 
 // A workgroup per unit, its waves deal out the blocks.
 template <class Core, bool PAGED, int NW>
-__global__ __launch_bounds__(NW* kWave, Core::OCC * 4 / NW > 0 ? Core::OCC * 4 / NW : 1) void decode_unit_kernel(const DecodeArgs a) {
+__global__ __launch_bounds__(NW* kWave, Core::OCC) void decode_unit_kernel(const DecodeArgs a) {
   typedef typename Core::Elt Elt;
   constexpr int BK = Core::BK, KPL = Core::KPL, NP = Core::NP;
   constexpr int TILES = NW * Core::LDS, SUMS = NW * NP * kWave * 16;
@@ -736,7 +736,7 @@ size_t decode_workspace_bytes(int32_t R, int32_t D) {
   return (size_t)2 * kDecodeWaves * (R < kDecodeRows ? R : kDecodeRows) * (D + 2) * sizeof(float);
 }
 bool decode_fits(int64_t B, int64_t Hkv, int64_t R, int64_t keys) {
-  // blocks of 16 rows and 16 keys (binary32, the smaller ones), and the rows themselves
+  // blocks of 16 rows and 16 keys (binary32, the smaller ones), and the rows themselves; keys <= 2^30, so their numbers are far from the end
   const double units = (double)B * Hkv * ((R + kDecodeRows - 1) / kDecodeRows);
   return units * ((keys + 15) / 16 + kUnitCost) < 2147483648.0 - 65536 && (double)B * Hkv * R < 2147483648.0 - 65536;
 }

@@ -46,7 +46,7 @@ def _cross(L, **change):
     *[(_plan, {n: None}, NULL) for n in "seq new state ring table seq_out added state_out slot".split()],
     *[(_plan, {n: 0}, SHAPE) for n in "S max_pages page n".split()],
     (_plan, dict(B=-1), SHAPE), (_plan, dict(n=1 << 27), SHAPE), (_plan, dict(max_pages=1 << 27, B=1), SHAPE),
-    (_plan, dict(max_pages=1 << 20, B=1 << 11), SHAPE), (_plan, dict(S=(1 << 26) + 1), SHAPE), (_plan, dict(B=(1 << 22) + 1), SHAPE),
+    (_plan, dict(max_pages=1 << 20, B=1 << 11), SHAPE), (_plan, dict(S=(1 << 25) + 1), SHAPE), (_plan, dict(max_pages=(1 << 26) + 1, B=1), SHAPE), (_plan, dict(B=(1 << 22) + 1), SHAPE),
     (_plan, dict(B=0), OK), (_plan, dict(B=0, seq=None), OK),
     *[(_append, {n: None}, NULL) for n in "K V slot kp vp".split()],
     *[(_append, {n: P + 8}, ALIGN) for n in "K V kp vp".split()],
@@ -61,14 +61,14 @@ def _cross(L, **change):
     *[(_paged, {n: 0}, SHAPE) for n in "Hq Hkv D n page max_pages".split()],
     (_paged, dict(Hq=9), SHAPE), (_paged, dict(B=-1), SHAPE), (_paged, dict(D=32), SHAPE), (_paged, dict(dtype=F16), DTYPE),
     (_paged, dict(scale=-1.0), SHAPE), (_paged, dict(scale=float("nan")), SHAPE), (_paged, dict(ws_bytes=1000), WORKSPACE),
-    (_paged, dict(max_pages=1 << 27), SHAPE), (_paged, dict(B=1 << 16, max_pages=1 << 20), SHAPE),
+    (_paged, dict(max_pages=1 << 27), SHAPE), (_paged, dict(max_pages=(1 << 26) + 1, B=1, Hq=1, Hkv=1), SHAPE), (_paged, dict(B=1 << 16, max_pages=1 << 20), SHAPE),
     (_paged, dict(stride=2 * 16 * 64 - 8), SHAPE), (_paged, dict(stride=2 * 16 * 64 + 4), ALIGN), (_paged, dict(B=0), OK),
     *[(_cross, {n: None}, NULL) for n in "Q K V O ws".split()],
     *[(_cross, {n: P + 8}, ALIGN) for n in "Q K V O ws".split()],
     *[(_cross, {n: 0}, SHAPE) for n in "Hq Hkv Sq Sk D".split()],
     (_cross, dict(Hq=9), SHAPE), (_cross, dict(B=-1), SHAPE), (_cross, dict(D=96), SHAPE), (_cross, dict(dtype=F16), DTYPE),
     (_cross, dict(dtype=F32, D=257), SHAPE), (_cross, dict(scale=-1.0), SHAPE), (_cross, dict(ws_bytes=1000), WORKSPACE),
-    (_cross, dict(Sq=1 << 23), SHAPE), (_cross, dict(dtype=F32, Sq=1 << 20, Sk=1 << 20), SHAPE), (_cross, dict(B=0), OK),
+    (_cross, dict(Sq=1 << 23), SHAPE), (_cross, dict(Sk=(1 << 30) + 1, B=1, Hq=1, Hkv=1), SHAPE), (_cross, dict(dtype=F32, Sq=1 << 20, Sk=1 << 20), SHAPE), (_cross, dict(B=0), OK),
 ], ids=lambda x: x.__name__[1:] if callable(x) else str(x))
 def test_refusals(L, call, change, status):
     assert call(L, **change) == status
