@@ -746,11 +746,16 @@ static hipError_t launch_decode_core(DecodeArgs& a, hipStream_t stream) {
   constexpr bool F32 = Core::BK == 16;
   const int64_t units = (int64_t)a.B * a.Hkv * a.rbs, rows = (int64_t)a.B * a.Hkv * a.R;
   const int blocks = (int)(((int64_t)a.Sk + Core::BK - 1) / Core::BK);   // the most of a unit
-  // One launch where no item can have many blocks: the longest unit is then over before a second launch would be.  us, runs and join /
-  // units, bf16 on pages: 4 x 8 heads of 64, up to 1,008 tokens (32 blocks) 9.7 / 8.5, up to 2,000 (63) 9.8 / 12.3; 128 units of 128, 1,000
-  // tokens 23.7 / 19.6, 2,000 31.9 / 33.2; 256 units, 2,000 65.9 / 49.4; 1,024 units, 100 to 4,000 tokens (125) 231 / 252, 128 to 4,096 129 / 156,
-  // all 4,000 711 / 685.  Eight waves a unit / four: the first 8.5 / 9.2, 128 units 19.5 / 19.7, 512 units of 500 tokens 26.3 / 23.2.
-  if (blocks <= (units >= 256 ? 64 : 32) && units <= (1 << 22)) {
+  // One launch where no unit can be large: it is then over before a second launch would be.  Up to 256 KB of K and V, what one compute unit
+  // reads in the time of that launch, 512 KB where there are 128 units, 64 blocks where there are units for the whole chip.  us, runs and
+  // join / units, bf16 on pages: 4 x 8 heads of 64, up to 1,008 tokens (256 KB) 8.8 / 8.4, up to 2,000 9.8 / 12.3; of 128, up to 500 (250 KB) 9.9 /
+  // 9.3, up to 700 9.9 / 11.0; 64 units of 128, 500 tokens 13.2 / 11.6, 1,000 17.1 / 19.1; 128 units, 1,000 (512 KB) 21.2 / 19.4, 2,000 31.9 /
+  // 33.2; 256 units, 2,000 (63 blocks) 65.9 / 49.4; 1,024 units, 128 to 4,096 tokens (128) 129 / 156, all 4,000 711 / 685; binary32, 32 units of 128,
+  // 200 tokens (208 KB) 10.5 / 11.0, 500 13.4 / 19.1.  Eight waves a unit / four: the first 8.5 / 9.2, 128 units 19.5 / 19.7, 512 units of 500
+  // tokens 26.3 / 23.2.
+  const int64_t unit_bytes = 2LL * blocks * Core::BK * a.D * (int64_t)sizeof(typename Core::Elt);
+  const bool small = units >= 256 ? blocks <= 64 : unit_bytes <= (units >= 128 ? 512 : 256) * 1024;
+  if (small && units <= (1 << 22)) {
     const int64_t heads = (int64_t)a.B * a.Hkv;
     const dim3 grid((unsigned)(a.rbs == 1 ? heads : (heads + 7) / 8 * 8 * a.rbs));
     if constexpr (Core::NP <= 8)

@@ -37,7 +37,12 @@ def test_every_kernel_is_reached(tmp_path):
     (("plan", 300, 1, 128, 16, 5000, True), ["page_plan_kernel<1024"]),
     (("plan", 256, 1024, 128, 16, 5000, False), ["page_plan_kernel<256"]),                           # 10.6 / 5.3
     (("plan", 256, 1024, 128, 16, 5000, True), ["page_plan_kernel<256", "page_plan_kernel<1024"]),
-    (("paged", 4, 32, 8, 64, 300, 16, 63, "bf16"), ["decode_unit_kernel"]),                          # 9.7 / 8.5
+    (("paged", 4, 32, 8, 64, 300, 16, 63, "bf16"), ["decode_unit_kernel"]),                          # 8.8 / 8.4
+    (("paged", 4, 32, 8, 128, 300, 16, 63, "bf16"), ["decode_run_kernel", "decode_join_kernel"]),    # 13.8 / 10.1
+    (("paged", 4, 32, 8, 128, 300, 16, 32, "bf16"), ["decode_unit_kernel"]),                         # 9.9 / 9.3
+    (("paged", 8, 32, 8, 128, 300, 16, 63, "bf16"), ["decode_run_kernel", "decode_join_kernel"]),    # 19.1 / 17.1
+    (("paged", 16, 32, 8, 128, 300, 16, 63, "bf16"), ["decode_unit_kernel"]),                        # 21.2 / 19.4
+    (("paged", 4, 24, 8, 128, 300, 10, 50, "f32"), ["decode_run_kernel", "decode_join_kernel"]),     # 19.1 / 13.4
     (("paged", 4, 32, 8, 64, 300, 16, 125, "bf16"), ["decode_run_kernel", "decode_join_kernel"]),    # 12.3 / 9.8
     (("paged", 32, 32, 8, 128, 300, 16, 125, "bf16"), ["decode_unit_kernel"]),                       # 65.9 / 49.4
     (("paged", 128, 32, 8, 128, 9000, 16, 256, "bf16"), ["decode_run_kernel", "decode_join_kernel"]),   # 156 / 129
