@@ -631,8 +631,8 @@ int32_t attncache_page_plan(const int32_t* seq_len, const int32_t* new_len, cons
   if (B < 0 || S < 1 || max_pages < 1 || page_size < 1 || n_pages < 1) return AC_ERR_SHAPE;
   if ((int64_t)n_pages * page_size > 0x7fffffffLL || (int64_t)max_pages * page_size > kMostTokens)
     return AC_ERR_SHAPE;
-  // what the requests need and give back is added up in 32 bits; a workgroup's slots are numbered in 31
-  if ((int64_t)B * max_pages > 0x7fffffffLL || S > (1 << 25) || B > (1 << 22)) return AC_ERR_SHAPE;
+  // what the requests need and give back is added up in 31 bits, and counted past its end by a workgroup; so are a workgroup's slots
+  if ((int64_t)B * max_pages > 0x7fffffffLL - 4096 || S > (1 << 25) || B > (1 << 22)) return AC_ERR_SHAPE;
   if (B == 0) return AC_OK;
   if (!seq_len || !new_len || !free_state || !free_pages || !page_table || !seq_len_out || !added ||
       !free_state_out || !slot)

@@ -168,7 +168,7 @@ __global__ __launch_bounds__(NT) void page_plan_kernel(const PlanArgs a) {
   if (writes_state && tid == 0) {
     const int taken = s_taken;
     a.state_out[0] = (int)(((unsigned)first + (unsigned)taken) % (unsigned)a.n);
-    a.state_out[1] = min(a.n, count - taken + before_give);
+    a.state_out[1] = (int)min((unsigned)a.n, (unsigned)(count - taken) + (unsigned)before_give);
   }
 }
 

@@ -47,6 +47,7 @@ def _cross(L, **change):
     *[(_plan, {n: 0}, SHAPE) for n in "S max_pages page n".split()],
     (_plan, dict(B=-1), SHAPE), (_plan, dict(n=1 << 27), SHAPE), (_plan, dict(max_pages=1 << 27, B=1), SHAPE),
     (_plan, dict(max_pages=1 << 20, B=1 << 11), SHAPE), (_plan, dict(S=(1 << 25) + 1), SHAPE), (_plan, dict(max_pages=(1 << 26) + 1, B=1), SHAPE), (_plan, dict(B=(1 << 22) + 1), SHAPE),
+    (_plan, dict(max_pages=((1 << 31) - 4096) // 3 + 1, B=3, page=1), SHAPE),
     (_plan, dict(B=0), OK), (_plan, dict(B=0, seq=None), OK),
     *[(_append, {n: None}, NULL) for n in "K V slot kp vp".split()],
     *[(_append, {n: P + 8}, ALIGN) for n in "K V kp vp".split()],
