@@ -14,7 +14,7 @@
 // a unit, too.
 //
 // decode_unit_kernel gives each unit to a workgroup, whose waves deal out the blocks and meet in LDS: one launch and no workspace,
-// where no item can have many keys.
+// where no unit can be large (the rule is at the launch).
 //
 // A wave's block: K rows go straight from memory to the lanes that multiply them (S^T = K Q^T, 16 keys x 16 rows a product), V rows
 // through a wave-private LDS tile where the transposing read wants them (O^T = V^T P^T; binary32: straight from memory).  A lane
