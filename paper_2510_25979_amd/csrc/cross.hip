@@ -248,13 +248,14 @@ __global__ __launch_bounds__(kThreads, 2) void cross_bf16_kernel(const CrossArgs
   };
   // Over many keys the reference points stay where the first keys put them: weights may be as large as 2^127, and no digit is lost
   // where later scores are larger.  A step then has a fifth fewer vector instructions and no exchange between lanes ahead of its
-  // exponentials.  A workgroup of which a row's sum or result leaves the range (or is NaN) walks again, with points that follow.
+  // exponentials.  A workgroup of which a row's sum or result leaves the range (or is NaN), or whose
+  // first keys were all -inf (no point to stay at), walks again, with points that follow.
   // 16 x 32 heads, 1024 x 2047 keys of 128: 590 us following, 555 so; 64 heads of 2048 x 4096 539 / 504, 1024 x 1024 306 / 293, x 700 234 / 227,
   // lengths of 100 to 500 as long.  Of 64 columns both take as long, and the code for both costs short calls a tenth: kernels of their own.
   bool follow = !STAY || full < kCrossLong;
   if (STAY && !follow) {
     walk(false);
-    bool again = !(l_run < kCrossRange);
+    bool again = !(l_run < kCrossRange) || m_run == -INFINITY;
 #pragma unroll
     for (int db = 0; db < D / 32; ++db)
 #pragma unroll

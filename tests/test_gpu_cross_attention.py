@@ -163,3 +163,15 @@ def test_scores_that_outgrow_the_first_keys(ac, keys):  # noqa: F811
     O = _call(ac, Q, K, V, None)
     _check(O, Q, K, V, None, [0, 3, 7, 19])
     _check(O, Q[:, :], K[:, :, 40:].contiguous(), V[:, :, 40:].contiguous(), None, [4])
+
+
+@pytest.mark.parametrize("far", [0.0, 40.0])
+def test_low_scores_behind_keys_that_nobody_sees(ac, far):  # noqa: F811
+    """Rows whose first keys are all -inf, and whose other scores are so low that 2^score is zero."""
+    Q, K, V, _ = _data(20, 8, 4, 70, 700, 128, "bf16", None)
+    Q.abs_()
+    K -= far
+    K[::2, :, :40] = -float("inf")
+    O = _call(ac, Q, K, V, None)
+    _check(O, Q, K, V, None, [1, 19])
+    _check(O, Q, K[:, :, 40:].contiguous(), V[:, :, 40:].contiguous(), None, [0, 18])
