@@ -540,7 +540,7 @@ int32_t attention_paged(const void *Q, const void *k_pages,
  *   scale      0 selects 1/sqrt(D).
  *   workspace  DEVICE, attention_cross_workspace_bytes(...) bytes, as for
  *              attention_paged; may be NULL where that is 0 (calls of many
- *              bf16 rows, and sizes that attention_cross refuses).
+ *              rows, and sizes that attention_cross refuses).
  *
  * Arithmetic as in attention_paged.  Hq / Hkv * Sq <= 2^24, B * Hkv <= 2^28,
  * Sk <= 2^30; AC_F32: B * Hkv * ceil(Hq / Hkv * Sq / 16) * (ceil(Sk / 16) + 2)

@@ -285,23 +285,24 @@ __global__ __launch_bounds__(kThreads, 2) void cross_bf16_kernel(const CrossArgs
 // Binary32 (the layout of f32_tile.hpp): a wave owns 16 rows, four waves share stages of 32 keys in LDS, the next stage's
 // rows are in registers while this one is multiplied.  Each 16-byte read of K or V feeds four products of 32 cycles, so the matrix
 // cores bound it: 8 x 24 heads on 8, 1000 x 1000 keys of 128 (lengths 100 to 1000) 341 us = 112 TFLOP/s of the 154 of a large
-// product.  32 rows a wave halve the reads, but leave one wave where two hide each other's exponentials: 360.
-template <int DB, int COLS>
+// product.  32 rows a wave halve the reads, but leave one wave where two hide each other's exponentials: 360.  SPLIT: two waves a row, which
+// add up their halves of the keys through LDS at the end (when and what it gains: at the launch).
+template <int DB, int COLS, int SPLIT>   // SPLIT: waves that share 16 rows, each with its 32 / SPLIT keys of every stage
 __global__ __launch_bounds__(kThreads, DB <= 2 ? 2 : 1) void cross_f32_kernel(const CrossArgs a) {
-  constexpr int KC = 32, NB = KC / kF32Rows;
+  constexpr int KC = 32, NB = KC / kF32Rows / SPLIT, WROWS = 4 / SPLIT;   // blocks of a wave and stage; waves' rows side by side
   typedef F32Stage<DB, KC, COLS> Stage;
   const int D = COLS == kAllCols ? 64 * DB : a.D;
   __shared__ __attribute__((aligned(16))) float kl[KC * Stage::LD];
   __shared__ __attribute__((aligned(16))) float vl[KC * Stage::LD];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int i = lane & 15, kq = lane >> 4;
+  const int i = lane & 15, kq = lane >> 4, part = wave / WROWS, key0 = part * kF32Rows * NB;
   const int slot = blockIdx.x >> 3, u = a.first + slot / a.per * 8 + (blockIdx.x & 7);
   if (u >= a.tiles) return;
   const int b = u / a.Hkv;
   if (a.row_sel && a.row_sel[b] >= 0) return;
   const int keys = a.len ? min(max(a.len[b], 0), a.Sk) : a.Sk;
-  const int r0 = (slot % a.per * 4 + wave) * kF32Rows;   // this wave's first row
+  const int r0 = (slot % a.per * WROWS + wave % WROWS) * kF32Rows;   // this wave's first row
   float* O = reinterpret_cast<float*>(a.O) + (size_t)u * a.R * D;
   if (keys == 0) {
     const int n = min(kF32Rows, a.R - r0) * D;
@@ -347,7 +348,7 @@ __global__ __launch_bounds__(kThreads, DB <= 2 ? 2 : 1) void cross_f32_kernel(co
 #pragma unroll
     for (int bk = 0; bk < NB; ++bk) {
       s[bk] = f32x4{0.f, 0.f, 0.f, 0.f};
-      const float* row = kl + (kF32Rows * bk + i) * Stage::LD + 4 * kq;
+      const float* row = kl + (key0 + kF32Rows * bk + i) * Stage::LD + 4 * kq;
       f32x4 k = *reinterpret_cast<const f32x4*>(row);
 #pragma unroll
       for (int kk = 0; kk < 4 * DB; ++kk)
@@ -364,7 +365,7 @@ __global__ __launch_bounds__(kThreads, DB <= 2 ? 2 : 1) void cross_f32_kernel(co
       for (int bk = 0; bk < NB; ++bk)
 #pragma unroll
         for (int x = 0; x < 4; ++x)
-          if (j0 + kF32Rows * bk + 4 * kq + x >= keys) s[bk][x] = -INFINITY;
+          if (j0 + key0 + kF32Rows * bk + 4 * kq + x >= keys) s[bk][x] = -INFINITY;
     }
     float mx = s[0][0];
 #pragma unroll
@@ -390,11 +391,30 @@ __global__ __launch_bounds__(kThreads, DB <= 2 ? 2 : 1) void cross_f32_kernel(co
         p[x] = __builtin_amdgcn_exp2f(fmaf(s[bk][x], a.scale_log2e, -ref));
         l += p[x];
       }
-      f32_weights_v<DB>(acc, vl + kF32Rows * bk * Stage::LD, p, i, kq);
+      f32_weights_v<DB>(acc, vl + (key0 + kF32Rows * bk) * Stage::LD, p, i, kq);
     }
   }
   float sum = l + __shfl_xor(l, 16);
   sum += __shfl_xor(sum, 32);
+  if constexpr (SPLIT == 2) {   // the second wave's sums through the stages, which nobody reads any more
+    static_assert(4 * DB * kWave * 4 * WROWS <= KC * Stage::LD, "sums of two waves");
+    f32x4* sums = reinterpret_cast<f32x4*>(kl) + wave % WROWS * 4 * DB * kWave + lane;
+    float* stats = vl + wave % WROWS * 2 * kWave + lane;
+    __syncthreads();
+    if (part > 0) {
+#pragma unroll
+      for (int x = 0; x < 4 * DB; ++x) sums[x * kWave] = acc[x];
+      stats[0] = m;
+      stats[kWave] = sum;
+    }
+    __syncthreads();
+    if (part > 0) return;
+    const float m1 = stats[0], top = fmaxf(m, m1);
+    const float f0 = m < top ? __builtin_amdgcn_exp2f(m - top) : 1.f, f1 = m1 < top ? __builtin_amdgcn_exp2f(m1 - top) : 1.f;
+    sum = sum * f0 + stats[kWave] * f1;
+#pragma unroll
+    for (int x = 0; x < 4 * DB; ++x) acc[x] = acc[x] * f0 + sums[x * kWave] * f1;
+  }
   if (r0 + i < a.R)
     f32_store_row<DB, COLS, true>(O + (size_t)(r0 + i) * D, acc, sum == 0.f ? 1.f : sum, kq, D);
 }
@@ -402,12 +422,13 @@ __global__ __launch_bounds__(kThreads, DB <= 2 ? 2 : 1) void cross_f32_kernel(co
 // Few rows leave most of these kernels' waves without any, and few workgroups most of the chip; decode.hip splits the keys instead,
 // and reads K and V again for every 16 rows.  us, there / here.  bf16, heads x rows x keys, by units of 16 rows: 128 x 32 x 1000 (256
 // units) 11.2 / 17.9 of 64, 18.4 / 25.5 of 128; 128 x 64 x 1000 (512) 18.5 / 18.0 and 32.5 / 25.9; 16 x 500 x 1500 (512) 24.2 / 22.6 and
-// 45.9 / 33.7; 512 x 32 x 100 (1,024) 7.8 / 7.7 and 12.5 / 12.3; 512 x 32 x 1000 33.9 / 27.6 and 66.4 / 53.1.  Binary32, by workgroups of 64
-// rows: 64 x 70 x 200 of 128 (128) 17.3 / 23.0; 64 x 282 x 333, ragged (320) 39.0 / 37.6, of 256 110 / 86; x 1000, ragged 64.7 / 76.6, 256 x 64 x
-// 1000, not ragged (256) 117 / 92; 512 x 40 x 300 (512) 60.9 / 54.6; 512 x 20 x 500 68.1 / 84.7.
+// 45.9 / 33.7; 512 x 32 x 100 (1,024) 7.8 / 7.7 and 12.5 / 12.3; 512 x 32 x 1000 33.9 / 27.6 and 66.4 / 53.1.  Binary32, by workgroups of 32
+// rows (as here where they are few): 64 x 64 x 300 of 128 (128) 14.3 / 21.1; 16 x 282 x 333, ragged (144) 16.5 / 16.9; 256 x 32 x 300 (256) 23.6 / 22.1,
+// ragged 17.8 / 21.2; 128 x 64 x 500 (256) 33.7 / 32.0, x 1000 of 256 226 / 133; 64 x 282 x 333, ragged (576) 38.5 / 33.2, x 1000 62.3 / 65.8; 512 x 20 x
+// 500 (512) 68 / 54.
 static bool cross_by_rows(int64_t B, int64_t Hkv, int64_t R, int64_t Sk, int32_t D, int32_t is_f32) {
   const int64_t heads = B * Hkv;
-  if (is_f32) return D >= 4 && R > 32 && heads * ((R + 4 * kF32Rows - 1) / (4 * kF32Rows)) >= (D > 128 || Sk <= 512 ? 256 : 512);
+  if (is_f32) return D >= 4 && R > 16 && heads * ((R + 2 * kF32Rows - 1) / (2 * kF32Rows)) >= 256;
   return !decode_fits(B, Hkv, R, Sk) || (R > 16 && heads * ((R + 15) / 16) >= 512);
 }
 size_t cross_workspace_bytes(int32_t B, int32_t Hkv, int32_t R, int32_t Sk, int32_t D, int32_t is_f32) {
@@ -431,7 +452,17 @@ static hipError_t cross_tiles(Kernel kernel, CrossArgs a, hipStream_t stream) {
 template <int DB, int COLS>
 static hipError_t launch_cross_f32(CrossArgs a, hipStream_t stream) {
   a.per = (a.R + 4 * kF32Rows - 1) / (4 * kF32Rows);
-  return cross_tiles(&cross_f32_kernel<DB, COLS>, a, stream);
+  // Two waves a row halve a workgroup's rows and its time, but stages of K and V serve half as many products.  us, four waves / two and two,
+  // workgroups of 64 rows, keys of 128: few of them, 128 x 64 x 500 (128) 45.4 / 32.0, of 256 x 1000 228 / 133, 256 x 64 x 1000 (256) 88 / 92;
+  // two a compute unit and ragged (a long one beside a long one), 64 x 282 x 333 (320) 37.5 / 33.2, 448 x 64 x 300 (448) 41.9 / 36.6, x 576
+  // (576) 49.7 / 48.4, not ragged (448) 54.6 / 61.1; last workgroups at most half full, 512 x 20 x 500 (512) 85 / 54, 512 x 130 x 300 (1,536) 145 /
+  // 142, 512 x 270 x 300 (2,560) 239 / 240; others, 512 x 40 x 300 (512) 55.8 / 67.4, 64 x 3000 x 1000 (3,008) 340 / 382.
+  const int64_t wgs = (int64_t)a.tiles * a.per;
+  if (wgs < 256 || (a.len && wgs < 512) || (a.R < 320 && (a.R - 1) % 64 < 32)) {
+    a.per = (a.R + 2 * kF32Rows - 1) / (2 * kF32Rows);
+    return cross_tiles(&cross_f32_kernel<DB, COLS, 2>, a, stream);
+  }
+  return cross_tiles(&cross_f32_kernel<DB, COLS, 1>, a, stream);
 }
 
 hipError_t launch_cross(const DecodeLaunch& p, hipStream_t stream) {

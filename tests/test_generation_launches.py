@@ -50,9 +50,13 @@ def test_every_kernel_is_reached(tmp_path):
     (("cross", 16, 8, 8, 32, 1000, 128, "bf16"), ["decode_unit_kernel"]),                            # 25.5 / 18.4
     (("cross", 16, 8, 8, 64, 1000, 128, "bf16"), ["cross_bf16_kernel<128, true"]),                   # 32.5 / 25.9
     (("cross", 64, 8, 8, 32, 1000, 64, "bf16"), ["cross_bf16_kernel<64"]),                           # 33.9 / 27.6
-    (("cross", 8, 24, 8, 94, 333, 256, "f32"), ["cross_f32_kernel<4"]),                              # 110 / 86
-    (("cross", 8, 24, 8, 94, 1000, 128, "f32"), ["decode_unit_kernel"]),                             # 76.6 / 64.7
-    (("cross", 64, 8, 8, 20, 500, 128, "f32"), ["decode_unit_kernel"]),                              # 84.7 / 68.1
+    (("cross", 8, 24, 8, 94, 333, 256, "f32"), ["cross_f32_kernel<4, 1, 2>"]),                       # 110 / 77
+    (("cross", 8, 24, 8, 94, 333, 128, "f32"), ["cross_f32_kernel<2, 2, 2>"]),                       # 37.5 / 33.2
+    (("cross", 2, 24, 8, 94, 333, 128, "f32"), ["decode_unit_kernel"]),                              # 16.9 / 16.5
+    (("cross", 16, 8, 8, 64, 500, 128, "f32"), ["cross_f32_kernel<2, 2, 2>"]),                       # 45.4 / 32.0
+    (("cross", 64, 8, 8, 20, 500, 128, "f32"), ["cross_f32_kernel<2, 2, 2>"]),                       # 68 / 54
+    (("cross", 64, 8, 8, 40, 300, 128, "f32"), ["cross_f32_kernel<2, 2, 1>"]),                       # 67.4 / 55.8
+    (("cross", 8, 24, 8, 1000, 1000, 128, "f32"), ["cross_f32_kernel<2, 2, 1>"]),                    # 382 / 340
 ], ids=str)
 def test_the_kernels_that_measured_best_serve_the_call(tmp_path, call, kernels):
     (status, ls), = gl.record([call], tmp_path)
