@@ -82,7 +82,7 @@ def test_workspace_sizes():
     assert paged(1, 8, 2, 64) == paged(1000, 8, 2, 64) < paged(1, 8, 1, 64) < paged(1, 8, 1, 128)
     assert cross(1, 8, 2, 1, 100, 64, torch.bfloat16) == paged(1, 8, 2, 64) == cross(1, 8, 2, 1, 100, 64)
     assert cross(64, 32, 8, 256, 1000, 64, torch.bfloat16) == cross(64, 32, 8, 256, 1000, 64, torch.float32) == 0
-    assert cross(16, 32, 8, 20, 1000, 64, torch.bfloat16) == 0 < cross(16, 32, 8, 20, 1000, 64, torch.float32) == cross(16, 32, 8, 20, 1000, 64)
+    assert cross(8, 32, 8, 25, 1000, 64, torch.float32) == 0 < cross(8, 32, 8, 25, 1000, 64, torch.bfloat16) == cross(8, 32, 8, 25, 1000, 64)
     assert cross(0, 8, 2, 1, 100, 64) == cross(1, 8, 3, 1, 100, 64) == cross(1, 8, 2, 1, 100, 65, torch.bfloat16) == 0
 
 
