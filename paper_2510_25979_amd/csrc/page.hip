@@ -8,6 +8,7 @@
 // Bound by latency: dependent loads (lengths -> sums -> ring -> slots), 4.8 us for 64 requests of one token.
 #include "common.hpp"
 #include "serve.h"
+#include "serve_index.h"
 
 namespace ac {
 
@@ -96,7 +97,7 @@ __global__ __launch_bounds__(NT) void page_plan_kernel(const PlanArgs a) {
   __shared__ int s_taken;
   const int tid = threadIdx.x;
   const int r0 = state_too ? 0 : blockIdx.x * a.rows, r1 = state_too ? a.B : min(a.B, r0 + a.rows);
-  const int first = (int)((a.state[0] % a.n + a.n) % a.n), count = min(max(a.state[1], 0), a.n);
+  const int first = ring_first(a.state[0], a.n), count = min(max(a.state[1], 0), a.n);
   int before_new = 0, before_give = 0;   // what the requests before this chunk need and give back
   if (r0 > 0) {
     int x = 0, y = 0, ix, iy;
