@@ -25,6 +25,7 @@
 #include "common.hpp"
 #include "f32_tile.hpp"
 #include "serve.h"
+#include "serve_index.h"
 
 namespace ac {
 
@@ -89,9 +90,7 @@ struct DecodeWalk {
     int t = __builtin_amdgcn_readlane(head, kWave - 1);
     if (a.B > kWave) t += further(a.B);
     total = t * units;
-    // Runs of one block as long as every second wave has none: more partial results cost the join more than the runs save (one
-    // request of 8,000 tokens of 8 heads of 128, 2,016 blocks for 2,048 waves: 18.6 us, runs of two 16.9; of 2,000 tokens 11.7 / 13.2).
-    per = 2 * total <= a.waves ? 1 : max(2, (total + a.waves - 1) / a.waves);
+    per = run_length(total, a.waves);
   }
   // number of the first block of item `item`
   __device__ __forceinline__ int start(int item) const {
@@ -509,7 +508,7 @@ __global__ __launch_bounds__(kThreads, Core::WGS) void decode_run_kernel(const D
       size_t row0;
       const int rows = rows_of(now, row0);
       const bool whole = begin == 0 && last;
-      const size_t slot = (size_t)(2 * run + (begin == 0)) * a.rp;
+      const size_t slot = (size_t)(2 * run + (begin == 0)) * a.rp;   // as partial_of has it
       if (core.i < rows) {
         const float inv = sum == 0.f ? 0.f : 1.f / sum;   // no key at all: zeros
         Elt* o = static_cast<Elt*>(a.O) + (row0 + core.i) * D;
@@ -654,10 +653,10 @@ __global__ __launch_bounds__(NW == 1 ? kThreads : NW * kWave) void decode_join_k
       if (w0 == w1) continue;   // one wave had all of it
       const int first = w0 + (NW == 1 ? 0 : wave);
       for (int w = first; w <= w1; w += NW * kWave) {
-        const int mine = w + NW * lane;
-        const size_t slot = (size_t)(2 * mine + (mine * walk.per <= from)) * a.rp + r % kDecodeRows;
+        const int mine = min(w + NW * lane, w1);
+        const size_t slot = (size_t)partial_of(mine, walk.per, from) * a.rp + r % kDecodeRows;
         float m = -INFINITY, l = 0.f;
-        if (mine <= w1) {
+        if (w + NW * lane <= w1) {
           m = a.stat[2 * slot];
           l = a.stat[2 * slot + 1];
         }

@@ -10,4 +10,19 @@ constexpr int ring_first(int first, int n) {
   return f < 0 ? f + n : f;
 }
 
+// Blocks of a run where `waves` waves share `total` of them (below 2^31 - 65536).  Runs of one block as long as every second wave has
+// none: more partial results cost the join more than the runs save (one request of 8,000 tokens of 8 heads of 128, 2,016 blocks
+// for 2,048 waves: 18.6 us, runs of two 16.9; of 2,000 tokens 11.7 / 13.2).
+constexpr int run_length(int total, int waves) {
+  if (total <= waves / 2) return 1;
+  const int even = (total + waves - 1) / waves;
+  return even > 2 ? even : 2;
+}
+
+// The partial result in which wave w leaves its part of the unit whose first block is `from`: the second of its two if its
+// run begins no later than the unit.  (Of a wave that has a part: the number of its run's first block is below 2^31 then.)
+constexpr int partial_of(int w, int per, int from) {
+  return 2 * w + (w * per <= from);
+}
+
 }  // namespace ac

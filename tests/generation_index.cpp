@@ -2,3 +2,5 @@
 #include "../paper_2510_25979_amd/csrc/serve_index.h"
 
 extern "C" int ring_first(int first, int n) { return ac::ring_first(first, n); }
+extern "C" int run_length(int total, int waves) { return ac::run_length(total, waves); }
+extern "C" int partial_of(int w, int per, int from) { return ac::partial_of(w, per, from); }

@@ -6,6 +6,8 @@ import subprocess
 
 import pytest
 
+from tests import generation_launches as gl
+
 HERE = os.path.dirname(os.path.abspath(__file__))
 TOP = 2**31 - 1
 
@@ -23,3 +25,54 @@ def test_the_first_entry_of_a_ring(index, n):
     """A ring of pages of one token has up to 2^31 - 1 entries."""
     for first in (0, 1, n - 1, n // 2 + 1, n // 2 - 1, 1_100_000_000, TOP, -1, -n, 1 - n, -TOP - 1):
         assert index.ring_first(first, n) == first % n, first
+
+
+RUN_WAVES = {"f32": 1024, "bf16": 2048}     # of decode_run_kernel
+KEYS = {"f32": 16, "bf16": 32}              # of a block
+MOST = 2**31 - 65536                        # what blocks of 16 keys add up to, two more a unit, has to stay below
+
+
+def _units(call):
+    """Units of 16 rows of a call, and keys of each."""
+    kind, *c = call
+    if kind == "paged":
+        B, Hq, Hkv, _, _, page, width, dt = c
+        rows, keys = Hq // Hkv, page * width
+    else:
+        B, Hq, Hkv, rows, keys, _, dt = c
+        rows *= Hq // Hkv
+    return B * Hkv * -(-rows // 16), keys, dt
+
+
+@pytest.mark.parametrize("waves", sorted(RUN_WAVES.values()))
+def test_runs_cover_all_blocks_and_no_more_than_their_waves(index, waves):
+    for total in (1, waves // 2, waves // 2 + 1, waves, waves + 1, 2 * waves, 2 * waves + 1, 10**6, 2**30 - 1, 2**30, 2**30 + 1, 1_073_774_592,
+                  1_082_130_432, 1_077_936_128, 1_500_000_000, MOST - 1):
+        per = index.run_length(total, waves)
+        assert per == (1 if 2 * total <= waves else max(2, -(-total // waves))), total
+        assert per * waves >= total and (waves - 1) * per <= TOP
+        assert (total - 1) // per < waves
+
+
+# calls whose blocks number more than 2^30: shared pages of many tokens, many rows over few keys, many requests; the last two end just
+# below what is refused
+LARGEST = [("paged", 2048, 8, 8, 1, 1, 1 << 20, 1, "f32"), ("cross", 64, 1, 1, 1 << 20, 4096, 2, "f32"),
+           ("paged", 1 << 19, 8, 8, 64, 9, 16, 509, "bf16"), ("paged", 4095, 8, 8, 64, 9, 1, (1 << 20) - 64, "f32"),
+           ("cross", 1 << 10, 128, 128, 1, 262_080, 2, "f32")]
+
+
+@pytest.mark.parametrize("call", LARGEST, ids=str)
+def test_partial_results_of_the_largest_calls_lie_in_the_workspace(index, tmp_path, call):
+    (status, ls), = gl.record([call], tmp_path)
+    assert status == 0 and [la[0].split("<")[0] for la in ls] == ["decode_run_kernel", "decode_join_kernel"]
+    units, keys, dt = _units(call)
+    cost = -(-keys // KEYS[dt]) + 2
+    waves, total = RUN_WAVES[dt], units * cost
+    assert 2**30 < total and units * (-(-keys // 16) + 2) < MOST
+    per = index.run_length(total, waves)
+    for u in sorted({0, 1, units // 3, units // 2, units - 2, units - 1} | {min(units - 1, w * per // cost) for w in (1, waves // 2, waves - 1)}):
+        start, end = u * cost, u * cost + cost - 3
+        w0, w1 = start // per, end // per
+        assert w1 < waves, u
+        for w in range(w0, w1 + 1):
+            assert index.partial_of(w, per, start) == 2 * w + (w * per <= start) < 2 * waves

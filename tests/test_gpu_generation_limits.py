@@ -3,6 +3,7 @@ test_generation_index.py, without a GPU.)"""
 import pytest
 import torch
 
+from tests import generation as gen
 from tests.test_gpu_parity_small import ac  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -30,3 +31,44 @@ def test_a_ring_of_more_than_two_to_the_thirty_pages(ac, n, first, in_place):  #
     assert slot.tolist() == [[p[4], p[5]], [p[6], -1], [-1, -1]]
     assert table.tolist() == [[p[4], p[5]] + [-1] * 6, [1, 2, 3, 4, 6, p[6], -1, -1], [7, 8, n - 1] + [-1] * 5]
     assert ring[around % n].tolist() == p[:14] + [7, 8, n - 1] + p[17:]
+
+
+def test_runs_of_more_than_two_to_the_thirty_blocks(ac):  # noqa: F811
+    """64 x 2^20 rows over 4,096 keys in binary32: 1,082,130,432 blocks of 16 x 16 with what the units count beside them, 1,056,769 a run.
+    Compared: rows of the first and last units, of the units in which runs begin and of some others."""
+    B, Sq, Sk, D = 64, 1 << 20, 4096, 2
+    g = torch.Generator(device="cuda").manual_seed(3)
+    Q, K, V = (torch.randn(B, 1, s, D, generator=g, device="cuda") for s in (Sq, Sk, Sk))
+    O = torch.full_like(Q, float("nan"))
+    ws = torch.full((ac.attention_cross_workspace_bytes(B, 1, 1, Sq, Sk, D, Q.dtype) // 4,), float("nan"), device="cuda")
+    ac.attention_cross(Q, K, V, O, ws)
+    assert O.isfinite().all()
+    per, cost = 1_056_769, Sk // 16 + 2
+    units = {0, 1, B * Sq // 16 - 1} | {w * per // cost + x for w in range(0, 1024, 31) for x in (-1, 0, 1)} | {12345 * i for i in range(300)}
+    by_item = {}
+    for u in units:
+        if 0 <= u < B * Sq // 16:
+            by_item.setdefault(u * 16 // Sq, []).append(u * 16 % Sq)
+    for b, rows in by_item.items():
+        at = (torch.tensor(rows, device="cuda")[:, None] + torch.arange(16, device="cuda")).flatten()
+        gen.check(O[b, 0, at], *gen.attend(Q[b, 0, at], K[b, 0], V[b, 0]))
+
+
+def test_more_than_two_to_the_thirty_blocks_of_many_requests(ac):  # noqa: F811
+    """2^19 requests on 8 heads, 8,144 tokens each in shared pages: 4,194,304 units of 255 blocks of 32 keys and two further ones."""
+    B, H, D, page, width, n = 1 << 19, 8, 64, 16, 509, 64
+    g = torch.Generator(device="cuda").manual_seed(4)
+    kp, vp = (torch.randn(n, H, page, D, generator=g, device="cuda").bfloat16() for _ in range(2))
+    Q = torch.randn(B, H, D, generator=g, device="cuda").bfloat16()
+    table = torch.randint(0, n, (B, width), generator=g, device="cuda", dtype=torch.int32)
+    lens = torch.full((B,), page * width, dtype=torch.int32, device="cuda")
+    O = torch.full_like(Q, float("nan"))
+    ws = torch.full((ac.attention_paged_workspace_bytes(B, H, H, D) // 4,), float("nan"), device="cuda")
+    ac.attention_paged(Q, kp, vp, table, lens, O, ws)
+    assert O.isfinite().all()
+    per, cost = -(-B * H * 257 // 2048), 257
+    runs = {w * per // cost // H for w in range(0, 2048, 97)}
+    for b in sorted({0, 1, B - 2, B - 1} | runs | {x + 1 for x in runs}):
+        k, v = (t[table[b].long()].transpose(0, 1).flatten(1, 2) for t in (kp, vp))
+        for h in range(H):
+            gen.check(O[b, h:h + 1], *gen.attend(Q[b, h:h + 1], k[h], v[h]))
