@@ -40,7 +40,7 @@ struct DecodeArgs {
   const int32_t *table, *len, *row_sel;
   float *part, *stat;   // partial results [2 waves][rp][D] and their (maximum, sum) [2 waves][rp][2]
   int32_t B, Hkv, R, rbs, rp, D, Sk;   // rbs: row blocks of a K/V head; rp: rows of a partial result
-  int32_t n_pages, ps, max_pages, waves;
+  int32_t n_pages, ps, max_pages, waves, join_rows;   // join_rows: output rows of a wave of the join
   int64_t page_stride, head_stride;
   Divider by_ps, by_rbs;
   float scale_log2e;
@@ -417,8 +417,13 @@ __global__ __launch_bounds__(kThreads, Core::WGS) void decode_run_kernel(const D
   const int D = core.dim();
 
   auto item = [&](DecodeItem& it, int b) {   // the first block of the first item from b on that has any (there is one)
-    int keys;
-    while ((keys = decode_keys_of(a, b)) == 0 && b + 1 < a.B) ++b;
+    int keys = decode_keys_of(a, b);
+    while (keys == 0 && b + 1 < a.B) {   // (64 a step: millions of items may have none)
+      const int other = b + 1 + lane;
+      const unsigned long long some = __ballot(other < a.B && decode_keys(a, other) > 0);
+      b = some ? b + 1 + (int)__builtin_ctzll(some) : min(b + kWave, a.B - 1);
+      keys = decode_keys_of(a, b);
+    }
     it.b = b;
     it.unit = 0;
     it.keys = keys;
@@ -640,21 +645,27 @@ __global__ __launch_bounds__(NW == 1 ? kThreads : NW * kWave) void decode_join_k
   const int sub = lane / G, d = 4 * (lane % G), D = a.D;
   const DecodeWalk<BK> walk(a, lane);
   const int n_rows = a.B * a.Hkv * a.R;   // of all items
-  for (int row = NW == 1 ? blockIdx.x * (kThreads / kWave) + wave : blockIdx.x; row < n_rows;
-       row += NW == 1 ? gridDim.x * (kThreads / kWave) : gridDim.x) {
+  // A wave has consecutive rows and goes from item to item with them: it looks through the items before its first row once, not for each.
+  const int mine = NW == 1 ? blockIdx.x * (kThreads / kWave) + wave : blockIdx.x, each = NW == 1 ? a.join_rows : 1;
+  const int row0 = mine * each;
+  int item = -1, first_block = -1, cost = 0;   // first_block: the item's, -1 until one is asked for; cost of its units
+  for (int row = row0; row < min(n_rows, row0 + each); ++row) {
     const int head = row / a.R, r = row - head * a.R, b = head / a.Hkv, hk = head - b * a.Hkv;
+    const int keys = decode_keys_of(a, b), nb = (keys + BK - 1) / BK;
+    if (b != item && first_block >= 0) first_block += cost * walk.units;
+    item = b;
+    cost = keys ? nb + kUnitCost : 0;
     if (a.row_sel && a.row_sel[b] >= 0) continue;
-    const int keys = decode_keys_of(a, b);
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
     float top = -INFINITY, total = 0.f;
     if (keys > 0) {
-      const int nb = (keys + BK - 1) / BK, from = walk.start(b) + (hk * a.rbs + r / kDecodeRows) * (nb + kUnitCost);
+      if (first_block < 0) first_block = walk.start(b);
+      const int from = first_block + (hk * a.rbs + r / kDecodeRows) * cost;
       const int w0 = from / walk.per, w1 = (from + nb - 1) / walk.per;
       if (w0 == w1) continue;   // one wave had all of it
       const int first = w0 + (NW == 1 ? 0 : wave);
       for (int w = first; w <= w1; w += NW * kWave) {
-        const int mine = min(w + NW * lane, w1);
-        const size_t slot = (size_t)partial_of(mine, walk.per, from) * a.rp + r % kDecodeRows;
+        const size_t slot = (size_t)partial_of(min(w + NW * lane, w1), walk.per, from) * a.rp + r % kDecodeRows;
         float m = -INFINITY, l = 0.f;
         if (w + NW * lane <= w1) {
           m = a.stat[2 * slot];
@@ -777,8 +788,9 @@ static hipError_t launch_decode_core(DecodeArgs& a, hipStream_t stream) {
   } else if (rows <= 1024) {
     hipLaunchKernelGGL((decode_join_kernel<F32, G, 4>), dim3((unsigned)rows), dim3(4 * kWave), 0, stream, a);
   } else {
-    const int64_t wgs = (rows + 3) / 4;
-    hipLaunchKernelGGL((decode_join_kernel<F32, G, 1>), dim3((unsigned)(wgs < 8192 ? wgs : 8192)), dim3(kThreads), 0, stream, a);
+    a.join_rows = rows_of_a_wave((int)rows, 4 * 8192);
+    const int64_t waves = (rows + a.join_rows - 1) / a.join_rows;
+    hipLaunchKernelGGL((decode_join_kernel<F32, G, 1>), dim3((unsigned)((waves + 3) / 4)), dim3(kThreads), 0, stream, a);
   }
   return hipGetLastError();
 }
@@ -796,6 +808,7 @@ hipError_t launch_decode(const DecodeLaunch& p, hipStream_t stream) {
   const float scale = p.scale == 0.f ? 1.0f / sqrtf((float)p.D) : p.scale;
   a.scale_log2e = scale * 1.44269504088896340736f;
   a.waves = 0;
+  a.join_rows = 1;
   a.stat = static_cast<float*>(p.ws);
   a.part = a.stat + (size_t)2 * kDecodeWaves * a.rp * 2;
   auto go = [&](auto paged) {

@@ -25,4 +25,9 @@ constexpr int partial_of(int w, int per, int from) {
   return 2 * w + (w * per <= from);
 }
 
+// Consecutive rows of a wave where at most `most` waves share `rows` of them (below 2^31 - 65536).
+constexpr int rows_of_a_wave(int rows, int most) {
+  return rows > most ? (rows - 1) / most + 1 : 1;
+}
+
 }  // namespace ac

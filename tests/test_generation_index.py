@@ -76,3 +76,28 @@ def test_partial_results_of_the_largest_calls_lie_in_the_workspace(index, tmp_pa
         assert w1 < waves, u
         for w in range(w0, w1 + 1):
             assert index.partial_of(w, per, start) == 2 * w + (w * per <= start) < 2 * waves
+
+
+JOIN_WAVES = 4 * 8192
+
+
+@pytest.mark.parametrize("rows", [1025, JOIN_WAVES - 1, JOIN_WAVES, JOIN_WAVES + 1, 2 * JOIN_WAVES, 10**6, 10**8 + 1, 2**30, MOST - JOIN_WAVES, MOST - 1])
+def test_each_row_of_the_join_is_one_waves(index, rows):
+    """Rows are dealt in one piece each, so that a wave looks through the items once; the numbers of idle waves stay in 31 bits, too."""
+    each = index.rows_of_a_wave(rows, JOIN_WAVES)
+    waves = -(-rows // each)
+    assert each >= 1 and waves <= JOIN_WAVES and (rows > JOIN_WAVES or each == 1)
+    assert -(-waves // 4) * 4 * each <= TOP
+
+
+@pytest.mark.parametrize("call", [
+    ("paged", 1 << 23, 1, 1, 64, 9, 1, 1, "bf16"), ("paged", 1 << 23, 4, 4, 64, 9, 16, 1, "f32"), ("cross", 1 << 24, 16, 1, 1, 7, 64, "bf16"),
+    ("paged", 1 << 19, 8, 8, 64, 9, 16, 509, "bf16"), ("paged", 3000, 16, 4, 64, 9, 16, 200, "bf16")], ids=str)
+def test_lengths_are_looked_through_once_a_wave(index, tmp_path, call):
+    """As many waves are launched as have a piece of the rows: each goes on from item to item, and none looks through the lengths again."""
+    (status, ls), = gl.record([call], tmp_path)
+    run, join = ls
+    assert status == 0 and run[0].startswith("decode_run_kernel") and join[0].startswith("decode_join_kernel")
+    rows = call[1] * call[2]
+    waves = -(-rows // index.rows_of_a_wave(rows, JOIN_WAVES))
+    assert join[1] * join[4] // 64 == -(-waves // 4) * 4 <= JOIN_WAVES

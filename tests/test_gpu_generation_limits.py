@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from tests import generation as gen
+from tests.test_gpu_paged_attention import Cache
 from tests.test_gpu_parity_small import ac  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -72,3 +73,50 @@ def test_more_than_two_to_the_thirty_blocks_of_many_requests(ac):  # noqa: F811
         k, v = (t[table[b].long()].transpose(0, 1).flatten(1, 2) for t in (kp, vp))
         for h in range(H):
             gen.check(O[b, h:h + 1], *gen.attend(Q[b, h:h + 1], k[h], v[h]))
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,dt", [(16, 2, 64, "bf16"), (12, 12, 64, "f32")])
+def test_every_row_of_many_requests(ac, Hq, Hkv, D, dt):  # noqa: F811
+    """More output rows than the join has waves: each wave has some that follow one another, over the ends of requests and over empty ones."""
+    rnd = torch.Generator().manual_seed(D + Hq)
+    lens = torch.randint(0, 130, (3000,), generator=rnd) * (torch.rand(3000, generator=rnd) < 0.7)
+    lens[[0, 17, 18, 1500, 2999]] = torch.tensor([2500, 0, 1900, 3100, 1])
+    c = Cache(lens.tolist(), Hkv, D, dt, 16, 5, width=200)
+    Q = torch.randn(3000, Hq, D, generator=c.gen, device="cuda").to(c.k.dtype)
+    O = c.call(ac, Q)
+    assert O.isfinite().all() and (O[c.len == 0] == 0).all()
+    c.check(O, Q, lens.nonzero().flatten().tolist())
+
+
+def test_long_stretches_of_empty_requests(ac):  # noqa: F811
+    """A run goes from a request to the next one that has tokens, past half a million that have none."""
+    B = (1 << 20) + 3
+    some = sorted({0, 1, 2, 64, 65, 200, 5000, 5063, 5064, 5065, 500_000, B - 130, B - 66, B - 65, B - 2, B - 1} | set(range(300_000, 300_400, 7)))
+    few = Cache([1 + 331 * i % 1997 for i in range(len(some))], 1, 64, "bf16", 16, 6, width=130)
+    c = Cache([0], 1, 64, "bf16", 16, 7)
+    c.k, c.v = few.k, few.v
+    c.table, c.len = torch.full((B, 130), -1, dtype=torch.int32, device="cuda"), torch.zeros(B, dtype=torch.int32, device="cuda")
+    c.table[some], c.len[some] = few.table, few.len
+    Q = torch.randn(B, 3, 64, generator=c.gen, device="cuda").bfloat16()
+    O = c.call(ac, Q)
+    few.check(O[some], Q[some])
+    assert (O[c.len == 0] == 0).all()
+
+
+def test_items_left_out_between_others(ac):  # noqa: F811
+    """Cross attention by runs with more rows than the join has waves, most items left out by row_sel and some empty."""
+    B, H, Sq, Sk, D = 3000, 2, 8, 2100, 64
+    g = torch.Generator(device="cuda").manual_seed(8)
+    Q, K, V = (torch.randn(B, H, s, D, generator=g, device="cuda", dtype=torch.bfloat16) for s in (Sq, Sk, Sk))
+    lens = torch.randint(0, 400, (B,), generator=torch.Generator().manual_seed(9)).int().cuda()
+    lens[::9], lens[5] = 0, Sk
+    sel = torch.full((B,), 3, dtype=torch.int32, device="cuda")
+    sel[5:1000:3] = sel[2000:2100] = sel[-1] = -1
+    O = torch.full_like(Q, 7.0)
+    ws = torch.full((ac.attention_cross_workspace_bytes(B, H, H, Sq, Sk, D, Q.dtype) // 4,), float("nan"), device="cuda")
+    ac.attention_cross(Q, K, V, O, ws, row_sel=sel, key_len=lens)
+    assert (O[sel >= 0] == 7.0).all()
+    for b in (sel < 0).nonzero().flatten().tolist():
+        n = int(lens[b])
+        for h in range(H):
+            gen.check(O[b, h], *gen.attend(Q[b, h], K[b, h, :n], V[b, h, :n]))
