@@ -174,7 +174,6 @@ __global__ __launch_bounds__(NT) void page_plan_kernel(const PlanArgs a) {
 }
 
 constexpr int kPlanSmall = 4096;   // slots that one workgroup writes
-constexpr int kPlanSlots = 1024;   // slots of a workgroup beyond that: 256 x 1,024 slots 5.3 us, 2,048 6.2; 2,000 x 500 24.6, 512 27.0
 hipError_t launch_plan(const PlanLaunch& p, hipStream_t stream) {
   PlanArgs a;
   a.seq_len = p.seq_len; a.new_len = p.new_len; a.state = p.free_state;
@@ -194,9 +193,8 @@ hipError_t launch_plan(const PlanLaunch& p, hipStream_t stream) {
     return hipGetLastError();
   }
   PlanArgs r = a;
-  r.rows = p.S >= kPlanSlots ? 1 : kPlanSlots / p.S;
-  if (r.rows > kThreads) r.rows = kThreads;
-  r.seg = p.S > kPlanSlots ? kPlanSlots : p.S;
+  r.rows = plan_rows(p.B, p.S);
+  r.seg = r.rows == 1 && p.S > kPlanSlots ? kPlanSlots : p.S;
   const unsigned gx = (unsigned)((p.B + r.rows - 1) / r.rows), gy = (unsigned)((p.S + r.seg - 1) / r.seg);
   if (p.seq_len_out != p.seq_len && p.added != p.new_len && p.free_state_out != p.free_state) {
     hipLaunchKernelGGL((page_plan_kernel<kThreads, kPlanBoth>), dim3(gx + 1, gy), dim3(kThreads), 0, stream, r);

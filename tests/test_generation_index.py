@@ -101,3 +101,20 @@ def test_lengths_are_looked_through_once_a_wave(index, tmp_path, call):
     rows = call[1] * call[2]
     waves = -(-rows // index.rows_of_a_wave(rows, JOIN_WAVES))
     assert join[1] * join[4] // 64 == -(-waves // 4) * 4 <= JOIN_WAVES
+
+
+@pytest.mark.parametrize("S", [1, 2, 3, 4, 5, 100, 511, 512, 513, 1023, 1024, 1025, 4000, 10**5, 1 << 25])
+def test_rows_of_a_workgroup_of_the_page_plan(index, S):
+    """At most 16,384 workgroups sum the requests before their own, as far as slots of all requests fit any memory (2^40 of them)."""
+    for B in (1, 2, 300, 4097, 16384, 16385, 100_000, (1 << 22) - 1, 1 << 22):
+        rows = index.plan_rows(B, S)
+        assert 1 <= rows <= 256 and rows * S <= TOP
+        assert -(-B // rows) <= 16384 or B * S > 2**40
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("B,S", [(1 << 22, 4000), (1 << 22, 1), (40_000, 1500), (256, 1024), (2, 5000)])
+def test_workgroups_of_the_page_plan(tmp_path, B, S, in_place):
+    (status, ls), = gl.record([("plan", B, S, 500, 16, 1000, in_place)], tmp_path)
+    assert status == 0 and len(ls) == 1 + in_place
+    assert ls[0][1] <= 16384 + 1 and (B > 2 or ls[0][2] == 5)       # a row of its own is shared

@@ -120,3 +120,21 @@ def test_items_left_out_between_others(ac):  # noqa: F811
         n = int(lens[b])
         for h in range(H):
             gen.check(O[b, h], *gen.attend(Q[b, h], K[b, h, :n], V[b, h, :n]))
+
+
+@pytest.mark.parametrize("B,S,fresh", [(40_000, 1500, True), (20_000, 1025, False), (200_000, 200, True)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_plans_of_more_requests_than_workgroups(ac, B, S, fresh, in_place):  # noqa: F811
+    """Several rows a workgroup although each has more slots than one writes elsewhere; more is wanted than is free."""
+    from perf import operators
+    st = operators.prepare(dict(kind="plan", B=B, S=S, page=16, max_pages=200, lo=1, hi=S if fresh else 1500, fresh=fresh,
+                                ended=0 if fresh else B // 5, short=True, spare=30), 11)
+    want = operators._plain_plan(st)
+    if in_place:
+        st.update(seq_len_out=st["seq_len"], added=st["new_len"], free_state_out=st["free_state"])
+    st["slot"].fill_(99)
+    ac.attncache_page_plan(*(st[n] for n in ("seq_len", "new_len", "free_state", "free_pages", "page_table", "seq_len_out", "added",
+                                             "free_state_out", "slot")), page_size=16)
+    assert 0 < int((want["added"] > 0).sum()) < B
+    for name, x in want.items():
+        assert torch.equal(st[name], x), name
