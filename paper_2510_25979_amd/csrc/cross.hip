@@ -6,7 +6,8 @@
 // formed transposed (S^T = K Q^T, O^T = V^T P^T), so that a lane holds scores of one row, and the weights go from the first
 // product to the second without leaving their registers.  4 Sk D flop a row against 4 Sk D / 128 bytes: the matrix cores and, more
 // so, the vector work beside them at the clock the chip grants bound it.  16 x 32 heads, 1024 x 2047 keys of 128: 555 us = 0.99 PFLOP/s (a
-// library's 16384^3 product reaches 1.36 on the card, an 8192^3 one 1.25).  Both blocks of a chunk take a softmax step of their own, in an
+// library's 16384^3 product reaches 1.36 on the card, an 8192^3 one 1.25) in turn with other work, 607 to 615 where such calls follow one another: the same cycles
+// at a lower clock.  The matrix pipe is busy in 54 % of them, 31 % of that together with vector work.  Both blocks of a chunk take a softmax step of their own, in an
 // order that lets matrix and vector work of a wave overlap.  Raised wave priority in either product or in the exponentials: 2 to 3 % slower.
 #include <type_traits>
 
@@ -141,8 +142,8 @@ __global__ __launch_bounds__(kThreads, 2) void cross_bf16_kernel(const CrossArgs
     const float m05 = fmaxf(fmaxf(s[12], s[13]), s[14]);
     return max_with_other_half(fmaxf(fmaxf(fmaxf(m01, m02), m03), fmaxf(fmaxf(m04, m05), s[15])));
   };
-  // Weights 2^(score - m) in bf16, the second product's operand; their sum is over the rounded ones, which V is multiplied
-  // with.  (m = -inf: no finite score so far, all weights are zero.)
+  // Weights 2^(score - m) in bf16, the second product's operand (it takes both factors in one type, and V is bf16); their sum is over the
+  // rounded ones, which V is multiplied with, so that they still add up to one.  (m = -inf: no finite score so far, all weights are zero.)
   typedef bf16_t bf16x2 __attribute__((ext_vector_type(2)));
   auto weights = [&](const f32x16& s, float m, u32x4(&pw)[2], float& sum) {
     const bf16x2 ones = {(bf16_t)1.0f, (bf16_t)1.0f};
@@ -246,10 +247,11 @@ __global__ __launch_bounds__(kThreads, 2) void cross_bf16_kernel(const CrossArgs
       step(kc, vc, min(kCrossChunk, keys - c * kCrossChunk), true, FOLLOW);
     }
   };
-  // Over many keys the reference points stay where the first keys put them: weights may be as large as 2^127, and no digit is lost
-  // where later scores are larger.  A step then has a fifth fewer vector instructions and no exchange between lanes ahead of its
+  // Over many keys the reference points stay where the first keys put them: weights may grow until a sum of them reaches 10^18 (2^60),
+  // and no digit is lost where later scores are larger.  A step then has a fifth fewer vector instructions and no exchange between lanes ahead of its
   // exponentials.  A workgroup of which a row's sum or result leaves the range (or is NaN), or whose
-  // first keys were all -inf (no point to stay at), walks again, with points that follow.
+  // first keys were all -inf (no point to stay at), walks again, with points that follow: all workgroups of 16 x 32 heads, 1024 x 2047 keys
+  // 1,095 us instead of 607, of 64 heads of 2048 x 4096 487 instead of 254 (calls following one another).
   // 16 x 32 heads, 1024 x 2047 keys of 128: 590 us following, 555 so; 64 heads of 2048 x 4096 539 / 504, 1024 x 1024 306 / 293, x 700 234 / 227,
   // lengths of 100 to 500 as long.  Of 64 columns both take as long, and the code for both costs short calls a tenth: kernels of their own.
   bool follow = !STAY || full < kCrossLong;
@@ -425,7 +427,8 @@ __global__ __launch_bounds__(kThreads, DB <= 2 ? 2 : 1) void cross_f32_kernel(co
 // 45.9 / 33.7; 512 x 32 x 100 (1,024) 7.8 / 7.7 and 12.5 / 12.3; 512 x 32 x 1000 33.9 / 27.6 and 66.4 / 53.1.  Binary32, by workgroups of 32
 // rows (as here where they are few): 64 x 64 x 300 of 128 (128) 14.3 / 21.1; 16 x 282 x 333, ragged (144) 16.5 / 16.9; 256 x 32 x 300 (256) 23.6 / 22.1,
 // ragged 17.8 / 21.2; 128 x 64 x 500 (256) 33.7 / 32.0, x 1000 of 256 226 / 133; 64 x 282 x 333, ragged (576) 38.5 / 33.2, x 1000 62.3 / 65.8; 512 x 20 x
-// 500 (512) 68 / 54.
+// 500 (512) 68 / 54.  (The host does not know the lengths: the line is where equal ones change sides, and two of the ragged sizes here lose by it.  Keys
+// beyond 1,500 were not swept.)
 static bool cross_by_rows(int64_t B, int64_t Hkv, int64_t R, int64_t Sk, int32_t D, int32_t is_f32) {
   const int64_t heads = B * Hkv;
   if (is_f32) return D >= 4 && R > 16 && heads * ((R + 2 * kF32Rows - 1) / (2 * kF32Rows)) >= 256;
@@ -456,7 +459,8 @@ static hipError_t launch_cross_f32(CrossArgs a, hipStream_t stream) {
   // workgroups of 64 rows, keys of 128: few of them, 128 x 64 x 500 (128) 45.4 / 32.0, of 256 x 1000 228 / 133, 256 x 64 x 1000 (256) 88 / 92;
   // two a compute unit and ragged (a long one beside a long one), 64 x 282 x 333 (320) 37.5 / 33.2, 448 x 64 x 300 (448) 41.9 / 36.6, x 576
   // (576) 49.7 / 48.4, not ragged (448) 54.6 / 61.1; last workgroups at most half full, 512 x 20 x 500 (512) 85 / 54, 512 x 130 x 300 (1,536) 145 /
-  // 142, 512 x 270 x 300 (2,560) 239 / 240; others, 512 x 40 x 300 (512) 55.8 / 67.4, 64 x 3000 x 1000 (3,008) 340 / 382.
+  // 142, 512 x 270 x 300 (2,560) 239 / 240; others, 512 x 40 x 300 (512) 55.8 / 67.4, 64 x 3000 x 1000 (3,008) 340 / 382.  (Whether lengths are given stands
+  // for ragged ones, since the host does not know them: where they are all the same, 448 workgroups take 61.1 and not 54.6.)
   const int64_t wgs = (int64_t)a.tiles * a.per;
   if (wgs < 256 || (a.len && wgs < 512) || (a.R < 320 && (a.R - 1) % 64 < 32)) {
     a.per = (a.R + 2 * kF32Rows - 1) / (2 * kF32Rows);

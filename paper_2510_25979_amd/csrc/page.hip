@@ -5,7 +5,8 @@
 // ones.  With P the running sum of d over the requests, request b takes entries [P_b - d_b, P_b) of the free pages'
 // ring if P_b does not exceed what is there.  Ended requests put their pages behind the ring's last one; these places are
 // not among those that are read, so pages go both ways in one launch and without an order among workgroups.
-// Bound by latency: dependent loads (lengths -> sums -> ring -> slots), 4.8 us for 64 requests of one token.
+// Bound by latency: dependent loads (lengths -> sums -> ring -> slots), 4.1 us for 64 requests of one token.  From some thousands of requests
+// on the workgroup that writes the new state, 256 of them a step, is the longest: 2^20 requests 4.9 ms, 2^22 41.
 #include "common.hpp"
 #include "serve.h"
 #include "serve_index.h"
@@ -84,7 +85,8 @@ __device__ __forceinline__ int row_of(const int* start, int rows, int e) {
 // What workgroups do: kPlanAll one alone does everything (it reads every array that may be written in place before it writes it);
 // kPlanRows page table, ring and slots of its rows, summing what lies before them for itself; kPlanState one alone the new lengths
 // and the ring's new state; kPlanBoth the last one the state, the others rows, where no output is an input.
-// us: 256 prompts of up to 1,024 tokens 10.6 in two launches, 5.3 in one; 64 requests of one token 4.8 in one workgroup.
+// us: 256 prompts of up to 1,024 tokens 10.6 in two launches, 5.3 in one; 64 requests of one token 4.1 in one workgroup of 256
+// threads.
 enum PlanWork { kPlanAll, kPlanRows, kPlanState, kPlanBoth };
 template <int NT, PlanWork WORK>
 __global__ __launch_bounds__(NT) void page_plan_kernel(const PlanArgs a) {
