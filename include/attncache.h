@@ -562,6 +562,123 @@ int32_t attention_cross(const void *Q, const void *K, const void *V, void *O,
                         void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * From a projection's product to Q, K and V: its rows are split into heads,
+ * Q and K heads normalised and rotated by their positions, and each head goes
+ * where the calls above want it, in one pass.
+ *
+ *   y = x / sqrt(mean(x^2) + eps) * weight     (where a weight is given)
+ *   (a, b) -> amplitude * (a cos t - b sin t, b cos t + a sin t)
+ *                      t = pos * freq[i], pair i of the first rot columns
+ *
+ *   X          DEVICE, B * S rows of dtype (AC_BF16: D 64 or 128; AC_F32:
+ *              D <= 256): Hq heads of Q, Hkv of K, Hkv of V, D elements each.
+ *              Rows lie row_stride elements apart (at least their size), items
+ *              batch_stride (any, with B 1 not looked at); where D elements are
+ *              a whole number of 16-byte pieces, both must be, too.
+ *   q_weight, k_weight  NULL (no normalisation) or DEVICE [D] float.
+ *   pos        DEVICE [B][S] int32.  Negative: the row is padding, and nothing
+ *              of it is written anywhere.
+ *   freq       DEVICE [rot / 2] double, radians a position, e.g. from
+ *              attncache_rotary_frequencies.  rot even, 0 to D; columns from
+ *              rot on are not rotated.  Angles are formed modulo one turn with
+ *              64 bits and hold at any position; |freq| below 2^40.
+ *   interleaved  0: pairs are columns (i, i + rot / 2), otherwise (2i, 2i + 1).
+ *   Q          DEVICE [B][Hq][S][D] out.
+ *   K, V       DEVICE [B][Hkv][S][D] out, or both NULL with slot.
+ *   slot       NULL, or DEVICE [B][S] int32: K and V rows also go to these
+ *              slots of k_pages and v_pages, as in attncache_page_append.
+ *
+ * binary32 inside, one rounding at the end.  eps >= 0.  The outputs may not
+ * overlap X.  Hq + 2 Hkv <= 65535, B * S below 2^31 - 4096.
+ */
+int32_t attncache_rotate(const void *X, const float *q_weight,
+                         const float *k_weight, const int32_t *pos,
+                         const double *freq, const int32_t *slot, void *Q,
+                         void *K, void *V, void *k_pages, void *v_pages,
+                         int32_t B, int32_t S, int32_t Hq, int32_t Hkv,
+                         int32_t D, int32_t rot, int64_t batch_stride,
+                         int64_t row_stride, int32_t n_pages,
+                         int32_t page_size, int64_t page_stride,
+                         int32_t dtype, int32_t interleaved, float eps,
+                         float amplitude, void *stream);
+
+/*
+ * freq[i] = base^(-2 i / rot), i < rot / 2, scaled for contexts `factor` times
+ * as long as the model was trained on.  freq is HOST memory; nothing runs on
+ * a GPU.  rot even, at least 2.
+ *
+ *   AC_ROTARY_PLAIN   not scaled (factor and what follows are not looked at)
+ *   AC_ROTARY_LINEAR  freq / factor
+ *   AC_ROTARY_BASE    base * factor^(rot / (rot - 2)) in the place of base: the
+ *                     fastest pair stays, the slowest is stretched by factor
+ *                     (rot at least 4)
+ *   AC_ROTARY_RAMP    pairs with at most `low` turns within original_len are
+ *                     stretched by factor, with at least `high` not at all,
+ *                     between them freq is a weighted mean of both
+ */
+#define AC_ROTARY_PLAIN 0
+#define AC_ROTARY_LINEAR 1
+#define AC_ROTARY_BASE 2
+#define AC_ROTARY_RAMP 3
+int32_t attncache_rotary_frequencies(double *freq, int32_t rot, double base,
+                                     int32_t scaling, double factor,
+                                     double original_len, double low,
+                                     double high);
+
+/*
+ * Rows of a paged cache become other rows: row b holds afterwards what row
+ * from[b] held before.  Beams change places, several answers begin at one
+ * prompt, requests end, and pages that a window has left behind go back.
+ *
+ *   from       DEVICE [B] int32.  b itself: the row goes on.  Outside [0, B),
+ *              such as -1: the row ends and holds nothing.
+ *   seq_len, free_state, free_pages  DEVICE, as in attncache_page_plan.
+ *   page_table DEVICE [B][max_pages] int32: entries below
+ *              ceil(seq_len / page_size) are read; those outside
+ *              [0, n_pages) name no page and are taken over as -1 or as they
+ *              are.
+ *   page_table_out  DEVICE [B][max_pages] int32: the new rows' entries; others
+ *              keep what they hold.
+ *   seq_len_out  DEVICE [B] int32: seq_len[from[b]], 0 for a row that ends, -1
+ *              for one that got no page (below), which holds nothing either.
+ *   free_state_out  DEVICE [2] int32.
+ *   k_pages, v_pages  DEVICE, with H heads (all layers: they fold into heads).
+ *   sinks, window  window 0: nothing.  Otherwise pages of which every token
+ *              j has j >= sinks and j < length - window go back, and their
+ *              entries become -1: what attention_paged_window with this window
+ *              sees of the row and of its later tokens stays.
+ *
+ * Full pages are shared among the rows that come from one.  A page that is
+ * not full is kept by one (the row itself if it goes on, otherwise the first
+ * that comes from it); each other takes a page from the ring, in order of
+ * row, and its tokens are copied.  Rows for which the ring has none left get
+ * nothing.  Pages that some row held and none holds afterwards go behind the
+ * ring's last one, in order of their number, for the next call.
+ *
+ * All rows of the cache belong into one call: a page that a row outside it
+ * holds would be given back.  attncache_page_plan goes on from the result (a
+ * page it writes to is one row's), but does not know about sharing: rows that
+ * share pages, or have lost some to a window, end here.
+ * The outputs may be the inputs of the same meaning, or not overlap them.
+ * workspace: DEVICE, attncache_page_fork_workspace_bytes(...) bytes, 16-byte
+ * aligned; scratch.  Three launches.  B <= 2^22, B * max_pages below
+ * 2^31 - 4096, page_size * D <= 2^30, otherwise as in attncache_page_plan.
+ */
+size_t attncache_page_fork_workspace_bytes(int32_t B, int32_t max_pages,
+                                           int32_t n_pages);
+int32_t attncache_page_fork(const int32_t *from, const int32_t *seq_len,
+                            const int32_t *free_state, int32_t *free_pages,
+                            const int32_t *page_table,
+                            int32_t *page_table_out, int32_t *seq_len_out,
+                            int32_t *free_state_out, void *k_pages,
+                            void *v_pages, int32_t B, int32_t H, int32_t D,
+                            int32_t max_pages, int32_t n_pages,
+                            int32_t page_size, int64_t page_stride,
+                            int32_t sinks, int32_t window, int32_t dtype,
+                            void *workspace, size_t workspace_bytes,
+                            void *stream);
+
+/*
  * Switches the per-call memory-space checks of pointers on (non-zero, the
  * default) or off for the whole process; returns the previous setting.
  * attncache_build_db always checks.

@@ -21,6 +21,7 @@ AC_F32, AC_F16, AC_BF16 = 0, 1, 2
 AC_IP, AC_L2 = 0, 1
 AC_LAYOUT_DENSE, AC_LAYOUT_PACKED = 0, 1
 AC_MAX_K = 64
+AC_ROTARY_PLAIN, AC_ROTARY_LINEAR, AC_ROTARY_BASE, AC_ROTARY_RAMP = 0, 1, 2, 3
 
 _DTYPE_CODE = {torch.float32: AC_F32, torch.float16: AC_F16, torch.bfloat16: AC_BF16}
 
@@ -30,7 +31,9 @@ SYMBOLS = ["attncache_workspace_bytes", "attncache_map_entry_bytes", "attncache_
            "attncache_cache_stats", "attncache_cache_reset",
            "attncache_project_workspace_bytes", "attncache_project",
            "attncache_page_plan", "attncache_page_append", "attention_paged_workspace_bytes", "attention_paged",
-           "attention_cross_workspace_bytes", "attention_cross", "attncache_status_string",
+           "attention_cross_workspace_bytes", "attention_cross",
+           "attncache_rotate", "attncache_rotary_frequencies", "attncache_page_fork_workspace_bytes", "attncache_page_fork",
+           "attncache_status_string",
            "attncache_last_hip_error", "attncache_version", "attncache_set_pointer_checks"]
 
 
@@ -107,6 +110,15 @@ def lib():
         L.attention_cross_workspace_bytes.argtypes = [i32] * 7
         L.attention_cross.restype = i32
         L.attention_cross.argtypes = [vp] * 6 + [i32] * 7 + [f32, vp, sz, vp]
+        f64 = ctypes.c_double
+        L.attncache_rotate.restype = i32
+        L.attncache_rotate.argtypes = [vp] * 11 + [i32] * 6 + [i64] * 2 + [i32] * 2 + [i64] + [i32] * 2 + [f32] * 2 + [vp]
+        L.attncache_rotary_frequencies.restype = i32
+        L.attncache_rotary_frequencies.argtypes = [vp, i32, f64, i32, f64, f64, f64, f64]
+        L.attncache_page_fork_workspace_bytes.restype = sz
+        L.attncache_page_fork_workspace_bytes.argtypes = [i32] * 3
+        L.attncache_page_fork.restype = i32
+        L.attncache_page_fork.argtypes = [vp] * 10 + [i32] * 6 + [i64] + [i32] * 3 + [vp, sz, vp]
         L.attncache_status_string.restype = ctypes.c_char_p
         L.attncache_status_string.argtypes = [i32]
         L.attncache_last_hip_error.restype = i32
@@ -536,3 +548,94 @@ def attention_cross(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, O: torch.
         _dev(workspace, "workspace"), workspace.numel() * workspace.element_size())
     _check(lib().attention_cross(qp, kp, vp, op, rp, lp, B, Hq, Hkv, Sq, Sk, D, _DTYPE_CODE[Q.dtype], float(scale),
                                  wp, w_bytes, _stream(stream)), "attention_cross")
+
+
+def attncache_rotary_frequencies(rot: int, *, base: float = 10000.0, scaling: int = AC_ROTARY_PLAIN, factor: float = 1.0,
+                                 original_len: float = 0.0, low: float = 1.0, high: float = 4.0) -> torch.Tensor:
+    """[rot/2] f64 on the host: what attncache_rotate takes, once it is on the device."""
+    freq = torch.empty(max(rot, 0) // 2, dtype=torch.float64)
+    _check(lib().attncache_rotary_frequencies(freq.data_ptr(), rot, base, scaling, factor, original_len, low, high),
+           "attncache_rotary_frequencies")
+    return freq
+
+
+def attncache_rotate(X: torch.Tensor, pos: torch.Tensor, freq: Optional[torch.Tensor], Q: torch.Tensor,
+                     K: Optional[torch.Tensor] = None, V: Optional[torch.Tensor] = None, *,
+                     q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                     amplitude: float = 1.0, interleaved: bool = False, slot: Optional[torch.Tensor] = None,
+                     k_pages: Optional[torch.Tensor] = None, v_pages: Optional[torch.Tensor] = None,
+                     stream: Optional[torch.cuda.Stream] = None) -> None:
+    """X [B,S,(Hq+2Hkv)*D] bf16 or f32, of any strides but the last; pos [B,S] int32; freq [rot/2] f64 or None; Q [B,Hq,S,D];
+    K,V [B,Hkv,S,D]; q_weight, k_weight [D] f32; slot [B,S] int32 with k_pages,v_pages [n_pages,Hkv,page_size,D]."""
+    if X.dim() != 3 or Q.dim() != 4:
+        raise ValueError("X must be [B,S,(Hq+2Hkv)*D] and Q [B,Hq,S,D]")
+    dtype = X.dtype
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("unsupported dtype")
+    (B, S, width), (_, Hq, _, D) = X.shape, Q.shape
+    Hkv = (width // D - Hq) // 2 if D > 0 else 0
+    if Hkv < 1 or (Hq + 2 * Hkv) * D != width:
+        raise ValueError(f"rows of X must hold {Hq} + 2 Hkv heads of {D}, have {width} elements")
+    if K is None and V is not None or V is None and K is not None:
+        raise ValueError("K and V must be given both, or none of them")
+    if (slot is None) != (k_pages is None) or (slot is None) != (v_pages is None):
+        raise ValueError("slot, k_pages and v_pages must be given all, or none of them")
+    if K is None and slot is None:
+        raise ValueError("K and V need a place: K and V, or slot, k_pages and v_pages")
+    i32, f32 = torch.int32, torch.float32
+    xp = _address(X, dtype, None)
+    if xp is None:
+        if not X.is_cuda:
+            raise ValueError("X must be a CUDA tensor")
+        if width > 1 and X.stride(2) != 1:
+            raise ValueError("rows of X must be contiguous")
+        xp = X.data_ptr()
+    # (the stride of a dimension of one element says nothing)
+    row_stride = X.stride(1) if S > 1 else width
+    batch_stride = X.stride(0) if B > 1 else 0
+    pp = _dev(pos, "pos", i32, (B, S))
+    rot = 0 if freq is None else 2 * freq.numel()
+    fp = None if rot == 0 else _dev(freq, "freq", torch.float64, (rot // 2,))
+    qw = None if q_weight is None else _dev(q_weight, "q_weight", f32, (D,))
+    kw = None if k_weight is None else _dev(k_weight, "k_weight", f32, (D,))
+    qp = _dev(Q, "Q", dtype, (B, Hq, S, D))
+    kp = None if K is None else _dev(K, "K", dtype, (B, Hkv, S, D))
+    vp = None if V is None else _dev(V, "V", dtype, (B, Hkv, S, D))
+    sp, kc, vc, n, page, stride = None, None, None, 0, 0, 0
+    if slot is not None:
+        sp = _dev(slot, "slot", i32, (B, S))
+        kc, vc, n, page, stride = _pages(k_pages, v_pages, dtype, Hkv, D)
+    _check(lib().attncache_rotate(xp, qw, kw, pp, fp, sp, qp, kp, vp, kc, vc, B, S, Hq, Hkv, D, rot, batch_stride, row_stride,
+                                  n, page, stride, _DTYPE_CODE[dtype], int(interleaved), float(eps), float(amplitude),
+                                  _stream(stream)), "attncache_rotate")
+
+
+def attncache_page_fork_workspace_bytes(B: int, max_pages: int, n_pages: int) -> int:
+    return int(lib().attncache_page_fork_workspace_bytes(B, max_pages, n_pages))
+
+
+def attncache_page_fork(from_row: torch.Tensor, seq_len: torch.Tensor, free_state: torch.Tensor, free_pages: torch.Tensor,
+                        page_table: torch.Tensor, page_table_out: torch.Tensor, seq_len_out: torch.Tensor,
+                        free_state_out: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, workspace: torch.Tensor, *,
+                        sinks: int = 0, window: int = 0, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """All int32: from_row, seq_len, seq_len_out [B]; free_state, free_state_out [2]; free_pages [n_pages]; page_table,
+    page_table_out [B,max_pages].  The outputs may be the inputs of the same meaning.  k_pages,v_pages
+    [n_pages,H,page_size,D] bf16 or f32, whose pages may lie further apart than their size."""
+    if page_table.dim() != 2 or k_pages.dim() != 4:
+        raise ValueError("page_table must be [B,max_pages], k_pages and v_pages [n_pages,H,page_size,D]")
+    if k_pages.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("unsupported dtype")
+    i32, (B, max_pages), (_, H, _, D) = torch.int32, page_table.shape, k_pages.shape
+    kc, vc, n, page, stride = _pages(k_pages, v_pages, k_pages.dtype, H, D)
+    rp = _dev(from_row, "from_row", i32, (B,))
+    lp = _dev(seq_len, "seq_len", i32, (B,))
+    fs = _dev(free_state, "free_state", i32, (2,))
+    fp = _dev(free_pages, "free_pages", i32, (n,))
+    tp = _dev(page_table, "page_table", i32)
+    to = _dev(page_table_out, "page_table_out", i32, (B, max_pages))
+    lo = _dev(seq_len_out, "seq_len_out", i32, (B,))
+    fo = _dev(free_state_out, "free_state_out", i32, (2,))
+    wp = _dev(workspace, "workspace")
+    _check(lib().attncache_page_fork(rp, lp, fs, fp, tp, to, lo, fo, kc, vc, B, H, D, max_pages, n, page, stride, sinks, window,
+                                     _DTYPE_CODE[k_pages.dtype], wp, workspace.numel() * workspace.element_size(),
+                                     _stream(stream)), "attncache_page_fork")

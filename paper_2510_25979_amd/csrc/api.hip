@@ -5,6 +5,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <cstdlib>
 #include <cstring>
 #include <initializer_list>
@@ -758,6 +759,115 @@ int32_t attention_cross(const void* Q, const void* K, const void* V, void* O, co
   p.n_pages = 1; p.page_size = 1; p.max_pages = 1; p.page_stride = 0;
   p.scale = scale; p.ws = workspace;
   const hipError_t e = ac::launch_cross(p, reinterpret_cast<hipStream_t>(stream));
+  return e == hipSuccess ? AC_OK : hip_fail(e);
+}
+
+int32_t attncache_rotary_frequencies(double* freq, int32_t rot, double base, int32_t scaling, double factor,
+                                     double original_len, double low, double high) {
+  if (rot < 2 || rot % 2 != 0) return AC_ERR_SHAPE;
+  if (!(base > 0) || !std::isfinite(base)) return AC_ERR_SHAPE;
+  if (scaling < AC_ROTARY_PLAIN || scaling > AC_ROTARY_RAMP) return AC_ERR_DTYPE;
+  if (scaling != AC_ROTARY_PLAIN && !(factor > 0 && std::isfinite(factor))) return AC_ERR_SHAPE;
+  if (scaling == AC_ROTARY_BASE && rot < 4) return AC_ERR_SHAPE;
+  if (scaling == AC_ROTARY_RAMP && !(original_len > 0 && high > low && std::isfinite(original_len) && std::isfinite(high - low)))
+    return AC_ERR_SHAPE;
+  if (!freq) return AC_ERR_NULL;
+  if (scaling == AC_ROTARY_BASE) base *= std::pow(factor, (double)rot / (rot - 2));
+  for (int32_t i = 0; i < rot / 2; ++i) {
+    double f = std::pow(base, -2.0 * i / rot);
+    if (scaling == AC_ROTARY_LINEAR) f /= factor;
+    if (scaling == AC_ROTARY_RAMP) {   // turns within the original length: few are stretched, many are not
+      const double turns = original_len * f / 6.283185307179586476925287;
+      const double keep = std::min(1.0, std::max(0.0, (turns - low) / (high - low)));
+      f = keep * f + (1.0 - keep) * f / factor;
+    }
+    freq[i] = f;
+  }
+  return AC_OK;
+}
+
+int32_t attncache_rotate(const void* X, const float* q_weight, const float* k_weight, const int32_t* pos, const double* freq,
+                         const int32_t* slot, void* Q, void* K, void* V, void* k_pages, void* v_pages, int32_t B, int32_t S,
+                         int32_t Hq, int32_t Hkv, int32_t D, int32_t rot, int64_t batch_stride, int64_t row_stride,
+                         int32_t n_pages, int32_t page_size, int64_t page_stride, int32_t dtype, int32_t interleaved,
+                         float eps, float amplitude, void* stream) {
+  if (B < 0 || S < 1 || Hq < 1 || Hkv < 1 || D < 1) return AC_ERR_SHAPE;
+  int32_t rc = check_head(D, dtype);
+  if (rc != AC_OK) return rc;
+  if (rot < 0 || rot > D || rot % 2 != 0) return AC_ERR_SHAPE;
+  const int64_t heads = (int64_t)Hq + 2LL * Hkv;
+  if (heads > 65535 || row_stride < heads * D || batch_stride < 0) return AC_ERR_SHAPE;
+  if ((double)B * S > 2147483647.0 - 4096) return AC_ERR_SHAPE;   // tokens are numbered in 31 bits
+  if (row_stride > INT64_MAX / 16 / S || (B > 1 && batch_stride > INT64_MAX / 16 / B)) return AC_ERR_SHAPE;
+  if (!(eps >= 0.f) || !std::isfinite(eps) || !std::isfinite(amplitude)) return AC_ERR_SHAPE;
+  if (slot) {
+    rc = check_pages(Hkv, D, n_pages, page_size, page_stride, dtype);
+    if (rc != AC_OK) return rc;
+  }
+  const int64_t piece = 16 / (int64_t)elt_size(dtype);
+  if (D % piece == 0 && (row_stride % piece != 0 || (B > 1 && batch_stride % piece != 0))) return AC_ERR_ALIGN;
+  if (B == 0) return AC_OK;
+  if (!X || !pos || !Q || (rot > 0 && !freq)) return AC_ERR_NULL;
+  if ((!K != !V) || (slot && (!k_pages || !v_pages)) || (!slot && !K)) return AC_ERR_NULL;
+  for (const void* p : {X, (const void*)Q, (const void*)K, (const void*)V, (const void*)q_weight, (const void*)k_weight})
+    if (!aligned16(p)) return AC_ERR_ALIGN;
+  if (slot && (!aligned16(k_pages) || !aligned16(v_pages))) return AC_ERR_ALIGN;
+  if (may_query(reinterpret_cast<hipStream_t>(stream))) {
+    rc = all_on_current_device({X, q_weight, k_weight, pos, rot > 0 ? freq : nullptr, slot, Q, K, V, slot ? k_pages : nullptr,
+                                slot ? v_pages : nullptr});
+    if (rc != AC_OK) return rc;
+  }
+  ac::RotateLaunch p;
+  p.X = X; p.q_weight = q_weight; p.k_weight = k_weight; p.pos = pos; p.freq = freq; p.slot = slot;
+  p.Q = Q; p.K = K; p.V = V; p.k_pages = k_pages; p.v_pages = v_pages;
+  p.batch_stride = B > 1 ? batch_stride : 0; p.row_stride = row_stride; p.page_stride = page_stride;
+  p.B = B; p.S = S; p.Hq = Hq; p.Hkv = Hkv; p.D = D; p.rot = rot; p.n_pages = n_pages; p.page_size = page_size;
+  p.is_f32 = dtype == AC_F32; p.interleaved = interleaved != 0; p.eps = eps; p.amplitude = amplitude;
+  const hipError_t e = ac::launch_rotate(p, reinterpret_cast<hipStream_t>(stream));
+  return e == hipSuccess ? AC_OK : hip_fail(e);
+}
+
+namespace {
+bool fork_sizes(int32_t B, int32_t max_pages, int32_t n_pages) {
+  return max_pages >= 1 && n_pages >= 1 && B <= (1 << 22) && (int64_t)B * max_pages <= 0x7fffffffLL - 4096;
+}
+}  // namespace
+
+size_t attncache_page_fork_workspace_bytes(int32_t B, int32_t max_pages, int32_t n_pages) {
+  return B < 1 || !fork_sizes(B, max_pages, n_pages) ? 0 : ac::fork_workspace_bytes(B, max_pages, n_pages);
+}
+
+int32_t attncache_page_fork(const int32_t* from, const int32_t* seq_len, const int32_t* free_state, int32_t* free_pages,
+                            const int32_t* page_table, int32_t* page_table_out, int32_t* seq_len_out,
+                            int32_t* free_state_out, void* k_pages, void* v_pages, int32_t B, int32_t H, int32_t D,
+                            int32_t max_pages, int32_t n_pages, int32_t page_size, int64_t page_stride, int32_t sinks,
+                            int32_t window, int32_t dtype, void* workspace, size_t workspace_bytes, void* stream) {
+  if (B < 0 || H < 1 || D < 1 || sinks < 0 || window < 0) return AC_ERR_SHAPE;
+  int32_t rc = check_head(D, dtype);
+  if (rc != AC_OK) return rc;
+  rc = check_pages(H, D, n_pages, page_size, page_stride, dtype);
+  if (rc != AC_OK) return rc;
+  if (!fork_sizes(B, max_pages, n_pages) || (int64_t)max_pages * page_size > kMostTokens) return AC_ERR_SHAPE;
+  if ((double)page_size * D > 1073741824.0) return AC_ERR_SHAPE;   // pieces of a head's page
+  if (B == 0) return AC_OK;
+  if (!from || !seq_len || !free_state || !free_pages || !page_table || !page_table_out || !seq_len_out || !free_state_out ||
+      !k_pages || !v_pages || !workspace)
+    return AC_ERR_NULL;
+  if (!aligned16(k_pages) || !aligned16(v_pages) || !aligned16(workspace)) return AC_ERR_ALIGN;
+  if (workspace_bytes < ac::fork_workspace_bytes(B, max_pages, n_pages)) return AC_ERR_WORKSPACE;
+  if (may_query(reinterpret_cast<hipStream_t>(stream))) {
+    rc = all_on_current_device({from, seq_len, free_state, free_pages, page_table, page_table_out, seq_len_out, free_state_out,
+                                k_pages, v_pages, workspace});
+    if (rc != AC_OK) return rc;
+  }
+  ac::ForkLaunch p;
+  p.from = from; p.seq_len = seq_len; p.free_state = free_state; p.page_table = page_table;
+  p.free_pages = free_pages; p.page_table_out = page_table_out; p.seq_len_out = seq_len_out; p.free_state_out = free_state_out;
+  p.k_pages = k_pages; p.v_pages = v_pages;
+  p.B = B; p.H = H; p.D = D; p.max_pages = max_pages; p.n_pages = n_pages; p.page_size = page_size;
+  p.sinks = sinks; p.window = window; p.elt = (int32_t)elt_size(dtype); p.page_stride = page_stride;
+  p.ws = workspace;
+  const hipError_t e = ac::launch_fork(p, reinterpret_cast<hipStream_t>(stream));
   return e == hipSuccess ? AC_OK : hip_fail(e);
 }
 

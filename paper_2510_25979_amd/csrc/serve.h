@@ -40,6 +40,33 @@ struct AppendLaunch {
 };
 hipError_t launch_append(const AppendLaunch& p, hipStream_t stream);
 
+// A projection's rows to heads (rotate.hip).
+struct RotateLaunch {
+  const void* X;                       // device [B][S] rows of Hq + 2 Hkv heads
+  const float *q_weight, *k_weight;    // device [D] or nullptr
+  const int32_t* pos;                  // device [B][S]
+  const double* freq;                  // device [rot / 2]
+  const int32_t* slot;                 // device [B][S] or nullptr
+  void *Q, *K, *V;                     // device [B][Hq][S][D], [B][Hkv][S][D] or nullptr
+  void *k_pages, *v_pages;             // with a slot
+  int64_t batch_stride, row_stride, page_stride;   // elements
+  int32_t B, S, Hq, Hkv, D, rot, n_pages, page_size, is_f32, interleaved;
+  float eps, amplitude;
+};
+hipError_t launch_rotate(const RotateLaunch& p, hipStream_t stream);
+
+// Rows of a paged cache that become other rows (fork.hip); the outputs may be the inputs of the same meaning.
+struct ForkLaunch {
+  const int32_t *from, *seq_len, *free_state, *page_table;   // device [B], [B], [2], [B][max_pages]
+  int32_t *free_pages, *page_table_out, *seq_len_out, *free_state_out;
+  void *k_pages, *v_pages;
+  int32_t B, H, D, max_pages, n_pages, page_size, sinks, window, elt;
+  int64_t page_stride;   // elements
+  void* ws;
+};
+size_t fork_workspace_bytes(int32_t B, int32_t max_pages, int32_t n_pages);
+hipError_t launch_fork(const ForkLaunch& p, hipStream_t stream);
+
 // Attention of R rows per (item, K/V head), which lie side by side in Q and O, over the keys of that head.
 struct DecodeLaunch {
   const void *Q, *K, *V;    // K, V: pages, or [B][Hkv][Sk][D]
