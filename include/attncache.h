@@ -679,6 +679,53 @@ int32_t attncache_page_fork(const int32_t *from, const int32_t *seq_len,
                             void *stream);
 
 /*
+ * Attention within a sliding window, with a few first tokens that stay
+ * visible: row t of a prompt sees keys j <= t with j > t - window or j < sinks.
+ *
+ *   Q, O       DEVICE [B][Hq][S][D]; K, V DEVICE [B][Hkv][S][D]; all of dtype
+ *              (AC_BF16: D 64 or 128; AC_F32: D <= 256), any S.
+ *   row_sel    NULL or DEVICE [B] int32: items with row_sel[b] >= 0 are
+ *              skipped and their rows of O not written (attncache_search's
+ *              hits: only misses are computed).
+ *   key_len    NULL or DEVICE [B] int32: tokens of item b that are real,
+ *              clamped to [0, S]; the other keys are hidden and may hold
+ *              anything.  Rows of padding are computed by the same rule; those
+ *              that see no key get zeros.
+ *   window     at least 1 (the token itself); S or more: causal attention.
+ *   sinks      0 or more.
+ *   scale      0 selects 1/sqrt(D).
+ *
+ * Arithmetic as in attention_paged.  Keys that are hidden from a row do not
+ * touch it, whatever K and V hold there (rows among 32, binary32 16, that meet
+ * an infinity or a NaN take a slower way).  Hq / Hkv * S <= 2^24, B * Hkv <=
+ * 2^28, B * Hq below 2^31.
+ */
+int32_t attention_window(const void *Q, const void *K, const void *V, void *O,
+                         const int32_t *row_sel, const int32_t *key_len,
+                         int32_t B, int32_t Hq, int32_t Hkv, int32_t S,
+                         int32_t D, int32_t dtype, int32_t window,
+                         int32_t sinks, float scale, void *stream);
+
+/*
+ * The same for one new token of each request over its pages: of seq_len[b] = n
+ * tokens those with j >= n - window or j < sinks are seen.  Everything else
+ * is as in attention_paged, the workspace too
+ * (attention_paged_workspace_bytes).  Pages of which no token is seen, and
+ * their entries of page_table, are not looked at: attncache_page_fork gives
+ * them back.  The limit counts window + sinks keys in the place of max_pages *
+ * page_size.
+ */
+int32_t attention_paged_window(const void *Q, const void *k_pages,
+                               const void *v_pages, const int32_t *page_table,
+                               const int32_t *seq_len, void *O, int32_t B,
+                               int32_t Hq, int32_t Hkv, int32_t D,
+                               int32_t n_pages, int32_t page_size,
+                               int32_t max_pages, int64_t page_stride,
+                               int32_t dtype, int32_t window, int32_t sinks,
+                               float scale, void *workspace,
+                               size_t workspace_bytes, void *stream);
+
+/*
  * Switches the per-call memory-space checks of pointers on (non-zero, the
  * default) or off for the whole process; returns the previous setting.
  * attncache_build_db always checks.

@@ -33,7 +33,7 @@ SYMBOLS = ["attncache_workspace_bytes", "attncache_map_entry_bytes", "attncache_
            "attncache_page_plan", "attncache_page_append", "attention_paged_workspace_bytes", "attention_paged",
            "attention_cross_workspace_bytes", "attention_cross",
            "attncache_rotate", "attncache_rotary_frequencies", "attncache_page_fork_workspace_bytes", "attncache_page_fork",
-           "attncache_status_string",
+           "attention_window", "attention_paged_window", "attncache_status_string",
            "attncache_last_hip_error", "attncache_version", "attncache_set_pointer_checks"]
 
 
@@ -119,6 +119,10 @@ def lib():
         L.attncache_page_fork_workspace_bytes.argtypes = [i32] * 3
         L.attncache_page_fork.restype = i32
         L.attncache_page_fork.argtypes = [vp] * 10 + [i32] * 6 + [i64] + [i32] * 3 + [vp, sz, vp]
+        L.attention_window.restype = i32
+        L.attention_window.argtypes = [vp] * 6 + [i32] * 8 + [f32, vp]
+        L.attention_paged_window.restype = i32
+        L.attention_paged_window.argtypes = [vp] * 6 + [i32] * 7 + [i64] + [i32] * 3 + [f32, vp, sz, vp]
         L.attncache_status_string.restype = ctypes.c_char_p
         L.attncache_status_string.argtypes = [i32]
         L.attncache_last_hip_error.restype = i32
@@ -639,3 +643,44 @@ def attncache_page_fork(from_row: torch.Tensor, seq_len: torch.Tensor, free_stat
     _check(lib().attncache_page_fork(rp, lp, fs, fp, tp, to, lo, fo, kc, vc, B, H, D, max_pages, n, page, stride, sinks, window,
                                      _DTYPE_CODE[k_pages.dtype], wp, workspace.numel() * workspace.element_size(),
                                      _stream(stream)), "attncache_page_fork")
+
+
+def attention_window(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, O: torch.Tensor, *, window: int, sinks: int = 0,
+                     scale: float = 0.0, row_sel: Optional[torch.Tensor] = None, key_len: Optional[torch.Tensor] = None,
+                     stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Q,O [B,Hq,S,D]; K,V [B,Hkv,S,D]; bf16 or f32; row_sel, key_len [B] int32."""
+    if Q.dim() != 4 or K.dim() != 4:
+        raise ValueError("Q must be [B,Hq,S,D] and K,V [B,Hkv,S,D]")
+    B, Hq, S, D = Q.shape
+    Hkv = K.shape[1]
+    if Q.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("unsupported dtype")
+    qp = _dev(Q, "Q")
+    kp = _dev(K, "K", Q.dtype, (B, Hkv, S, D))
+    vp = _dev(V, "V", Q.dtype, (B, Hkv, S, D))
+    op = _dev(O, "O", Q.dtype, (B, Hq, S, D))
+    rp = None if row_sel is None else _dev(row_sel, "row_sel", torch.int32, (B,))
+    lp = None if key_len is None else _dev(key_len, "key_len", torch.int32, (B,))
+    _check(lib().attention_window(qp, kp, vp, op, rp, lp, B, Hq, Hkv, S, D, _DTYPE_CODE[Q.dtype], window, sinks, float(scale),
+                                  _stream(stream)), "attention_window")
+
+
+def attention_paged_window(Q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor,
+                           seq_len: torch.Tensor, O: torch.Tensor, workspace: torch.Tensor, *, window: int, sinks: int = 0,
+                           scale: float = 0.0, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """As attention_paged, of whose keys the first ``sinks`` and the last ``window`` of each request are seen."""
+    if Q.dim() != 3 or k_pages.dim() != 4 or page_table.dim() != 2:
+        raise ValueError("Q must be [B,Hq,D], k_pages and v_pages [n_pages,Hkv,page_size,D], page_table [B,max_pages]")
+    B, Hq, D = Q.shape
+    Hkv, max_pages = k_pages.shape[1], page_table.shape[1]
+    if Q.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("unsupported dtype")
+    qp = _dev(Q, "Q")
+    op = _dev(O, "O", Q.dtype, (B, Hq, D))
+    tp = _dev(page_table, "page_table", torch.int32, (B, max_pages))
+    lp = _dev(seq_len, "seq_len", torch.int32, (B,))
+    kc, vc, n, page, stride = _pages(k_pages, v_pages, Q.dtype, Hkv, D)
+    wp = _dev(workspace, "workspace")
+    _check(lib().attention_paged_window(qp, kc, vc, tp, lp, op, B, Hq, Hkv, D, n, page, max_pages, stride,
+                                        _DTYPE_CODE[Q.dtype], window, sinks, float(scale), wp,
+                                        workspace.numel() * workspace.element_size(), _stream(stream)), "attention_paged_window")

@@ -871,4 +871,61 @@ int32_t attncache_page_fork(const int32_t* from, const int32_t* seq_len, const i
   return e == hipSuccess ? AC_OK : hip_fail(e);
 }
 
+int32_t attention_window(const void* Q, const void* K, const void* V, void* O, const int32_t* row_sel, const int32_t* key_len,
+                         int32_t B, int32_t Hq, int32_t Hkv, int32_t S, int32_t D, int32_t dtype, int32_t window,
+                         int32_t sinks, float scale, void* stream) {
+  if (B < 0 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || S < 1 || window < 1 || sinks < 0) return AC_ERR_SHAPE;
+  int32_t rc = check_head(D, dtype);
+  if (rc != AC_OK) return rc;
+  // units of a K/V head, and tiles, are counted in 31 bits; so are the elements of an item's heads, 32 rows at a time
+  if ((int64_t)(Hq / Hkv) * S > (1 << 24) || (int64_t)B * Hkv > (1 << 28) || (int64_t)B * Hq > 0x7fffffffLL) return AC_ERR_SHAPE;
+  if (!(scale >= 0.f)) return AC_ERR_SHAPE;
+  if (B == 0) return AC_OK;
+  if (!Q || !K || !V || !O) return AC_ERR_NULL;
+  if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(O)) return AC_ERR_ALIGN;
+  if (may_query(reinterpret_cast<hipStream_t>(stream))) {
+    rc = all_on_current_device({Q, K, V, O, row_sel, key_len});
+    if (rc != AC_OK) return rc;
+  }
+  ac::WindowLaunch p;
+  p.Q = Q; p.K = K; p.V = V; p.O = O; p.row_sel = row_sel; p.key_len = key_len;
+  p.B = B; p.Hq = Hq; p.Hkv = Hkv; p.S = S; p.D = D; p.window = window; p.sinks = sinks; p.is_f32 = dtype == AC_F32;
+  p.scale = scale;
+  const hipError_t e = ac::launch_window(p, reinterpret_cast<hipStream_t>(stream));
+  return e == hipSuccess ? AC_OK : hip_fail(e);
+}
+
+int32_t attention_paged_window(const void* Q, const void* k_pages, const void* v_pages, const int32_t* page_table,
+                               const int32_t* seq_len, void* O, int32_t B, int32_t Hq, int32_t Hkv, int32_t D,
+                               int32_t n_pages, int32_t page_size, int32_t max_pages, int64_t page_stride, int32_t dtype,
+                               int32_t window, int32_t sinks, float scale, void* workspace, size_t workspace_bytes,
+                               void* stream) {
+  if (B < 0 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || max_pages < 1 || window < 1 || sinks < 0) return AC_ERR_SHAPE;
+  int32_t rc = check_head(D, dtype);
+  if (rc != AC_OK) return rc;
+  rc = check_pages(Hkv, D, n_pages, page_size, page_stride, dtype);
+  if (rc != AC_OK) return rc;
+  const int64_t most = (int64_t)max_pages * page_size;
+  if (most > kMostTokens) return AC_ERR_SHAPE;
+  if (!ac::decode_fits(B, Hkv, Hq / Hkv, std::min(most, (int64_t)window + sinks))) return AC_ERR_SHAPE;
+  if (!(scale >= 0.f)) return AC_ERR_SHAPE;
+  if (B == 0) return AC_OK;
+  if (!Q || !k_pages || !v_pages || !page_table || !seq_len || !O || !workspace) return AC_ERR_NULL;
+  if (!aligned16(Q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(O) || !aligned16(workspace))
+    return AC_ERR_ALIGN;
+  if (workspace_bytes < ac::decode_workspace_bytes(Hq / Hkv, D)) return AC_ERR_WORKSPACE;
+  if (may_query(reinterpret_cast<hipStream_t>(stream))) {
+    rc = all_on_current_device({Q, k_pages, v_pages, page_table, seq_len, O, workspace});
+    if (rc != AC_OK) return rc;
+  }
+  ac::DecodeLaunch p;
+  p.Q = Q; p.K = k_pages; p.V = v_pages; p.O = O;
+  p.table = page_table; p.len = seq_len; p.row_sel = nullptr;
+  p.B = B; p.Hkv = Hkv; p.R = Hq / Hkv; p.D = D; p.Sk = (int32_t)most; p.is_f32 = dtype == AC_F32;
+  p.n_pages = n_pages; p.page_size = page_size; p.max_pages = max_pages; p.page_stride = page_stride;
+  p.scale = scale; p.ws = workspace; p.sinks = sinks; p.window = window;
+  const hipError_t e = ac::launch_window_step(p, reinterpret_cast<hipStream_t>(stream));
+  return e == hipSuccess ? AC_OK : hip_fail(e);
+}
+
 }  // extern "C"

@@ -79,14 +79,26 @@ struct DecodeLaunch {
   int64_t page_stride;
   float scale;              // 0: 1 / sqrt(D)
   void* ws;
+  int32_t sinks, window;    // launch_window_step: first and last keys that are seen
 };
 size_t decode_workspace_bytes(int32_t R, int32_t D);
 bool decode_fits(int64_t B, int64_t Hkv, int64_t R, int64_t keys);   // the blocks of a call can be counted in 31 bits
 hipError_t launch_decode(const DecodeLaunch& p, hipStream_t stream);
+hipError_t launch_window_step(const DecodeLaunch& p, hipStream_t stream);   // over pages (window_step.hip)
 
 // Cross attention: the same call, not paged.  Many rows go to a kernel that shares K and V between them and needs no
 // workspace (cross_workspace_bytes says 0), few to the one above.
 size_t cross_workspace_bytes(int32_t B, int32_t Hkv, int32_t R, int32_t Sk, int32_t D, int32_t is_f32);
 hipError_t launch_cross(const DecodeLaunch& p, hipStream_t stream);
+
+// Attention of prompts within a window (window.hip).
+struct WindowLaunch {
+  const void *Q, *K, *V;    // device [B][Hq|Hkv][S][D]
+  void* O;
+  const int32_t *row_sel, *key_len;   // device [B] or nullptr
+  int32_t B, Hq, Hkv, S, D, window, sinks, is_f32;
+  float scale;
+};
+hipError_t launch_window(const WindowLaunch& p, hipStream_t stream);
 
 }  // namespace ac

@@ -1,0 +1,487 @@
+// Attention of prompts within a sliding window: row t sees keys j <= t with j > t - window or j < sinks, of the item's first key_len.
+//
+// Rows are cut into units of 32 tokens (binary32: 16) of one head; the units of the g heads that share K and V are numbered token block first, head
+// second, and four consecutive ones are a workgroup, so that its waves see (nearly) the same keys: with four heads on one K and V a
+// workgroup reads no key that only some of its waves need.  It walks the chunks of 64 keys (32) that hold a first token or lie in the window of one
+// of its rows; a wave passes over blocks that none of its rows sees, and compares keys with rows only where some do and some do not.
+//
+// bf16: the machinery of cross.hip -- chunks copied straight into two LDS stages, both products transposed, weights from the first to the second in
+// their registers.  Bound by the softmax's vector work beside the matrix pipe.
+//
+// A hidden key must not touch a row even if its V is infinite or NaN, which a product over a block cannot avoid (0 * inf): a wave that ends with
+// such a result forms its rows again key by key.
+#include "common.hpp"
+#include "f32_tile.hpp"
+#include "serve.h"
+
+namespace ac {
+
+constexpr int kWindowChunk = 64;
+constexpr float kWindowSlack = 8.0f;   // the reference point of a row moves when a score has outgrown it by 2^8
+
+struct WindowArgs {
+  const void *Q, *K, *V;
+  void* O;
+  const int32_t *len, *row_sel;
+  int32_t Hkv, g, S, D, window, sinks, first, tiles, per, units;   // first: of the launch's tiles; per, units: workgroups, units of a tile
+  float scale_log2e;
+  Divider by_g, by_per;
+};
+
+// Chunks of C keys of a workgroup with tokens [lo, hi): `head` of them from the first on, then `count - head` from `from` on.
+template <int C>
+struct WindowChunks {
+  int head, from, count;
+  __device__ __forceinline__ WindowChunks(const WindowArgs& a, int lo, int hi, int keys) {
+    const int end = (min(hi, keys) + C - 1) / C, seen = min(a.sinks, min(hi, keys));
+    head = (seen + C - 1) / C;
+    from = max(head, max(0, lo - a.window + 1) / C);
+    count = head + max(0, end - from);
+  }
+  __device__ __forceinline__ int at(int i) const { return i < head ? i : i - head + from; }
+};
+// What rows [t0, t0 + R) see of keys [k0, k0 + C).
+enum WindowBlock { kNone, kSome, kEvery };
+template <int R, int C>
+__device__ __forceinline__ WindowBlock window_block(const WindowArgs& a, int t0, int k0, int keys) {
+  if (k0 > t0 + R - 1 || k0 >= keys || (k0 + C - 1 <= t0 - a.window && k0 >= a.sinks)) return kNone;
+  return k0 + C - 1 <= t0 && k0 + C <= keys && (k0 > t0 + R - 1 - a.window || k0 + C <= a.sinks) ? kEvery : kSome;
+}
+__device__ __forceinline__ bool window_hides(const WindowArgs& a, int t, int key, int keys) {
+  return key > t || key >= keys || (key <= t - a.window && key >= a.sinks);
+}
+
+// Rows [t0, t0 + n) of a head key by key: lane l has columns l, l + 64, ...
+template <typename T, int NC>
+__device__ __forceinline__ void window_rows_again(const WindowArgs& a, const T* Q, const T* K, const T* V, T* O, int t0, int n, int keys, int lane) {
+  const int D = a.D;
+  for (int t = t0; t < t0 + n; ++t) {
+    float q[NC], o[NC], m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      q[c] = lane + kWave * c < D ? (float)Q[(size_t)t * D + lane + kWave * c] : 0.f;
+      o[c] = 0.f;
+    }
+    for (int j = 0; j < min(t + 1, keys); ++j) {
+      if (j >= a.sinks && j <= t - a.window) {   // to the end of the gap
+        j = t - a.window + 1;
+        if (j >= keys) break;
+      }
+      float s = 0.f;
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+        if (lane + kWave * c < D) s = fmaf(q[c], (float)K[(size_t)j * D + lane + kWave * c], s);
+#pragma unroll
+      for (int off = 32; off > 0; off >>= 1) s += __shfl_xor(s, off);
+      s *= a.scale_log2e;
+      if (s > m) {
+        const float alpha = __builtin_amdgcn_exp2f(m - s);
+        l *= alpha;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) o[c] = m == -INFINITY ? 0.f : o[c] * alpha;
+        m = s;
+      }
+      const float p = s == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s - m);
+      l += p;
+      if (s != -INFINITY)
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+          if (lane + kWave * c < D) o[c] = fmaf(p, (float)V[(size_t)j * D + lane + kWave * c], o[c]);
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+      if (lane + kWave * c < D) O[(size_t)t * D + lane + kWave * c] = (T)(o[c] * inv);
+  }
+}
+
+template <int D>
+__global__ __launch_bounds__(kThreads, 2) void window_bf16_kernel(const WindowArgs a) {
+  constexpr int PPR = D / 8;                             // 16-byte pieces of a row
+  constexpr int NCOPY = kWindowChunk * PPR / kWave / 4;  // copy instructions of a wave, tensor and chunk
+  __shared__ __attribute__((aligned(16))) bf16_t kb0[kWindowChunk * D];
+  __shared__ __attribute__((aligned(16))) bf16_t vb0[kWindowChunk * D];
+  __shared__ __attribute__((aligned(16))) bf16_t kb1[kWindowChunk * D];
+  __shared__ __attribute__((aligned(16))) bf16_t vb1[kWindowChunk * D];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int il = lane & 31, kh = lane >> 5;
+  // workgroups with ids equal mod 8 (one XCD) share K and V in its L2
+  const int slot = blockIdx.x >> 3, group = a.by_per.div(slot), u = a.first + group * 8 + (blockIdx.x & 7);
+  if (u >= a.tiles) return;
+  const int b = u / a.Hkv, hk = u - b * a.Hkv;
+  if (a.row_sel && a.row_sel[b] >= 0) return;
+  const int keys = a.len ? min(max(a.len[b], 0), a.S) : a.S;
+  const int unit0 = 4 * (slot - group * a.per), last = min(unit0 + 3, a.units - 1);
+  const int unit = min(unit0 + wave, last), tb = a.by_g.div(unit), t0 = kRowsPerWave * tb;
+  const bool live = unit0 + wave <= last;
+  const size_t row0 = ((size_t)(b * a.Hkv + hk) * a.g + (unit - tb * a.g)) * a.S;   // the head's first row
+  const int rows = min(kRowsPerWave, a.S - t0);
+  const WindowChunks<kWindowChunk> chunks(a, kRowsPerWave * a.by_g.div(unit0), min(a.S, kRowsPerWave * (a.by_g.div(last) + 1)), keys);
+  const bf16_t* Ksrc = reinterpret_cast<const bf16_t*>(a.K) + (size_t)u * a.S * D;
+  const bf16_t* Vsrc = reinterpret_cast<const bf16_t*>(a.V) + (size_t)u * a.S * D;
+  bf16_t* O = reinterpret_cast<bf16_t*>(a.O) + (row0 + t0) * D;
+  // (the scale through a vector instruction: straight from a scalar load it makes the compiler wait for all LDS reads)
+  const float scale_log2e = __builtin_bit_cast(
+      float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, a.scale_log2e) + (lane & 0)));
+
+  // copies and operand addresses as in cross.hip
+  const int slot0 = kWave * wave + lane, crow = slot0 / PPR, cpos = slot0 % PPR;
+  const int koff0 = crow * D + 8 * (cpos ^ k_piece_swizzle<D>(crow)), voff0 = crow * D + 8 * (cpos ^ v_piece_swizzle<D>(crow));
+  auto copy = [&](bf16_t* kb, bf16_t* vb, int c) {
+    const int there = keys - c * kWindowChunk;
+    const bf16_t* ks = Ksrc + (size_t)c * kWindowChunk * D;
+    const bf16_t* vs = Vsrc + (size_t)c * kWindowChunk * D;
+    if (there >= kWindowChunk) {
+#pragma unroll
+      for (int i = 0; i < NCOPY; ++i) {
+        __builtin_amdgcn_global_load_lds(ks + koff0 + 2048 * i, kb + kWave * 8 * (wave + 4 * i), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds(vs + voff0 + 2048 * i, vb + kWave * 8 * (wave + 4 * i), 16, 0, 0);
+      }
+    } else {   // K rows behind the keys repeat the last one, their scores are replaced; V rows are zeros
+#pragma unroll
+      for (int i = 0; i < NCOPY; ++i) {
+        const int row = crow + 256 / PPR * i;
+        __builtin_amdgcn_global_load_lds(ks + koff0 - crow * D + min(row, there - 1) * D, kb + kWave * 8 * (wave + 4 * i), 16, 0, 0);
+        bf16_t* to = vb + kWave * 8 * (wave + 4 * i);
+        if (row < there) __builtin_amdgcn_global_load_lds(vs + voff0 + 2048 * i, to, 16, 0, 0);
+        else *reinterpret_cast<u32x4*>(to + 8 * lane) = u32x4{0, 0, 0, 0};
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  int koff[D / 16], voff[2][D / 32];
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ++ks) koff[ks] = il * D + 8 * ((2 * ks + kh) ^ k_piece_swizzle<D>(il));
+#pragma unroll
+  for (int half = 0; half < 2; ++half)
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) {
+      const int t = lane & 15, j = 4 * kh + 8 * half + (t >> 2), d0 = 32 * db + 16 * (il >> 4) + 4 * (t & 3);
+      voff[half][db] = j * D + 8 * ((d0 >> 3) ^ v_piece_swizzle<D>(j)) + (d0 & 7);
+    }
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  typedef short s16x8 __attribute__((ext_vector_type(8)));
+  auto vop = [&](const bf16_t* vb, int db, int jb, int s2) {
+    const bf16_t* at = vb + (32 * jb + 16 * s2) * D;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(at + voff[0][db]));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(at + voff[1][db]));
+    const s16x8 w = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    return __builtin_bit_cast(bf16x8, w);
+  };
+
+  if (chunks.count > 0) copy(kb0, vb0, chunks.at(0));
+  u32x4 q[D / 16];
+  {
+    const bf16_t* src = reinterpret_cast<const bf16_t*>(a.Q) + (row0 + min(t0 + il, a.S - 1)) * D + 8 * kh;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) q[ks] = *reinterpret_cast<const u32x4*>(src + 16 * ks);
+  }
+  f32x16 acc[D / 32];
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[db][v] = 0.f;
+  float m_run = -INFINITY, l_run = 0.f;
+
+  auto qk = [&](const bf16_t* kb, int jb) {
+    f32x16 s;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) s[v] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks)
+      s = mfma_bf16(*reinterpret_cast<const bf16x8*>(kb + koff[ks] + 32 * jb * D), __builtin_bit_cast(bf16x8, q[ks]), s);
+    return s;
+  };
+  auto hide = [&](f32x16& s, int k0) {
+#pragma unroll
+    for (int v = 0; v < 16; ++v)
+      if (window_hides(a, t0 + il, k0 + mfma_row(v, kh), keys)) s[v] = -INFINITY;
+  };
+  auto row_max = [&](const f32x16& s) {
+    const float m01 = fmaxf(fmaxf(s[0], s[1]), s[2]), m02 = fmaxf(fmaxf(s[3], s[4]), s[5]);
+    const float m03 = fmaxf(fmaxf(s[6], s[7]), s[8]), m04 = fmaxf(fmaxf(s[9], s[10]), s[11]);
+    const float m05 = fmaxf(fmaxf(s[12], s[13]), s[14]);
+    return max_with_other_half(fmaxf(fmaxf(fmaxf(m01, m02), m03), fmaxf(fmaxf(m04, m05), s[15])));
+  };
+  // Weights 2^(score - m) in bf16, the second product's operand (it takes both factors in one type, and V is bf16); their sum is over the
+  // rounded ones, which V is multiplied with, so that they still add up to one.  (m = -inf: no finite score so far, all weights are zero.)
+  typedef bf16_t bf16x2 __attribute__((ext_vector_type(2)));
+  auto weights = [&](const f32x16& s, float m, u32x4(&pw)[2], float& sum) {
+    const bf16x2 ones = {(bf16_t)1.0f, (bf16_t)1.0f};
+    const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+      const float e0 = __builtin_amdgcn_exp2f(fmaf(s[2 * w], scale_log2e, -ref));
+      const float e1 = __builtin_amdgcn_exp2f(fmaf(s[2 * w + 1], scale_log2e, -ref));
+      const uint32_t pk = pack_bf16(e0, e1);
+      pw[w >> 2][w & 3] = pk;
+      sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pk), ones, sum, false);
+    }
+  };
+  auto pv = [&](const bf16_t* vb, int jb, const u32x4(&pw)[2]) {
+#pragma unroll
+    for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+        acc[db] = mfma_bf16(vop(vb, db, jb, s2), __builtin_bit_cast(bf16x8, pw[s2]), acc[db]);
+  };
+  auto rescale = [&](float m_new) {
+    const float alpha = m_new > m_run ? __builtin_amdgcn_exp2f(m_run - m_new) : 1.f;
+    l_run *= alpha;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[db][v] *= alpha;
+  };
+  auto step = [&](const bf16_t* kb, const bf16_t* vb, int c) __attribute__((always_inline)) {
+    if (!live) return;
+    const int k0 = c * kWindowChunk;
+    const WindowBlock b0 = window_block<32, 32>(a, t0, k0, keys), b1 = window_block<32, 32>(a, t0, k0 + 32, keys);
+    if (b0 == kEvery && b1 == kEvery) {
+      // the scores of block 1 are requested before the exponentials of block 0, the second product of block 0 before those of block 1
+      f32x16 s0 = qk(kb, 0);
+      float cand = fmaxf(m_run, row_max(s0) * scale_log2e);
+      if (__any(cand > m_run + kWindowSlack)) {
+        rescale(cand);
+        m_run = cand;
+      }
+      f32x16 s1 = qk(kb, 1);
+      u32x4 p0[2], p1[2];
+      float sum = 0.f, sum1 = 0.f, m1 = m_run;
+      weights(s0, m_run, p0, sum);
+      l_run += sum;
+      cand = fmaxf(m_run, row_max(s1) * scale_log2e);
+      const bool moved = __any(cand > m_run + kWindowSlack);
+      if (moved) m1 = cand;
+      pv(vb, 0, p0);
+      weights(s1, m1, p1, sum1);
+      if (moved) rescale(m1);
+      m_run = m1;
+      l_run += sum1;
+      pv(vb, 1, p1);
+      return;
+    }
+#pragma unroll 1
+    for (int jb = 0; jb < 2; ++jb) {
+      const WindowBlock bl = jb ? b1 : b0;
+      if (bl == kNone) continue;
+      f32x16 s = qk(kb, jb);
+      if (bl == kSome) hide(s, k0 + 32 * jb);
+      const float cand = fmaxf(m_run, row_max(s) * scale_log2e);
+      if (__any(cand > m_run + kWindowSlack)) {
+        rescale(cand);
+        m_run = cand;
+      }
+      u32x4 p[2];
+      float sum = 0.f;
+      weights(s, m_run, p, sum);
+      l_run += sum;
+      pv(vb, jb, p);
+    }
+  };
+  auto publish = [&]() {   // this wave's copies have landed, then everybody's; the other stage is no longer read
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+  };
+  for (int i = 0; i < chunks.count; i += 2) {
+    publish();
+    if (i + 1 < chunks.count) copy(kb1, vb1, chunks.at(i + 1));
+    step(kb0, vb0, chunks.at(i));
+    if (i + 1 >= chunks.count) break;
+    publish();
+    if (i + 2 < chunks.count) copy(kb0, vb0, chunks.at(i + 2));
+    step(kb1, vb1, chunks.at(i + 1));
+  }
+  __syncthreads();   // every wave is done with both stages: they now stage the output
+  if (!live) return;
+  const float sum = l_run + __shfl_xor(l_run, 32);
+  bool odd = !(sum < INFINITY);
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) odd |= !(fabsf(acc[db][v]) < INFINITY);
+  if (__any(odd && il < rows)) {
+    window_rows_again<bf16_t, D / 64>(a, reinterpret_cast<const bf16_t*>(a.Q) + row0 * D, Ksrc, Vsrc, reinterpret_cast<bf16_t*>(a.O) + row0 * D, t0,
+                                      rows, keys, lane);
+    return;
+  }
+  const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+  bf16_t* ost = wave == 0 ? kb0 : wave == 1 ? vb0 : wave == 2 ? kb1 : vb1;
+  if (rows == kRowsPerWave) {
+    store_tile_bf16<D>(acc, inv, ost, O, lane);
+  } else if (il < rows) {
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int vq = 0; vq < 4; ++vq)
+        *reinterpret_cast<u32x2*>(O + (size_t)il * D + 32 * db + 8 * vq + 4 * kh) =
+            u32x2{pack_bf16(acc[db][4 * vq] * inv, acc[db][4 * vq + 1] * inv),
+                  pack_bf16(acc[db][4 * vq + 2] * inv, acc[db][4 * vq + 3] * inv)};
+  }
+}
+
+// Binary32 (the layout of f32_tile.hpp): four waves share stages of 32 keys, the next stage's rows are in registers while this one is multiplied.
+template <int DB, int COLS>
+__global__ __launch_bounds__(kThreads, DB <= 2 ? 2 : 1) void window_f32_kernel(const WindowArgs a) {
+  constexpr int KC = 32, NB = KC / kF32Rows;
+  typedef F32Stage<DB, KC, COLS> Stage;
+  const int D = COLS == kAllCols ? 64 * DB : a.D;
+  __shared__ __attribute__((aligned(16))) float kl[KC * Stage::LD];
+  __shared__ __attribute__((aligned(16))) float vl[KC * Stage::LD];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int i = lane & 15, kq = lane >> 4;
+  const int slot = blockIdx.x >> 3, group = a.by_per.div(slot), u = a.first + group * 8 + (blockIdx.x & 7);
+  if (u >= a.tiles) return;
+  const int b = u / a.Hkv, hk = u - b * a.Hkv;
+  if (a.row_sel && a.row_sel[b] >= 0) return;
+  const int keys = a.len ? min(max(a.len[b], 0), a.S) : a.S;
+  const int unit0 = 4 * (slot - group * a.per), last = min(unit0 + 3, a.units - 1);
+  const int unit = min(unit0 + wave, last), tb = a.by_g.div(unit), t0 = kF32Rows * tb;
+  const bool live = unit0 + wave <= last;
+  const size_t row0 = ((size_t)(b * a.Hkv + hk) * a.g + (unit - tb * a.g)) * a.S;
+  const WindowChunks<KC> chunks(a, kF32Rows * a.by_g.div(unit0), min(a.S, kF32Rows * (a.by_g.div(last) + 1)), keys);
+  const float* K = reinterpret_cast<const float*>(a.K) + (size_t)u * a.S * D;
+  const float* V = reinterpret_cast<const float*>(a.V) + (size_t)u * a.S * D;
+  const float* Q = reinterpret_cast<const float*>(a.Q) + row0 * D;
+  float* O = reinterpret_cast<float*>(a.O) + row0 * D;
+  f32x4 q[4 * DB], acc[4 * DB];
+  {
+    const float* src = Q + (size_t)min(t0 + i, a.S - 1) * D;
+#pragma unroll
+    for (int kk = 0; kk < 4 * DB; ++kk) {
+      const int c = 16 * kk + 4 * kq;
+      q[kk] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (COLS == kAllCols || c + 4 <= D) {
+        q[kk] = *reinterpret_cast<const f32x4_dw*>(src + c);
+      } else {
+#pragma unroll
+        for (int x = 0; x < 3; ++x)
+          if (c + x < D) q[kk][x] = src[c + x];
+      }
+    }
+  }
+#pragma unroll
+  for (int x = 0; x < 4 * DB; ++x) acc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+  Stage ks, vs;
+  if (chunks.count > 0) {
+    ks.load(K, KC * chunks.at(0), keys, D, tid);
+    vs.load(V, KC * chunks.at(0), keys, D, tid);
+  }
+  for (int n = 0; n < chunks.count; ++n) {
+    const int j0 = KC * chunks.at(n);
+    ks.template mask<false>(j0, keys, D, tid);   // (scores of keys that are not there are replaced)
+    vs.template mask<true>(j0, keys, D, tid);
+    __syncthreads();   // the previous stage has been read by everybody
+    ks.commit(kl, tid);
+    vs.commit(vl, tid);
+    __syncthreads();
+    if (n + 1 < chunks.count) {
+      ks.load(K, KC * chunks.at(n + 1), keys, D, tid);
+      vs.load(V, KC * chunks.at(n + 1), keys, D, tid);
+    }
+    const WindowBlock bl = window_block<kF32Rows, KC>(a, t0, j0, keys);
+    if (!live || bl == kNone) continue;
+    f32x4 s[NB];
+#pragma unroll
+    for (int bk = 0; bk < NB; ++bk) {
+      s[bk] = f32x4{0.f, 0.f, 0.f, 0.f};
+      const float* row = kl + (kF32Rows * bk + i) * Stage::LD + 4 * kq;
+      f32x4 k = *reinterpret_cast<const f32x4*>(row);
+#pragma unroll
+      for (int kk = 0; kk < 4 * DB; ++kk)
+        if (COLS == kAllCols || 16 * kk < D) {   // uniform
+          const f32x4 next = *reinterpret_cast<const f32x4*>(row + 16 * ((kk + 1) & (4 * DB - 1)));
+#pragma unroll
+          for (int x = 0; x < 4; ++x) s[bk] = mfma_f32(k[x], q[kk][x], s[bk]);
+          k = next;
+          __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    if (bl == kSome) {
+#pragma unroll
+      for (int bk = 0; bk < NB; ++bk)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          if (window_hides(a, t0 + i, j0 + kF32Rows * bk + 4 * kq + x, keys)) s[bk][x] = -INFINITY;
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int bk = 0; bk < NB; ++bk)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) mx = fmaxf(mx, s[bk][x]);
+    mx = fmaxf(mx, __shfl_xor(mx, 16));
+    mx = fmaxf(mx, __shfl_xor(mx, 32));
+    const float m_new = fmaxf(m, mx * a.scale_log2e);
+    if (__any(m_new > m)) {
+      const float alpha = m_new > m ? __builtin_amdgcn_exp2f(m - m_new) : 1.f;
+      l *= alpha;
+#pragma unroll
+      for (int x = 0; x < 4 * DB; ++x) acc[x] *= alpha;
+      m = m_new;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;   // no finite score so far: all weights are zero
+#pragma unroll
+    for (int bk = 0; bk < NB; ++bk) {
+      f32x4 p;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        p[x] = __builtin_amdgcn_exp2f(fmaf(s[bk][x], a.scale_log2e, -ref));
+        l += p[x];
+      }
+      f32_weights_v<DB>(acc, vl + kF32Rows * bk * Stage::LD, p, i, kq);
+    }
+  }
+  if (!live) return;
+  float sum = l + __shfl_xor(l, 16);
+  sum += __shfl_xor(sum, 32);
+  const int rows = min(kF32Rows, a.S - t0);
+  bool odd = !(sum < INFINITY);
+#pragma unroll
+  for (int x = 0; x < 4 * DB; ++x) odd |= f32_not_finite(acc[x]);
+  if (__any(odd && i < rows)) {
+    window_rows_again<float, DB>(a, Q, K, V, O, t0, rows, keys, lane);
+    return;
+  }
+  if (i < rows) f32_store_row<DB, COLS, true>(O + (size_t)(t0 + i) * D, acc, sum == 0.f ? 1.f : sum, kq, D);
+}
+
+// All tiles, in launches of at most 2^23 workgroups (a multiple of eight tiles each).
+template <typename Kernel>
+static hipError_t window_tiles(Kernel kernel, WindowArgs a, int rows, hipStream_t stream) {
+  a.units = (a.S + rows - 1) / rows * a.g;
+  a.per = (a.units + 3) / 4;
+  a.by_per = Divider((uint32_t)a.per);
+  const int64_t most = ((1 << 23) / a.per > 8 ? (1 << 23) / a.per : 8) & ~7LL;
+  for (int64_t first = 0; first < a.tiles; first += most) {
+    a.first = (int)first;
+    const int64_t n = a.tiles - first < most ? a.tiles - first : most;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((n + 7) / 8 * 8 * a.per)), dim3(kThreads), 0, stream, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+hipError_t launch_window(const WindowLaunch& p, hipStream_t stream) {
+  WindowArgs a;
+  a.Q = p.Q; a.K = p.K; a.V = p.V; a.O = p.O; a.len = p.key_len; a.row_sel = p.row_sel;
+  a.Hkv = p.Hkv; a.g = p.Hq / p.Hkv; a.S = p.S; a.D = p.D;
+  a.window = p.window < p.S ? p.window : p.S;   // (t - window stays in 32 bits)
+  a.sinks = p.sinks < p.S ? p.sinks : p.S;
+  a.tiles = p.B * p.Hkv;
+  a.by_g = Divider((uint32_t)a.g);
+  const float scale = p.scale == 0.f ? 1.0f / sqrtf((float)p.D) : p.scale;
+  a.scale_log2e = scale * 1.44269504088896340736f;
+  if (!p.is_f32) return p.D == 64 ? window_tiles(&window_bf16_kernel<64>, a, 32, stream) : window_tiles(&window_bf16_kernel<128>, a, 32, stream);
+  if (p.D == 64) return window_tiles(&window_f32_kernel<1, kAllCols>, a, kF32Rows, stream);
+  if (p.D == 128) return window_tiles(&window_f32_kernel<2, kAllCols>, a, kF32Rows, stream);
+  if (p.D < 4) return window_tiles(&window_f32_kernel<1, kFewCols>, a, kF32Rows, stream);
+  if (p.D < 64) return p.D % 4 ? window_tiles(&window_f32_kernel<1, kAnyCols>, a, kF32Rows, stream) : window_tiles(&window_f32_kernel<1, kVecCols>, a, kF32Rows, stream);
+  if (p.D < 128) return p.D % 4 ? window_tiles(&window_f32_kernel<2, kAnyCols>, a, kF32Rows, stream) : window_tiles(&window_f32_kernel<2, kVecCols>, a, kF32Rows, stream);
+  return p.D % 4 ? window_tiles(&window_f32_kernel<4, kAnyCols>, a, kF32Rows, stream) : window_tiles(&window_f32_kernel<4, kVecCols>, a, kF32Rows, stream);
+}
+
+}  // namespace ac
