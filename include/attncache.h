@@ -679,6 +679,48 @@ int32_t attncache_page_fork(const int32_t *from, const int32_t *seq_len,
                             void *stream);
 
 /*
+ * attention_paged for a batch in which requests share long prefixes (several
+ * answers to one prompt, one instruction before many questions): K and V of a
+ * prefix are read once for all its requests.  The result is that of
+ * attention_paged.
+ *
+ *   share_first  DEVICE [G + 1] int32: group q is requests share_first[q] ...
+ *              share_first[q + 1] - 1, which lie side by side in the batch; in
+ *              ascending order (a smaller number counts as the largest before
+ *              it), clamped to [0, B].  Other requests share nothing.
+ *   share_len  DEVICE [G] int32: tokens that the group's requests have in
+ *              common, clamped to [0, max_pages * page_size].  Any number: a
+ *              prefix may end inside a page.  Requests with fewer tokens
+ *              attend to theirs by themselves, as does a group of one.
+ *   page_table, seq_len  as in attention_paged: a request's row names the
+ *              pages of its prefix, too.  They are read through the first
+ *              request of the group that has the whole prefix; the other
+ *              rows' pages of the prefix must hold the same (be the same
+ *              pages, or copies, as attncache_page_fork leaves them).
+ *   workspace  DEVICE, attention_paged_shared_workspace_bytes(...) bytes,
+ *              16-byte aligned; scratch, and written by a call before it is
+ *              read.  Calls that may overlap in time need one each.
+ *
+ * G >= 0, and 0 groups need no share_len.  B and G at most 2^20; three or four
+ * launches; deterministic.  Hkv * (B * ceil(g / 16) + B * g / 16 + G) *
+ * (ceil(max_pages * page_size / 16) + 2) and B * Hq below 2^31 - 65536, with
+ * g = Hq / Hkv.  One workgroup looks through the requests, 1,024 a step.
+ */
+size_t attention_paged_shared_workspace_bytes(int32_t B, int32_t Hq,
+                                              int32_t Hkv, int32_t D,
+                                              int32_t G);
+int32_t attention_paged_shared(const void *Q, const void *k_pages,
+                               const void *v_pages, const int32_t *page_table,
+                               const int32_t *seq_len,
+                               const int32_t *share_first,
+                               const int32_t *share_len, void *O, int32_t B,
+                               int32_t Hq, int32_t Hkv, int32_t D, int32_t G,
+                               int32_t n_pages, int32_t page_size,
+                               int32_t max_pages, int64_t page_stride,
+                               int32_t dtype, float scale, void *workspace,
+                               size_t workspace_bytes, void *stream);
+
+/*
  * Attention within a sliding window, with a few first tokens that stay
  * visible: row t of a prompt sees keys j <= t with j > t - window or j < sinks.
  *

@@ -33,7 +33,8 @@ SYMBOLS = ["attncache_workspace_bytes", "attncache_map_entry_bytes", "attncache_
            "attncache_page_plan", "attncache_page_append", "attention_paged_workspace_bytes", "attention_paged",
            "attention_cross_workspace_bytes", "attention_cross",
            "attncache_rotate", "attncache_rotary_frequencies", "attncache_page_fork_workspace_bytes", "attncache_page_fork",
-           "attention_window", "attention_paged_window", "attncache_status_string",
+           "attention_paged_shared_workspace_bytes", "attention_paged_shared", "attention_window", "attention_paged_window",
+           "attncache_status_string",
            "attncache_last_hip_error", "attncache_version", "attncache_set_pointer_checks"]
 
 
@@ -119,6 +120,10 @@ def lib():
         L.attncache_page_fork_workspace_bytes.argtypes = [i32] * 3
         L.attncache_page_fork.restype = i32
         L.attncache_page_fork.argtypes = [vp] * 10 + [i32] * 6 + [i64] + [i32] * 3 + [vp, sz, vp]
+        L.attention_paged_shared_workspace_bytes.restype = sz
+        L.attention_paged_shared_workspace_bytes.argtypes = [i32] * 5
+        L.attention_paged_shared.restype = i32
+        L.attention_paged_shared.argtypes = [vp] * 8 + [i32] * 8 + [i64, i32, f32, vp, sz, vp]
         L.attention_window.restype = i32
         L.attention_window.argtypes = [vp] * 6 + [i32] * 8 + [f32, vp]
         L.attention_paged_window.restype = i32
@@ -643,6 +648,34 @@ def attncache_page_fork(from_row: torch.Tensor, seq_len: torch.Tensor, free_stat
     _check(lib().attncache_page_fork(rp, lp, fs, fp, tp, to, lo, fo, kc, vc, B, H, D, max_pages, n, page, stride, sinks, window,
                                      _DTYPE_CODE[k_pages.dtype], wp, workspace.numel() * workspace.element_size(),
                                      _stream(stream)), "attncache_page_fork")
+
+
+def attention_paged_shared_workspace_bytes(B: int, Hq: int, Hkv: int, D: int, G: int) -> int:
+    return int(lib().attention_paged_shared_workspace_bytes(B, Hq, Hkv, D, G))
+
+
+def attention_paged_shared(Q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor,
+                           seq_len: torch.Tensor, share_first: torch.Tensor, share_len: torch.Tensor, O: torch.Tensor,
+                           workspace: torch.Tensor, *, scale: float = 0.0, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """As attention_paged; share_first [G+1] and share_len [G] int32: requests share_first[q] to share_first[q+1]-1 have their
+    first share_len[q] tokens in common."""
+    if Q.dim() != 3 or k_pages.dim() != 4 or page_table.dim() != 2 or share_len.dim() != 1:
+        raise ValueError("Q must be [B,Hq,D], k_pages and v_pages [n_pages,Hkv,page_size,D], page_table [B,max_pages], share_len [G]")
+    (B, Hq, D), G = Q.shape, share_len.shape[0]
+    Hkv, max_pages = k_pages.shape[1], page_table.shape[1]
+    if Q.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("unsupported dtype")
+    qp = _dev(Q, "Q")
+    op = _dev(O, "O", Q.dtype, (B, Hq, D))
+    tp = _dev(page_table, "page_table", torch.int32, (B, max_pages))
+    lp = _dev(seq_len, "seq_len", torch.int32, (B,))
+    fp = _dev(share_first, "share_first", torch.int32, (G + 1,))
+    sp = _dev(share_len, "share_len", torch.int32)
+    kc, vc, n, page, stride = _pages(k_pages, v_pages, Q.dtype, Hkv, D)
+    wp = _dev(workspace, "workspace")
+    _check(lib().attention_paged_shared(qp, kc, vc, tp, lp, fp, sp, op, B, Hq, Hkv, D, G, n, page, max_pages, stride,
+                                        _DTYPE_CODE[Q.dtype], float(scale), wp,
+                                        workspace.numel() * workspace.element_size(), _stream(stream)), "attention_paged_shared")
 
 
 def attention_window(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, O: torch.Tensor, *, window: int, sinks: int = 0,

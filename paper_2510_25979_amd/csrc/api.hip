@@ -928,4 +928,43 @@ int32_t attention_paged_window(const void* Q, const void* k_pages, const void* v
   return e == hipSuccess ? AC_OK : hip_fail(e);
 }
 
+size_t attention_paged_shared_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t G) {
+  if (B < 1 || Hq < 1 || Hkv < 1 || D < 1 || D > 256 || G < 0 || Hq % Hkv != 0 || B > (1 << 20) || G > (1 << 20)) return 0;
+  return ac::shared_workspace_bytes(B, Hq, Hkv, D, G);
+}
+
+int32_t attention_paged_shared(const void* Q, const void* k_pages, const void* v_pages, const int32_t* page_table,
+                               const int32_t* seq_len, const int32_t* share_first, const int32_t* share_len, void* O,
+                               int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t G, int32_t n_pages, int32_t page_size,
+                               int32_t max_pages, int64_t page_stride, int32_t dtype, float scale, void* workspace,
+                               size_t workspace_bytes, void* stream) {
+  if (B < 0 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || max_pages < 1 || G < 0) return AC_ERR_SHAPE;
+  int32_t rc = check_head(D, dtype);
+  if (rc != AC_OK) return rc;
+  rc = check_pages(Hkv, D, n_pages, page_size, page_stride, dtype);
+  if (rc != AC_OK) return rc;
+  const int64_t most = (int64_t)max_pages * page_size;
+  if (most > kMostTokens || B > (1 << 20) || G > (1 << 20) || !ac::shared_fits(B, Hkv, Hq / Hkv, G, most)) return AC_ERR_SHAPE;
+  if (!(scale >= 0.f)) return AC_ERR_SHAPE;
+  if (B == 0) return AC_OK;
+  if (!Q || !k_pages || !v_pages || !page_table || !seq_len || !share_first || (G > 0 && !share_len) || !O || !workspace)
+    return AC_ERR_NULL;
+  if (!aligned16(Q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(O) || !aligned16(workspace))
+    return AC_ERR_ALIGN;
+  if (workspace_bytes < ac::shared_workspace_bytes(B, Hq, Hkv, D, G)) return AC_ERR_WORKSPACE;
+  if (may_query(reinterpret_cast<hipStream_t>(stream))) {
+    rc = all_on_current_device({Q, k_pages, v_pages, page_table, seq_len, share_first, G > 0 ? share_len : nullptr, O, workspace});
+    if (rc != AC_OK) return rc;
+  }
+  ac::SharedLaunch p;
+  p.d.Q = Q; p.d.K = k_pages; p.d.V = v_pages; p.d.O = O;
+  p.d.table = page_table; p.d.len = seq_len; p.d.row_sel = nullptr;
+  p.d.B = B; p.d.Hkv = Hkv; p.d.R = Hq / Hkv; p.d.D = D; p.d.Sk = (int32_t)most; p.d.is_f32 = dtype == AC_F32;
+  p.d.n_pages = n_pages; p.d.page_size = page_size; p.d.max_pages = max_pages; p.d.page_stride = page_stride;
+  p.d.scale = scale; p.d.ws = workspace;
+  p.share_first = share_first; p.share_len = share_len; p.G = G;
+  const hipError_t e = ac::launch_shared(p, reinterpret_cast<hipStream_t>(stream));
+  return e == hipSuccess ? AC_OK : hip_fail(e);
+}
+
 }  // extern "C"

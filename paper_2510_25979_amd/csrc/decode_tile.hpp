@@ -175,11 +175,11 @@ struct DecodeBf16 {
     m = -INFINITY;
     l = 0.f;
   }
-  __device__ __forceinline__ void load_q(Query& q, const Elt* rows, int n_rows) const {
-    const Elt* src = rows + (size_t)min(i, n_rows - 1) * D_ + 8 * kq;
+  __device__ __forceinline__ void load_row(Query& q, const Elt* row) const {   // the lane's row of Q
 #pragma unroll
-    for (int s = 0; s < KS; ++s) q.r[s] = *reinterpret_cast<const u32x4*>(src + 32 * s);
+    for (int s = 0; s < KS; ++s) q.r[s] = *reinterpret_cast<const u32x4*>(row + 8 * kq + 32 * s);
   }
+  __device__ __forceinline__ void load_q(Query& q, const Elt* rows, int n_rows) const { load_row(q, rows + (size_t)min(i, n_rows - 1) * D_); }
   __device__ __forceinline__ void rows_of(u32x4 (&r)[2][KS], const Elt* base, const int64_t (&at)[2]) const {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -313,11 +313,11 @@ struct DecodeF32 {
     }
     return r;
   }
-  __device__ __forceinline__ void load_q(Query& q, const Elt* rows, int n_rows) const {
-    const float* src = rows + (size_t)min(i, n_rows - 1) * dim();
+  __device__ __forceinline__ void load_row(Query& q, const Elt* row) const {
 #pragma unroll
-    for (int s = 0; s < 4 * DB; ++s) q.r[s] = four(src, 16 * s + 4 * kq);
+    for (int s = 0; s < 4 * DB; ++s) q.r[s] = four(row, 16 * s + 4 * kq);
   }
+  __device__ __forceinline__ void load_q(Query& q, const Elt* rows, int n_rows) const { load_row(q, rows + (size_t)min(i, n_rows - 1) * dim()); }
   __device__ __forceinline__ void load_k(const Elt* base, const int64_t (&at)[1]) {
     const float* src = base + (at[0] < 0 ? 0 : at[0]);
 #pragma unroll

@@ -91,6 +91,16 @@ hipError_t launch_window_step(const DecodeLaunch& p, hipStream_t stream);   // o
 size_t cross_workspace_bytes(int32_t B, int32_t Hkv, int32_t R, int32_t Sk, int32_t D, int32_t is_f32);
 hipError_t launch_cross(const DecodeLaunch& p, hipStream_t stream);
 
+// One new token of each request over its pages, where consecutive requests share prefixes (shared.hip).
+struct SharedLaunch {
+  DecodeLaunch d;                            // as for launch_decode, over pages; R heads a K/V head
+  const int32_t *share_first, *share_len;    // device [G + 1], [G]
+  int32_t G;
+};
+size_t shared_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t G);
+bool shared_fits(int64_t B, int64_t Hkv, int64_t g, int64_t G, int64_t keys);
+hipError_t launch_shared(const SharedLaunch& p, hipStream_t stream);
+
 // Attention of prompts within a window (window.hip).
 struct WindowLaunch {
   const void *Q, *K, *V;    // device [B][Hq|Hkv][S][D]

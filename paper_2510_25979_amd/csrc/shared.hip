@@ -1,0 +1,742 @@
+// Attention of one new token of each request over its pages, where requests share long prefixes: K and V of a prefix are read once for all
+// requests of its group, not once for each.
+//
+// A group is consecutive rows of the batch whose first P tokens are the same.  The work is a list of items, first the groups' prefixes (the g heads of
+// all the group's requests on P keys), then each request's own keys behind its prefix (g heads on n - P keys); a request that shares nothing has all its
+// keys there.  Every item's result is partial: row maximum, sum, sum of weighted V, in binary32; a row's two items are added up at the end.
+//
+// shared_plan_kernel writes the list: who is in which group, what each item has and where its blocks are numbered.
+// shared_prefix_kernel (bf16) forms prefixes of many rows: workgroups of 128 rows that share chunks of 64 keys in LDS, as cross.hip has them, each an equal
+//   run of all such chunks, so that few groups fill the chip and many short ones do, too.
+// shared_run_kernel forms everything else in units of 16 rows of one (item, K/V head), cut into equal runs of blocks by wave, as decode.hip.
+// shared_join_kernel adds up an output row's parts.
+//
+// Bound by memory where own keys prevail, by the prefixes' products and the partial results' way through memory otherwise.
+#include <type_traits>
+
+#include "decode_tile.hpp"
+
+namespace ac {
+
+constexpr int kSharedRows = 128, kSharedChunk = 64;   // of a workgroup of shared_prefix_kernel
+constexpr int kSharedWgs = 512;                       // most workgroups of it
+constexpr int kSharedLeast = 8;                       // chunks of a run at least: each run leaves two results of 128 rows at the most
+constexpr int kSharedUnitCost = 1;                    // what a unit of it costs beside its chunks
+
+struct SharedItem {
+  int keys, key0, row;     // keys [key0, key0 + keys) of the request whose table has them
+  int b0, R;               // rows of a K/V head: the g heads of requests b0, b0 + 1, ...
+  int rbs, start;          // row blocks of a K/V head; number of the first block
+  int group;               // of a request: its group's number, -1: shares nothing; of a group: 1 if shared_prefix_kernel forms it
+};
+
+struct SharedArgs {
+  DecodeArgs d;            // Q, K, V, O, table, len and sizes
+  const int32_t *share_first, *share_len;
+  int32_t *sums, *first, *leader, *count, *start, *start1;   // sums: blocks of all items, chunks of all prefixes, chunks of a run
+  SharedItem* item;        // [G + B]
+  float *part, *stat;      // partial results: rows' own whole ones, rows' prefixes' whole ones, two of each run
+  int32_t G, g, own_rbs, big_rows, wgs;   // big_rows: rows from which on shared_prefix_kernel forms a prefix
+  Divider by_g;
+};
+
+// Records: own whole results [B Hq], prefixes' [B Hq], of runs [2 waves][16], of workgroups [2 wgs][128].
+__device__ __forceinline__ size_t shared_rows(const SharedArgs& a) { return (size_t)a.d.B * a.d.Hkv * a.g; }
+
+constexpr int kPlanThreads = 1024;
+template <typename Op>
+__device__ __forceinline__ int shared_scan(int x, int& all, int* part, Op op, int none) {   // inclusive, over the workgroup
+  constexpr int NW = kPlanThreads / kWave;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int off = 1; off < kWave; off <<= 1) {
+    const int p = __shfl_up(x, off);
+    if (lane >= off) x = op(x, p);
+  }
+  if (lane == kWave - 1) part[wave] = x;
+  __syncthreads();
+  int before = none;
+  all = none;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    const int p = part[w];
+    if (w < wave) before = op(before, p);
+    all = op(all, p);
+  }
+  __syncthreads();
+  return op(x, before);
+}
+
+// What this launch has written, past the first-level cache.
+__device__ __forceinline__ int shared_peek(const int32_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+template <int BK>
+__global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedArgs a) {
+  __shared__ int part[kPlanThreads / kWave], part1[kPlanThreads / kWave];
+  const int tid = threadIdx.x, B = a.d.B, G = a.G, cap = a.d.Sk;
+  auto add = [](int x, int y) { return x + y; };
+  auto top = [](int x, int y) { return max(x, y); };
+  // where groups begin: in order, whatever is given
+  int before = 0;
+  for (int c = 0; c <= G; c += kPlanThreads) {
+    const int i = c + tid;
+    int all;
+    const int f = shared_scan(i <= G ? min(max(a.share_first[i], 0), B) : 0, all, part, top, 0);
+    if (i <= G) a.first[i] = max(before, f);
+    if (i < G) {
+      a.leader[i] = B;
+      a.count[i] = 0;
+    }
+    before = max(before, all);
+  }
+  __threadfence();
+  __syncthreads();
+  auto group_of = [&](int b) {   // the last group that begins at b or before it, if b is in it
+    int lo = -1, hi = G;         // first[lo] <= b < first[hi], but for the ends
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (shared_peek(a.first + mid) <= b) lo = mid;
+      else hi = mid;
+    }
+    return lo >= 0 && b < shared_peek(a.first + lo + 1) ? lo : -1;
+  };
+  auto tokens = [&](int b) { return min(max(a.d.len[b], 0), cap); };
+  auto prefix = [&](int q) { return min(max(a.share_len[q], 0), cap); };
+  for (int b = tid; b < B; b += kPlanThreads) {
+    const int q = group_of(b);
+    a.item[G + b].group = q;
+    if (q < 0) continue;
+    const int P = prefix(q);
+    if (P > 0 && tokens(b) >= P) {   // shorter ones have their keys for themselves
+      atomicMin(&a.leader[q], b);
+      atomicAdd(&a.count[q], 1);
+    }
+  }
+  __threadfence();
+  __syncthreads();
+  int begun = 0, begun1 = 0;
+  for (int c = 0; c < G + B; c += kPlanThreads) {
+    const int i = c + tid;
+    SharedItem it = {0, 0, 0, 0, 0, 1, 0, 0};
+    int cost = 0, cost1 = 0;
+    if (i < G) {
+      const int f = shared_peek(a.first + i), n = shared_peek(a.first + i + 1) - f;
+      if (shared_peek(a.count + i) > 1) {
+        it.keys = prefix(i);
+        it.row = shared_peek(a.leader + i);
+        it.b0 = f;
+        it.R = n * a.g;
+        it.group = it.R >= a.big_rows;
+        if (it.group) {
+          it.rbs = (it.R + kSharedRows - 1) / kSharedRows;
+          cost1 = a.d.Hkv * it.rbs * ((it.keys + kSharedChunk - 1) / kSharedChunk + kSharedUnitCost);
+        } else {
+          it.rbs = (it.R + kDecodeRows - 1) / kDecodeRows;
+          cost = a.d.Hkv * it.rbs * ((it.keys + BK - 1) / BK + kUnitCost);
+        }
+      }
+    } else if (i < G + B) {
+      const int b = i - G, q = shared_peek(&a.item[i].group), n = tokens(b);
+      it.group = q;
+      if (q >= 0) {
+        const int P = prefix(q);
+        if (n >= P && shared_peek(a.count + q) > 1) it.key0 = P;
+      }
+      it.keys = n - it.key0;
+      it.row = it.b0 = b;
+      it.R = a.g;
+      it.rbs = a.own_rbs;
+      if (it.keys > 0) cost = a.d.Hkv * it.rbs * ((it.keys + BK - 1) / BK + kUnitCost);
+    }
+    int all, all1;
+    const int upto = begun + shared_scan(cost, all, part, add, 0), upto1 = begun1 + shared_scan(cost1, all1, part1, add, 0);
+    if (i < G + B) {
+      it.start = i < G && it.group ? upto1 - cost1 : upto - cost;
+      a.item[i] = it;
+      a.start[i] = upto - cost;
+      if (i < G) a.start1[i] = upto1 - cost1;
+    }
+    begun += all;
+    begun1 += all1;
+  }
+  if (tid == 0) {
+    a.sums[0] = begun;
+    a.sums[1] = begun1;
+    const int even = (begun1 - 1) / a.wgs + 1;
+    a.sums[2] = even > kSharedLeast ? even : kSharedLeast;
+  }
+}
+
+// The last of n items that begins at block x or before it (items without a block begin where the next one does).  64 looked at a step.
+__device__ __forceinline__ int shared_locate(const int32_t* start, int n, int x, int lane) {
+  int lo = 0, hi = n;   // it is in [lo, hi)
+  while (hi - lo > 1) {
+    const int step = (hi - lo + kWave - 1) / kWave, at = lo + lane * step;
+    const unsigned long long up = __ballot(at < hi && start[at] <= x);   // (lane 0 always)
+    const int last = 63 - (int)__builtin_clzll(up);
+    const int from = lo + last * step;
+    hi = min(hi, from + step);
+    lo = from;
+  }
+  return __builtin_amdgcn_readfirstlane(lo);
+}
+__device__ __forceinline__ SharedItem shared_item(const SharedItem* items, int i) {   // by scalar loads
+  typedef const SharedItem __attribute__((address_space(4)))* scalar_ptr;
+  scalar_ptr p = (scalar_ptr)(uintptr_t)(items + __builtin_amdgcn_readfirstlane(i));
+  SharedItem it;
+  it.keys = p->keys; it.key0 = p->key0; it.row = p->row; it.b0 = p->b0; it.R = p->R; it.rbs = p->rbs; it.start = p->start; it.group = p->group;
+  return it;
+}
+// Row r of K/V head hk of an item, in Q, O and the records.
+__device__ __forceinline__ size_t shared_row(const SharedArgs& a, int b0, int hk, int r) {
+  const int n = a.by_g.div(r);
+  return ((size_t)(b0 + n) * a.d.Hkv + hk) * a.g + (r - n * a.g);
+}
+
+// ---- units of 16 rows
+struct SharedBlock {
+  int i, unit, blk, nb, left;   // item, its unit, block of the unit, blocks of a unit, what is left of the run
+  SharedItem it;
+};
+
+template <class Core>
+__global__ __launch_bounds__(kThreads, Core::WGS) void shared_run_kernel(const SharedArgs a) {
+  typedef typename Core::Elt Elt;
+  constexpr int BK = Core::BK, KPL = Core::KPL;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[Core::LDS ? 4 * Core::LDS : 16];
+  const DecodeArgs& d = a.d;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int run = blockIdx.x * 4 + wave, n_items = a.G + d.B;
+  const int total = a.sums[0], per = run_length(total, d.waves);
+  if (run >= d.waves || (int64_t)run * per >= total) return;
+  Core core(d, lds + wave * Core::LDS, lane);
+  const int D = core.dim();
+
+  auto item = [&](SharedBlock& s, int i) {
+    s.i = i;
+    s.it = shared_item(a.item, i);
+    s.unit = 0;
+    s.nb = (s.it.keys + BK - 1) / BK;
+  };
+  auto next = [&](SharedBlock& s) {   // false: the run ends
+    const bool last = s.blk + 1 == s.nb;
+    s.left -= last ? 1 + kUnitCost : 1;
+    s.blk = last ? 0 : s.blk + 1;
+    s.unit += last ? 1 : 0;
+    if (last && s.left > 0 && s.unit == d.Hkv * s.it.rbs) {   // the next item that has a block
+      const int done = s.it.start + s.unit * (s.nb + kUnitCost);
+      int i = s.i + 1;
+      for (;; i += kWave) {   // (there is one)
+        const unsigned long long up = __ballot(i + lane + 1 >= n_items || a.start[i + lane + 1] > done);
+        if (up) {
+          i += (int)__builtin_ctzll(up);
+          break;
+        }
+      }
+      item(s, i);
+    }
+    return s.left > 0;
+  };
+  SharedBlock now, then, later;
+  {
+    const int x = run * per;
+    item(now, shared_locate(a.start, n_items, x, lane));
+    now.left = min(per, total - x);
+    const int in = x - now.it.start, cost = now.nb + kUnitCost;
+    now.unit = in / cost;
+    now.blk = in - now.unit * cost;
+    if (now.blk >= now.nb) {   // behind a unit's last block
+      now.left -= now.nb + kUnitCost - now.blk - 1;
+      now.blk = now.nb - 1;
+      now.left += kUnitCost;
+      if (!next(now)) return;
+    }
+  }
+  auto ask = [&](const SharedBlock& s, int(&page)[KPL]) {
+#pragma unroll
+    for (int t = 0; t < KPL; ++t) {
+      const int j = BK * s.blk + core.key(t);
+      page[t] = j < s.it.keys ? d.table[(size_t)s.it.row * d.max_pages + d.by_ps.div(s.it.key0 + j)] : 0;
+    }
+  };
+  auto place = [&](const SharedBlock& s, const int(&page)[KPL], int64_t(&at)[KPL]) {
+#pragma unroll
+    for (int t = 0; t < KPL; ++t) {
+      const int j = BK * s.blk + core.key(t), token = s.it.key0 + j;
+      at[t] = j < s.it.keys && (unsigned)page[t] < (unsigned)d.n_pages
+                  ? page[t] * d.page_stride + (int64_t)(token - d.by_ps.div(token) * d.ps) * D : -1;
+    }
+  };
+  auto head_of = [&](const SharedBlock& s) { return s.it.rbs == 1 ? s.unit : s.unit / s.it.rbs; };
+  auto base_of = [&](const void* p, const SharedBlock& s) { return static_cast<const Elt*>(p) + (size_t)head_of(s) * d.head_stride; };
+  auto load_q = [&](typename Core::Query& q, const SharedBlock& s) {
+    const int hk = head_of(s), r = kDecodeRows * (s.unit - hk * s.it.rbs) + core.i;
+    core.load_row(q, static_cast<const Elt*>(d.Q) + shared_row(a, s.it.b0, hk, min(r, s.it.R - 1)) * D);
+  };
+
+  typename Core::Query q, q_then;
+  int page[KPL];
+  int64_t at[KPL], at_then[KPL];
+  ask(now, page);
+  load_q(q, now);
+  then = now;
+  bool more = next(then);
+  place(now, page, at);
+  core.load_k(base_of(d.K, now), at);
+  core.load_v(base_of(d.V, now), at);
+  if (more) ask(then, page);
+  core.reset();
+  int begin = now.blk;
+  while (true) {
+    typename Core::Scores s;
+    core.scores(s, q);
+    const bool last = now.blk + 1 == now.nb;   // of its unit
+    later = then;
+    bool more_later = false;
+    if (more) {
+      place(then, page, at_then);
+      if (last) load_q(q_then, then);
+      core.load_k(base_of(d.K, then), at_then);
+      more_later = next(later);
+      if (more_later) ask(later, page);
+    }
+    core.hide(s, at);
+    core.stage_v();
+    if (Core::LDS && more) core.load_v(base_of(d.V, then), at_then);
+    if (Core::LDS) wave_fence();
+    core.add(s, d.scale_log2e);
+    if (Core::LDS) wave_fence();   // the tile is read before the next block's rows are written
+    if (!Core::LDS && more) core.load_v(base_of(d.V, then), at_then);
+    if (last || !more) {
+      const float sum = sum_of_four(core.l);
+      const int hk = head_of(now), r = kDecodeRows * (now.unit - hk * now.it.rbs) + core.i;
+      if (r < now.it.R) {
+        const size_t rows = shared_rows(a);
+        const size_t rec = begin == 0 && last ? (now.i < a.G ? rows : 0) + shared_row(a, now.it.b0, hk, r)
+                                              : 2 * rows + (size_t)(2 * run + (begin == 0)) * kDecodeRows + core.i;   // as partial_of has it
+#pragma unroll
+        for (int n = 0; n < Core::NP; ++n) {
+          const int c = core.col(n);
+          store_partial(a.part + rec * D + c, decode_piece(core, n), c, D);
+        }
+        if (core.kq == 0) {
+          a.stat[2 * rec] = core.m;
+          a.stat[2 * rec + 1] = sum;
+        }
+      }
+      if (!more) break;
+      core.reset();
+      q = q_then;
+      begin = 0;
+    }
+    now = then;
+    then = later;
+    more = more_later;
+#pragma unroll
+    for (int t = 0; t < KPL; ++t) at[t] = at_then[t];
+  }
+}
+
+// ---- prefixes of many rows
+template <int D>
+__global__ __launch_bounds__(kThreads, 2) void shared_prefix_kernel(const SharedArgs a) {
+  constexpr int PPR = D / 8, NCOPY = kSharedChunk * PPR / kWave / 4;
+  __shared__ __attribute__((aligned(16))) bf16_t kb0[kSharedChunk * D];
+  __shared__ __attribute__((aligned(16))) bf16_t vb0[kSharedChunk * D];
+  __shared__ __attribute__((aligned(16))) bf16_t kb1[kSharedChunk * D];
+  __shared__ __attribute__((aligned(16))) bf16_t vb1[kSharedChunk * D];
+  const DecodeArgs& d = a.d;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int il = lane & 31, kh = lane >> 5;
+  const int total = a.sums[1], per = a.sums[2];
+  if ((int64_t)blockIdx.x * per >= total) return;
+  const float scale_log2e = __builtin_bit_cast(
+      float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, d.scale_log2e) + (lane & 0)));
+  // copies and operand addresses as in cross.hip
+  const int slot0 = kWave * wave + lane, crow = slot0 / PPR, cpos = slot0 % PPR;
+  const int kpiece = 8 * (cpos ^ k_piece_swizzle<D>(crow)), vpiece = 8 * (cpos ^ v_piece_swizzle<D>(crow));
+  int koff[D / 16], voff[2][D / 32];
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ++ks) koff[ks] = il * D + 8 * ((2 * ks + kh) ^ k_piece_swizzle<D>(il));
+#pragma unroll
+  for (int half = 0; half < 2; ++half)
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) {
+      const int t = lane & 15, j = 4 * kh + 8 * half + (t >> 2), d0 = 32 * db + 16 * (il >> 4) + 4 * (t & 3);
+      voff[half][db] = j * D + 8 * ((d0 >> 3) ^ v_piece_swizzle<D>(j)) + (d0 & 7);
+    }
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  typedef short s16x8 __attribute__((ext_vector_type(8)));
+  auto vop = [&](const bf16_t* vb, int db, int jb, int s2) {
+    const bf16_t* at = vb + (32 * jb + 16 * s2) * D;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(at + voff[0][db]));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(at + voff[1][db]));
+    const s16x8 w = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    return __builtin_bit_cast(bf16x8, w);
+  };
+  u32x4 q[D / 16];
+  f32x16 acc[D / 32];
+  float m_run, l_run;
+  auto qk = [&](const bf16_t* kb, int jb) {
+    f32x16 s;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) s[v] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks)
+      s = mfma_bf16(*reinterpret_cast<const bf16x8*>(kb + koff[ks] + 32 * jb * D), __builtin_bit_cast(bf16x8, q[ks]), s);
+    return s;
+  };
+  auto row_max = [&](const f32x16& s) {
+    const float m01 = fmaxf(fmaxf(s[0], s[1]), s[2]), m02 = fmaxf(fmaxf(s[3], s[4]), s[5]);
+    const float m03 = fmaxf(fmaxf(s[6], s[7]), s[8]), m04 = fmaxf(fmaxf(s[9], s[10]), s[11]);
+    const float m05 = fmaxf(fmaxf(s[12], s[13]), s[14]);
+    return max_with_other_half(fmaxf(fmaxf(fmaxf(m01, m02), m03), fmaxf(fmaxf(m04, m05), s[15])));
+  };
+  typedef bf16_t bf16x2 __attribute__((ext_vector_type(2)));
+  auto weights = [&](const f32x16& s, float m, u32x4(&pw)[2], float& sum) {   // rounded to bf16 as in decode_tile.hpp
+    const bf16x2 ones = {(bf16_t)1.0f, (bf16_t)1.0f};
+    const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+      const float e0 = __builtin_amdgcn_exp2f(fmaf(s[2 * w], scale_log2e, -ref));
+      const float e1 = __builtin_amdgcn_exp2f(fmaf(s[2 * w + 1], scale_log2e, -ref));
+      const uint32_t pk = pack_bf16(e0, e1);
+      pw[w >> 2][w & 3] = pk;
+      sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pk), ones, sum, false);
+    }
+  };
+  auto pv = [&](const bf16_t* vb, int jb, const u32x4(&pw)[2]) {
+#pragma unroll
+    for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+        acc[db] = mfma_bf16(vop(vb, db, jb, s2), __builtin_bit_cast(bf16x8, pw[s2]), acc[db]);
+  };
+  auto rescale = [&](float m_new) {
+    const float alpha = m_new > m_run ? __builtin_amdgcn_exp2f(m_run - m_new) : 1.f;
+    l_run *= alpha;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[db][v] *= alpha;
+  };
+  auto step = [&](const bf16_t* kb, const bf16_t* vb, unsigned long long there) __attribute__((always_inline)) {
+    f32x16 s0 = qk(kb, 0);
+    auto hide = [&](f32x16& s, uint32_t bits) {
+      if (bits != 0xffffffffu)   // uniform
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+          if (!((bits >> mfma_row(v, kh)) & 1)) s[v] = -INFINITY;
+    };
+    hide(s0, (uint32_t)there);
+    float cand = fmaxf(m_run, row_max(s0) * scale_log2e);
+    if (__any(cand > m_run + kDecodeSlack)) {
+      rescale(cand);
+      m_run = cand;
+    }
+    f32x16 s1 = qk(kb, 1);
+    u32x4 p0[2], p1[2];
+    float sum = 0.f, sum1 = 0.f, m1 = m_run;
+    weights(s0, m_run, p0, sum);
+    l_run += sum;
+    hide(s1, (uint32_t)(there >> 32));
+    cand = fmaxf(m_run, row_max(s1) * scale_log2e);
+    const bool moved = __any(cand > m_run + kDecodeSlack);
+    if (moved) m1 = cand;
+    pv(vb, 0, p0);
+    weights(s1, m1, p1, sum1);
+    if (moved) rescale(m1);
+    m_run = m1;
+    l_run += sum1;
+    pv(vb, 1, p1);
+  };
+  auto publish = [&]() {   // this wave's copies have landed, then everybody's; the other stage is no longer read
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+  };
+
+  int x = blockIdx.x * per;
+  const int end = min(total, x + per);
+  int i = shared_locate(a.start1, a.G, x, lane);
+  while (x < end) {
+    const SharedItem it = shared_item(a.item, i);
+    const int nc = (it.keys + kSharedChunk - 1) / kSharedChunk, cost = nc + kSharedUnitCost;
+    const int in = x - it.start, unit = in / cost, c0 = in - unit * cost, c1 = min(nc, c0 + end - x);
+    if (unit >= d.Hkv * it.rbs) {   // the next group that has chunks
+      i = shared_locate(a.start1, a.G, x, lane);
+      continue;
+    }
+    if (c0 >= nc) {   // behind a unit's last chunk
+      x += cost - c0;
+      continue;
+    }
+    const int hk = unit / it.rbs, r = kSharedRows * (unit - hk * it.rbs) + kRowsPerWave * wave + il;
+    const bf16_t* K = static_cast<const bf16_t*>(d.K) + (size_t)hk * d.head_stride;
+    const bf16_t* V = static_cast<const bf16_t*>(d.V) + (size_t)hk * d.head_stride;
+    // lane l knows the place of key l of a chunk: its page is asked for a chunk ahead
+    auto ask = [&](int c) {
+      const int j = c * kSharedChunk + lane;
+      return j < it.keys ? d.table[(size_t)it.row * d.max_pages + d.by_ps.div(j)] : -1;
+    };
+    auto copy = [&](bf16_t* kb, bf16_t* vb, int c, int page) {   // which keys are there
+      const int j = c * kSharedChunk + lane;
+      const bool is = (unsigned)page < (unsigned)d.n_pages;
+      const int64_t at = is ? page * d.page_stride + (int64_t)(j - d.by_ps.div(j) * d.ps) * D : 0;   // (0: there, and not used)
+      const unsigned long long there = __ballot(is);
+#pragma unroll
+      for (int n = 0; n < NCOPY; ++n) {
+        const int row = crow + 256 / PPR * n;
+        const int64_t from = __shfl((long long)at, row);
+        __builtin_amdgcn_global_load_lds(K + from + kpiece, kb + kWave * 8 * (wave + 4 * n), 16, 0, 0);
+        bf16_t* to = vb + kWave * 8 * (wave + 4 * n);
+        if ((there >> row) & 1) __builtin_amdgcn_global_load_lds(V + from + vpiece, to, 16, 0, 0);
+        else *reinterpret_cast<u32x4*>(to + 8 * lane) = u32x4{0, 0, 0, 0};   // a weight of zero does not make a NaN vanish
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      return there;
+    };
+    __syncthreads();   // the stages are no longer read
+    int page = ask(c0);
+    {
+      const bf16_t* src = static_cast<const bf16_t*>(d.Q) + shared_row(a, it.b0, hk, min(r, it.R - 1)) * D + 8 * kh;
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks) q[ks] = *reinterpret_cast<const u32x4*>(src + 16 * ks);
+    }
+    unsigned long long there0 = copy(kb0, vb0, c0, page), there1 = 0;
+    if (c0 + 1 < c1) page = ask(c0 + 1);
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[db][v] = 0.f;
+    m_run = -INFINITY;
+    l_run = 0.f;
+    for (int c = c0; c < c1; c += 2) {
+      publish();
+      if (c + 1 < c1) {
+        there1 = copy(kb1, vb1, c + 1, page);
+        if (c + 2 < c1) page = ask(c + 2);
+      }
+      step(kb0, vb0, there0);
+      if (c + 1 >= c1) break;
+      publish();
+      if (c + 2 < c1) {
+        there0 = copy(kb0, vb0, c + 2, page);
+        if (c + 3 < c1) page = ask(c + 3);
+      }
+      step(kb1, vb1, there1);
+    }
+    const float sum = l_run + __shfl_xor(l_run, 32);
+    if (r < it.R) {
+      const size_t rows = shared_rows(a);
+      const size_t rec = c0 == 0 && c1 == nc ? rows + shared_row(a, it.b0, hk, r)
+                                             : 2 * rows + (size_t)2 * d.waves * kDecodeRows +
+                                                   (size_t)(2 * blockIdx.x + (c0 == 0)) * kSharedRows + kRowsPerWave * wave + il;
+      float* to = a.part + rec * D + 4 * kh;
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int vq = 0; vq < 4; ++vq)
+          *reinterpret_cast<f32x4*>(to + 32 * db + 8 * vq) = f32x4{acc[db][4 * vq], acc[db][4 * vq + 1], acc[db][4 * vq + 2], acc[db][4 * vq + 3]};
+      if (kh == 0) {
+        a.stat[2 * rec] = m_run;
+        a.stat[2 * rec + 1] = sum;
+      }
+    }
+    x += c1 - c0 + (c1 == nc ? kSharedUnitCost : 0);
+  }
+}
+
+// ---- parts of an output row
+// NW waves add up one row (or, NW 1, a wave each): a lane holds four columns, G lanes a partial result; a wave knows the weights of 64 at once.
+template <bool F32, int G, int NW>
+__global__ __launch_bounds__(NW == 1 ? kThreads : NW * kWave) void shared_join_kernel(const SharedArgs a) {
+  typedef typename std::conditional<F32, float, bf16_t>::type Elt;
+  constexpr int BK = F32 ? 16 : 32, SUB = kWave / G;
+  __shared__ __attribute__((aligned(16))) f32x4 sums[NW][G];
+  __shared__ float ms[NW], ls[NW];
+  const DecodeArgs& d = a.d;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int sub = lane / G, col = 4 * (lane % G), D = d.D;
+  const size_t rows = shared_rows(a);
+  const size_t row = NW == 1 ? (size_t)blockIdx.x * (kThreads / kWave) + wave : blockIdx.x;
+  if (row >= rows) return;   // (all of the workgroup's waves, where they meet)
+  const int head = (int)(row / a.g), x = (int)(row - (size_t)head * a.g), b = head / d.Hkv, hk = head - b * d.Hkv;
+  const int per = run_length(a.sums[0], d.waves), per1 = a.sums[2];
+  // the parts of an item's row: of runs [w0, w0 + n), or (whole) one by itself
+  struct Parts {
+    int n, w0, per, from;
+    size_t base;     // record of the first part, or of run 0
+    int stride;      // records of a run; 0: whole
+  };
+  auto parts_of = [&](const SharedItem& it, int r, bool big, size_t whole) {
+    Parts p = {0, 0, 1, 0, whole, 0};
+    const int br = big ? kSharedRows : kDecodeRows, blocks = big ? (it.keys + kSharedChunk - 1) / kSharedChunk : (it.keys + BK - 1) / BK;
+    if (blocks == 0) return p;
+    p.per = big ? per1 : per;
+    p.from = it.start + (hk * it.rbs + r / br) * (blocks + (big ? kSharedUnitCost : kUnitCost));
+    p.w0 = p.from / p.per;
+    p.n = (p.from + blocks - 1) / p.per - p.w0 + 1;
+    if (p.n > 1) {
+      p.base = 2 * rows + (big ? (size_t)2 * d.waves * kDecodeRows : 0) + r % br;
+      p.stride = br;
+    }
+    return p;
+  };
+  const SharedItem own = shared_item(a.item, a.G + b);
+  const Parts mine = parts_of(own, x, false, row);
+  Parts theirs = {0, 0, 1, 0, 0, 0};
+  if (own.key0 > 0) {
+    const SharedItem pre = shared_item(a.item, own.group);
+    theirs = parts_of(pre, (b - pre.b0) * a.g + x, pre.group != 0, rows + row);
+  }
+  const int n = mine.n + theirs.n;
+  auto record = [&](int e) {
+    const Parts& p = e < mine.n ? mine : theirs;
+    const int w = p.w0 + (e < mine.n ? e : e - mine.n);
+    return p.base + (p.stride ? (size_t)partial_of(w, p.per, p.from) * p.stride : 0);
+  };
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  float top = -INFINITY, total = 0.f;
+  for (int e0 = NW == 1 ? 0 : wave; e0 < n; e0 += NW * kWave) {
+    const int e = min(e0 + NW * lane, n - 1);
+    const size_t rec = record(e);
+    float m = -INFINITY, l = 0.f;
+    if (e0 + NW * lane < n) {
+      m = a.stat[2 * rec];
+      l = a.stat[2 * rec + 1];
+    }
+    float t = fmaxf(top, m);
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) t = fmaxf(t, __shfl_xor(t, off));
+    const float old = top < t ? __builtin_amdgcn_exp2f(top - t) : 1.f, f = m < t ? __builtin_amdgcn_exp2f(m - t) : 1.f;
+    top = t;
+    total *= old;
+    o *= old;
+    l *= f;
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) l += __shfl_xor(l, off);
+    total += l;
+    const int here = min(kWave, (n - 1 - e0) / NW + 1);
+    for (int k0 = 0; k0 < here; k0 += 4 * SUB) {   // four loads of a lane on their way at once
+      f32x4 y[4];
+      float weight[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int k = k0 + j * SUB + sub, from_lane = min(k, here - 1);
+        const float w_j = __shfl(f, from_lane);
+        weight[j] = k < here ? w_j : 0.f;
+        const float* src = a.part + (size_t)__shfl((long long)rec, from_lane) * D + col;
+        y[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (k >= here || col >= D) continue;
+        if (!F32 || col + 4 <= D) {
+          y[j] = *reinterpret_cast<const f32x4_dw*>(src);
+        } else {
+#pragma unroll
+          for (int c = 0; c < 3; ++c)
+            if (col + c < D) y[j][c] = src[c];
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o += y[j] * weight[j];
+    }
+  }
+#pragma unroll
+  for (int off = G; off < kWave; off <<= 1)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) o[c] += __shfl_xor(o[c], off);
+  if (NW > 1) {
+    if (lane < G) sums[wave][lane] = o;
+    if (lane == 0) {
+      ms[wave] = top;
+      ls[wave] = total;
+    }
+    __syncthreads();
+    if (wave > 0) return;
+    for (int w = 1; w < NW; ++w) top = fmaxf(top, ms[w]);
+    total = 0.f;
+    o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float f = ms[w] < top ? __builtin_amdgcn_exp2f(ms[w] - top) : 1.f;
+      total = fmaf(ls[w], f, total);
+      o += sums[w][lane % G] * f;
+    }
+  }
+  if (sub == 0 && col < D) {
+    const float inv = total == 0.f ? 0.f : 1.f / total;   // no key at all: zeros
+    Elt* to = static_cast<Elt*>(d.O) + row * D + col;
+    if constexpr (F32) store_partial(to, o * inv, col, D);
+    else DecodeBf16<64>::store(to, o, inv, col, D);
+  }
+}
+
+// ---- launches
+static size_t shared_ints(int64_t B, int64_t G) {   // sums, first, leader, count, start, start1, items; in whole pieces of 16 bytes
+  return (size_t)((4 + (G + 1) + G + G + (G + B) + G + 3) / 4 * 4 + (G + B) * (int64_t)(sizeof(SharedItem) / 4));
+}
+static bool shared_big(int64_t B, int32_t g, int32_t D) { return (D == 64 || D == 128) && B * g > 16; }   // some group may have many rows
+static size_t shared_records(int64_t B, int64_t Hq, int32_t g, int32_t D) {
+  return (size_t)(2 * B * Hq) + (size_t)2 * kDecodeWaves * kDecodeRows + (shared_big(B, g, D) ? (size_t)2 * kSharedWgs * kSharedRows : 0);
+}
+size_t shared_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t G) {
+  return 4 * shared_ints(B, G) + shared_records(B, Hq, Hq / Hkv, D) * (size_t)(D + 2) * sizeof(float);
+}
+bool shared_fits(int64_t B, int64_t Hkv, int64_t g, int64_t G, int64_t keys) {
+  // own items' blocks and prefixes' (a group's last row block may be a single row)
+  const double units = (double)Hkv * (B * (double)((g + kDecodeRows - 1) / kDecodeRows) + (double)B * g / kDecodeRows + G);
+  return units * ((keys + 15) / 16 + kUnitCost) < 2147483648.0 - 65536 && (double)B * Hkv * g < 2147483648.0 - 65536;
+}
+
+template <class Core>
+static hipError_t launch_shared_as(SharedArgs& a, bool big, hipStream_t stream) {
+  constexpr bool F32 = Core::BK == 16;
+  constexpr int G = Core::NP * 4;
+  a.d.waves = 4 * 256 * Core::WGS;
+  hipLaunchKernelGGL((shared_plan_kernel<Core::BK>), dim3(1), dim3(kPlanThreads), 0, stream, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if constexpr (!F32)
+    if (big) {
+      hipLaunchKernelGGL((shared_prefix_kernel<Core::NP * 16>), dim3((unsigned)a.wgs), dim3(kThreads), 0, stream, a);
+      e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+  hipLaunchKernelGGL((shared_run_kernel<Core>), dim3((unsigned)(a.d.waves / 4)), dim3(kThreads), 0, stream, a);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int64_t rows = (int64_t)a.d.B * a.d.Hkv * a.g;
+  if (rows <= 4096) hipLaunchKernelGGL((shared_join_kernel<F32, G, 4>), dim3((unsigned)rows), dim3(4 * kWave), 0, stream, a);
+  else hipLaunchKernelGGL((shared_join_kernel<F32, G, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(kThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_shared(const SharedLaunch& p, hipStream_t stream) {
+  SharedArgs a;
+  a.d = decode_args(p.d);
+  a.g = p.d.R; a.G = p.G;
+  a.own_rbs = a.d.rbs;
+  a.share_first = p.share_first; a.share_len = p.share_len;
+  a.by_g = Divider((uint32_t)a.g);
+  const bool big = !p.d.is_f32 && shared_big(p.d.B, a.g, p.d.D);
+  a.big_rows = big ? 33 : 0x7fffffff;
+  a.wgs = kSharedWgs;
+  const int64_t B = p.d.B, G = p.G;
+  int32_t* ws = static_cast<int32_t*>(p.d.ws);
+  a.sums = ws;
+  a.first = ws + 4;
+  a.leader = a.first + G + 1; a.count = a.leader + G; a.start = a.count + G; a.start1 = a.start + G + B;
+  const size_t ints = shared_ints(B, G);
+  a.item = reinterpret_cast<SharedItem*>(ws + ints - (size_t)(G + B) * (sizeof(SharedItem) / 4));
+  a.part = reinterpret_cast<float*>(ws + ints);
+  const size_t records = shared_records(B, (int64_t)p.d.Hkv * a.g, a.g, p.d.D);
+  a.stat = a.part + records * p.d.D;
+  if (!p.d.is_f32) return p.d.D == 64 ? launch_shared_as<DecodeBf16<64>>(a, big, stream) : launch_shared_as<DecodeBf16<128>>(a, big, stream);
+  if (p.d.D == 64) return launch_shared_as<DecodeF32<1, true>>(a, big, stream);
+  if (p.d.D == 128) return launch_shared_as<DecodeF32<2, true>>(a, big, stream);
+  if (p.d.D < 64) return launch_shared_as<DecodeF32<1, false>>(a, big, stream);
+  if (p.d.D < 128) return launch_shared_as<DecodeF32<2, false>>(a, big, stream);
+  return launch_shared_as<DecodeF32<4, false>>(a, big, stream);
+}
+
+}  // namespace ac
