@@ -229,7 +229,8 @@ struct DecodeBf16 {
       for (int c = 0; c < KS; ++c)
         *reinterpret_cast<u32x4*>(vt + key(t) * D_ + 8 * ((4 * c + kq) ^ piece(i))) = v[t][c];
   }
-  __device__ __forceinline__ void add(Scores& s, float scale_log2e) {
+  __device__ __forceinline__ void add(Scores& s, float scale_log2e) { add(s, scale_log2e, acc, m, l); }
+  __device__ __forceinline__ void add(Scores& s, float scale_log2e, f32x4 (&acc)[NP], float& m, float& l) const {
     float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
                      fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
     const float cand = fmaxf(m, max_of_four(mx) * scale_log2e);

@@ -5,9 +5,10 @@
 // one row keeps it (the row itself if it goes on, otherwise the first that takes it) and each other takes a page from the ring and copies its
 // tokens.  A page is free when some row had it and no row has it: two bitmaps of the pages, before and after, say so without a count a page.
 //
-// Three launches, since each needs all of the one before: the rows (who keeps, who copies, which of the ring's pages; one workgroup, which
-// looks at 1,024 rows a step, while others clear the bitmaps), tables, bitmaps and tokens (the whole chip), the ring (one workgroup, pages in order
-// of their number; others bring tables that are replaced in place into place).
+// Bookkeeping of up to 1,024 rows, 16,384 entries and 65,536 pages is one workgroup's work, in LDS; then the tokens are copied by the whole chip.
+// Otherwise three launches, since each needs all of the one before: the rows (who keeps, who copies, which of the ring's pages; one workgroup,
+// which looks at 1,024 rows a step, while others clear the bitmaps), tables and bitmaps, then the ring (one workgroup, pages in order of their
+// number) beside the copies and the way back of tables that are replaced in place.
 #include "common.hpp"
 #include "serve.h"
 #include "serve_index.h"
@@ -18,13 +19,14 @@ struct ForkArgs {
   const int32_t *from, *seq_len, *state, *table;
   int32_t *ring, *table_out, *seq_out, *state_out;
   void *kp, *vp;
-  // workspace: of each row its source (-1: none), tokens and entry of the ring (-1: no copy), of each source who keeps its last page; rows
-  // that copy, their number and the ring's first entry and number; bitmaps; new tables that replace their source
-  int32_t *src, *len, *take, *keeper, *list, *sums, *staged;
+  // workspace: of each row its source (-1: none), tokens and entry of the ring (-1: no copy), of each source who keeps its last page; copies
+  // (from page, to page, tokens), their number and the ring's first entry and number; bitmaps; new tables that replace their source
+  int32_t *src, *len, *take, *keeper, *sums, *staged;
+  int4* copy;
   uint32_t *had, *has;
-  int32_t B, H, D, max_pages, n, ps, sinks, window, words, segs, row_pieces;
+  int32_t B, H, max_pages, n, ps, sinks, window, words, segs, row_pieces, wgs;   // wgs: workgroups that copy
   int64_t page_stride;   // pieces
-  Divider by_ps, by_segs;
+  Divider by_ps, by_segs, by_max_pages;
 };
 
 constexpr int kForkRows = 1024;   // threads of the workgroup that plans
@@ -103,10 +105,7 @@ __global__ __launch_bounds__(kForkRows) void fork_rows_kernel(const ForkArgs a) 
       a.src[b] = served ? f : -1;
       a.len[b] = f < 0 ? 0 : served ? len : -1;
       a.take[b] = copies && served ? upto - 1 : -1;
-      if (copies && served) {
-        a.list[upto - 1] = b;
-        atomicMax(&s_taken, upto);
-      }
+      if (copies && served) atomicMax(&s_taken, upto);
     }
     before += all;
   }
@@ -123,47 +122,146 @@ __device__ __forceinline__ int fork_ring_page(const ForkArgs& a, int first, int 
   return a.ring[at >= (unsigned)a.n ? at - a.n : at];
 }
 
-// T: a piece of a row, 16 bytes, or 4 where rows are no whole number of those.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void fork_tables_kernel(const ForkArgs a, int table_wgs) {
+__global__ __launch_bounds__(kThreads) void fork_tables_kernel(const ForkArgs a) {
   const int tid = threadIdx.x;
-  if ((int)blockIdx.x < table_wgs) {
-    const int b = a.by_segs.div(blockIdx.x), j0 = (blockIdx.x - b * a.segs) * kForkEntries + tid;
-    const int held = fork_pages_of(a, fork_tokens(a, b)), src = a.src[b], len = a.len[b], take = a.take[b];
-    const int now = src >= 0 ? fork_pages_of(a, len) : 0;
-    const int32_t* mine = a.table + (size_t)b * a.max_pages;
-    const int32_t* theirs = a.table + (size_t)max(src, 0) * a.max_pages;
-    int32_t* out = (a.table_out == a.table ? a.staged : a.table_out) + (size_t)b * a.max_pages;
-    auto mark = [&](uint32_t* bits, int page) {
-      if ((unsigned)page < (unsigned)a.n) atomicOr(&bits[page >> 5], 1u << (page & 31));
-    };
+  const int b = a.by_segs.div(blockIdx.x), j0 = (blockIdx.x - b * a.segs) * kForkEntries + tid;
+  const int held = fork_pages_of(a, fork_tokens(a, b)), src = a.src[b], len = a.len[b], take = a.take[b];
+  const int now = src >= 0 ? fork_pages_of(a, len) : 0;
+  const int32_t* mine = a.table + (size_t)b * a.max_pages;
+  const int32_t* theirs = a.table + (size_t)max(src, 0) * a.max_pages;
+  int32_t* out = (a.table_out == a.table ? a.staged : a.table_out) + (size_t)b * a.max_pages;
+  auto mark = [&](uint32_t* bits, int page) {
+    if ((unsigned)page < (unsigned)a.n) atomicOr(&bits[page >> 5], 1u << (page & 31));
+  };
 #pragma unroll
-    for (int i = 0; i < kForkEntries / kThreads; ++i) {
-      const int j = j0 + i * kThreads;
-      if (j < held) mark(a.had, mine[j]);
-      if (j < now) {
-        int page = j == now - 1 && take >= 0 ? fork_ring_page(a, a.sums[0], take) : theirs[j];
-        if (fork_gone(a, len, j)) page = -1;
-        out[j] = page;
-        mark(a.has, page);
+  for (int i = 0; i < kForkEntries / kThreads; ++i) {
+    const int j = j0 + i * kThreads;
+    if (j < held) mark(a.had, mine[j]);
+    if (j < now) {
+      int page = theirs[j];
+      if (j == now - 1 && take >= 0) {
+        const int fresh = fork_ring_page(a, a.sums[0], take);
+        a.copy[take] = make_int4(page, fresh, len - j * a.ps, 0);
+        page = fresh;
+      }
+      if (fork_gone(a, len, j)) page = -1;
+      out[j] = page;
+      mark(a.has, page);
+    }
+  }
+}
+
+// The whole plan by one workgroup.  Everything is read before anything is written, since outputs may be inputs.
+constexpr int kForkSmallEntries = 16384, kForkSmallWords = 2048;
+__global__ __launch_bounds__(kForkRows) void fork_small_kernel(const ForkArgs a) {
+  constexpr int N = kForkSmallEntries / kForkRows, NW = kForkSmallWords / kForkRows;
+  __shared__ int s_keeper[kForkRows], s_src[kForkRows], s_len[kForkRows], s_take[kForkRows], s_held[kForkRows];
+  __shared__ uint32_t s_had[kForkSmallWords], s_has[kForkSmallWords];
+  __shared__ int part[kForkRows / kWave];
+  __shared__ int s_taken;
+  const int tid = threadIdx.x;
+  const int first = ring_first(a.state[0], a.n), count = min(max(a.state[1], 0), a.n);
+  int f = -1, len = 0;
+  if (tid < a.B) {
+    f = a.from[tid];
+    if ((unsigned)f >= (unsigned)a.B) f = -1;
+    len = fork_tokens(a, tid);
+  }
+  s_len[tid] = len;
+  s_held[tid] = fork_pages_of(a, len);
+  s_keeper[tid] = a.B;
+  for (int w = tid; w < a.words; w += kForkRows) s_had[w] = s_has[w] = 0;
+  if (tid == 0) s_taken = 0;
+  __syncthreads();
+  if (f >= 0) {
+    atomicMin(&s_keeper[f], f == tid ? -1 : tid);
+    len = s_len[f];
+  }
+  __syncthreads();
+  int all;
+  const bool copies = f >= 0 && len - a.by_ps.div(len) * a.ps > 0 && (s_keeper[f] == -1 ? f : s_keeper[f]) != tid;
+  const int upto = fork_sum<kForkRows>(copies, all, part);
+  const bool served = !copies || upto <= count;
+  len = f < 0 ? 0 : served ? len : -1;
+  s_src[tid] = served ? f : -1;
+  s_take[tid] = copies && served ? upto - 1 : -1;
+  s_len[tid] = len;
+  if (copies && served) atomicMax(&s_taken, upto);
+  __syncthreads();
+  const int entries = a.B * a.max_pages;
+  int page[N];
+  auto mark = [&](uint32_t* bits, int q) {
+    if ((unsigned)q < (unsigned)a.n) atomicOr(&bits[q >> 5], 1u << (q & 31));
+  };
+#pragma unroll
+  for (int i = 0; i < N; ++i) {   // (what no row has stays: -2)
+    page[i] = -2;
+    const int e = i * kForkRows + tid;
+    if (i * kForkRows < entries && e < entries) {
+      const int b = a.by_max_pages.div(e), j = e - b * a.max_pages, src = s_src[b];
+      if (j < s_held[b]) mark(s_had, a.table[e]);
+      if (src >= 0 && j < s_held[src]) {
+        int q = a.table[src * a.max_pages + j];
+        const int take = s_take[b];
+        if (take >= 0 && j == s_held[src] - 1) {
+          const int fresh = fork_ring_page(a, first, take);
+          a.copy[take] = make_int4(q, fresh, s_len[b] - j * a.ps, 0);
+          q = fresh;
+        }
+        if (fork_gone(a, s_len[b], j)) q = -1;
+        page[i] = q == -2 ? -1 : q;
+        mark(s_has, q);
       }
     }
-    return;
   }
-  // Tokens: workgroup w of W serves copy w mod (their number), pieces of it in turn with the others that do.
-  const int taken = a.sums[2], w = blockIdx.x - table_wgs, W = gridDim.x - table_wgs;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (page[i] != -2) a.table_out[i * kForkRows + tid] = page[i];
+  const unsigned end = ((unsigned)first + (unsigned)count) % (unsigned)a.n;
+  uint32_t free[NW];
+  int n = 0;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    const int at = tid * NW + w;
+    free[w] = at < a.words ? s_had[at] & ~s_has[at] : 0;
+    n += __popc(free[w]);
+  }
+  unsigned at = (unsigned)(fork_sum<kForkRows>(n, all, part) - n);
+#pragma unroll
+  for (int w = 0; w < NW; ++w)
+    while (free[w]) {
+      const int bit = __ffs(free[w]) - 1;
+      free[w] &= free[w] - 1;
+      a.ring[(end + at % (unsigned)a.n) % (unsigned)a.n] = 32 * (tid * NW + w) + bit;
+      ++at;
+    }
+  if (tid < a.B) a.seq_out[tid] = len;
+  if (tid == 0) {
+    a.sums[2] = s_taken;
+    a.state_out[0] = (int)(((unsigned)first + (unsigned)s_taken) % (unsigned)a.n);
+    a.state_out[1] = (int)min((unsigned)a.n, (unsigned)(count - s_taken) + (unsigned)all);
+  }
+}
+
+// Tokens: workgroup w of W serves copy w mod (their number), pieces of it in turn with the others that do.  T: a piece of a row, 16 bytes,
+// or 4 where rows are no whole number of those.
+template <typename T>
+__device__ __forceinline__ void fork_copy(const ForkArgs& a, int w, int W) {
+  const int tid = threadIdx.x, taken = a.sums[2];
   if (taken == 0) return;
   for (int i = w % taken; i < taken; i += W) {
     const int slices = taken >= W ? 1 : W / taken + (i < W % taken), slice = taken >= W ? 0 : w / taken;
-    const int b = a.list[i], len = a.len[b], src = a.src[b], last = fork_pages_of(a, len) - 1;
-    const int page = a.table[(size_t)src * a.max_pages + last], fresh = fork_ring_page(a, a.sums[0], i);
-    if ((unsigned)page >= (unsigned)a.n || (unsigned)fresh >= (unsigned)a.n) continue;
-    const int run = (len - last * a.ps) * a.row_pieces;   // pieces of a head's tokens, which lie side by side
+    const int4 c = a.copy[i];
+    if ((unsigned)c.x >= (unsigned)a.n || (unsigned)c.y >= (unsigned)a.n) continue;
+    const int run = c.z * a.row_pieces;   // pieces of a head's tokens, which lie side by side
     const int64_t all = (int64_t)a.H * run, head = (int64_t)a.ps * a.row_pieces, step = (int64_t)slices * kThreads;
-    const T* kf = static_cast<const T*>(a.kp) + page * a.page_stride;
-    const T* vf = static_cast<const T*>(a.vp) + page * a.page_stride;
-    T* kt = static_cast<T*>(a.kp) + fresh * a.page_stride;
-    T* vt = static_cast<T*>(a.vp) + fresh * a.page_stride;
+    const Divider by_run((uint32_t)run);
+    const bool small = all < 0x7fffffff;
+    const T* kf = static_cast<const T*>(a.kp) + c.x * a.page_stride;
+    const T* vf = static_cast<const T*>(a.vp) + c.x * a.page_stride;
+    T* kt = static_cast<T*>(a.kp) + c.y * a.page_stride;
+    T* vt = static_cast<T*>(a.vp) + c.y * a.page_stride;
     for (int64_t x0 = slice * kThreads + tid; x0 < all; x0 += 2 * step) {
       T k[2], v[2];
       int64_t at[2];
@@ -172,7 +270,7 @@ __global__ __launch_bounds__(kThreads) void fork_tables_kernel(const ForkArgs a,
         const int64_t x = x0 + u * step;
         at[u] = -1;
         if (x < all) {
-          const int h = (int)((uint64_t)x / (uint32_t)run);
+          const int h = small ? by_run.div((int)x) : (int)((uint64_t)x / (uint32_t)run);
           at[u] = h * head + (x - (int64_t)h * run);
           k[u] = kf[at[u]];
           v[u] = vf[at[u]];
@@ -187,25 +285,29 @@ __global__ __launch_bounds__(kThreads) void fork_tables_kernel(const ForkArgs a,
     }
   }
 }
+template <typename T>
+__global__ __launch_bounds__(kThreads) void fork_copy_kernel(const ForkArgs a) { fork_copy<T>(a, blockIdx.x, gridDim.x); }
 
-__global__ __launch_bounds__(kForkRows) void fork_ring_kernel(const ForkArgs a) {
+template <typename T>
+__global__ __launch_bounds__(kThreads) void fork_ring_kernel(const ForkArgs a) {
   const int tid = threadIdx.x;
+  if ((int)blockIdx.x >= (int)gridDim.x - a.wgs) return fork_copy<T>(a, blockIdx.x - (gridDim.x - a.wgs), a.wgs);
   if (blockIdx.x > 0) {   // tables that are replaced in place
-    for (int b = blockIdx.x - 1; b < a.B; b += gridDim.x - 1) {
+    for (int b = blockIdx.x - 1; b < a.B; b += gridDim.x - a.wgs - 1) {
       const int now = a.src[b] >= 0 ? fork_pages_of(a, a.len[b]) : 0;
-      for (int j = tid; j < now; j += kForkRows) a.table_out[(size_t)b * a.max_pages + j] = a.staged[(size_t)b * a.max_pages + j];
+      for (int j = tid; j < now; j += kThreads) a.table_out[(size_t)b * a.max_pages + j] = a.staged[(size_t)b * a.max_pages + j];
     }
     return;
   }
-  __shared__ int part[kForkRows / kWave];
+  __shared__ int part[kThreads / kWave];
   const int first = a.sums[0], count = a.sums[1], taken = a.sums[2];
   const unsigned end = ((unsigned)first + (unsigned)count) % (unsigned)a.n;
   int before = 0;
-  for (int c = 0; c < a.words; c += kForkRows) {
+  for (int c = 0; c < a.words; c += kThreads) {
     uint32_t free = c + tid < a.words ? a.had[c + tid] & ~a.has[c + tid] : 0;
     int all;
     const int n = __popc(free);
-    unsigned at = (unsigned)(before + fork_sum<kForkRows>(n, all, part) - n);
+    unsigned at = (unsigned)(before + fork_sum<kThreads>(n, all, part) - n);
     while (free) {
       const int bit = __ffs(free) - 1;
       free &= free - 1;
@@ -214,7 +316,7 @@ __global__ __launch_bounds__(kForkRows) void fork_ring_kernel(const ForkArgs a) 
     }
     before += all;
   }
-  for (int b = tid; b < a.B; b += kForkRows) a.seq_out[b] = a.len[b];
+  for (int b = tid; b < a.B; b += kThreads) a.seq_out[b] = a.len[b];
   if (tid == 0) {
     a.state_out[0] = (int)(((unsigned)first + (unsigned)taken) % (unsigned)a.n);
     a.state_out[1] = (int)min((unsigned)a.n, (unsigned)(count - taken) + (unsigned)before);
@@ -223,7 +325,29 @@ __global__ __launch_bounds__(kForkRows) void fork_ring_kernel(const ForkArgs a) 
 
 static size_t fork_words(int32_t n) { return ((size_t)n + 31) / 32; }
 size_t fork_workspace_bytes(int32_t B, int32_t max_pages, int32_t n_pages) {
-  return 4 * (4 + 2 * fork_words(n_pages) + 5 * (size_t)B + (size_t)B * max_pages);
+  return 16 * (size_t)B + 4 * (4 + 2 * fork_words(n_pages) + 4 * (size_t)B + (size_t)B * max_pages);
+}
+
+template <typename T>
+static hipError_t launch_fork_as(const ForkArgs& a, hipStream_t stream) {
+  const int entries = a.B * a.max_pages;
+  if (a.B <= kForkRows && entries <= kForkSmallEntries && a.words <= kForkSmallWords) {
+    hipLaunchKernelGGL(fork_small_kernel, dim3(1), dim3(kForkRows), 0, stream, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((fork_copy_kernel<T>), dim3((unsigned)a.wgs), dim3(kThreads), 0, stream, a);
+    return hipGetLastError();
+  }
+  const int clear = (int)((2LL * a.words + kForkRows - 1) / kForkRows);
+  hipLaunchKernelGGL(fork_rows_kernel, dim3((unsigned)(1 + (clear < 1024 ? clear : 1024))), dim3(kForkRows), 0, stream, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(fork_tables_kernel, dim3((unsigned)(a.B * a.segs)), dim3(kThreads), 0, stream, a);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int back = a.table_out == a.table ? (a.B < 1024 ? a.B : 1024) : 0;
+  hipLaunchKernelGGL((fork_ring_kernel<T>), dim3((unsigned)(1 + back + a.wgs)), dim3(kThreads), 0, stream, a);
+  return hipGetLastError();
 }
 
 hipError_t launch_fork(const ForkLaunch& p, hipStream_t stream) {
@@ -231,15 +355,15 @@ hipError_t launch_fork(const ForkLaunch& p, hipStream_t stream) {
   a.from = p.from; a.seq_len = p.seq_len; a.state = p.free_state; a.table = p.page_table;
   a.ring = p.free_pages; a.table_out = p.page_table_out; a.seq_out = p.seq_len_out; a.state_out = p.free_state_out;
   a.kp = p.k_pages; a.vp = p.v_pages;
-  a.B = p.B; a.H = p.H; a.D = p.D; a.max_pages = p.max_pages; a.n = p.n_pages; a.ps = p.page_size;
+  a.B = p.B; a.H = p.H; a.max_pages = p.max_pages; a.n = p.n_pages; a.ps = p.page_size;
   a.sinks = p.sinks; a.window = p.window;
   a.words = (int)fork_words(p.n_pages);
-  int32_t* ws = static_cast<int32_t*>(p.ws);
-  a.sums = ws;
-  a.had = reinterpret_cast<uint32_t*>(ws + 4);
+  a.copy = static_cast<int4*>(p.ws);
+  a.sums = static_cast<int32_t*>(p.ws) + 4 * (size_t)p.B;
+  a.had = reinterpret_cast<uint32_t*>(a.sums + 4);
   a.has = a.had + a.words;
-  a.src = ws + 4 + 2 * (size_t)a.words;
-  a.len = a.src + p.B; a.take = a.len + p.B; a.keeper = a.take + p.B; a.list = a.keeper + p.B; a.staged = a.list + p.B;
+  a.src = a.sums + 4 + 2 * (size_t)a.words;
+  a.len = a.src + p.B; a.take = a.len + p.B; a.keeper = a.take + p.B; a.staged = a.keeper + p.B;
   a.segs = (p.max_pages + kForkEntries - 1) / kForkEntries;
   const int row_bytes = p.D * p.elt;
   const bool wide = row_bytes % 16 == 0;
@@ -247,20 +371,11 @@ hipError_t launch_fork(const ForkLaunch& p, hipStream_t stream) {
   a.page_stride = p.page_stride * p.elt / (wide ? 16 : 4);
   a.by_ps = Divider((uint32_t)p.page_size);
   a.by_segs = Divider((uint32_t)a.segs);
-  const int clear = (int)((2LL * a.words + kForkRows - 1) / kForkRows);
-  hipLaunchKernelGGL(fork_rows_kernel, dim3((unsigned)(1 + (clear < 1024 ? clear : 1024))), dim3(kForkRows), 0, stream, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  const int tables = p.B * a.segs, copies = 2048;
-  if (wide)
-    hipLaunchKernelGGL((fork_tables_kernel<u32x4>), dim3((unsigned)(tables + copies)), dim3(kThreads), 0, stream, a, tables);
-  else
-    hipLaunchKernelGGL((fork_tables_kernel<uint32_t>), dim3((unsigned)(tables + copies)), dim3(kThreads), 0, stream, a, tables);
-  e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  const int back = p.page_table_out == p.page_table ? (p.B < 1024 ? p.B : 1024) : 0;
-  hipLaunchKernelGGL(fork_ring_kernel, dim3((unsigned)(1 + back)), dim3(kForkRows), 0, stream, a);
-  return hipGetLastError();
+  a.by_max_pages = Divider((uint32_t)p.max_pages);
+  // workgroups that copy: as many as 1,024 pieces of the most that there can be make, eight a compute unit
+  const double most = (double)p.B * (((double)p.H * p.page_size * a.row_pieces + 1023) / 1024);
+  a.wgs = most < 2048 ? (int)most + 1 : 2048;
+  return wide ? launch_fork_as<u32x4>(a, stream) : launch_fork_as<uint32_t>(a, stream);
 }
 
 }  // namespace ac

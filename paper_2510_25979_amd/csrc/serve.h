@@ -14,7 +14,7 @@ namespace ac {
 struct Divider {
   uint32_t d, m, s;
   Divider() = default;
-  explicit Divider(uint32_t by) : d(by), s(by > 1 ? 32 - __builtin_clz(by - 1) : 0) {
+  __host__ __device__ explicit Divider(uint32_t by) : d(by), s(by > 1 ? 32 - __builtin_clz(by - 1) : 0) {
     m = (uint32_t)((((1ull << s) - d) << 32) / d + 1);
   }
   __device__ __forceinline__ int div(int n) const {

@@ -40,7 +40,36 @@ struct SharedArgs {
   Divider by_g;
 };
 
-// Records: own whole results [B Hq], prefixes' [B Hq], of runs [2 waves][16], of workgroups [2 wgs][128].
+// A wave's work on a block for two blocks of 16 rows, which share the keys' way from memory (the second may be empty): a prefix of eight requests of
+// four heads is read once and not twice.
+template <int D_>
+struct SharedBf16 : DecodeBf16<D_> {
+  typedef DecodeBf16<D_> One;
+  static constexpr int RB = 2;
+  f32x4 acc1[One::NP];
+  float m1, l1;
+  using One::One;
+  __device__ __forceinline__ void reset() {
+    One::reset();
+#pragma unroll
+    for (int n = 0; n < One::NP; ++n) acc1[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    m1 = -INFINITY;
+    l1 = 0.f;
+  }
+  __device__ __forceinline__ void add1(typename One::Scores& s, float scale_log2e) { One::add(s, scale_log2e, acc1, m1, l1); }
+  __device__ __forceinline__ f32x4 piece1(int n) const { return acc1[n]; }
+};
+template <int DB, bool FULL>
+struct SharedF32 : DecodeF32<DB, FULL> {
+  typedef DecodeF32<DB, FULL> One;
+  static constexpr int RB = 1;
+  float m1 = 0.f, l1 = 0.f;
+  using One::One;
+  __device__ __forceinline__ void add1(typename One::Scores&, float) {}
+  __device__ __forceinline__ f32x4 piece1(int) const { return f32x4{0.f, 0.f, 0.f, 0.f}; }
+};
+
+// Records: own whole results [B Hq], prefixes' [B Hq], of runs [2 waves][unit], of workgroups [2 wgs][128].
 __device__ __forceinline__ size_t shared_rows(const SharedArgs& a) { return (size_t)a.d.B * a.d.Hkv * a.g; }
 
 constexpr int kPlanThreads = 1024;
@@ -67,80 +96,108 @@ __device__ __forceinline__ int shared_scan(int x, int& all, int* part, Op op, in
   return op(x, before);
 }
 
-// What this launch has written, past the first-level cache.
-__device__ __forceinline__ int shared_peek(const int32_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+// Groups of the plan: in LDS up to kPlanThreads of them, otherwise in the workspace, where what this launch has written is read past the
+// first-level cache.
+constexpr int kPlanGroups = kPlanThreads;
+template <bool LDS>
+__device__ __forceinline__ int shared_peek(const int* p) {
+  return LDS ? *p : __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
 
-template <int BK>
+// Bound by latency: lengths and groups -> who shares -> sums -> list.  64 requests 14.3 us with the groups in the workspace, LDS_US so.
+template <int BK, int UNIT, bool LDS>   // keys of a block, rows of a unit
 __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedArgs a) {
   __shared__ int part[kPlanThreads / kWave], part1[kPlanThreads / kWave];
+  __shared__ int s_first[LDS ? kPlanGroups + 1 : 1], s_leader[LDS ? kPlanGroups : 1], s_count[LDS ? kPlanGroups : 1], s_len[LDS ? kPlanGroups : 1];
   const int tid = threadIdx.x, B = a.d.B, G = a.G, cap = a.d.Sk;
+  int* first = LDS ? s_first : a.first;
+  int* leader = LDS ? s_leader : a.leader;
+  int* count = LDS ? s_count : a.count;
   auto add = [](int x, int y) { return x + y; };
   auto top = [](int x, int y) { return max(x, y); };
+  auto tokens = [&](int b) { return min(max(a.d.len[b], 0), cap); };
+  int mine = tid < B ? tokens(tid) : 0;   // of the first 1,024 requests: asked for at once
   // where groups begin: in order, whatever is given
   int before = 0;
   for (int c = 0; c <= G; c += kPlanThreads) {
     const int i = c + tid;
+    if (LDS && i < G) s_len[i] = min(max(a.share_len[i], 0), cap);
     int all;
     const int f = shared_scan(i <= G ? min(max(a.share_first[i], 0), B) : 0, all, part, top, 0);
-    if (i <= G) a.first[i] = max(before, f);
+    if (i <= G) first[i] = max(before, f);
     if (i < G) {
-      a.leader[i] = B;
-      a.count[i] = 0;
+      leader[i] = B;
+      count[i] = 0;
     }
     before = max(before, all);
   }
-  __threadfence();
+  if (!LDS) __threadfence();
   __syncthreads();
+  auto prefix = [&](int q) { return LDS ? s_len[q] : min(max(a.share_len[q], 0), cap); };
   auto group_of = [&](int b) {   // the last group that begins at b or before it, if b is in it
     int lo = -1, hi = G;         // first[lo] <= b < first[hi], but for the ends
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (shared_peek(a.first + mid) <= b) lo = mid;
+      if (shared_peek<LDS>(first + mid) <= b) lo = mid;
       else hi = mid;
     }
-    return lo >= 0 && b < shared_peek(a.first + lo + 1) ? lo : -1;
+    return lo >= 0 && b < shared_peek<LDS>(first + lo + 1) ? lo : -1;
   };
-  auto tokens = [&](int b) { return min(max(a.d.len[b], 0), cap); };
-  auto prefix = [&](int q) { return min(max(a.share_len[q], 0), cap); };
+  int group = -1;   // of this thread's request among the first 1,024
   for (int b = tid; b < B; b += kPlanThreads) {
-    const int q = group_of(b);
-    a.item[G + b].group = q;
+    const int q = group_of(b), n = b == tid ? mine : tokens(b);
+    if (b == tid) group = q;
     if (q < 0) continue;
     const int P = prefix(q);
-    if (P > 0 && tokens(b) >= P) {   // shorter ones have their keys for themselves
-      atomicMin(&a.leader[q], b);
-      atomicAdd(&a.count[q], 1);
+    if (P > 0 && n >= P) {   // shorter ones have their keys for themselves
+      atomicMin(&leader[q], b);
+      atomicAdd(&count[q], 1);
     }
   }
-  __threadfence();
+  if (!LDS) __threadfence();
   __syncthreads();
+  // First the groups, then the requests: the same thread has a request here and above.
   int begun = 0, begun1 = 0;
-  for (int c = 0; c < G + B; c += kPlanThreads) {
+  for (int c = 0; c < G; c += kPlanThreads) {
     const int i = c + tid;
     SharedItem it = {0, 0, 0, 0, 0, 1, 0, 0};
     int cost = 0, cost1 = 0;
-    if (i < G) {
-      const int f = shared_peek(a.first + i), n = shared_peek(a.first + i + 1) - f;
-      if (shared_peek(a.count + i) > 1) {
-        it.keys = prefix(i);
-        it.row = shared_peek(a.leader + i);
-        it.b0 = f;
-        it.R = n * a.g;
-        it.group = it.R >= a.big_rows;
-        if (it.group) {
-          it.rbs = (it.R + kSharedRows - 1) / kSharedRows;
-          cost1 = a.d.Hkv * it.rbs * ((it.keys + kSharedChunk - 1) / kSharedChunk + kSharedUnitCost);
-        } else {
-          it.rbs = (it.R + kDecodeRows - 1) / kDecodeRows;
-          cost = a.d.Hkv * it.rbs * ((it.keys + BK - 1) / BK + kUnitCost);
-        }
+    if (i < G && shared_peek<LDS>(count + i) > 1) {
+      const int f = shared_peek<LDS>(first + i), n = shared_peek<LDS>(first + i + 1) - f;
+      it.keys = prefix(i);
+      it.row = shared_peek<LDS>(leader + i);
+      it.b0 = f;
+      it.R = n * a.g;
+      it.group = it.R >= a.big_rows;
+      if (it.group) {
+        it.rbs = (it.R + kSharedRows - 1) / kSharedRows;
+        cost1 = a.d.Hkv * it.rbs * ((it.keys + kSharedChunk - 1) / kSharedChunk + kSharedUnitCost);
+      } else {
+        it.rbs = (it.R + UNIT - 1) / UNIT;
+        cost = a.d.Hkv * it.rbs * ((it.keys + BK - 1) / BK + kUnitCost);
       }
-    } else if (i < G + B) {
-      const int b = i - G, q = shared_peek(&a.item[i].group), n = tokens(b);
+    }
+    int all, all1;
+    const int upto = begun + shared_scan(cost, all, part, add, 0), upto1 = begun1 + shared_scan(cost1, all1, part1, add, 0);
+    if (i < G) {
+      it.start = it.group ? upto1 - cost1 : upto - cost;
+      a.item[i] = it;
+      a.start[i] = upto - cost;
+      a.start1[i] = upto1 - cost1;
+    }
+    begun += all;
+    begun1 += all1;
+  }
+  for (int c = 0; c < B; c += kPlanThreads) {
+    const int b = c + tid;
+    SharedItem it = {0, 0, 0, 0, 0, 1, 0, -1};
+    int cost = 0;
+    if (b < B) {
+      const int q = c == 0 ? group : group_of(b), n = c == 0 ? mine : tokens(b);
       it.group = q;
       if (q >= 0) {
         const int P = prefix(q);
-        if (n >= P && shared_peek(a.count + q) > 1) it.key0 = P;
+        if (n >= P && shared_peek<LDS>(count + q) > 1) it.key0 = P;
       }
       it.keys = n - it.key0;
       it.row = it.b0 = b;
@@ -148,16 +205,14 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedA
       it.rbs = a.own_rbs;
       if (it.keys > 0) cost = a.d.Hkv * it.rbs * ((it.keys + BK - 1) / BK + kUnitCost);
     }
-    int all, all1;
-    const int upto = begun + shared_scan(cost, all, part, add, 0), upto1 = begun1 + shared_scan(cost1, all1, part1, add, 0);
-    if (i < G + B) {
-      it.start = i < G && it.group ? upto1 - cost1 : upto - cost;
-      a.item[i] = it;
-      a.start[i] = upto - cost;
-      if (i < G) a.start1[i] = upto1 - cost1;
+    int all;
+    const int upto = begun + shared_scan(cost, all, part, add, 0);
+    if (b < B) {
+      it.start = upto - cost;
+      a.item[G + b] = it;
+      a.start[G + b] = upto - cost;
     }
     begun += all;
-    begun1 += all1;
   }
   if (tid == 0) {
     a.sums[0] = begun;
@@ -200,16 +255,15 @@ struct SharedBlock {
 };
 
 template <class Core>
-__global__ __launch_bounds__(kThreads, Core::WGS) void shared_run_kernel(const SharedArgs a) {
+__device__ __forceinline__ void shared_run(const SharedArgs& a, unsigned char* lds) {   // lds: the wave's Core::LDS bytes
   typedef typename Core::Elt Elt;
-  constexpr int BK = Core::BK, KPL = Core::KPL;
-  __shared__ __attribute__((aligned(16))) unsigned char lds[Core::LDS ? 4 * Core::LDS : 16];
+  constexpr int BK = Core::BK, KPL = Core::KPL, RB = Core::RB, UNIT = RB * kDecodeRows;
   const DecodeArgs& d = a.d;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int run = blockIdx.x * 4 + wave, n_items = a.G + d.B;
   const int total = a.sums[0], per = run_length(total, d.waves);
   if (run >= d.waves || (int64_t)run * per >= total) return;
-  Core core(d, lds + wave * Core::LDS, lane);
+  Core core(d, lds, lane);
   const int D = core.dim();
 
   auto item = [&](SharedBlock& s, int i) {
@@ -269,16 +323,18 @@ __global__ __launch_bounds__(kThreads, Core::WGS) void shared_run_kernel(const S
   };
   auto head_of = [&](const SharedBlock& s) { return s.it.rbs == 1 ? s.unit : s.unit / s.it.rbs; };
   auto base_of = [&](const void* p, const SharedBlock& s) { return static_cast<const Elt*>(p) + (size_t)head_of(s) * d.head_stride; };
-  auto load_q = [&](typename Core::Query& q, const SharedBlock& s) {
-    const int hk = head_of(s), r = kDecodeRows * (s.unit - hk * s.it.rbs) + core.i;
-    core.load_row(q, static_cast<const Elt*>(d.Q) + shared_row(a, s.it.b0, hk, min(r, s.it.R - 1)) * D);
+  auto row_of = [&](const SharedBlock& s) { return UNIT * (s.unit - head_of(s) * s.it.rbs) + core.i; };   // the lane's, of the item's rows
+  auto both = [&](const SharedBlock& s) { return RB == 2 && UNIT * (s.unit - head_of(s) * s.it.rbs) + kDecodeRows < s.it.R; };   // uniform
+  auto load_q = [&](typename Core::Query& q, const SharedBlock& s, int x) {   // of row block x
+    core.load_row(q, static_cast<const Elt*>(d.Q) + shared_row(a, s.it.b0, head_of(s), min(row_of(s) + kDecodeRows * x, s.it.R - 1)) * D);
   };
 
-  typename Core::Query q, q_then;
+  typename Core::Query q, q1, q_then;   // (q1 is not asked for ahead: registers)
   int page[KPL];
   int64_t at[KPL], at_then[KPL];
   ask(now, page);
-  load_q(q, now);
+  load_q(q, now, 0);
+  if (both(now)) load_q(q1, now, 1);
   then = now;
   bool more = next(then);
   place(now, page, at);
@@ -288,45 +344,53 @@ __global__ __launch_bounds__(kThreads, Core::WGS) void shared_run_kernel(const S
   core.reset();
   int begin = now.blk;
   while (true) {
-    typename Core::Scores s;
+    typename Core::Scores s, s1;
+    const bool two = both(now);
     core.scores(s, q);
+    if (RB == 2 && two) core.scores(s1, q1);
     const bool last = now.blk + 1 == now.nb;   // of its unit
     later = then;
     bool more_later = false;
     if (more) {
       place(then, page, at_then);
-      if (last) load_q(q_then, then);
+      if (last) load_q(q_then, then, 0);
       core.load_k(base_of(d.K, then), at_then);
       more_later = next(later);
       if (more_later) ask(later, page);
     }
     core.hide(s, at);
+    if (RB == 2 && two) core.hide(s1, at);
     core.stage_v();
     if (Core::LDS && more) core.load_v(base_of(d.V, then), at_then);
     if (Core::LDS) wave_fence();
     core.add(s, d.scale_log2e);
+    if (RB == 2 && two) core.add1(s1, d.scale_log2e);
     if (Core::LDS) wave_fence();   // the tile is read before the next block's rows are written
     if (!Core::LDS && more) core.load_v(base_of(d.V, then), at_then);
     if (last || !more) {
-      const float sum = sum_of_four(core.l);
-      const int hk = head_of(now), r = kDecodeRows * (now.unit - hk * now.it.rbs) + core.i;
-      if (r < now.it.R) {
-        const size_t rows = shared_rows(a);
+      const int hk = head_of(now);
+      const size_t rows = shared_rows(a);
+#pragma unroll
+      for (int x = 0; x < RB; ++x) {
+        const float sum = sum_of_four(x ? core.l1 : core.l);
+        const int r = row_of(now) + kDecodeRows * x;
+        if (r >= now.it.R) continue;
         const size_t rec = begin == 0 && last ? (now.i < a.G ? rows : 0) + shared_row(a, now.it.b0, hk, r)
-                                              : 2 * rows + (size_t)(2 * run + (begin == 0)) * kDecodeRows + core.i;   // as partial_of has it
+                                              : 2 * rows + (size_t)(2 * run + (begin == 0)) * UNIT + kDecodeRows * x + core.i;   // as partial_of has it
 #pragma unroll
         for (int n = 0; n < Core::NP; ++n) {
           const int c = core.col(n);
-          store_partial(a.part + rec * D + c, decode_piece(core, n), c, D);
+          store_partial(a.part + rec * D + c, x ? core.piece1(n) : decode_piece(static_cast<const typename Core::One&>(core), n), c, D);
         }
         if (core.kq == 0) {
-          a.stat[2 * rec] = core.m;
+          a.stat[2 * rec] = x ? core.m1 : core.m;
           a.stat[2 * rec + 1] = sum;
         }
       }
       if (!more) break;
       core.reset();
       q = q_then;
+      if (both(then)) load_q(q1, then, 1);
       begin = 0;
     }
     now = then;
@@ -339,12 +403,8 @@ __global__ __launch_bounds__(kThreads, Core::WGS) void shared_run_kernel(const S
 
 // ---- prefixes of many rows
 template <int D>
-__global__ __launch_bounds__(kThreads, 2) void shared_prefix_kernel(const SharedArgs a) {
-  constexpr int PPR = D / 8, NCOPY = kSharedChunk * PPR / kWave / 4;
-  __shared__ __attribute__((aligned(16))) bf16_t kb0[kSharedChunk * D];
-  __shared__ __attribute__((aligned(16))) bf16_t vb0[kSharedChunk * D];
-  __shared__ __attribute__((aligned(16))) bf16_t kb1[kSharedChunk * D];
-  __shared__ __attribute__((aligned(16))) bf16_t vb1[kSharedChunk * D];
+__device__ __forceinline__ void shared_prefix(const SharedArgs& a, bf16_t* kb0, bf16_t* vb0, bf16_t* kb1, bf16_t* vb1) {
+  constexpr int PPR = D / 8, NCOPY = kSharedChunk * PPR / kWave / 4, UNIT = SharedBf16<D>::RB * kDecodeRows;
   const DecodeArgs& d = a.d;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -530,7 +590,7 @@ __global__ __launch_bounds__(kThreads, 2) void shared_prefix_kernel(const Shared
     if (r < it.R) {
       const size_t rows = shared_rows(a);
       const size_t rec = c0 == 0 && c1 == nc ? rows + shared_row(a, it.b0, hk, r)
-                                             : 2 * rows + (size_t)2 * d.waves * kDecodeRows +
+                                             : 2 * rows + (size_t)2 * d.waves * UNIT +
                                                    (size_t)(2 * blockIdx.x + (c0 == 0)) * kSharedRows + kRowsPerWave * wave + il;
       float* to = a.part + rec * D + 4 * kh;
 #pragma unroll
@@ -547,12 +607,31 @@ __global__ __launch_bounds__(kThreads, 2) void shared_prefix_kernel(const Shared
   }
 }
 
+template <class Core>
+__global__ __launch_bounds__(kThreads, Core::WGS) void shared_run_kernel(const SharedArgs a) {
+  __shared__ __attribute__((aligned(16))) unsigned char lds[Core::LDS ? 4 * Core::LDS : 16];
+  shared_run<Core>(a, lds + (Core::LDS ? (threadIdx.x >> 6) * Core::LDS : 0));
+}
+// Both in one launch: a workgroup has its share of the one and of the other.
+template <int D>
+__global__ __launch_bounds__(kThreads, 2) void shared_both_kernel(const SharedArgs a) {
+  __shared__ __attribute__((aligned(16))) bf16_t kb0[kSharedChunk * D];
+  __shared__ __attribute__((aligned(16))) bf16_t vb0[kSharedChunk * D];
+  __shared__ __attribute__((aligned(16))) bf16_t kb1[kSharedChunk * D];
+  __shared__ __attribute__((aligned(16))) bf16_t vb1[kSharedChunk * D];
+  static_assert(DecodeBf16<D>::LDS <= (int)sizeof(kb0), "a wave's V tile in a stage");
+  shared_prefix<D>(a, kb0, vb0, kb1, vb1);
+  __syncthreads();
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  shared_run<SharedBf16<D>>(a, reinterpret_cast<unsigned char*>(wave == 0 ? kb0 : wave == 1 ? vb0 : wave == 2 ? kb1 : vb1));
+}
+
 // ---- parts of an output row
 // NW waves add up one row (or, NW 1, a wave each): a lane holds four columns, G lanes a partial result; a wave knows the weights of 64 at once.
 template <bool F32, int G, int NW>
 __global__ __launch_bounds__(NW == 1 ? kThreads : NW * kWave) void shared_join_kernel(const SharedArgs a) {
   typedef typename std::conditional<F32, float, bf16_t>::type Elt;
-  constexpr int BK = F32 ? 16 : 32, SUB = kWave / G;
+  constexpr int BK = F32 ? 16 : 32, UNIT = F32 ? 16 : 32, SUB = kWave / G;
   __shared__ __attribute__((aligned(16))) f32x4 sums[NW][G];
   __shared__ float ms[NW], ls[NW];
   const DecodeArgs& d = a.d;
@@ -571,14 +650,14 @@ __global__ __launch_bounds__(NW == 1 ? kThreads : NW * kWave) void shared_join_k
   };
   auto parts_of = [&](const SharedItem& it, int r, bool big, size_t whole) {
     Parts p = {0, 0, 1, 0, whole, 0};
-    const int br = big ? kSharedRows : kDecodeRows, blocks = big ? (it.keys + kSharedChunk - 1) / kSharedChunk : (it.keys + BK - 1) / BK;
+    const int br = big ? kSharedRows : UNIT, blocks = big ? (it.keys + kSharedChunk - 1) / kSharedChunk : (it.keys + BK - 1) / BK;
     if (blocks == 0) return p;
     p.per = big ? per1 : per;
     p.from = it.start + (hk * it.rbs + r / br) * (blocks + (big ? kSharedUnitCost : kUnitCost));
     p.w0 = p.from / p.per;
     p.n = (p.from + blocks - 1) / p.per - p.w0 + 1;
     if (p.n > 1) {
-      p.base = 2 * rows + (big ? (size_t)2 * d.waves * kDecodeRows : 0) + r % br;
+      p.base = 2 * rows + (big ? (size_t)2 * d.waves * UNIT : 0) + r % br;
       p.stride = br;
     }
     return p;
@@ -675,9 +754,9 @@ __global__ __launch_bounds__(NW == 1 ? kThreads : NW * kWave) void shared_join_k
 static size_t shared_ints(int64_t B, int64_t G) {   // sums, first, leader, count, start, start1, items; in whole pieces of 16 bytes
   return (size_t)((4 + (G + 1) + G + G + (G + B) + G + 3) / 4 * 4 + (G + B) * (int64_t)(sizeof(SharedItem) / 4));
 }
-static bool shared_big(int64_t B, int32_t g, int32_t D) { return (D == 64 || D == 128) && B * g > 16; }   // some group may have many rows
+static bool shared_big(int64_t B, int32_t g, int32_t D) { return (D == 64 || D == 128) && B * g > 2 * kDecodeRows; }   // some group may have many rows
 static size_t shared_records(int64_t B, int64_t Hq, int32_t g, int32_t D) {
-  return (size_t)(2 * B * Hq) + (size_t)2 * kDecodeWaves * kDecodeRows + (shared_big(B, g, D) ? (size_t)2 * kSharedWgs * kSharedRows : 0);
+  return (size_t)(2 * B * Hq) + (size_t)2 * kDecodeWaves * 2 * kDecodeRows + (shared_big(B, g, D) ? (size_t)2 * kSharedWgs * kSharedRows : 0);
 }
 size_t shared_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t G) {
   return 4 * shared_ints(B, G) + shared_records(B, Hq, Hq / Hkv, D) * (size_t)(D + 2) * sizeof(float);
@@ -691,18 +770,20 @@ bool shared_fits(int64_t B, int64_t Hkv, int64_t g, int64_t G, int64_t keys) {
 template <class Core>
 static hipError_t launch_shared_as(SharedArgs& a, bool big, hipStream_t stream) {
   constexpr bool F32 = Core::BK == 16;
-  constexpr int G = Core::NP * 4;
+  constexpr int G = Core::NP * 4, UNIT = Core::RB * kDecodeRows;
   a.d.waves = 4 * 256 * Core::WGS;
-  hipLaunchKernelGGL((shared_plan_kernel<Core::BK>), dim3(1), dim3(kPlanThreads), 0, stream, a);
+  a.own_rbs = (a.g + UNIT - 1) / UNIT;
+  if (a.G <= kPlanGroups - 1) hipLaunchKernelGGL((shared_plan_kernel<Core::BK, UNIT, true>), dim3(1), dim3(kPlanThreads), 0, stream, a);
+  else hipLaunchKernelGGL((shared_plan_kernel<Core::BK, UNIT, false>), dim3(1), dim3(kPlanThreads), 0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if constexpr (!F32)
-    if (big) {
-      hipLaunchKernelGGL((shared_prefix_kernel<Core::NP * 16>), dim3((unsigned)a.wgs), dim3(kThreads), 0, stream, a);
-      e = hipGetLastError();
-      if (e != hipSuccess) return e;
-    }
-  hipLaunchKernelGGL((shared_run_kernel<Core>), dim3((unsigned)(a.d.waves / 4)), dim3(kThreads), 0, stream, a);
+  if constexpr (!F32) {
+    static_assert(Core::WGS == 2, "a workgroup has a share of both");
+    if (big) hipLaunchKernelGGL((shared_both_kernel<Core::NP * 16>), dim3((unsigned)a.wgs), dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL((shared_run_kernel<Core>), dim3((unsigned)(a.d.waves / 4)), dim3(kThreads), 0, stream, a);
+  } else {
+    hipLaunchKernelGGL((shared_run_kernel<Core>), dim3((unsigned)(a.d.waves / 4)), dim3(kThreads), 0, stream, a);
+  }
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int64_t rows = (int64_t)a.d.B * a.d.Hkv * a.g;
@@ -715,7 +796,6 @@ hipError_t launch_shared(const SharedLaunch& p, hipStream_t stream) {
   SharedArgs a;
   a.d = decode_args(p.d);
   a.g = p.d.R; a.G = p.G;
-  a.own_rbs = a.d.rbs;
   a.share_first = p.share_first; a.share_len = p.share_len;
   a.by_g = Divider((uint32_t)a.g);
   const bool big = !p.d.is_f32 && shared_big(p.d.B, a.g, p.d.D);
@@ -731,12 +811,12 @@ hipError_t launch_shared(const SharedLaunch& p, hipStream_t stream) {
   a.part = reinterpret_cast<float*>(ws + ints);
   const size_t records = shared_records(B, (int64_t)p.d.Hkv * a.g, a.g, p.d.D);
   a.stat = a.part + records * p.d.D;
-  if (!p.d.is_f32) return p.d.D == 64 ? launch_shared_as<DecodeBf16<64>>(a, big, stream) : launch_shared_as<DecodeBf16<128>>(a, big, stream);
-  if (p.d.D == 64) return launch_shared_as<DecodeF32<1, true>>(a, big, stream);
-  if (p.d.D == 128) return launch_shared_as<DecodeF32<2, true>>(a, big, stream);
-  if (p.d.D < 64) return launch_shared_as<DecodeF32<1, false>>(a, big, stream);
-  if (p.d.D < 128) return launch_shared_as<DecodeF32<2, false>>(a, big, stream);
-  return launch_shared_as<DecodeF32<4, false>>(a, big, stream);
+  if (!p.d.is_f32) return p.d.D == 64 ? launch_shared_as<SharedBf16<64>>(a, big, stream) : launch_shared_as<SharedBf16<128>>(a, big, stream);
+  if (p.d.D == 64) return launch_shared_as<SharedF32<1, true>>(a, big, stream);
+  if (p.d.D == 128) return launch_shared_as<SharedF32<2, true>>(a, big, stream);
+  if (p.d.D < 64) return launch_shared_as<SharedF32<1, false>>(a, big, stream);
+  if (p.d.D < 128) return launch_shared_as<SharedF32<2, false>>(a, big, stream);
+  return launch_shared_as<SharedF32<4, false>>(a, big, stream);
 }
 
 }  // namespace ac
