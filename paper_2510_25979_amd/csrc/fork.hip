@@ -190,8 +190,8 @@ __global__ __launch_bounds__(kForkRows) void fork_small_kernel(const ForkArgs a)
   __syncthreads();
   const int entries = a.B * a.max_pages;
   int page[N];
-  auto mark = [&](uint32_t* bits, int q) {
-    if ((unsigned)q < (unsigned)a.n) atomicOr(&bits[q >> 5], 1u << (q & 31));
+  auto mark = [&](uint32_t* bits, int q) {   // (rows share pages: most bits are there already, and atomics on one word take turns)
+    if ((unsigned)q < (unsigned)a.n && !((bits[q >> 5] >> (q & 31)) & 1)) atomicOr(&bits[q >> 5], 1u << (q & 31));
   };
 #pragma unroll
   for (int i = 0; i < N; ++i) {   // (what no row has stays: -2)

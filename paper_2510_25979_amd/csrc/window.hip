@@ -238,9 +238,10 @@ __global__ __launch_bounds__(kThreads, 2) void window_bf16_kernel(const WindowAr
     if (!live) return;
     const int k0 = c * kWindowChunk;
     const WindowBlock b0 = window_block<32, 32>(a, t0, k0, keys), b1 = window_block<32, 32>(a, t0, k0 + 32, keys);
-    if (b0 == kEvery && b1 == kEvery) {
+    if (b0 != kNone && b1 != kNone) {
       // the scores of block 1 are requested before the exponentials of block 0, the second product of block 0 before those of block 1
       f32x16 s0 = qk(kb, 0);
+      if (b0 == kSome) hide(s0, k0);
       float cand = fmaxf(m_run, row_max(s0) * scale_log2e);
       if (__any(cand > m_run + kWindowSlack)) {
         rescale(cand);
@@ -251,6 +252,7 @@ __global__ __launch_bounds__(kThreads, 2) void window_bf16_kernel(const WindowAr
       float sum = 0.f, sum1 = 0.f, m1 = m_run;
       weights(s0, m_run, p0, sum);
       l_run += sum;
+      if (b1 == kSome) hide(s1, k0 + 32);
       cand = fmaxf(m_run, row_max(s1) * scale_log2e);
       const bool moved = __any(cand > m_run + kWindowSlack);
       if (moved) m1 = cand;
@@ -382,12 +384,13 @@ __global__ __launch_bounds__(kThreads, DB <= 2 ? 2 : 1) void window_f32_kernel(c
       ks.load(K, KC * chunks.at(n + 1), keys, D, tid);
       vs.load(V, KC * chunks.at(n + 1), keys, D, tid);
     }
-    const WindowBlock bl = window_block<kF32Rows, KC>(a, t0, j0, keys);
-    if (!live || bl == kNone) continue;
-    f32x4 s[NB];
+    if (!live) continue;
 #pragma unroll
     for (int bk = 0; bk < NB; ++bk) {
-      s[bk] = f32x4{0.f, 0.f, 0.f, 0.f};
+      const int k0 = j0 + kF32Rows * bk;
+      const WindowBlock bl = window_block<kF32Rows, kF32Rows>(a, t0, k0, keys);
+      if (bl == kNone) continue;   // uniform
+      f32x4 s = {0.f, 0.f, 0.f, 0.f};
       const float* row = kl + (kF32Rows * bk + i) * Stage::LD + 4 * kq;
       f32x4 k = *reinterpret_cast<const f32x4*>(row);
 #pragma unroll
@@ -395,40 +398,31 @@ __global__ __launch_bounds__(kThreads, DB <= 2 ? 2 : 1) void window_f32_kernel(c
         if (COLS == kAllCols || 16 * kk < D) {   // uniform
           const f32x4 next = *reinterpret_cast<const f32x4*>(row + 16 * ((kk + 1) & (4 * DB - 1)));
 #pragma unroll
-          for (int x = 0; x < 4; ++x) s[bk] = mfma_f32(k[x], q[kk][x], s[bk]);
+          for (int x = 0; x < 4; ++x) s = mfma_f32(k[x], q[kk][x], s);
           k = next;
           __builtin_amdgcn_sched_barrier(0);
         }
-    }
-    if (bl == kSome) {
-#pragma unroll
-      for (int bk = 0; bk < NB; ++bk)
+      if (bl == kSome) {
 #pragma unroll
         for (int x = 0; x < 4; ++x)
-          if (window_hides(a, t0 + i, j0 + kF32Rows * bk + 4 * kq + x, keys)) s[bk][x] = -INFINITY;
-    }
-    float mx = s[0][0];
+          if (window_hides(a, t0 + i, k0 + 4 * kq + x, keys)) s[x] = -INFINITY;
+      }
+      float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+      mx = fmaxf(mx, __shfl_xor(mx, 16));
+      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      const float m_new = fmaxf(m, mx * a.scale_log2e);
+      if (__any(m_new > m)) {
+        const float alpha = m_new > m ? __builtin_amdgcn_exp2f(m - m_new) : 1.f;
+        l *= alpha;
 #pragma unroll
-    for (int bk = 0; bk < NB; ++bk)
-#pragma unroll
-      for (int x = 0; x < 4; ++x) mx = fmaxf(mx, s[bk][x]);
-    mx = fmaxf(mx, __shfl_xor(mx, 16));
-    mx = fmaxf(mx, __shfl_xor(mx, 32));
-    const float m_new = fmaxf(m, mx * a.scale_log2e);
-    if (__any(m_new > m)) {
-      const float alpha = m_new > m ? __builtin_amdgcn_exp2f(m - m_new) : 1.f;
-      l *= alpha;
-#pragma unroll
-      for (int x = 0; x < 4 * DB; ++x) acc[x] *= alpha;
-      m = m_new;
-    }
-    const float ref = m == -INFINITY ? 0.f : m;   // no finite score so far: all weights are zero
-#pragma unroll
-    for (int bk = 0; bk < NB; ++bk) {
+        for (int x = 0; x < 4 * DB; ++x) acc[x] *= alpha;
+        m = m_new;
+      }
+      const float ref = m == -INFINITY ? 0.f : m;   // no finite score so far: all weights are zero
       f32x4 p;
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
-        p[x] = __builtin_amdgcn_exp2f(fmaf(s[bk][x], a.scale_log2e, -ref));
+        p[x] = __builtin_amdgcn_exp2f(fmaf(s[x], a.scale_log2e, -ref));
         l += p[x];
       }
       f32_weights_v<DB>(acc, vl + kF32Rows * bk * Stage::LD, p, i, kq);
