@@ -13,11 +13,11 @@
 #include "common.hpp"
 #include "f32_tile.hpp"
 #include "serve.h"
+#include "stream_tile.hpp"
 
 namespace ac {
 
-constexpr int kWindowChunk = 64;
-constexpr float kWindowSlack = 8.0f;   // the reference point of a row moves when a score has outgrown it by 2^8
+constexpr int kWindowChunk = kStreamChunk;
 
 struct WindowArgs {
   const void *Q, *K, *V;
@@ -121,172 +121,54 @@ __global__ __launch_bounds__(kThreads, 2) void window_bf16_kernel(const WindowAr
   const bf16_t* Ksrc = reinterpret_cast<const bf16_t*>(a.K) + (size_t)u * a.S * D;
   const bf16_t* Vsrc = reinterpret_cast<const bf16_t*>(a.V) + (size_t)u * a.S * D;
   bf16_t* O = reinterpret_cast<bf16_t*>(a.O) + (row0 + t0) * D;
-  // (the scale through a vector instruction: straight from a scalar load it makes the compiler wait for all LDS reads)
-  const float scale_log2e = __builtin_bit_cast(
-      float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, a.scale_log2e) + (lane & 0)));
-
-  // copies and operand addresses as in cross.hip
+  StreamTile<D> tile(a.scale_log2e, lane);
+  // copies as in cross.hip
   const int slot0 = kWave * wave + lane, crow = slot0 / PPR, cpos = slot0 % PPR;
-  const int koff0 = crow * D + 8 * (cpos ^ k_piece_swizzle<D>(crow)), voff0 = crow * D + 8 * (cpos ^ v_piece_swizzle<D>(crow));
-  auto copy = [&](bf16_t* kb, bf16_t* vb, int c) {
-    const int there = keys - c * kWindowChunk;
+  const int kpiece = 8 * (cpos ^ k_piece_swizzle<D>(crow)), vpiece = 8 * (cpos ^ v_piece_swizzle<D>(crow));
+  auto copy = [&](bf16_t* kb, bf16_t* vb, int c) {   // (rows behind the keys repeat the last one: their weights are zero)
+    const int there = keys - 1 - c * kWindowChunk;
     const bf16_t* ks = Ksrc + (size_t)c * kWindowChunk * D;
     const bf16_t* vs = Vsrc + (size_t)c * kWindowChunk * D;
-    if (there >= kWindowChunk) {
 #pragma unroll
-      for (int i = 0; i < NCOPY; ++i) {
-        __builtin_amdgcn_global_load_lds(ks + koff0 + 2048 * i, kb + kWave * 8 * (wave + 4 * i), 16, 0, 0);
-        __builtin_amdgcn_global_load_lds(vs + voff0 + 2048 * i, vb + kWave * 8 * (wave + 4 * i), 16, 0, 0);
-      }
-    } else {   // K rows behind the keys repeat the last one, their scores are replaced; V rows are zeros
-#pragma unroll
-      for (int i = 0; i < NCOPY; ++i) {
-        const int row = crow + 256 / PPR * i;
-        __builtin_amdgcn_global_load_lds(ks + koff0 - crow * D + min(row, there - 1) * D, kb + kWave * 8 * (wave + 4 * i), 16, 0, 0);
-        bf16_t* to = vb + kWave * 8 * (wave + 4 * i);
-        if (row < there) __builtin_amdgcn_global_load_lds(vs + voff0 + 2048 * i, to, 16, 0, 0);
-        else *reinterpret_cast<u32x4*>(to + 8 * lane) = u32x4{0, 0, 0, 0};
-      }
+    for (int i = 0; i < NCOPY; ++i) {
+      const int at = min(crow + 256 / PPR * i, there) * D;
+      __builtin_amdgcn_global_load_lds(ks + at + kpiece, kb + kWave * 8 * (wave + 4 * i), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds(vs + at + vpiece, vb + kWave * 8 * (wave + 4 * i), 16, 0, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
   };
-  int koff[D / 16], voff[2][D / 32];
-#pragma unroll
-  for (int ks = 0; ks < D / 16; ++ks) koff[ks] = il * D + 8 * ((2 * ks + kh) ^ k_piece_swizzle<D>(il));
-#pragma unroll
-  for (int half = 0; half < 2; ++half)
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db) {
-      const int t = lane & 15, j = 4 * kh + 8 * half + (t >> 2), d0 = 32 * db + 16 * (il >> 4) + 4 * (t & 3);
-      voff[half][db] = j * D + 8 * ((d0 >> 3) ^ v_piece_swizzle<D>(j)) + (d0 & 7);
-    }
-  typedef short s16x4 __attribute__((ext_vector_type(4)));
-  typedef short s16x8 __attribute__((ext_vector_type(8)));
-  auto vop = [&](const bf16_t* vb, int db, int jb, int s2) {
-    const bf16_t* at = vb + (32 * jb + 16 * s2) * D;
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(at + voff[0][db]));
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(at + voff[1][db]));
-    const s16x8 w = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-    return __builtin_bit_cast(bf16x8, w);
-  };
-
   if (chunks.count > 0) copy(kb0, vb0, chunks.at(0));
-  u32x4 q[D / 16];
-  {
-    const bf16_t* src = reinterpret_cast<const bf16_t*>(a.Q) + (row0 + min(t0 + il, a.S - 1)) * D + 8 * kh;
+  tile.load_q(reinterpret_cast<const bf16_t*>(a.Q) + (row0 + min(t0 + il, a.S - 1)) * D);
+  tile.reset();
+  // Where some row does not see some key: c is a key's place in the chunk but for the lane's part of it, a constant of the register.
+  auto step = [&](const bf16_t* kb, const bf16_t* vb, int chunk) __attribute__((always_inline)) {
+    tile.chunk(kb, vb, [&](f32x16& s0, f32x16& s1) {
+      const int k0 = chunk * kWindowChunk, mine = k0 + 4 * kh, t = t0 + il;
+      if (k0 + kWindowChunk - 1 > min(t0, keys - 1)) {   // keys behind the row or the item's last
+        const int hi = min(t, keys - 1) - mine;
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) q[ks] = *reinterpret_cast<const u32x4*>(src + 16 * ks);
-  }
-  f32x16 acc[D / 32];
-#pragma unroll
-  for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-    for (int v = 0; v < 16; ++v) acc[db][v] = 0.f;
-  float m_run = -INFINITY, l_run = 0.f;
-
-  auto qk = [&](const bf16_t* kb, int jb) {
-    f32x16 s;
-#pragma unroll
-    for (int v = 0; v < 16; ++v) s[v] = 0.f;
-#pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks)
-      s = mfma_bf16(*reinterpret_cast<const bf16x8*>(kb + koff[ks] + 32 * jb * D), __builtin_bit_cast(bf16x8, q[ks]), s);
-    return s;
-  };
-  auto hide = [&](f32x16& s, int k0) {
-#pragma unroll
-    for (int v = 0; v < 16; ++v)
-      if (window_hides(a, t0 + il, k0 + mfma_row(v, kh), keys)) s[v] = -INFINITY;
-  };
-  auto row_max = [&](const f32x16& s) {
-    const float m01 = fmaxf(fmaxf(s[0], s[1]), s[2]), m02 = fmaxf(fmaxf(s[3], s[4]), s[5]);
-    const float m03 = fmaxf(fmaxf(s[6], s[7]), s[8]), m04 = fmaxf(fmaxf(s[9], s[10]), s[11]);
-    const float m05 = fmaxf(fmaxf(s[12], s[13]), s[14]);
-    return max_with_other_half(fmaxf(fmaxf(fmaxf(m01, m02), m03), fmaxf(fmaxf(m04, m05), s[15])));
-  };
-  // Weights 2^(score - m) in bf16, the second product's operand (it takes both factors in one type, and V is bf16); their sum is over the
-  // rounded ones, which V is multiplied with, so that they still add up to one.  (m = -inf: no finite score so far, all weights are zero.)
-  typedef bf16_t bf16x2 __attribute__((ext_vector_type(2)));
-  auto weights = [&](const f32x16& s, float m, u32x4(&pw)[2], float& sum) {
-    const bf16x2 ones = {(bf16_t)1.0f, (bf16_t)1.0f};
-    const float ref = m == -INFINITY ? 0.f : m;
-#pragma unroll
-    for (int w = 0; w < 8; ++w) {
-      const float e0 = __builtin_amdgcn_exp2f(fmaf(s[2 * w], scale_log2e, -ref));
-      const float e1 = __builtin_amdgcn_exp2f(fmaf(s[2 * w + 1], scale_log2e, -ref));
-      const uint32_t pk = pack_bf16(e0, e1);
-      pw[w >> 2][w & 3] = pk;
-      sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pk), ones, sum, false);
-    }
-  };
-  auto pv = [&](const bf16_t* vb, int jb, const u32x4(&pw)[2]) {
-#pragma unroll
-    for (int s2 = 0; s2 < 2; ++s2)
-#pragma unroll
-      for (int db = 0; db < D / 32; ++db)
-        acc[db] = mfma_bf16(vop(vb, db, jb, s2), __builtin_bit_cast(bf16x8, pw[s2]), acc[db]);
-  };
-  auto rescale = [&](float m_new) {
-    const float alpha = m_new > m_run ? __builtin_amdgcn_exp2f(m_run - m_new) : 1.f;
-    l_run *= alpha;
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) acc[db][v] *= alpha;
-  };
-  auto step = [&](const bf16_t* kb, const bf16_t* vb, int c) __attribute__((always_inline)) {
-    if (!live) return;
-    const int k0 = c * kWindowChunk;
-    const WindowBlock b0 = window_block<32, 32>(a, t0, k0, keys), b1 = window_block<32, 32>(a, t0, k0 + 32, keys);
-    if (b0 != kNone && b1 != kNone) {
-      // the scores of block 1 are requested before the exponentials of block 0, the second product of block 0 before those of block 1
-      f32x16 s0 = qk(kb, 0);
-      if (b0 == kSome) hide(s0, k0);
-      float cand = fmaxf(m_run, row_max(s0) * scale_log2e);
-      if (__any(cand > m_run + kWindowSlack)) {
-        rescale(cand);
-        m_run = cand;
+        for (int v = 0; v < 16; ++v) {
+          s0[v] = mfma_row(v, 0) > hi ? -INFINITY : s0[v];
+          s1[v] = 32 + mfma_row(v, 0) > hi ? -INFINITY : s1[v];
+        }
       }
-      f32x16 s1 = qk(kb, 1);
-      u32x4 p0[2], p1[2];
-      float sum = 0.f, sum1 = 0.f, m1 = m_run;
-      weights(s0, m_run, p0, sum);
-      l_run += sum;
-      if (b1 == kSome) hide(s1, k0 + 32);
-      cand = fmaxf(m_run, row_max(s1) * scale_log2e);
-      const bool moved = __any(cand > m_run + kWindowSlack);
-      if (moved) m1 = cand;
-      pv(vb, 0, p0);
-      weights(s1, m1, p1, sum1);
-      if (moved) rescale(m1);
-      m_run = m1;
-      l_run += sum1;
-      pv(vb, 1, p1);
-      return;
-    }
-#pragma unroll 1
-    for (int jb = 0; jb < 2; ++jb) {
-      const WindowBlock bl = jb ? b1 : b0;
-      if (bl == kNone) continue;
-      f32x16 s = qk(kb, jb);
-      if (bl == kSome) hide(s, k0 + 32 * jb);
-      const float cand = fmaxf(m_run, row_max(s) * scale_log2e);
-      if (__any(cand > m_run + kWindowSlack)) {
-        rescale(cand);
-        m_run = cand;
+      if (k0 <= t0 + kRowsPerWave - 1 - a.window && k0 + kWindowChunk > a.sinks) {   // keys in the gap
+        const int from = a.sinks - mine;
+        const unsigned n = (unsigned)max(t - a.window - a.sinks + 1, 0);
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          s0[v] = (unsigned)(mfma_row(v, 0) - from) < n ? -INFINITY : s0[v];
+          s1[v] = (unsigned)(32 + mfma_row(v, 0) - from) < n ? -INFINITY : s1[v];
+        }
       }
-      u32x4 p[2];
-      float sum = 0.f;
-      weights(s, m_run, p, sum);
-      l_run += sum;
-      pv(vb, jb, p);
-    }
+    });
   };
   auto publish = [&]() {   // this wave's copies have landed, then everybody's; the other stage is no longer read
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
   };
-  for (int i = 0; i < chunks.count; i += 2) {
+#pragma unroll 1
+  for (int i = 0; i < chunks.count; i += 2) {   // (two a trip: the stages alternate without pointer arithmetic)
     publish();
     if (i + 1 < chunks.count) copy(kb1, vb1, chunks.at(i + 1));
     step(kb0, vb0, chunks.at(i));
@@ -297,7 +179,8 @@ __global__ __launch_bounds__(kThreads, 2) void window_bf16_kernel(const WindowAr
   }
   __syncthreads();   // every wave is done with both stages: they now stage the output
   if (!live) return;
-  const float sum = l_run + __shfl_xor(l_run, 32);
+  f32x16(&acc)[D / 32] = tile.acc;
+  const float sum = tile.sum();
   bool odd = !(sum < INFINITY);
 #pragma unroll
   for (int db = 0; db < D / 32; ++db)
