@@ -9,6 +9,17 @@ namespace ac {
 constexpr int kStreamChunk = 64;
 constexpr float kStreamSlack = 8.0f;   // the reference point of a row moves when a score has outgrown it by 2^8
 
+// Copies from memory straight into LDS by buffer loads.  (The compiler takes a global load to LDS for one that may also read LDS, and lets every
+// LDS read wait for all others as long as one is under way.  A buffer load it knows: reads and products wait for what they need.)
+struct StreamSource {
+  __amdgpu_buffer_rsrc_t rsrc;
+  __device__ __forceinline__ StreamSource(const void* from, uint32_t bytes)   // uniform; bytes behind the last read as zeros
+      : rsrc(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(from), 0, bytes, 0x00020000)) {}
+  __device__ __forceinline__ void copy(bf16_t* lds, uint32_t offset) const {   // 16 bytes of each lane, side by side in LDS
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)lds, 16, offset, 0, 0, 0);
+  }
+};
+
 template <int D>
 struct StreamTile {
   static constexpr int KS = D / 16, DB = D / 32;   // products of a block of 32 keys, first and second (twice DB)

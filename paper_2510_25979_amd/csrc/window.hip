@@ -125,15 +125,19 @@ __global__ __launch_bounds__(kThreads, 2) void window_bf16_kernel(const WindowAr
   // copies as in cross.hip
   const int slot0 = kWave * wave + lane, crow = slot0 / PPR, cpos = slot0 % PPR;
   const int kpiece = 8 * (cpos ^ k_piece_swizzle<D>(crow)), vpiece = 8 * (cpos ^ v_piece_swizzle<D>(crow));
-  auto copy = [&](bf16_t* kb, bf16_t* vb, int c) {   // (rows behind the keys repeat the last one: their weights are zero)
-    const int there = keys - 1 - c * kWindowChunk;
-    const bf16_t* ks = Ksrc + (size_t)c * kWindowChunk * D;
-    const bf16_t* vs = Vsrc + (size_t)c * kWindowChunk * D;
+  uint32_t kfrom[NCOPY], vfrom[NCOPY];   // bytes from a chunk's first row
+#pragma unroll
+  for (int i = 0; i < NCOPY; ++i) {
+    kfrom[i] = 2 * ((crow + 256 / PPR * i) * D + kpiece);
+    vfrom[i] = 2 * ((crow + 256 / PPR * i) * D + vpiece);
+  }
+  auto copy = [&](bf16_t* kb, bf16_t* vb, int c) {   // (rows behind the keys are not read)
+    const uint32_t bytes = min(keys - c * kWindowChunk, kWindowChunk) * D * 2;
+    const StreamSource ks(Ksrc + (size_t)c * kWindowChunk * D, bytes), vs(Vsrc + (size_t)c * kWindowChunk * D, bytes);
 #pragma unroll
     for (int i = 0; i < NCOPY; ++i) {
-      const int at = min(crow + 256 / PPR * i, there) * D;
-      __builtin_amdgcn_global_load_lds(ks + at + kpiece, kb + kWave * 8 * (wave + 4 * i), 16, 0, 0);
-      __builtin_amdgcn_global_load_lds(vs + at + vpiece, vb + kWave * 8 * (wave + 4 * i), 16, 0, 0);
+      ks.copy(kb + kWave * 8 * (wave + 4 * i), kfrom[i]);
+      vs.copy(vb + kWave * 8 * (wave + 4 * i), vfrom[i]);
     }
     __builtin_amdgcn_sched_barrier(0);
   };
