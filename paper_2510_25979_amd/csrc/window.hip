@@ -28,11 +28,11 @@ struct WindowArgs {
   Divider by_g, by_per;
 };
 
-// Chunks of C keys of a workgroup with tokens [lo, hi): `head` of them from the first on, then `count - head` from `from` on.
+// Blocks of C keys that a workgroup with tokens [lo, hi) looks at: `head` of them from the first on, then `count - head` from `from` on.
 template <int C>
-struct WindowChunks {
+struct WindowBlocks {
   int head, from, count;
-  __device__ __forceinline__ WindowChunks(const WindowArgs& a, int lo, int hi, int keys) {
+  __device__ __forceinline__ WindowBlocks(const WindowArgs& a, int lo, int hi, int keys) {
     const int end = (min(hi, keys) + C - 1) / C, seen = min(a.sinks, min(hi, keys));
     head = (seen + C - 1) / C;
     from = max(head, max(0, lo - a.window + 1) / C);
@@ -117,7 +117,7 @@ __global__ __launch_bounds__(kThreads, 2) void window_bf16_kernel(const WindowAr
   const bool live = unit0 + wave <= last;
   const size_t row0 = ((size_t)(b * a.Hkv + hk) * a.g + (unit - tb * a.g)) * a.S;   // the head's first row
   const int rows = min(kRowsPerWave, a.S - t0);
-  const WindowChunks<kWindowChunk> chunks(a, kRowsPerWave * a.by_g.div(unit0), min(a.S, kRowsPerWave * (a.by_g.div(last) + 1)), keys);
+  const WindowBlocks<32> blocks(a, kRowsPerWave * a.by_g.div(unit0), min(a.S, kRowsPerWave * (a.by_g.div(last) + 1)), keys);
   const bf16_t* Ksrc = reinterpret_cast<const bf16_t*>(a.K) + (size_t)u * a.S * D;
   const bf16_t* Vsrc = reinterpret_cast<const bf16_t*>(a.V) + (size_t)u * a.S * D;
   bf16_t* O = reinterpret_cast<bf16_t*>(a.O) + (row0 + t0) * D;
@@ -125,46 +125,51 @@ __global__ __launch_bounds__(kThreads, 2) void window_bf16_kernel(const WindowAr
   // copies as in cross.hip
   const int slot0 = kWave * wave + lane, crow = slot0 / PPR, cpos = slot0 % PPR;
   const int kpiece = 8 * (cpos ^ k_piece_swizzle<D>(crow)), vpiece = 8 * (cpos ^ v_piece_swizzle<D>(crow));
-  uint32_t kfrom[NCOPY], vfrom[NCOPY];   // bytes from a chunk's first row
+  // A chunk is two blocks of 32 keys that follow one another in the workgroup's list; the second of the last may be missing.
+  constexpr int NROW = NCOPY / 2;        // copies of a block
+  uint32_t kfrom[NROW], vfrom[NROW];     // bytes from a block's first row
 #pragma unroll
-  for (int i = 0; i < NCOPY; ++i) {
+  for (int i = 0; i < NROW; ++i) {
     kfrom[i] = 2 * ((crow + 256 / PPR * i) * D + kpiece);
     vfrom[i] = 2 * ((crow + 256 / PPR * i) * D + vpiece);
   }
-  auto copy = [&](bf16_t* kb, bf16_t* vb, int c) {   // (rows behind the keys are not read)
-    const uint32_t bytes = min(keys - c * kWindowChunk, kWindowChunk) * D * 2;
-    const StreamSource ks(Ksrc + (size_t)c * kWindowChunk * D, bytes), vs(Vsrc + (size_t)c * kWindowChunk * D, bytes);
+  auto copy = [&](bf16_t* kb, bf16_t* vb, int c) {   // (rows behind the keys are not read; in the place of a missing block lies the one before it)
 #pragma unroll
-    for (int i = 0; i < NCOPY; ++i) {
-      ks.copy(kb + kWave * 8 * (wave + 4 * i), kfrom[i]);
-      vs.copy(vb + kWave * 8 * (wave + 4 * i), vfrom[i]);
+    for (int jb = 0; jb < 2; ++jb) {
+      const int k0 = kRowsPerWave * blocks.at(min(2 * c + jb, blocks.count - 1));
+      const uint32_t bytes = min(keys - k0, 32) * D * 2;
+      const StreamSource ks(Ksrc + (size_t)k0 * D, bytes), vs(Vsrc + (size_t)k0 * D, bytes);
+#pragma unroll
+      for (int i = 0; i < NROW; ++i) {
+        ks.copy(kb + 32 * D * jb + kWave * 8 * (wave + 4 * i), kfrom[i]);
+        vs.copy(vb + 32 * D * jb + kWave * 8 * (wave + 4 * i), vfrom[i]);
+      }
     }
     __builtin_amdgcn_sched_barrier(0);
   };
-  if (chunks.count > 0) copy(kb0, vb0, chunks.at(0));
+  const int n_chunk = (blocks.count + 1) / 2;
+  if (n_chunk > 0) copy(kb0, vb0, 0);
   tile.load_q(reinterpret_cast<const bf16_t*>(a.Q) + (row0 + min(t0 + il, a.S - 1)) * D);
   tile.reset();
-  // Where some row does not see some key: c is a key's place in the chunk but for the lane's part of it, a constant of the register.
-  auto step = [&](const bf16_t* kb, const bf16_t* vb, int chunk) __attribute__((always_inline)) {
+  // (mfma_row(v, 0) is a key's place in its block but for the lane's part of it, a constant of the register)
+  auto hide = [&](f32x16& s, int k0) {
+    const int mine = k0 + 4 * kh, t = t0 + il;
+    if (k0 + 31 > min(t0, keys - 1)) {   // keys behind the row or the item's last
+      const int hi = min(t, keys - 1) - mine;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[v] = mfma_row(v, 0) > hi ? -INFINITY : s[v];
+    }
+    if (k0 <= t0 + kRowsPerWave - 1 - a.window && k0 + 32 > a.sinks) {   // keys in the gap
+      const int from = a.sinks - mine;
+      const unsigned n = (unsigned)max(t - a.window - a.sinks + 1, 0);
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[v] = (unsigned)(mfma_row(v, 0) - from) < n ? -INFINITY : s[v];
+    }
+  };
+  auto step = [&](const bf16_t* kb, const bf16_t* vb, int c) __attribute__((always_inline)) {
     tile.chunk(kb, vb, [&](f32x16& s0, f32x16& s1) {
-      const int k0 = chunk * kWindowChunk, mine = k0 + 4 * kh, t = t0 + il;
-      if (k0 + kWindowChunk - 1 > min(t0, keys - 1)) {   // keys behind the row or the item's last
-        const int hi = min(t, keys - 1) - mine;
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          s0[v] = mfma_row(v, 0) > hi ? -INFINITY : s0[v];
-          s1[v] = 32 + mfma_row(v, 0) > hi ? -INFINITY : s1[v];
-        }
-      }
-      if (k0 <= t0 + kRowsPerWave - 1 - a.window && k0 + kWindowChunk > a.sinks) {   // keys in the gap
-        const int from = a.sinks - mine;
-        const unsigned n = (unsigned)max(t - a.window - a.sinks + 1, 0);
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          s0[v] = (unsigned)(mfma_row(v, 0) - from) < n ? -INFINITY : s0[v];
-          s1[v] = (unsigned)(32 + mfma_row(v, 0) - from) < n ? -INFINITY : s1[v];
-        }
-      }
+      hide(s0, 32 * blocks.at(2 * c));
+      hide(s1, 2 * c + 1 < blocks.count ? 32 * blocks.at(2 * c + 1) : keys);
     });
   };
   auto publish = [&]() {   // this wave's copies have landed, then everybody's; the other stage is no longer read
@@ -172,14 +177,14 @@ __global__ __launch_bounds__(kThreads, 2) void window_bf16_kernel(const WindowAr
     __syncthreads();
   };
 #pragma unroll 1
-  for (int i = 0; i < chunks.count; i += 2) {   // (two a trip: the stages alternate without pointer arithmetic)
+  for (int c = 0; c < n_chunk; c += 2) {   // (two a trip: the stages alternate without pointer arithmetic)
     publish();
-    if (i + 1 < chunks.count) copy(kb1, vb1, chunks.at(i + 1));
-    step(kb0, vb0, chunks.at(i));
-    if (i + 1 >= chunks.count) break;
+    if (c + 1 < n_chunk) copy(kb1, vb1, c + 1);
+    step(kb0, vb0, c);
+    if (c + 1 >= n_chunk) break;
     publish();
-    if (i + 2 < chunks.count) copy(kb0, vb0, chunks.at(i + 2));
-    step(kb1, vb1, chunks.at(i + 1));
+    if (c + 2 < n_chunk) copy(kb0, vb0, c + 2);
+    step(kb1, vb1, c + 1);
   }
   __syncthreads();   // every wave is done with both stages: they now stage the output
   if (!live) return;
@@ -230,7 +235,7 @@ __global__ __launch_bounds__(kThreads, DB <= 2 ? 2 : 1) void window_f32_kernel(c
   const int unit = min(unit0 + wave, last), tb = a.by_g.div(unit), t0 = kF32Rows * tb;
   const bool live = unit0 + wave <= last;
   const size_t row0 = ((size_t)(b * a.Hkv + hk) * a.g + (unit - tb * a.g)) * a.S;
-  const WindowChunks<KC> chunks(a, kF32Rows * a.by_g.div(unit0), min(a.S, kF32Rows * (a.by_g.div(last) + 1)), keys);
+  const WindowBlocks<KC> chunks(a, kF32Rows * a.by_g.div(unit0), min(a.S, kF32Rows * (a.by_g.div(last) + 1)), keys);
   const float* K = reinterpret_cast<const float*>(a.K) + (size_t)u * a.S * D;
   const float* V = reinterpret_cast<const float*>(a.V) + (size_t)u * a.S * D;
   const float* Q = reinterpret_cast<const float*>(a.Q) + row0 * D;
