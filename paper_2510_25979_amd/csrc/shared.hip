@@ -15,10 +15,11 @@
 #include <type_traits>
 
 #include "decode_tile.hpp"
+#include "stream_tile.hpp"
 
 namespace ac {
 
-constexpr int kSharedRows = 128, kSharedChunk = 64;   // of a workgroup of shared_prefix_kernel
+constexpr int kSharedRows = 128, kSharedChunk = kStreamChunk;   // of a workgroup of shared_prefix_kernel
 constexpr int kSharedWgs = 512;                       // most workgroups of it
 constexpr int kSharedLeast = 4, kSharedMost = 16;     // chunks of a run: at least; at most while there is one for each compute unit (see the plan)
 constexpr int kSharedUnitCost = 1;                    // what a unit of it costs beside its chunks
@@ -408,119 +409,22 @@ __device__ __forceinline__ void shared_run(const SharedArgs& a, unsigned char* l
 }
 
 // ---- prefixes of many rows
-template <int D>
+// FAR: the cache is larger than a buffer load's 32 bits reach.
+template <int D, bool FAR>
 __device__ __forceinline__ void shared_prefix(const SharedArgs& a, bf16_t* kb0, bf16_t* vb0, bf16_t* kb1, bf16_t* vb1) {
   constexpr int PPR = D / 8, NCOPY = kSharedChunk * PPR / kWave / 4, UNIT = SharedBf16<D>::RB * kDecodeRows;
+  typedef typename std::conditional<FAR, int64_t, uint32_t>::type Place;   // elements from the head's first row of the first page; FAR or bytes
   const DecodeArgs& d = a.d;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int il = lane & 31, kh = lane >> 5;
   const int total = a.sums[1], per = a.sums[2];
   if ((int64_t)blockIdx.x * per >= total) return;
-  const float scale_log2e = __builtin_bit_cast(
-      float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, d.scale_log2e) + (lane & 0)));
-  // copies and operand addresses as in cross.hip
+  // copies as in cross.hip
   const int slot0 = kWave * wave + lane, crow = slot0 / PPR, cpos = slot0 % PPR;
   const int kpiece = 8 * (cpos ^ k_piece_swizzle<D>(crow)), vpiece = 8 * (cpos ^ v_piece_swizzle<D>(crow));
-  int koff[D / 16], voff[2][D / 32];
-#pragma unroll
-  for (int ks = 0; ks < D / 16; ++ks) koff[ks] = il * D + 8 * ((2 * ks + kh) ^ k_piece_swizzle<D>(il));
-#pragma unroll
-  for (int half = 0; half < 2; ++half)
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db) {
-      const int t = lane & 15, j = 4 * kh + 8 * half + (t >> 2), d0 = 32 * db + 16 * (il >> 4) + 4 * (t & 3);
-      voff[half][db] = j * D + 8 * ((d0 >> 3) ^ v_piece_swizzle<D>(j)) + (d0 & 7);
-    }
-  typedef short s16x4 __attribute__((ext_vector_type(4)));
-  typedef short s16x8 __attribute__((ext_vector_type(8)));
-  auto vop = [&](const bf16_t* vb, int db, int jb, int s2) {
-    const bf16_t* at = vb + (32 * jb + 16 * s2) * D;
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(at + voff[0][db]));
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(at + voff[1][db]));
-    const s16x8 w = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-    return __builtin_bit_cast(bf16x8, w);
-  };
-  u32x4 q[D / 16];
-  f32x16 acc[D / 32];
-  float m_run, l_run;
-  auto qk = [&](const bf16_t* kb, int jb) {
-    f32x16 s;
-#pragma unroll
-    for (int v = 0; v < 16; ++v) s[v] = 0.f;
-#pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks)
-      s = mfma_bf16(*reinterpret_cast<const bf16x8*>(kb + koff[ks] + 32 * jb * D), __builtin_bit_cast(bf16x8, q[ks]), s);
-    return s;
-  };
-  auto row_max = [&](const f32x16& s) {
-    const float m01 = fmaxf(fmaxf(s[0], s[1]), s[2]), m02 = fmaxf(fmaxf(s[3], s[4]), s[5]);
-    const float m03 = fmaxf(fmaxf(s[6], s[7]), s[8]), m04 = fmaxf(fmaxf(s[9], s[10]), s[11]);
-    const float m05 = fmaxf(fmaxf(s[12], s[13]), s[14]);
-    return max_with_other_half(fmaxf(fmaxf(fmaxf(m01, m02), m03), fmaxf(fmaxf(m04, m05), s[15])));
-  };
-  typedef bf16_t bf16x2 __attribute__((ext_vector_type(2)));
-  auto weights = [&](const f32x16& s, float m, u32x4(&pw)[2], float& sum) {   // rounded to bf16 as in decode_tile.hpp
-    const bf16x2 ones = {(bf16_t)1.0f, (bf16_t)1.0f};
-    const float ref = m == -INFINITY ? 0.f : m;
-#pragma unroll
-    for (int w = 0; w < 8; ++w) {
-      const float e0 = __builtin_amdgcn_exp2f(fmaf(s[2 * w], scale_log2e, -ref));
-      const float e1 = __builtin_amdgcn_exp2f(fmaf(s[2 * w + 1], scale_log2e, -ref));
-      const uint32_t pk = pack_bf16(e0, e1);
-      pw[w >> 2][w & 3] = pk;
-      sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pk), ones, sum, false);
-    }
-  };
-  auto pv = [&](const bf16_t* vb, int jb, const u32x4(&pw)[2]) {
-#pragma unroll
-    for (int s2 = 0; s2 < 2; ++s2)
-#pragma unroll
-      for (int db = 0; db < D / 32; ++db)
-        acc[db] = mfma_bf16(vop(vb, db, jb, s2), __builtin_bit_cast(bf16x8, pw[s2]), acc[db]);
-  };
-  auto rescale = [&](float m_new) {
-    const float alpha = m_new > m_run ? __builtin_amdgcn_exp2f(m_run - m_new) : 1.f;
-    l_run *= alpha;
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) acc[db][v] *= alpha;
-  };
-  auto step = [&](const bf16_t* kb, const bf16_t* vb, unsigned long long there) __attribute__((always_inline)) {
-    f32x16 s0 = qk(kb, 0);
-    auto hide = [&](f32x16& s, uint32_t bits) {
-      if (bits != 0xffffffffu)   // uniform
-#pragma unroll
-        for (int v = 0; v < 16; ++v)
-          if (!((bits >> mfma_row(v, kh)) & 1)) s[v] = -INFINITY;
-    };
-    hide(s0, (uint32_t)there);
-    float cand = fmaxf(m_run, row_max(s0) * scale_log2e);
-    if (__any(cand > m_run + kDecodeSlack)) {
-      rescale(cand);
-      m_run = cand;
-    }
-    f32x16 s1 = qk(kb, 1);
-    u32x4 p0[2], p1[2];
-    float sum = 0.f, sum1 = 0.f, m1 = m_run;
-    weights(s0, m_run, p0, sum);
-    l_run += sum;
-    hide(s1, (uint32_t)(there >> 32));
-    cand = fmaxf(m_run, row_max(s1) * scale_log2e);
-    const bool moved = __any(cand > m_run + kDecodeSlack);
-    if (moved) m1 = cand;
-    pv(vb, 0, p0);
-    weights(s1, m1, p1, sum1);
-    if (moved) rescale(m1);
-    m_run = m1;
-    l_run += sum1;
-    pv(vb, 1, p1);
-  };
-  auto publish = [&]() {   // this wave's copies have landed, then everybody's; the other stage is no longer read
-    __builtin_amdgcn_s_waitcnt(0);
-    __syncthreads();
-  };
+  StreamTile<D> tile(d.scale_log2e, lane);
+  const uint32_t bytes = FAR ? 0 : (uint32_t)(((int64_t)(d.n_pages - 1) * d.page_stride + d.head_stride) * 2);   // of a head, in all pages
 
   int x = blockIdx.x * per;
   const int end = min(total, x + per);
@@ -538,61 +442,90 @@ __device__ __forceinline__ void shared_prefix(const SharedArgs& a, bf16_t* kb0, 
       continue;
     }
     const int hk = unit / it.rbs, r = kSharedRows * (unit - hk * it.rbs) + kRowsPerWave * wave + il;
-    const bf16_t* K = static_cast<const bf16_t*>(d.K) + (size_t)hk * d.head_stride;
-    const bf16_t* V = static_cast<const bf16_t*>(d.V) + (size_t)hk * d.head_stride;
-    // lane l knows the place of key l of a chunk: its page is asked for a chunk ahead
+    const bf16_t* K = uniform_ptr(static_cast<const bf16_t*>(d.K) + (size_t)hk * d.head_stride);
+    const bf16_t* V = uniform_ptr(static_cast<const bf16_t*>(d.V) + (size_t)hk * d.head_stride);
+    const StreamSource ks(K, bytes), vs(V, bytes);
+    // Lane l asks for the page of key l of a chunk, two chunks ahead of the products; a chunk ahead it knows the key's place and hands it to the lanes that
+    // copy its row.
     auto ask = [&](int c) {
       const int j = c * kSharedChunk + lane;
       return j < it.keys ? d.table[(size_t)it.row * d.max_pages + d.by_ps.div(j)] : -1;
     };
-    auto copy = [&](bf16_t* kb, bf16_t* vb, int c, int page) {   // which keys are there
+    struct Rows { Place at[NCOPY]; unsigned long long there; };
+    auto place = [&](Rows& w, int c, int page) {
       const int j = c * kSharedChunk + lane;
       const bool is = (unsigned)page < (unsigned)d.n_pages;
       const int64_t at = is ? page * d.page_stride + (int64_t)(j - d.by_ps.div(j) * d.ps) * D : 0;   // (0: there, and not used)
-      const unsigned long long there = __ballot(is);
+      w.there = __ballot(is);
 #pragma unroll
       for (int n = 0; n < NCOPY; ++n) {
-        const int row = crow + 256 / PPR * n;
-        const int64_t from = __shfl((long long)at, row);
-        __builtin_amdgcn_global_load_lds(K + from + kpiece, kb + kWave * 8 * (wave + 4 * n), 16, 0, 0);
+        if constexpr (FAR) w.at[n] = __shfl((long long)at, crow + 256 / PPR * n);
+        else w.at[n] = (uint32_t)__shfl((int)(uint32_t)(2 * at), crow + 256 / PPR * n);
+      }
+    };
+    auto copy = [&](bf16_t* kb, bf16_t* vb, const Rows& w) {
+#pragma unroll
+      for (int n = 0; n < NCOPY; ++n) {
+        bf16_t* to = kb + kWave * 8 * (wave + 4 * n);
+        if constexpr (FAR) __builtin_amdgcn_global_load_lds(K + w.at[n] + kpiece, to, 16, 0, 0);
+        else ks.copy(to, w.at[n] + 2 * kpiece);
+      }
+      auto values = [&](int n) {
         bf16_t* to = vb + kWave * 8 * (wave + 4 * n);
-        if ((there >> row) & 1) __builtin_amdgcn_global_load_lds(V + from + vpiece, to, 16, 0, 0);
-        else *reinterpret_cast<u32x4*>(to + 8 * lane) = u32x4{0, 0, 0, 0};   // a weight of zero does not make a NaN vanish
+        if constexpr (FAR) __builtin_amdgcn_global_load_lds(V + w.at[n] + vpiece, to, 16, 0, 0);
+        else vs.copy(to, w.at[n] + 2 * vpiece);
+      };
+      if (w.there == ~0ull) {   // uniform
+#pragma unroll
+        for (int n = 0; n < NCOPY; ++n) values(n);
+      } else {   // a weight of zero does not make a NaN vanish
+#pragma unroll
+        for (int n = 0; n < NCOPY; ++n) {
+          if ((w.there >> (crow + 256 / PPR * n)) & 1) values(n);
+          else *reinterpret_cast<u32x4*>(vb + kWave * 8 * (wave + 4 * n) + 8 * lane) = u32x4{0, 0, 0, 0};
+        }
       }
       __builtin_amdgcn_sched_barrier(0);
-      return there;
+    };
+    auto step = [&](const bf16_t* kb, const bf16_t* vb, unsigned long long there) __attribute__((always_inline)) {
+      tile.chunk(kb, vb, [&](f32x16& s0, f32x16& s1) {
+        if (there != ~0ull) {   // uniform
+          const uint32_t lo = (uint32_t)there >> (4 * kh), hi = (uint32_t)(there >> 32) >> (4 * kh);
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            s0[v] = (lo >> mfma_row(v, 0)) & 1 ? s0[v] : -INFINITY;
+            s1[v] = (hi >> mfma_row(v, 0)) & 1 ? s1[v] : -INFINITY;
+          }
+        }
+      });
+    };
+    auto publish = [&]() {   // this wave's copies have landed, then everybody's; the other stage is no longer read
+      __builtin_amdgcn_s_waitcnt(0);
+      __syncthreads();
     };
     __syncthreads();   // the stages are no longer read
+    Rows now, next;
     int page = ask(c0);
-    {
-      const bf16_t* src = static_cast<const bf16_t*>(d.Q) + shared_row(a, it.b0, hk, min(r, it.R - 1)) * D + 8 * kh;
-#pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks) q[ks] = *reinterpret_cast<const u32x4*>(src + 16 * ks);
-    }
-    unsigned long long there0 = copy(kb0, vb0, c0, page), there1 = 0;
-    if (c0 + 1 < c1) page = ask(c0 + 1);
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) acc[db][v] = 0.f;
-    m_run = -INFINITY;
-    l_run = 0.f;
-    for (int c = c0; c < c1; c += 2) {
+    tile.load_q(static_cast<const bf16_t*>(d.Q) + shared_row(a, it.b0, hk, min(r, it.R - 1)) * D);
+    place(now, c0, page);
+    copy(kb0, vb0, now);
+    if (c0 + 1 < c1) place(next, c0 + 1, ask(c0 + 1));
+    tile.reset();
+#pragma unroll 1
+    for (int c = c0; c < c1; c += 2) {   // now: what lies in the first stage; next: the chunk behind it
       publish();
-      if (c + 1 < c1) {
-        there1 = copy(kb1, vb1, c + 1, page);
-        if (c + 2 < c1) page = ask(c + 2);
-      }
-      step(kb0, vb0, there0);
+      if (c + 1 < c1) copy(kb1, vb1, next);
+      if (c + 2 < c1) page = ask(c + 2);
+      step(kb0, vb0, now.there);
       if (c + 1 >= c1) break;
+      if (c + 2 < c1) place(now, c + 2, page);
       publish();
-      if (c + 2 < c1) {
-        there0 = copy(kb0, vb0, c + 2, page);
-        if (c + 3 < c1) page = ask(c + 3);
-      }
-      step(kb1, vb1, there1);
+      if (c + 2 < c1) copy(kb0, vb0, now);
+      if (c + 3 < c1) page = ask(c + 3);
+      step(kb1, vb1, next.there);
+      if (c + 3 < c1) place(next, c + 3, page);
     }
-    const float sum = l_run + __shfl_xor(l_run, 32);
+    const float sum = tile.sum();
     if (r < it.R) {
       const size_t rows = shared_rows(a);
       const size_t rec = c0 == 0 && c1 == nc ? rows + shared_row(a, it.b0, hk, r)
@@ -602,10 +535,12 @@ __device__ __forceinline__ void shared_prefix(const SharedArgs& a, bf16_t* kb0, 
 #pragma unroll
       for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-        for (int vq = 0; vq < 4; ++vq)
-          *reinterpret_cast<f32x4*>(to + 32 * db + 8 * vq) = f32x4{acc[db][4 * vq], acc[db][4 * vq + 1], acc[db][4 * vq + 2], acc[db][4 * vq + 3]};
+        for (int vq = 0; vq < 4; ++vq) {
+          const f32x16& t = tile.acc[db];
+          *reinterpret_cast<f32x4*>(to + 32 * db + 8 * vq) = f32x4{t[4 * vq], t[4 * vq + 1], t[4 * vq + 2], t[4 * vq + 3]};
+        }
       if (kh == 0) {
-        a.stat[2 * rec] = m_run;
+        a.stat[2 * rec] = tile.m;
         a.stat[2 * rec + 1] = sum;
       }
     }
@@ -619,14 +554,14 @@ __global__ __launch_bounds__(kThreads, Core::WGS) void shared_run_kernel(const S
   shared_run<Core>(a, lds + (Core::LDS ? (threadIdx.x >> 6) * Core::LDS : 0));
 }
 // Both in one launch: a workgroup has its share of the one and of the other.
-template <int D>
+template <int D, bool FAR>
 __global__ __launch_bounds__(kThreads, 2) void shared_both_kernel(const SharedArgs a) {
   __shared__ __attribute__((aligned(16))) bf16_t kb0[kSharedChunk * D];
   __shared__ __attribute__((aligned(16))) bf16_t vb0[kSharedChunk * D];
   __shared__ __attribute__((aligned(16))) bf16_t kb1[kSharedChunk * D];
   __shared__ __attribute__((aligned(16))) bf16_t vb1[kSharedChunk * D];
   static_assert(DecodeBf16<D>::LDS <= (int)sizeof(kb0), "a wave's V tile in a stage");
-  shared_prefix<D>(a, kb0, vb0, kb1, vb1);
+  shared_prefix<D, FAR>(a, kb0, vb0, kb1, vb1);
   __syncthreads();
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   shared_run<SharedBf16<D>>(a, reinterpret_cast<unsigned char*>(wave == 0 ? kb0 : wave == 1 ? vb0 : wave == 2 ? kb1 : vb1));
@@ -785,7 +720,9 @@ static hipError_t launch_shared_as(SharedArgs& a, bool big, hipStream_t stream) 
   if (e != hipSuccess) return e;
   if constexpr (!F32) {
     static_assert(Core::WGS == 2, "a workgroup has a share of both");
-    if (big) hipLaunchKernelGGL((shared_both_kernel<Core::NP * 16>), dim3((unsigned)a.wgs), dim3(kThreads), 0, stream, a);
+    const bool far = ((double)a.d.n_pages * (double)a.d.page_stride) * 2 >= 4294967296.0;
+    if (big && far) hipLaunchKernelGGL((shared_both_kernel<Core::NP * 16, true>), dim3((unsigned)a.wgs), dim3(kThreads), 0, stream, a);
+    else if (big) hipLaunchKernelGGL((shared_both_kernel<Core::NP * 16, false>), dim3((unsigned)a.wgs), dim3(kThreads), 0, stream, a);
     else hipLaunchKernelGGL((shared_run_kernel<Core>), dim3((unsigned)(a.d.waves / 4)), dim3(kThreads), 0, stream, a);
   } else {
     hipLaunchKernelGGL((shared_run_kernel<Core>), dim3((unsigned)(a.d.waves / 4)), dim3(kThreads), 0, stream, a);
