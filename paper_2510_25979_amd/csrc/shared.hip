@@ -73,10 +73,9 @@ struct SharedF32 : DecodeF32<DB, FULL> {
 // Records: own whole results [B Hq], prefixes' [B Hq], of runs [2 waves][unit], of workgroups [2 wgs][128].
 __device__ __forceinline__ size_t shared_rows(const SharedArgs& a) { return (size_t)a.d.B * a.d.Hkv * a.g; }
 
-constexpr int kPlanThreads = 1024;
-template <typename Op>
+template <int NT, typename Op>
 __device__ __forceinline__ int shared_scan(int x, int& all, int* part, Op op, int none) {   // inclusive, over the workgroup
-  constexpr int NW = kPlanThreads / kWave;
+  constexpr int NW = NT / kWave;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
   for (int off = 1; off < kWave; off <<= 1) {
@@ -97,19 +96,18 @@ __device__ __forceinline__ int shared_scan(int x, int& all, int* part, Op op, in
   return op(x, before);
 }
 
-// Groups of the plan: in LDS up to kPlanThreads of them, otherwise in the workspace, where what this launch has written is read past the
+// Groups of the plan: in LDS while each has a thread, otherwise in the workspace, where what this launch has written is read past the
 // first-level cache.
-constexpr int kPlanGroups = kPlanThreads;
 template <bool LDS>
 __device__ __forceinline__ int shared_peek(const int* p) {
   return LDS ? *p : __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
 // Bound by latency: lengths and groups -> who shares -> sums -> list.  64 requests 14.3 us with the groups in the workspace, LDS_US so.
-template <int BK, int UNIT, bool LDS>   // keys of a block, rows of a unit
-__global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedArgs a) {
-  __shared__ int part[kPlanThreads / kWave], part1[kPlanThreads / kWave];
-  __shared__ int s_first[LDS ? kPlanGroups + 1 : 1], s_leader[LDS ? kPlanGroups : 1], s_count[LDS ? kPlanGroups : 1], s_len[LDS ? kPlanGroups : 1];
+template <int BK, int UNIT, int NT, bool LDS>   // keys of a block, rows of a unit, threads
+__global__ __launch_bounds__(NT) void shared_plan_kernel(const SharedArgs a) {
+  __shared__ int part[NT / kWave], part1[NT / kWave];
+  __shared__ int s_first[LDS ? NT + 1 : 1], s_leader[LDS ? NT : 1], s_count[LDS ? NT : 1], s_len[LDS ? NT : 1];
   const int tid = threadIdx.x, B = a.d.B, G = a.G, cap = a.d.Sk;
   int* first = LDS ? s_first : a.first;
   int* leader = LDS ? s_leader : a.leader;
@@ -117,14 +115,14 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedA
   auto add = [](int x, int y) { return x + y; };
   auto top = [](int x, int y) { return max(x, y); };
   auto tokens = [&](int b) { return min(max(a.d.len[b], 0), cap); };
-  int mine = tid < B ? tokens(tid) : 0;   // of the first 1,024 requests: asked for at once
+  int mine = tid < B ? tokens(tid) : 0;   // of the first requests: asked for at once
   // where groups begin: in order, whatever is given
   int before = 0;
-  for (int c = 0; c <= G; c += kPlanThreads) {
+  for (int c = 0; c <= G; c += NT) {
     const int i = c + tid;
     if (LDS && i < G) s_len[i] = min(max(a.share_len[i], 0), cap);
     int all;
-    const int f = shared_scan(i <= G ? min(max(a.share_first[i], 0), B) : 0, all, part, top, 0);
+    const int f = shared_scan<NT>(i <= G ? min(max(a.share_first[i], 0), B) : 0, all, part, top, 0);
     if (i <= G) first[i] = max(before, f);
     if (i < G) {
       leader[i] = B;
@@ -144,8 +142,8 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedA
     }
     return lo >= 0 && b < shared_peek<LDS>(first + lo + 1) ? lo : -1;
   };
-  int group = -1;   // of this thread's request among the first 1,024
-  for (int b = tid; b < B; b += kPlanThreads) {
+  int group = -1;   // of this thread's request among the first
+  for (int b = tid; b < B; b += NT) {
     const int q = group_of(b), n = b == tid ? mine : tokens(b);
     if (b == tid) group = q;
     if (q < 0) continue;
@@ -159,7 +157,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedA
   __syncthreads();
   // First the groups, then the requests: the same thread has a request here and above.
   int begun = 0, begun1 = 0;
-  for (int c = 0; c < G; c += kPlanThreads) {
+  for (int c = 0; c < G; c += NT) {
     const int i = c + tid;
     SharedItem it = {0, 0, 0, 0, 0, 1, 0, 0};
     int cost = 0, cost1 = 0;
@@ -179,7 +177,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedA
       }
     }
     int all, all1;
-    const int upto = begun + shared_scan(cost, all, part, add, 0), upto1 = begun1 + shared_scan(cost1, all1, part1, add, 0);
+    const int upto = begun + shared_scan<NT>(cost, all, part, add, 0), upto1 = begun1 + shared_scan<NT>(cost1, all1, part1, add, 0);
     if (i < G) {
       it.start = it.group ? upto1 - cost1 : upto - cost;
       a.item[i] = it;
@@ -189,7 +187,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedA
     begun += all;
     begun1 += all1;
   }
-  for (int c = 0; c < B; c += kPlanThreads) {
+  for (int c = 0; c < B; c += NT) {
     const int b = c + tid;
     SharedItem it = {0, 0, 0, 0, 0, 1, 0, -1};
     int cost = 0;
@@ -207,7 +205,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedA
       if (it.keys > 0) cost = a.d.Hkv * it.rbs * ((it.keys + BK - 1) / BK + kUnitCost);
     }
     int all;
-    const int upto = begun + shared_scan(cost, all, part, add, 0);
+    const int upto = begun + shared_scan<NT>(cost, all, part, add, 0);
     if (b < B) {
       it.start = upto - cost;
       a.item[G + b] = it;
@@ -621,11 +619,31 @@ __global__ __launch_bounds__(NW == 1 ? kThreads : NW * kWave) void shared_join_k
   for (int e0 = NW == 1 ? 0 : wave; e0 < n; e0 += NW * kWave) {
     const int e = min(e0 + NW * lane, n - 1);
     const size_t rec = record(e);
+    const int here = min(kWave, (n - 1 - e0) / NW + 1);
+    // the first parts are asked for beside their maxima and sums; four loads of a lane are on their way at once
+    f32x4 y[4];
+    auto parts = [&](int k0) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int k = k0 + j * SUB + sub;
+        const float* src = a.part + (size_t)__shfl((long long)rec, min(k, here - 1)) * D + col;
+        y[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (k >= here || col >= D) continue;
+        if (!F32 || col + 4 <= D) {
+          y[j] = *reinterpret_cast<const f32x4_dw*>(src);
+        } else {
+#pragma unroll
+          for (int c = 0; c < 3; ++c)
+            if (col + c < D) y[j][c] = src[c];
+        }
+      }
+    };
     float m = -INFINITY, l = 0.f;
     if (e0 + NW * lane < n) {
       m = a.stat[2 * rec];
       l = a.stat[2 * rec + 1];
     }
+    parts(0);
     float t = fmaxf(top, m);
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) t = fmaxf(t, __shfl_xor(t, off));
@@ -637,28 +655,15 @@ __global__ __launch_bounds__(NW == 1 ? kThreads : NW * kWave) void shared_join_k
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) l += __shfl_xor(l, off);
     total += l;
-    const int here = min(kWave, (n - 1 - e0) / NW + 1);
-    for (int k0 = 0; k0 < here; k0 += 4 * SUB) {   // four loads of a lane on their way at once
-      f32x4 y[4];
-      float weight[4];
+    for (int k0 = 0; k0 < here;) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int k = k0 + j * SUB + sub, from_lane = min(k, here - 1);
-        const float w_j = __shfl(f, from_lane);
-        weight[j] = k < here ? w_j : 0.f;
-        const float* src = a.part + (size_t)__shfl((long long)rec, from_lane) * D + col;
-        y[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (k >= here || col >= D) continue;
-        if (!F32 || col + 4 <= D) {
-          y[j] = *reinterpret_cast<const f32x4_dw*>(src);
-        } else {
-#pragma unroll
-          for (int c = 0; c < 3; ++c)
-            if (col + c < D) y[j][c] = src[c];
-        }
+        const int k = k0 + j * SUB + sub;
+        const float weight = __shfl(f, min(k, here - 1));
+        o += y[j] * (k < here ? weight : 0.f);
       }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) o += y[j] * weight[j];
+      k0 += 4 * SUB;
+      if (k0 < here) parts(k0);
     }
   }
 #pragma unroll
@@ -714,8 +719,9 @@ static hipError_t launch_shared_as(SharedArgs& a, bool big, hipStream_t stream) 
   constexpr int G = Core::NP * 4, UNIT = Core::RB * kDecodeRows;
   a.d.waves = 4 * 256 * Core::WGS;
   a.own_rbs = (a.g + UNIT - 1) / UNIT;
-  if (a.G <= kPlanGroups - 1) hipLaunchKernelGGL((shared_plan_kernel<Core::BK, UNIT, true>), dim3(1), dim3(kPlanThreads), 0, stream, a);
-  else hipLaunchKernelGGL((shared_plan_kernel<Core::BK, UNIT, false>), dim3(1), dim3(kPlanThreads), 0, stream, a);
+  if (a.G <= 256 && a.d.B <= 256) hipLaunchKernelGGL((shared_plan_kernel<Core::BK, UNIT, 256, true>), dim3(1), dim3(256), 0, stream, a);
+  else if (a.G <= 1024) hipLaunchKernelGGL((shared_plan_kernel<Core::BK, UNIT, 1024, true>), dim3(1), dim3(1024), 0, stream, a);
+  else hipLaunchKernelGGL((shared_plan_kernel<Core::BK, UNIT, 1024, false>), dim3(1), dim3(1024), 0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if constexpr (!F32) {
@@ -730,7 +736,8 @@ static hipError_t launch_shared_as(SharedArgs& a, bool big, hipStream_t stream) 
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int64_t rows = (int64_t)a.d.B * a.d.Hkv * a.g;
-  if (rows <= 4096) hipLaunchKernelGGL((shared_join_kernel<F32, G, 4>), dim3((unsigned)rows), dim3(4 * kWave), 0, stream, a);
+  // us, four waves a row / one: 408 rows of 30 parts 24.7 / 24.9, 2,048 of 17 52.5 / 50.8 (the chip starts some 420 workgroups a us), 4,288 of few 63.8 / 55.1
+  if (rows <= 1024) hipLaunchKernelGGL((shared_join_kernel<F32, G, 4>), dim3((unsigned)rows), dim3(4 * kWave), 0, stream, a);
   else hipLaunchKernelGGL((shared_join_kernel<F32, G, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(kThreads), 0, stream, a);
   return hipGetLastError();
 }
