@@ -5,10 +5,11 @@
 // all the group's requests on P keys), then each request's own keys behind its prefix (g heads on n - P keys); a request that shares nothing has all its
 // keys there.  Every item's result is partial: row maximum, sum, sum of weighted V, in binary32; a row's two items are added up at the end.
 //
-// shared_plan_kernel writes the list: who is in which group, what each item has and where its blocks are numbered.
-// shared_prefix_kernel (bf16) forms prefixes of many rows: workgroups of 128 rows that share chunks of 64 keys in LDS, as cross.hip has them, each an equal
+// The list says who is in which group, what each item has and where its blocks are numbered.  Up to 256 requests and 255 groups each workgroup makes it
+// for itself, in LDS; otherwise shared_plan_kernel writes it before.
+// shared_prefix (bf16) forms prefixes of many rows: workgroups of 128 rows that share chunks of 64 keys in LDS, as cross.hip has them, each an equal
 //   run of all such chunks, so that few groups fill the chip and many short ones do, too.
-// shared_run_kernel forms everything else in units of 16 rows of one (item, K/V head), cut into equal runs of blocks by wave, as decode.hip.
+// shared_run forms everything else in units of 16 rows of one (item, K/V head), cut into equal runs of blocks by wave, as decode.hip.
 // shared_join_kernel adds up an output row's parts.
 //
 // Bound by memory where own keys prevail, by the prefixes' products and the partial results' way through memory otherwise.
@@ -94,6 +95,17 @@ __device__ __forceinline__ int shared_scan(int x, int& all, int* part, Op op, in
   }
   __syncthreads();
   return op(x, before);
+}
+
+// What the list adds up to: blocks of shared_run, chunks of shared_prefix, chunks of a run of the latter, waves of the former.
+// One workgroup of prefixes a compute unit up to 16 chunks each, beside it one that has runs, then two.  Each leaves up to two partial results of 128
+// rows, so that more of them cost the join what they save: 64 requests of a prefix of 16,000 tokens (4,016 chunks) in 502 runs of 8 66.6 us, in
+// 251 of 16 61.8, and 58.4 with the runs on the other half of the workgroups.
+__device__ __forceinline__ int shared_sum(const SharedArgs& a, int blocks, int chunks, int which) {
+  if (which < 2) return which ? chunks : blocks;
+  if (which == 3) return (int64_t)chunks * 128 >= (int64_t)blocks * a.d.D ? a.d.waves / 2 : a.d.waves;
+  const int one = chunks > 0 ? (chunks - 1) / (a.wgs / 2) + 1 : 0, two = chunks > 0 ? (chunks - 1) / a.wgs + 1 : 0;
+  return max(max(one < kSharedMost ? one : kSharedMost, two), kSharedLeast);
 }
 
 // Groups of the plan: in LDS while each has a thread, otherwise in the workspace, where what this launch has written is read past the
@@ -213,18 +225,16 @@ __global__ __launch_bounds__(NT) void shared_plan_kernel(const SharedArgs a) {
     }
     begun += all;
   }
-  if (tid == 0) {
-    a.sums[0] = begun;
-    a.sums[1] = begun1;
-    // One workgroup of prefixes a compute unit up to 16 chunks each, beside it one that has runs, then two.  Each leaves up to two partial results of 128
-    // rows, so that more of them cost the join what they save: 64 requests of a prefix of 16,000 tokens (4,016 chunks) in 502 runs of 8 66.6 us, in
-    // 251 of 16 61.8, and 58.4 with the runs on the other half of the workgroups.
-    const int one = begun1 > 0 ? (begun1 - 1) / (a.wgs / 2) + 1 : 0, two = begun1 > 0 ? (begun1 - 1) / a.wgs + 1 : 0;
-    const int some = one < kSharedMost ? one : kSharedMost;
-    a.sums[2] = max(max(some, two), kSharedLeast);
-    a.sums[3] = (int64_t)begun1 * 128 >= (int64_t)begun * a.d.D ? a.d.waves / 2 : a.d.waves;
-  }
+  if (tid < 4) a.sums[tid] = shared_sum(a, begun, begun1, tid);
 }
+
+// The list of few requests and groups, in LDS: each workgroup makes its own and needs no launch before it.
+constexpr int kSmall = 256;
+struct SharedSmall {
+  int first[kSmall + 1], leader[kSmall], count[kSmall], len[kSmall], start1[kSmall];
+  int tokens[kSmall], key0[kSmall], group[kSmall], start[2 * kSmall];
+  int sums[4], part[kThreads / kWave], part1[kThreads / kWave];
+};
 
 // The last of n items that begins at block x or before it (items without a block begin where the next one does).  64 looked at a step.
 __device__ __forceinline__ int shared_locate(const int32_t* start, int n, int x, int lane) {
@@ -246,6 +256,112 @@ __device__ __forceinline__ SharedItem shared_item(const SharedItem* items, int i
   it.keys = p->keys; it.key0 = p->key0; it.row = p->row; it.b0 = p->b0; it.R = p->R; it.rbs = p->rbs; it.start = p->start; it.group = p->group;
   return it;
 }
+// What a kernel knows of the list: from the workspace, or (SMALL) from its own.
+template <int BK, int UNIT, bool SMALL>
+struct SharedList {
+  const SharedArgs& a;
+  SharedSmall* s;
+  __device__ __forceinline__ int sum(int k) const { return SMALL ? __builtin_amdgcn_readfirstlane(s->sums[k]) : a.sums[k]; }
+  __device__ __forceinline__ int start(int i) const { return SMALL ? s->start[i] : a.start[i]; }
+  __device__ __forceinline__ int locate(int x, int lane) const {
+    return SMALL ? shared_locate(s->start, a.G + a.d.B, x, lane) : shared_locate(a.start, a.G + a.d.B, x, lane);
+  }
+  __device__ __forceinline__ int locate1(int x, int lane) const {
+    return SMALL ? shared_locate(s->start1, a.G, x, lane) : shared_locate(a.start1, a.G, x, lane);
+  }
+  __device__ __forceinline__ SharedItem group(int i) const {   // SMALL
+    SharedItem it = {0, 0, 0, 0, 0, 1, 0, 0};
+    if (s->count[i] > 1) {
+      it.keys = s->len[i];
+      it.row = s->leader[i];
+      it.b0 = s->first[i];
+      it.R = (s->first[i + 1] - it.b0) * a.g;
+      it.group = it.R >= a.big_rows;
+      it.rbs = it.group ? (it.R + kSharedRows - 1) / kSharedRows : (it.R + UNIT - 1) / UNIT;
+    }
+    it.start = it.group ? s->start1[i] : s->start[i];
+    return it;
+  }
+  __device__ __forceinline__ SharedItem request(int b) const {   // SMALL
+    const int key0 = s->key0[b];
+    return SharedItem{s->tokens[b] - key0, key0, b, b, a.g, a.own_rbs, s->start[a.G + b], s->group[b]};
+  }
+  __device__ __forceinline__ SharedItem item(int i) const {   // uniform
+    if (!SMALL) return shared_item(a.item, i);
+    SharedItem it = i < a.G ? group(i) : request(i - a.G);
+    int* f = reinterpret_cast<int*>(&it);
+#pragma unroll
+    for (int k = 0; k < (int)(sizeof(it) / 4); ++k) f[k] = __builtin_amdgcn_readfirstlane(f[k]);
+    return it;
+  }
+  __device__ __forceinline__ int cost(const SharedItem& it) const {   // blocks of an item that shared_run forms
+    return it.keys > 0 ? a.d.Hkv * it.rbs * ((it.keys + BK - 1) / BK + kUnitCost) : 0;
+  }
+  __device__ __forceinline__ int cost1(const SharedItem& it) const {   // chunks of one that shared_prefix forms
+    return a.d.Hkv * it.rbs * ((it.keys + kSharedChunk - 1) / kSharedChunk + kSharedUnitCost);
+  }
+  // B <= kSmall, G < kSmall, kThreads threads.  `write`: into the workspace, too, for the join.
+  __device__ __forceinline__ void plan(bool write) {
+    const int tid = threadIdx.x, B = a.d.B, G = a.G, cap = a.d.Sk;
+    const int n = tid < B ? min(max(a.d.len[tid], 0), cap) : 0;
+    const int P = tid < G ? min(max(a.share_len[tid], 0), cap) : 0;
+    const int f = tid <= G ? min(max(a.share_first[tid], 0), B) : 0;
+    auto add = [](int x, int y) { return x + y; };
+    auto top = [](int x, int y) { return max(x, y); };
+    int all, all1;
+    const int first = shared_scan<kThreads>(f, all, s->part, top, 0);
+    s->len[tid] = P;
+    s->leader[tid] = B;
+    s->count[tid] = 0;
+    s->tokens[tid] = n;
+    if (tid <= G) s->first[tid] = first;
+    __syncthreads();
+    int q = -1;
+    if (tid < B) {
+      int lo = -1, hi = G;   // as in shared_plan_kernel
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (s->first[mid] <= tid) lo = mid;
+        else hi = mid;
+      }
+      if (lo >= 0 && tid < s->first[lo + 1]) q = lo;
+      if (q >= 0 && s->len[q] > 0 && n >= s->len[q]) {
+        atomicMin(&s->leader[q], tid);
+        atomicAdd(&s->count[q], 1);
+      }
+    }
+    s->group[tid] = q;
+    __syncthreads();
+    SharedItem it = {0, 0, 0, 0, 0, 1, 0, 0};
+    if (tid < G) it = group(tid);   // (its start is not known yet)
+    const int c = it.group ? 0 : cost(it), c1 = it.group ? cost1(it) : 0;
+    const int upto = shared_scan<kThreads>(c, all, s->part, add, 0), upto1 = shared_scan<kThreads>(c1, all1, s->part1, add, 0);
+    if (tid < G) {
+      it.start = it.group ? upto1 - c1 : upto - c;
+      s->start[tid] = upto - c;
+      s->start1[tid] = upto1 - c1;
+      if (write) a.item[tid] = it;
+    }
+    SharedItem own = {0, 0, 0, 0, 0, 1, 0, -1};
+    s->key0[tid] = q >= 0 && n >= s->len[q] && s->count[q] > 1 ? s->len[q] : 0;
+    if (tid < B) own = request(tid);
+    const int co = tid < B ? cost(own) : 0;
+    int all_own;
+    const int own_upto = all + shared_scan<kThreads>(co, all_own, s->part, add, 0);
+    if (tid < B) {
+      own.start = own_upto - co;
+      s->start[G + tid] = own.start;
+      if (write) a.item[G + tid] = own;
+    }
+    if (tid < 4) {
+      const int v = shared_sum(a, all + all_own, all1, tid);
+      s->sums[tid] = v;
+      if (write) a.sums[tid] = v;
+    }
+    __syncthreads();
+  }
+};
+
 // Row r of K/V head hk of an item, in Q, O and the records.
 __device__ __forceinline__ size_t shared_row(const SharedArgs& a, int b0, int hk, int r) {
   const int n = a.by_g.div(r);
@@ -258,22 +374,22 @@ struct SharedBlock {
   SharedItem it;
 };
 
-template <class Core>
-__device__ __forceinline__ void shared_run(const SharedArgs& a, unsigned char* lds) {   // lds: the wave's Core::LDS bytes
+template <class Core, class List>
+__device__ __forceinline__ void shared_run(const SharedArgs& a, const List& list, unsigned char* lds) {   // lds: the wave's Core::LDS bytes
   typedef typename Core::Elt Elt;
   constexpr int BK = Core::BK, KPL = Core::KPL, RB = Core::RB, UNIT = RB * kDecodeRows;
   const DecodeArgs& d = a.d;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // where prefixes are most of the work, the second half of the workgroups has the runs
-  const int waves = a.sums[3], n_items = a.G + d.B, run = blockIdx.x * 4 + wave - (d.waves - waves);
-  const int total = a.sums[0], per = run_length(total, waves);
+  const int waves = list.sum(3), n_items = a.G + d.B, run = blockIdx.x * 4 + wave - (d.waves - waves);
+  const int total = list.sum(0), per = run_length(total, waves);
   if (run < 0 || (int64_t)run * per >= total) return;
   Core core(d, lds, lane);
   const int D = core.dim();
 
   auto item = [&](SharedBlock& s, int i) {
     s.i = i;
-    s.it = shared_item(a.item, i);
+    s.it = list.item(i);
     s.unit = 0;
     s.nb = (s.it.keys + BK - 1) / BK;
   };
@@ -286,7 +402,7 @@ __device__ __forceinline__ void shared_run(const SharedArgs& a, unsigned char* l
       const int done = s.it.start + s.unit * (s.nb + kUnitCost);
       int i = s.i + 1;
       for (;; i += kWave) {   // (there is one)
-        const unsigned long long up = __ballot(i + lane + 1 >= n_items || a.start[i + lane + 1] > done);
+        const unsigned long long up = __ballot(i + lane + 1 >= n_items || list.start(i + lane + 1) > done);
         if (up) {
           i += (int)__builtin_ctzll(up);
           break;
@@ -299,7 +415,7 @@ __device__ __forceinline__ void shared_run(const SharedArgs& a, unsigned char* l
   SharedBlock now, then, later;
   {
     const int x = run * per;
-    item(now, shared_locate(a.start, n_items, x, lane));
+    item(now, list.locate(x, lane));
     now.left = min(per, total - x);
     const int in = x - now.it.start, cost = now.nb + kUnitCost;
     now.unit = in / cost;
@@ -408,31 +524,33 @@ __device__ __forceinline__ void shared_run(const SharedArgs& a, unsigned char* l
 
 // ---- prefixes of many rows
 // FAR: the cache is larger than a buffer load's 32 bits reach.
-template <int D, bool FAR>
-__device__ __forceinline__ void shared_prefix(const SharedArgs& a, bf16_t* kb0, bf16_t* vb0, bf16_t* kb1, bf16_t* vb1) {
+template <int D, bool FAR, class List>
+__device__ __forceinline__ void shared_prefix(const SharedArgs& a, const List& list, bf16_t* kb0, bf16_t* vb0, bf16_t* kb1, bf16_t* vb1) {
   constexpr int PPR = D / 8, NCOPY = kSharedChunk * PPR / kWave / 4, UNIT = SharedBf16<D>::RB * kDecodeRows;
   typedef typename std::conditional<FAR, int64_t, uint32_t>::type Place;   // elements from the head's first row of the first page; FAR or bytes
   const DecodeArgs& d = a.d;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int il = lane & 31, kh = lane >> 5;
-  const int total = a.sums[1], per = a.sums[2];
-  if ((int64_t)blockIdx.x * per >= total) return;
+  const int total = list.sum(1), per = list.sum(2);
+  // runs that follow one another are workgroups with ids equal mod 8 (one XCD): the row blocks of a head read K and V from its L2 after the first
+  const int eighth = ((total - 1) / per + 8) / 8, run = (blockIdx.x & 7) * eighth + (blockIdx.x >> 3);
+  if ((int)(blockIdx.x >> 3) >= eighth || (int64_t)run * per >= total) return;
   // copies as in cross.hip
   const int slot0 = kWave * wave + lane, crow = slot0 / PPR, cpos = slot0 % PPR;
   const int kpiece = 8 * (cpos ^ k_piece_swizzle<D>(crow)), vpiece = 8 * (cpos ^ v_piece_swizzle<D>(crow));
   StreamTile<D> tile(d.scale_log2e, lane);
   const uint32_t bytes = FAR ? 0 : (uint32_t)(((int64_t)(d.n_pages - 1) * d.page_stride + d.head_stride) * 2);   // of a head, in all pages
 
-  int x = blockIdx.x * per;
+  int x = run * per;
   const int end = min(total, x + per);
-  int i = shared_locate(a.start1, a.G, x, lane);
+  int i = list.locate1(x, lane);
   while (x < end) {
-    const SharedItem it = shared_item(a.item, i);
+    const SharedItem it = list.item(i);
     const int nc = (it.keys + kSharedChunk - 1) / kSharedChunk, cost = nc + kSharedUnitCost;
     const int in = x - it.start, unit = in / cost, c0 = in - unit * cost, c1 = min(nc, c0 + end - x);
     if (unit >= d.Hkv * it.rbs) {   // the next group that has chunks
-      i = shared_locate(a.start1, a.G, x, lane);
+      i = list.locate1(x, lane);
       continue;
     }
     if (c0 >= nc) {   // behind a unit's last chunk
@@ -528,7 +646,7 @@ __device__ __forceinline__ void shared_prefix(const SharedArgs& a, bf16_t* kb0, 
       const size_t rows = shared_rows(a);
       const size_t rec = c0 == 0 && c1 == nc ? rows + shared_row(a, it.b0, hk, r)
                                              : 2 * rows + (size_t)2 * d.waves * UNIT +
-                                                   (size_t)(2 * blockIdx.x + (c0 == 0)) * kSharedRows + kRowsPerWave * wave + il;
+                                                   (size_t)(2 * run + (c0 == 0)) * kSharedRows + kRowsPerWave * wave + il;
       float* to = a.part + rec * D + 4 * kh;
 #pragma unroll
       for (int db = 0; db < D / 32; ++db)
@@ -547,22 +665,47 @@ __device__ __forceinline__ void shared_prefix(const SharedArgs& a, bf16_t* kb0, 
 }
 
 template <class Core>
+using SharedListOf = SharedList<Core::BK, Core::RB * kDecodeRows, true>;
+template <class Core>
+using SharedListIn = SharedList<Core::BK, Core::RB * kDecodeRows, false>;
+
+template <class Core, bool SMALL>
 __global__ __launch_bounds__(kThreads, Core::WGS) void shared_run_kernel(const SharedArgs a) {
   __shared__ __attribute__((aligned(16))) unsigned char lds[Core::LDS ? 4 * Core::LDS : 16];
-  shared_run<Core>(a, lds + (Core::LDS ? (threadIdx.x >> 6) * Core::LDS : 0));
+  unsigned char* mine = lds + (Core::LDS ? (threadIdx.x >> 6) * Core::LDS : 0);
+  if constexpr (SMALL) {
+    __shared__ SharedSmall small;
+    SharedListOf<Core> list{a, &small};
+    list.plan(blockIdx.x == 0);
+    shared_run<Core>(a, list, mine);
+  } else {
+    shared_run<Core>(a, SharedListIn<Core>{a, nullptr}, mine);
+  }
 }
 // Both in one launch: a workgroup has its share of the one and of the other.
-template <int D, bool FAR>
+template <int D, bool FAR, bool SMALL>
 __global__ __launch_bounds__(kThreads, 2) void shared_both_kernel(const SharedArgs a) {
+  typedef SharedBf16<D> Core;
   __shared__ __attribute__((aligned(16))) bf16_t kb0[kSharedChunk * D];
   __shared__ __attribute__((aligned(16))) bf16_t vb0[kSharedChunk * D];
   __shared__ __attribute__((aligned(16))) bf16_t kb1[kSharedChunk * D];
   __shared__ __attribute__((aligned(16))) bf16_t vb1[kSharedChunk * D];
-  static_assert(DecodeBf16<D>::LDS <= (int)sizeof(kb0), "a wave's V tile in a stage");
-  shared_prefix<D, FAR>(a, kb0, vb0, kb1, vb1);
-  __syncthreads();
+  static_assert(Core::LDS <= (int)sizeof(kb0), "a wave's V tile in a stage");
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  shared_run<SharedBf16<D>>(a, reinterpret_cast<unsigned char*>(wave == 0 ? kb0 : wave == 1 ? vb0 : wave == 2 ? kb1 : vb1));
+  unsigned char* mine = reinterpret_cast<unsigned char*>(wave == 0 ? kb0 : wave == 1 ? vb0 : wave == 2 ? kb1 : vb1);
+  auto both = [&](const auto& list) __attribute__((always_inline)) {
+    shared_prefix<D, FAR>(a, list, kb0, vb0, kb1, vb1);
+    __syncthreads();
+    shared_run<Core>(a, list, mine);
+  };
+  if constexpr (SMALL) {
+    __shared__ SharedSmall small;
+    SharedListOf<Core> list{a, &small};
+    list.plan(blockIdx.x == 0);
+    both(list);
+  } else {
+    both(SharedListIn<Core>{a, nullptr});
+  }
 }
 
 // ---- parts of an output row
@@ -719,19 +862,25 @@ static hipError_t launch_shared_as(SharedArgs& a, bool big, hipStream_t stream) 
   constexpr int G = Core::NP * 4, UNIT = Core::RB * kDecodeRows;
   a.d.waves = 4 * 256 * Core::WGS;
   a.own_rbs = (a.g + UNIT - 1) / UNIT;
-  if (a.G <= 256 && a.d.B <= 256) hipLaunchKernelGGL((shared_plan_kernel<Core::BK, UNIT, 256, true>), dim3(1), dim3(256), 0, stream, a);
-  else if (a.G <= 1024) hipLaunchKernelGGL((shared_plan_kernel<Core::BK, UNIT, 1024, true>), dim3(1), dim3(1024), 0, stream, a);
-  else hipLaunchKernelGGL((shared_plan_kernel<Core::BK, UNIT, 1024, false>), dim3(1), dim3(1024), 0, stream, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  const bool small = a.d.B <= kSmall && a.G < kSmall;
+  hipError_t e = hipSuccess;
+  if (!small) {
+    if (a.G <= 1024) hipLaunchKernelGGL((shared_plan_kernel<Core::BK, UNIT, 1024, true>), dim3(1), dim3(1024), 0, stream, a);
+    else hipLaunchKernelGGL((shared_plan_kernel<Core::BK, UNIT, 1024, false>), dim3(1), dim3(1024), 0, stream, a);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  auto go = [&](auto kernel, int wgs) { hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(kThreads), 0, stream, a); };
+  const int wgs = a.d.waves / 4;
   if constexpr (!F32) {
     static_assert(Core::WGS == 2, "a workgroup has a share of both");
-    const bool far = ((double)a.d.n_pages * (double)a.d.page_stride) * 2 >= 4294967296.0;
-    if (big && far) hipLaunchKernelGGL((shared_both_kernel<Core::NP * 16, true>), dim3((unsigned)a.wgs), dim3(kThreads), 0, stream, a);
-    else if (big) hipLaunchKernelGGL((shared_both_kernel<Core::NP * 16, false>), dim3((unsigned)a.wgs), dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL((shared_run_kernel<Core>), dim3((unsigned)(a.d.waves / 4)), dim3(kThreads), 0, stream, a);
+    constexpr int D = Core::NP * 16;
+    const bool far = (double)a.d.n_pages * (double)a.d.page_stride * 2 >= 4294967296.0;
+    if (big && far) small ? go(&shared_both_kernel<D, true, true>, a.wgs) : go(&shared_both_kernel<D, true, false>, a.wgs);
+    else if (big) small ? go(&shared_both_kernel<D, false, true>, a.wgs) : go(&shared_both_kernel<D, false, false>, a.wgs);
+    else small ? go(&shared_run_kernel<Core, true>, wgs) : go(&shared_run_kernel<Core, false>, wgs);
   } else {
-    hipLaunchKernelGGL((shared_run_kernel<Core>), dim3((unsigned)(a.d.waves / 4)), dim3(kThreads), 0, stream, a);
+    small ? go(&shared_run_kernel<Core, true>, wgs) : go(&shared_run_kernel<Core, false>, wgs);
   }
   e = hipGetLastError();
   if (e != hipSuccess) return e;
