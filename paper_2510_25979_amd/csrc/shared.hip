@@ -20,8 +20,8 @@
 
 namespace ac {
 
-constexpr int kSharedRows = 128, kSharedChunk = kStreamChunk;   // of a workgroup of shared_prefix_kernel
-constexpr int kSharedWgs = 512;                       // most workgroups of it
+constexpr int kSharedRows = 128, kSharedChunk = kStreamChunk;   // of a workgroup of shared_prefix
+constexpr int kSharedWgs = 512;                       // most workgroups
 constexpr int kSharedLeast = 4, kSharedMost = 16;     // chunks of a run: at least; at most while there is one for each compute unit (see the plan)
 constexpr int kSharedUnitCost = 1;                    // what a unit of it costs beside its chunks
 
@@ -29,7 +29,7 @@ struct SharedItem {
   int keys, key0, row;     // keys [key0, key0 + keys) of the request whose table has them
   int b0, R;               // rows of a K/V head: the g heads of requests b0, b0 + 1, ...
   int rbs, start;          // row blocks of a K/V head; number of the first block
-  int group;               // of a request: its group's number, -1: shares nothing; of a group: 1 if shared_prefix_kernel forms it
+  int group;               // of a request: its group's number, -1: shares nothing; of a group: 1 if shared_prefix forms it
 };
 
 struct SharedArgs {
@@ -38,9 +38,17 @@ struct SharedArgs {
   int32_t *sums, *first, *leader, *count, *start, *start1;   // sums: blocks of all items, chunks of all prefixes, chunks of a run
   SharedItem* item;        // [G + B]
   float *part, *stat;      // partial results: rows' own whole ones, rows' prefixes' whole ones, two of each run
-  int32_t G, g, own_rbs, big_rows, wgs;   // big_rows: rows from which on shared_prefix_kernel forms a prefix
+  int32_t G, g, own_rbs, big_rows, big_keys, wgs;   // see shared_is_big
   Divider by_g;
 };
+
+// Whether shared_prefix forms a prefix: one of more than 32 rows, or of more than 16 where it is long and a head has 128 columns.  us, 32 rows a wave / workgroups of 128:
+// 64 rows a group, prefixes of 16,000 tokens 43.4 / 28.8, eight of 2,000 53.1 / 40.7, 16 of 4,000 of 64 columns 69.3 / 57.4; 48 rows, eight of 2,000 48.7 /
+// 38.2; 96 rows 70.6 / 51.7; 32 rows, one of 16,000 34.2 / 26.7, eight of 4,000 55.5 / 46.1, four of 1,000 23.4 / 25.3, 64 of 500 107 / 112; of 64 columns
+// 16 of 4,000 45.3 / 44.5, of 24 rows 41.9 / 43.8; 20 rows, one of 16,000 31.1 / 25.4.
+__device__ __forceinline__ int shared_is_big(const SharedArgs& a, int R, int keys) {
+  return R > a.big_rows || (R > kDecodeRows && keys >= a.big_keys);
+}
 
 // A wave's work on a block for two blocks of 16 rows, which share the keys' way from memory (the second may be empty): a prefix of eight requests of
 // four heads is read once and not twice.
@@ -115,7 +123,7 @@ __device__ __forceinline__ int shared_peek(const int* p) {
   return LDS ? *p : __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// Bound by latency: lengths and groups -> who shares -> sums -> list.  64 requests 14.3 us with the groups in the workspace, LDS_US so.
+// Bound by latency: lengths and groups -> who shares -> sums -> list.  64 requests 14.3 us with the groups in the workspace, 6.0 so.
 template <int BK, int UNIT, int NT, bool LDS>   // keys of a block, rows of a unit, threads
 __global__ __launch_bounds__(NT) void shared_plan_kernel(const SharedArgs a) {
   __shared__ int part[NT / kWave], part1[NT / kWave];
@@ -179,7 +187,7 @@ __global__ __launch_bounds__(NT) void shared_plan_kernel(const SharedArgs a) {
       it.row = shared_peek<LDS>(leader + i);
       it.b0 = f;
       it.R = n * a.g;
-      it.group = it.R >= a.big_rows;
+      it.group = shared_is_big(a, it.R, it.keys);
       if (it.group) {
         it.rbs = (it.R + kSharedRows - 1) / kSharedRows;
         cost1 = a.d.Hkv * it.rbs * ((it.keys + kSharedChunk - 1) / kSharedChunk + kSharedUnitCost);
@@ -276,7 +284,7 @@ struct SharedList {
       it.row = s->leader[i];
       it.b0 = s->first[i];
       it.R = (s->first[i + 1] - it.b0) * a.g;
-      it.group = it.R >= a.big_rows;
+      it.group = shared_is_big(a, it.R, it.keys);
       it.rbs = it.group ? (it.R + kSharedRows - 1) / kSharedRows : (it.R + UNIT - 1) / UNIT;
     }
     it.start = it.group ? s->start1[i] : s->start[i];
@@ -533,9 +541,8 @@ __device__ __forceinline__ void shared_prefix(const SharedArgs& a, const List& l
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int il = lane & 31, kh = lane >> 5;
   const int total = list.sum(1), per = list.sum(2);
-  // runs that follow one another are workgroups with ids equal mod 8 (one XCD): the row blocks of a head read K and V from its L2 after the first
-  const int eighth = ((total - 1) / per + 8) / 8, run = (blockIdx.x & 7) * eighth + (blockIdx.x >> 3);
-  if ((int)(blockIdx.x >> 3) >= eighth || (int64_t)run * per >= total) return;
+  const int run = blockIdx.x;   // (neighbouring runs on one XCD, which then share K and V in its L2: as long, at two row blocks a head and at eight)
+  if ((int64_t)run * per >= total) return;
   // copies as in cross.hip
   const int slot0 = kWave * wave + lane, crow = slot0 / PPR, cpos = slot0 % PPR;
   const int kpiece = 8 * (cpos ^ k_piece_swizzle<D>(crow)), vpiece = 8 * (cpos ^ v_piece_swizzle<D>(crow));
@@ -843,7 +850,7 @@ __global__ __launch_bounds__(NW == 1 ? kThreads : NW * kWave) void shared_join_k
 static size_t shared_ints(int64_t B, int64_t G) {   // sums, first, leader, count, start, start1, items; in whole pieces of 16 bytes
   return (size_t)((4 + (G + 1) + G + G + (G + B) + G + 3) / 4 * 4 + (G + B) * (int64_t)(sizeof(SharedItem) / 4));
 }
-static bool shared_big(int64_t B, int32_t g, int32_t D) { return (D == 64 || D == 128) && B * g > 2 * kDecodeRows; }   // some group may have many rows
+static bool shared_big(int64_t B, int32_t g, int32_t D) { return (D == 64 || D == 128) && B * g > kDecodeRows; }   // some group may have many rows
 static size_t shared_records(int64_t B, int64_t Hq, int32_t g, int32_t D) {
   return (size_t)(2 * B * Hq) + (size_t)2 * kDecodeWaves * 2 * kDecodeRows + (shared_big(B, g, D) ? (size_t)2 * kSharedWgs * kSharedRows : 0);
 }
@@ -898,7 +905,8 @@ hipError_t launch_shared(const SharedLaunch& p, hipStream_t stream) {
   a.share_first = p.share_first; a.share_len = p.share_len;
   a.by_g = Divider((uint32_t)a.g);
   const bool big = !p.d.is_f32 && shared_big(p.d.B, a.g, p.d.D);
-  a.big_rows = big ? 33 : 0x7fffffff;
+  a.big_rows = big ? 2 * kDecodeRows : 0x7fffffff;
+  a.big_keys = big && p.d.D == 128 ? 2048 : 0x7fffffff;
   a.wgs = kSharedWgs;
   const int64_t B = p.d.B, G = p.G;
   int32_t* ws = static_cast<int32_t*>(p.d.ws);
