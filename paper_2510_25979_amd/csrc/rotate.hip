@@ -3,15 +3,14 @@
 //   y = x / sqrt(mean(x^2) + eps) * w                       of each Q and K head, where weights are given
 //   (a, b) -> amp (a cos t - b sin t, b cos t + a sin t)    of its first `rot` columns in pairs, t = position * freq[pair]
 //
-// Bound by memory: every element is read once from HBM and written once (K and V twice where they go to the cache, too).  A workgroup
-// takes a few tokens and some or all of their heads.  It forms the sines and cosines of its tokens once, in LDS; G lanes share a head, a lane
-// keeps its columns, and the other half of a pair that is not in its own piece is loaded a second time (from L1).
+// Bound by memory: every element is read once from HBM and written once (K and V twice where they go to the cache, too): 32 prompts of up to 1,024 tokens,
+// 48 heads of 64 (232 MB) 50 us = 4.7 TB/s, 4,000 tokens of 48 heads of 128 25.  A workgroup takes a few tokens and some or all of their heads.  It forms
+// the sines and cosines of its tokens once, through LDS; the other half of a pair that is not in a lane's own piece is loaded a second time (from L1).
+// Few tokens are bound by latency, position -> angle -> store, 128 of one token each 5.2 us.
 //
 // Angles: a position is a whole number, and only the fraction of a turn counts.  freq / 2 pi is taken modulo one turn as a 64-bit
 // fixed-point number, whose product with the position wraps by itself: the angle is off by 2^-52 of itself, as freq is, at any position, where
 // a binary32 product would be off by a turn at 10^7.
-#include <type_traits>
-
 #include "common.hpp"
 #include "serve.h"
 
@@ -24,182 +23,214 @@ struct RotateArgs {
   const double* freq;
   void *Q, *K, *V, *kp, *vp;
   int64_t batch_stride, row_stride, page_stride;   // elements
-  int32_t S, Hq, Hkv, D, half, n_tokens, tokens, heads, n_slots, ps, begin;   // tokens and heads of a workgroup; begin: its first token's number / tokens
-  Divider by_s, by_ps, by_tokens, by_half;
+  int32_t S, Hq, Hkv, D, half, n_tokens, heads, n_slots, ps, begin;   // heads of a workgroup; begin: of the launch's groups of tokens
+  Divider by_s, by_ps, by_half;
   float eps, amp;
   int32_t interleaved;
 };
 
-constexpr int kRotateTokens = 16;    // most tokens of a workgroup
-constexpr int kRotateAngles = 512;   // and angles (one token may have 128)
-
+// VEC columns of a row as they lie in memory: 16 bytes, or 1 column where a row or a pair's other half is no whole number of those.
 template <typename T, int VEC>
-struct RotateVec {
+struct RotatePiece {
   T v[VEC];
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (VEC * sizeof(T) % 16 == 0) {
+      struct Words { u32x4 w[VEC * sizeof(T) / 16]; };
+      *this = __builtin_bit_cast(RotatePiece, *reinterpret_cast<const Words*>(p));
+    } else {
+      v[0] = p[0];
+    }
+  }
+  __device__ __forceinline__ void store(T* p) const {
+    if constexpr (VEC * sizeof(T) == 16) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, *this), reinterpret_cast<u32x4*>(p));
+    else p[0] = v[0];
+  }
 };
-template <typename T, int VEC>
-__device__ __forceinline__ void rotate_load(float (&x)[VEC], const T* p) {
-  if constexpr (VEC * sizeof(T) == 16) {
-    const auto r = __builtin_bit_cast(RotateVec<T, VEC>, *reinterpret_cast<const u32x4*>(p));
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) x[i] = (float)r.v[i];
-  } else {
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) x[i] = (float)p[i];
-  }
-}
-template <typename T, int VEC>
-__device__ __forceinline__ void rotate_store(T* p, const float (&x)[VEC]) {
-  if constexpr (VEC * sizeof(T) == 16) {
-    RotateVec<T, VEC> r;
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) r.v[i] = (T)x[i];   // results are rounded once, to nearest even
-    __builtin_nontemporal_store(__builtin_bit_cast(u32x4, r), reinterpret_cast<u32x4*>(p));
-  } else {
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) p[i] = (T)x[i];
-  }
-}
 
-// VEC: columns of a piece (16 bytes, or 1 where a row or a pair's other half is no whole number of those); G lanes a head; NP pieces a lane.
-template <typename T, int VEC, int G, int NP>
+// G lanes a row, NP pieces a lane: a wave has 64 / G tokens, and a lane keeps its token and its columns, so that addresses, sines, cosines and weights are the
+// lane's for all heads, of which the wave takes every fourth, U at a time.  (With heads dealt to threads and tables of tokens in LDS the vector work of
+// addresses took longer than the memory: 59 us and 87 where it is 50 and 25 now.)
+template <typename T, int VEC, int G, int NP, int U>
 __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a) {
-  constexpr int RPP = kThreads / G;   // heads that the workgroup deals with at once
-  __shared__ float2 turn[kRotateAngles];
-  __shared__ int64_t in_at[kRotateTokens], page_at[kRotateTokens], out_b[kRotateTokens];   // out_b: the item's number, -1: nothing to do
-  __shared__ int out_s[kRotateTokens];
-  const int tid = threadIdx.x, lane = tid % G, sub = tid / G, D = a.D, half = a.half;
-  const int t0 = (a.begin + blockIdx.x) * a.tokens, n = min(a.tokens, a.n_tokens - t0);
-  const int h0 = blockIdx.y * a.heads, nh = min(a.heads, a.Hq + 2 * a.Hkv - h0);
-  if (tid < n) {
-    const int b = a.by_s.div(t0 + tid), s = t0 + tid - b * a.S;
-    const bool real = a.pos[t0 + tid] >= 0;
-    out_b[tid] = real ? b : -1;
-    out_s[tid] = s;
-    in_at[tid] = b * a.batch_stride + s * a.row_stride;
-    int64_t at = -1;
-    if (real && a.slot) {
-      const int slot = a.slot[t0 + tid];
-      if ((unsigned)slot < (unsigned)a.n_slots) {
-        const int page = a.by_ps.div(slot);
-        at = page * a.page_stride + (int64_t)(slot - page * a.ps) * D;
-      }
-    }
-    page_at[tid] = at;
-  }
-  if (h0 < a.Hq + a.Hkv)
-    for (int i = tid; i < n * half; i += kThreads) {
-      const int t = a.by_half.div(i);
-      double f = a.freq[i - t * half] * 0.15915494309189533577;
-      f -= floor(f);
-      const uint64_t step = (uint64_t)(f * 18446744073709551616.0);
-      const int32_t frac = (int32_t)((step * (uint64_t)(uint32_t)max(a.pos[t0 + t], 0)) >> 32);   // of a turn, from -1/2 on
-      float s, c;
-      sincospif((float)frac * 4.656612873077392578125e-10f, &s, &c);   // 2^-31: half turns
-      turn[i] = make_float2(c * a.amp, s * a.amp);
-    }
-  __syncthreads();
-  const int rows = nh * n;
-  const T* X = static_cast<const T*>(a.X);
-  for (int r = sub; r < rows; r += RPP) {   // (token fastest: rows of one head and neighbouring tokens lie side by side in the outputs)
-    const int hh = n == a.tokens ? a.by_tokens.div(r) : r / n, t = r - hh * n, h = h0 + hh;
-    const int64_t b = out_b[t];
-    if (b < 0) continue;   // (all lanes of the head)
-    const T* x = X + in_at[t] + (int64_t)h * D;
-    const int kind = h < a.Hq ? 0 : h < a.Hq + a.Hkv ? 1 : 2;
-    const float* w = kind == 0 ? a.qw : kind == 1 ? a.kw : nullptr;
-    float y[NP][VEC], z[NP][VEC];   // a piece, and for pairs across halves the other one's
+  typedef RotatePiece<T, VEC> Piece;
+  constexpr int TOKENS = kWave / G, CS = VEC > 1 ? VEC : 1;
+  __shared__ float2 turn[kThreads];   // (TOKENS * half <= kThreads)
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), D = a.D, half = a.half;
+  const int sub = (tid & 63) / G, lane = tid % G;
+  const int first = (a.begin + blockIdx.x) * TOKENS, token = min(first + sub, a.n_tokens - 1);
+  const int h0 = blockIdx.y * a.heads + wave, h1 = min(blockIdx.y * a.heads + a.heads, a.Hq + 2 * a.Hkv), rotated = a.Hq + a.Hkv;
+  const bool real = first + sub < a.n_tokens && a.pos[token] >= 0;
+  const int b = a.by_s.div(token), s = token - b * a.S;
+  const T* x = static_cast<const T*>(a.X) + b * a.batch_stride + s * a.row_stride;
+  auto other = [&](int c) { return a.interleaved ? c ^ 1 : c < half ? c + half : c - half; };   // of a pair's columns
+  const bool apart = !a.interleaved || VEC == 1;   // a pair's other half is not in the lane's piece
+  Piece y[U][NP], z[U][NP];
+  auto fetch = [&](int u, int h) {
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       const int c = VEC * (lane + G * i);
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) y[i][e] = z[i][e] = 0.f;
       if (c < D) {
-        rotate_load<T, VEC>(y[i], x + c);
-        if (kind < 2 && c < 2 * half) {
-          if (!a.interleaved) rotate_load<T, VEC>(z[i], x + (c < half ? c + half : c - half));
-          else if (VEC == 1) rotate_load<T, VEC>(z[i], x + (c ^ 1));
-        }
+        y[u][i].load(x + (int64_t)h * D + c);
+        if (apart && h < rotated && c < 2 * half) z[u][i].load(x + (int64_t)h * D + other(c));
       }
     }
-    if (w) {
+  };
+  // (where there are few tokens they are asked for before it is known whether they are padding)
+  const bool early = gridDim.y > 1;
+  if (early)
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (h0 + 4 * u < h1) fetch(u, h0 + 4 * u);
+  // the weights of the lane's columns and of their pairs' other halves, of the kind of head that they were last loaded for
+  RotatePiece<float, VEC> wy[NP], wz[NP];
+  int weights_of = -1;
+  auto weights = [&](int kind) {   // 0, 1: Q, K
+    const float* w = kind == 0 ? a.qw : a.kw;
+    if (!w || weights_of == kind) return;
+    weights_of = kind;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int c = VEC * (lane + G * i);
+      if (c < D) {
+        wy[i].load(w + c);
+        if (apart && c < 2 * half) wz[i].load(w + other(c));
+      }
+    }
+  };
+  if (h0 < rotated) weights(h0 < a.Hq ? 0 : 1);
+  if (!__syncthreads_or(real)) return;   // padding
+  if (real && !early)
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (h0 + 4 * u < h1) fetch(u, h0 + 4 * u);
+  // one angle a thread
+  if (blockIdx.y * a.heads < rotated && tid < TOKENS * half) {
+    const int t = a.by_half.div(tid);
+    double f = a.freq[tid - t * half] * 0.15915494309189533577;
+    f -= floor(f);
+    const uint64_t step = (uint64_t)(f * 18446744073709551616.0);
+    const int32_t frac = (int32_t)((step * (uint64_t)(uint32_t)max(a.pos[min(first + t, a.n_tokens - 1)], 0)) >> 32);   // of a turn, from -1/2 on
+    float sn, cn;
+    sincospif((float)frac * 4.656612873077392578125e-10f, &sn, &cn);   // 2^-31: half turns
+    turn[tid] = make_float2(cn * a.amp, sn * a.amp);
+  }
+  __syncthreads();
+  if (!real) return;
+  float2 cs[NP][CS];   // of the lane's columns; the sine's sign is the first half's
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    const int c = VEC * (lane + G * i);
+    if (c < 2 * half) {
+      if (apart) {
+        const int o = other(c), pair = a.interleaved ? c >> 1 : min(c, o);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          cs[i][e] = turn[sub * half + pair + e];
+          if (c < o) cs[i][e].y = -cs[i][e].y;
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < VEC / 2; ++e)
+          if (c + 2 * e < 2 * half) cs[i][e] = turn[sub * half + (c >> 1) + e];
+      }
+    }
+  }
+  int64_t page = -1;
+  if (a.slot) {
+    const int slot = a.slot[token];
+    if ((unsigned)slot < (unsigned)a.n_slots) {
+      const int p = a.by_ps.div(slot);
+      page = p * a.page_stride + (int64_t)(slot - p * a.ps) * D;
+    }
+  }
+  const int64_t head = (int64_t)a.S * D, page_head = (int64_t)a.ps * D;   // elements from head to head
+  T* Q = static_cast<T*>(a.Q) + b * a.Hq * head + (int64_t)s * D;
+  const int64_t kv = b * a.Hkv * head + (int64_t)s * D;
+  auto finish = [&](int u, int h) {   // (h, and which kind it is of, is the wave's)
+    const int kind = h < a.Hq ? 0 : h < rotated ? 1 : 2, hk = h - a.Hq - (kind == 2 ? a.Hkv : 0);
+    const float* weight = kind == 0 ? a.qw : kind == 1 ? a.kw : nullptr;
+    if (kind < 2) weights(kind);
+    float inv = 1.f;
+    if (weight) {
       float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < NP; ++i)
+        if (VEC * (lane + G * i) < D)
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) sum = fmaf(y[i][e], y[i][e], sum);
+          for (int e = 0; e < VEC; ++e) sum = fmaf((float)y[u][i].v[e], (float)y[u][i].v[e], sum);
 #pragma unroll
       for (int off = G / 2; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
-      const float inv = 1.f / sqrtf(sum / (float)D + a.eps);
-#pragma unroll
-      for (int i = 0; i < NP; ++i) {
-        const int c = VEC * (lane + G * i);
-        if (c >= D) continue;
-        const int o = a.interleaved ? c ^ 1 : c < half ? c + half : c - half;   // (read only where it is a pair's other half)
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          y[i][e] *= inv * w[c + e];
-          if (c < 2 * half && (!a.interleaved || VEC == 1)) z[i][e] *= inv * w[o + e];
-        }
-      }
+      inv = 1.f / sqrtf(sum / (float)D + a.eps);
     }
-    const float2* cs = turn + t * half;
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       const int c = VEC * (lane + G * i);
       if (c >= D) continue;
-      if (kind < 2 && c < 2 * half) {
-        if (!a.interleaved || VEC == 1) {
-          const bool first = a.interleaved ? !(c & 1) : c < half;
-          const int p = a.interleaved ? c >> 1 : first ? c : c - half;
+      Piece out = y[u][i];
+      if (kind < 2) {   // results are rounded once, to nearest even
+        float p[VEC];
 #pragma unroll
-          for (int e = 0; e < VEC; ++e) {
-            const float2 f = cs[p + e];
-            y[i][e] = first ? y[i][e] * f.x - z[i][e] * f.y : y[i][e] * f.x + z[i][e] * f.y;
-          }
-        } else if constexpr (VEC > 1) {
+        for (int e = 0; e < VEC; ++e) p[e] = (float)y[u][i].v[e];
+        if (weight)
 #pragma unroll
-          for (int e = 0; e < VEC; e += 2)
-            if (c + e < 2 * half) {
-              const float2 f = cs[(c + e) >> 1];
-              const float u = y[i][e], v = y[i][e + 1];
-              y[i][e] = u * f.x - v * f.y;
-              y[i][e + 1] = v * f.x + u * f.y;
+          for (int e = 0; e < VEC; ++e) p[e] *= inv * wy[i].v[e];
+        if (c < 2 * half) {
+          if (apart) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+              float q = (float)z[u][i].v[e];
+              if (weight) q *= inv * wz[i].v[e];
+              p[e] = p[e] * cs[i][e].x + q * cs[i][e].y;
             }
+          } else if constexpr (VEC > 1) {
+#pragma unroll
+            for (int e = 0; e < VEC; e += 2)
+              if (c + e < 2 * half) {
+                const float2 f = cs[i][e / 2];
+                const float u0 = p[e], u1 = p[e + 1];
+                p[e] = u0 * f.x - u1 * f.y;
+                p[e + 1] = u1 * f.x + u0 * f.y;
+              }
+          }
         }
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) out.v[e] = (T)p[e];
       }
-      const int s = out_s[t];
       if (kind == 0) {
-        rotate_store<T, VEC>(static_cast<T*>(a.Q) + ((b * a.Hq + h) * a.S + s) * D + c, y[i]);
+        out.store(Q + h * head + c);
       } else {
-        const int hk = h - a.Hq - (kind == 2 ? a.Hkv : 0);
         T* dense = static_cast<T*>(kind == 1 ? a.K : a.V);
-        if (dense) rotate_store<T, VEC>(dense + ((b * a.Hkv + hk) * a.S + s) * D + c, y[i]);
-        if (page_at[t] >= 0)
-          rotate_store<T, VEC>(static_cast<T*>(kind == 1 ? a.kp : a.vp) + page_at[t] + (int64_t)hk * a.ps * D + c, y[i]);
+        if (dense) out.store(dense + kv + hk * head + c);
+        if (page >= 0) out.store(static_cast<T*>(kind == 1 ? a.kp : a.vp) + page + hk * page_head + c);
       }
     }
+  };
+  for (int h = h0; h < h1; h += 4 * U) {
+    if (h != h0)
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (h + 4 * u < h1) fetch(u, h + 4 * u);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (h + 4 * u < h1) finish(u, h + 4 * u);
   }
 }
 
-template <typename T, int VEC, int G, int NP>
+template <typename T, int VEC, int G, int NP, int U>
 static hipError_t launch_rotate_as(RotateArgs a, hipStream_t stream) {
-  const int all = a.Hq + 2 * a.Hkv, RPP = kThreads / G;
-  // tokens of a workgroup: as many as there are angles for 256 threads, while there are workgroups enough
-  int t = a.half ? (kThreads + a.half - 1) / a.half : kRotateTokens;
-  t = t < kRotateTokens ? t : kRotateTokens;
-  while (t > 1 && a.n_tokens / t < 1024) t >>= 1;
-  a.tokens = t;
-  // heads: all of them, or what the threads deal with at once where there are few tokens
-  const int64_t blocks = ((int64_t)a.n_tokens + t - 1) / t;
-  a.heads = blocks >= 1024 ? all : RPP / t > 1 ? RPP / t : 1;
-  a.by_tokens = Divider((uint32_t)a.tokens);
+  constexpr int TOKENS = kWave / G;
+  const int all = a.Hq + 2 * a.Hkv;
+  const int64_t blocks = ((int64_t)a.n_tokens + TOKENS - 1) / TOKENS;
+  // heads of a workgroup: all of them where there are many tokens, otherwise so few that there are some 2,048 workgroups
+  const int64_t parts = blocks >= 2048 ? 1 : 2048 / blocks;
+  int heads = (int)((all + parts - 1) / parts);
+  a.heads = heads < 4 ? 4 : (heads + 3) / 4 * 4;
   const unsigned gy = (unsigned)((all + a.heads - 1) / a.heads);
   const int64_t most = 1 << 23;
   for (int64_t begin = 0; begin < blocks; begin += most) {
     a.begin = (int)begin;
     const int64_t wgs = blocks - begin < most ? blocks - begin : most;
-    hipLaunchKernelGGL((rotate_kernel<T, VEC, G, NP>), dim3((unsigned)wgs, gy), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((rotate_kernel<T, VEC, G, NP, U>), dim3((unsigned)wgs, gy), dim3(kThreads), 0, stream, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -224,17 +255,17 @@ hipError_t launch_rotate(const RotateLaunch& p, hipStream_t stream) {
   const bool whole = p.D % vec == 0 && p.row_stride % vec == 0 && p.batch_stride % vec == 0 &&
                      (p.interleaved || a.half % vec == 0);
   if (!p.is_f32) {
-    if (whole) return p.D == 64 ? launch_rotate_as<bf16_t, 8, 8, 1>(a, stream) : launch_rotate_as<bf16_t, 8, 16, 1>(a, stream);
-    return p.D == 64 ? launch_rotate_as<bf16_t, 1, 64, 1>(a, stream) : launch_rotate_as<bf16_t, 1, 64, 2>(a, stream);
+    if (whole) return p.D == 64 ? launch_rotate_as<bf16_t, 8, 8, 1, 4>(a, stream) : launch_rotate_as<bf16_t, 8, 16, 1, 3>(a, stream);
+    return p.D == 64 ? launch_rotate_as<bf16_t, 1, 64, 1, 4>(a, stream) : launch_rotate_as<bf16_t, 1, 64, 2, 4>(a, stream);
   }
   if (whole) {
-    if (p.D <= 64) return launch_rotate_as<float, 4, 16, 1>(a, stream);
-    if (p.D <= 128) return launch_rotate_as<float, 4, 32, 1>(a, stream);
-    return launch_rotate_as<float, 4, 64, 1>(a, stream);
+    if (p.D <= 64) return launch_rotate_as<float, 4, 16, 1, 3>(a, stream);
+    if (p.D <= 128) return launch_rotate_as<float, 4, 32, 1, 3>(a, stream);
+    return launch_rotate_as<float, 4, 64, 1, 3>(a, stream);
   }
-  if (p.D <= 64) return launch_rotate_as<float, 1, 64, 1>(a, stream);
-  if (p.D <= 128) return launch_rotate_as<float, 1, 64, 2>(a, stream);
-  return launch_rotate_as<float, 1, 64, 4>(a, stream);
+  if (p.D <= 64) return launch_rotate_as<float, 1, 64, 1, 4>(a, stream);
+  if (p.D <= 128) return launch_rotate_as<float, 1, 64, 2, 4>(a, stream);
+  return launch_rotate_as<float, 1, 64, 4, 2>(a, stream);
 }
 
 }  // namespace ac
