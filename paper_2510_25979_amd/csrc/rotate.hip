@@ -50,7 +50,7 @@ struct RotatePiece {
 // G lanes a row, NP pieces a lane: a wave has 64 / G tokens, and a lane keeps its token and its columns, so that addresses, sines, cosines and weights are the
 // lane's for all heads, of which the wave takes every fourth, U at a time.  (With heads dealt to threads and tables of tokens in LDS the vector work of
 // addresses took longer than the memory: 59 us and 87 where it is 50 and 25 now.)
-template <typename T, int VEC, int G, int NP, int U>
+template <typename T, int VEC, int G, int NP, int U, bool NORM>
 __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a) {
   typedef RotatePiece<T, VEC> Piece;
   constexpr int TOKENS = kWave / G, CS = VEC > 1 ? VEC : 1;
@@ -82,14 +82,14 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a) {
     for (int u = 0; u < U; ++u)
       if (h0 + 4 * u < h1) fetch(u, h0 + 4 * u);
   // the weights of the lane's columns and of their pairs' other halves, of the kind of head that they were last loaded for
-  RotatePiece<float, VEC> wy[NP], wz[NP];
+  RotatePiece<float, VEC> wy[NORM ? NP : 1], wz[NORM ? NP : 1];
   int weights_of = -1;
   auto weights = [&](int kind) {   // 0, 1: Q, K
     const float* w = kind == 0 ? a.qw : a.kw;
-    if (!w || weights_of == kind) return;
+    if (!NORM || !w || weights_of == kind) return;
     weights_of = kind;
 #pragma unroll
-    for (int i = 0; i < NP; ++i) {
+    for (int i = 0; i < (NORM ? NP : 1); ++i) {
       const int c = VEC * (lane + G * i);
       if (c < D) {
         wy[i].load(w + c);
@@ -148,7 +148,7 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a) {
   const int64_t kv = b * a.Hkv * head + (int64_t)s * D;
   auto finish = [&](int u, int h) {   // (h, and which kind it is of, is the wave's)
     const int kind = h < a.Hq ? 0 : h < rotated ? 1 : 2, hk = h - a.Hq - (kind == 2 ? a.Hkv : 0);
-    const float* weight = kind == 0 ? a.qw : kind == 1 ? a.kw : nullptr;
+    const bool weight = NORM && (kind == 0 ? a.qw : kind == 1 ? a.kw : nullptr) != nullptr;
     if (kind < 2) weights(kind);
     float inv = 1.f;
     if (weight) {
@@ -173,13 +173,13 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a) {
         for (int e = 0; e < VEC; ++e) p[e] = (float)y[u][i].v[e];
         if (weight)
 #pragma unroll
-          for (int e = 0; e < VEC; ++e) p[e] *= inv * wy[i].v[e];
+          for (int e = 0; e < VEC; ++e) p[e] *= inv * wy[NORM ? i : 0].v[e];
         if (c < 2 * half) {
           if (apart) {
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
               float q = (float)z[u][i].v[e];
-              if (weight) q *= inv * wz[i].v[e];
+              if (weight) q *= inv * wz[NORM ? i : 0].v[e];
               p[e] = p[e] * cs[i][e].x + q * cs[i][e].y;
             }
           } else if constexpr (VEC > 1) {
@@ -216,7 +216,7 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a) {
   }
 }
 
-template <typename T, int VEC, int G, int NP, int U>
+template <typename T, int VEC, int G, int NP, int U, int UN = U>   // UN: without weights
 static hipError_t launch_rotate_as(RotateArgs a, hipStream_t stream) {
   constexpr int TOKENS = kWave / G;
   const int all = a.Hq + 2 * a.Hkv;
@@ -230,7 +230,8 @@ static hipError_t launch_rotate_as(RotateArgs a, hipStream_t stream) {
   for (int64_t begin = 0; begin < blocks; begin += most) {
     a.begin = (int)begin;
     const int64_t wgs = blocks - begin < most ? blocks - begin : most;
-    hipLaunchKernelGGL((rotate_kernel<T, VEC, G, NP, U>), dim3((unsigned)wgs, gy), dim3(kThreads), 0, stream, a);
+    if (a.qw || a.kw) hipLaunchKernelGGL((rotate_kernel<T, VEC, G, NP, U, true>), dim3((unsigned)wgs, gy), dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL((rotate_kernel<T, VEC, G, NP, UN, false>), dim3((unsigned)wgs, gy), dim3(kThreads), 0, stream, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -255,7 +256,7 @@ hipError_t launch_rotate(const RotateLaunch& p, hipStream_t stream) {
   const bool whole = p.D % vec == 0 && p.row_stride % vec == 0 && p.batch_stride % vec == 0 &&
                      (p.interleaved || a.half % vec == 0);
   if (!p.is_f32) {
-    if (whole) return p.D == 64 ? launch_rotate_as<bf16_t, 8, 8, 1, 4>(a, stream) : launch_rotate_as<bf16_t, 8, 16, 1, 3>(a, stream);
+    if (whole) return p.D == 64 ? launch_rotate_as<bf16_t, 8, 8, 1, 2, 3>(a, stream) : launch_rotate_as<bf16_t, 8, 16, 1, 3>(a, stream);
     return p.D == 64 ? launch_rotate_as<bf16_t, 1, 64, 1, 4>(a, stream) : launch_rotate_as<bf16_t, 1, 64, 2, 4>(a, stream);
   }
   if (whole) {
