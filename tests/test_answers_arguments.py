@@ -1,0 +1,174 @@
+"""What the operators of several answers to long prompts refuse, before anything is launched, and the frequencies of rotated heads.  Host code,
+no GPU: the pointers are never followed."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+OK, NULL, SHAPE, DTYPE, ALIGN, WORKSPACE, MEMSPACE = 0, -1, -2, -3, -4, -6, -9
+P, F32, F16, BF16 = 1 << 20, 0, 1, 2
+BIG = 1 << 40
+
+
+@pytest.fixture(scope="module")
+def L():
+    from paper_2510_25979_amd import binding
+    return binding.lib()
+
+
+def _call(fn, names, given, **change):
+    values = dict(zip(names.split(), given))
+    assert not set(change) - set(values), change
+    values.update(change)
+    return fn(*values.values())
+
+
+def _rotate(L, **change):
+    return _call(L.attncache_rotate, "X qw kw pos freq slot Q K V kp vp B S Hq Hkv D rot batch row n page stride dtype inter eps amp stream",
+                 [P] * 11 + [4, 3, 4, 2, 64, 64, 3 * 8 * 64, 8 * 64, 10, 16, 2 * 16 * 64, BF16, 0, 1e-6, 1.0, None], **change)
+
+
+def _fork(L, **change):
+    return _call(L.attncache_page_fork, "source seq state ring table table_out seq_out state_out kp vp B H D max_pages n page stride sinks window dtype ws ws_bytes stream",
+                 [P] * 10 + [4, 2, 64, 8, 10, 16, 2 * 16 * 64, 0, 0, BF16, P, BIG, None], **change)
+
+
+def _shared(L, **change):
+    return _call(L.attention_paged_shared, "Q kp vp table len first share O B Hq Hkv D G n page max_pages stride dtype scale ws ws_bytes stream",
+                 [P] * 8 + [4, 8, 2, 64, 2, 10, 16, 8, 2 * 16 * 64, BF16, 0.0, P, BIG, None], **change)
+
+
+def _window(L, **change):
+    return _call(L.attention_window, "Q K V O sel len B Hq Hkv S D dtype window sinks scale stream",
+                 [P] * 6 + [4, 8, 2, 50, 64, BF16, 10, 2, 0.0, None], **change)
+
+
+def _step(L, **change):
+    return _call(L.attention_paged_window, "Q kp vp table len O B Hq Hkv D n page max_pages stride dtype window sinks scale ws ws_bytes stream",
+                 [P] * 6 + [4, 8, 2, 64, 10, 16, 8, 2 * 16 * 64, BF16, 10, 2, 0.0, P, BIG, None], **change)
+
+
+@pytest.mark.parametrize("call,change,status", [
+    *[(_rotate, {n: None}, NULL) for n in "X pos freq Q K V kp vp".split()], (_rotate, dict(K=None, V=None, slot=None), NULL),
+    *[(_rotate, {n: P + 8}, ALIGN) for n in "X qw kw Q K V kp vp".split()],
+    *[(_rotate, {n: 0}, SHAPE) for n in "S Hq Hkv D n page".split()],
+    (_rotate, dict(B=-1), SHAPE), (_rotate, dict(D=96), SHAPE), (_rotate, dict(D=257, dtype=F32, row=BIG, stride=BIG), SHAPE), (_rotate, dict(dtype=F16), DTYPE),
+    (_rotate, dict(rot=65), SHAPE), (_rotate, dict(rot=66), SHAPE), (_rotate, dict(rot=-2), SHAPE), (_rotate, dict(row=8 * 64 - 1), SHAPE), (_rotate, dict(row=8 * 64 + 4), ALIGN),
+    (_rotate, dict(batch=3 * 8 * 64 + 4), ALIGN), (_rotate, dict(batch=-8), SHAPE), (_rotate, dict(Hq=65533, row=BIG), SHAPE), (_rotate, dict(B=1 << 20, S=1 << 11), SHAPE),
+    (_rotate, dict(row=1 << 60), SHAPE), (_rotate, dict(batch=1 << 62), SHAPE), (_rotate, dict(eps=-1.0), SHAPE), (_rotate, dict(eps=float("nan")), SHAPE),
+    (_rotate, dict(amp=float("inf")), SHAPE), (_rotate, dict(stride=2 * 16 * 64 - 1), SHAPE), (_rotate, dict(stride=2 * 16 * 64 + 4), ALIGN), (_rotate, dict(B=0), OK),
+    (_rotate, dict(B=0, X=None, kp=None), OK), (_rotate, dict(B=0, batch=4), OK),
+    *[(_fork, {n: None}, NULL) for n in "source seq state ring table table_out seq_out state_out kp vp ws".split()],
+    *[(_fork, {n: P + 8}, ALIGN) for n in "kp vp ws".split()], *[(_fork, {n: 0}, SHAPE) for n in "H D max_pages n page".split()],
+    (_fork, dict(B=-1), SHAPE), (_fork, dict(B=(1 << 22) + 1), SHAPE), (_fork, dict(B=1 << 11, max_pages=1 << 20), SHAPE), (_fork, dict(max_pages=(1 << 26) + 1, B=1), SHAPE),
+    (_fork, dict(sinks=-1), SHAPE), (_fork, dict(window=-1), SHAPE), (_fork, dict(dtype=F16), DTYPE), (_fork, dict(D=96), SHAPE), (_fork, dict(ws_bytes=100), WORKSPACE),
+    (_fork, dict(stride=2 * 16 * 64 - 1), SHAPE), (_fork, dict(stride=2 * 16 * 64 + 4), ALIGN), (_fork, dict(n=1 << 27), SHAPE), (_fork, dict(B=0), OK), (_fork, dict(B=0, ws=None), OK),
+    (_fork, dict(page=1 << 25, n=2, max_pages=1, stride=1 << 40, D=64), SHAPE),
+    *[(_shared, {n: None}, NULL) for n in "Q kp vp table len first share O ws".split()], *[(_shared, {n: P + 8}, ALIGN) for n in "Q kp vp O ws".split()],
+    *[(_shared, {n: 0}, SHAPE) for n in "Hq Hkv D n page max_pages".split()],
+    (_shared, dict(Hq=9), SHAPE), (_shared, dict(B=-1), SHAPE), (_shared, dict(G=-1), SHAPE), (_shared, dict(G=(1 << 20) + 1), SHAPE), (_shared, dict(B=(1 << 20) + 1), SHAPE),
+    (_shared, dict(D=32), SHAPE), (_shared, dict(dtype=F16), DTYPE), (_shared, dict(scale=-1.0), SHAPE), (_shared, dict(scale=float("nan")), SHAPE), (_shared, dict(ws_bytes=1000), WORKSPACE),
+    (_shared, dict(max_pages=1 << 27), SHAPE), (_shared, dict(max_pages=(1 << 26) + 1, B=1, Hq=1, Hkv=1), SHAPE), (_shared, dict(B=1 << 16, max_pages=1 << 20), SHAPE),
+    (_shared, dict(G=1 << 16, max_pages=1 << 20), SHAPE), (_shared, dict(stride=2 * 16 * 64 - 8), SHAPE), (_shared, dict(stride=2 * 16 * 64 + 4), ALIGN), (_shared, dict(B=0), OK),
+    *[(_window, {n: None}, NULL) for n in "Q K V O".split()], *[(_window, {n: P + 8}, ALIGN) for n in "Q K V O".split()],
+    *[(_window, {n: 0}, SHAPE) for n in "Hq Hkv S D window".split()],
+    (_window, dict(Hq=9), SHAPE), (_window, dict(B=-1), SHAPE), (_window, dict(D=96), SHAPE), (_window, dict(dtype=F32, D=257), SHAPE), (_window, dict(dtype=F16), DTYPE),
+    (_window, dict(window=-1), SHAPE), (_window, dict(sinks=-1), SHAPE), (_window, dict(scale=-1.0), SHAPE), (_window, dict(S=1 << 23), SHAPE), (_window, dict(B=1 << 28, Hq=2, Hkv=2), SHAPE),
+    (_window, dict(B=1 << 28, Hq=8, Hkv=1), SHAPE), (_window, dict(B=0), OK),
+    *[(_step, {n: None}, NULL) for n in "Q kp vp table len O ws".split()], *[(_step, {n: P + 8}, ALIGN) for n in "Q kp vp O ws".split()],
+    *[(_step, {n: 0}, SHAPE) for n in "Hq Hkv D n page max_pages window".split()],
+    (_step, dict(Hq=9), SHAPE), (_step, dict(B=-1), SHAPE), (_step, dict(sinks=-1), SHAPE), (_step, dict(window=-5), SHAPE), (_step, dict(D=32), SHAPE), (_step, dict(dtype=F16), DTYPE),
+    (_step, dict(scale=-1.0), SHAPE), (_step, dict(ws_bytes=1000), WORKSPACE), (_step, dict(max_pages=(1 << 26) + 1, B=1, Hq=1, Hkv=1), SHAPE),
+    (_step, dict(B=1 << 16, max_pages=1 << 20, window=1 << 24), SHAPE), (_step, dict(stride=2 * 16 * 64 + 4), ALIGN), (_step, dict(B=0), OK),
+], ids=lambda x: x.__name__[1:] if callable(x) else str(x))
+def test_refusals(L, call, change, status):
+    assert call(L, **change) == status
+
+
+def test_workspace_sizes():
+    from paper_2510_25979_amd import binding as ac
+    fork, shared = ac.attncache_page_fork_workspace_bytes, ac.attention_paged_shared_workspace_bytes
+    assert fork(0, 8, 10) == fork(4, 0, 10) == fork(4, 8, 0) == fork(1 << 23, 8, 10) == fork(1 << 16, 1 << 16, 10) == 0
+    assert 0 < fork(4, 8, 10) < fork(5, 8, 10) < fork(5, 9, 10) < fork(5, 9, 1000)
+    assert shared(0, 8, 2, 64, 1) == shared(1, 8, 3, 64, 1) == shared(1, 8, 2, 0, 1) == shared(1, 8, 2, 64, -1) == shared(1, 8, 2, 300, 1) == shared(1 << 21, 8, 2, 64, 1) == 0
+    assert 0 < shared(1, 8, 2, 64, 0) < shared(2, 8, 2, 64, 0) < shared(2, 8, 2, 64, 3) < shared(2, 8, 2, 128, 3)
+    # prefixes of many rows need room for their partial results; binary32 dimensions have none
+    assert shared(5, 8, 2, 64, 1) - shared(4, 8, 2, 64, 1) > 1 << 24 > shared(5, 8, 2, 80, 1) - shared(4, 8, 2, 80, 1)
+
+
+def test_the_binding_names_what_is_wrong():
+    from paper_2510_25979_amd import binding as ac
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    q, pages, kv = torch.zeros(2, 4, 64).bfloat16(), torch.zeros(5, 2, 16, 64).bfloat16(), torch.zeros(2, 4, 3, 64).bfloat16()
+    X, freq = torch.zeros(2, 3, 8 * 64).bfloat16(), torch.zeros(32, dtype=torch.float64)
+    for call, what in (
+            (lambda: ac.attncache_rotate(X, i32(2, 3), freq, kv, kv[:, :2], kv[:, :2]), "X must be a CUDA tensor"),
+            (lambda: ac.attncache_rotate(X[0], i32(2, 3), freq, kv), "X must be"),
+            (lambda: ac.attncache_rotate(X.half(), i32(2, 3), freq, kv), "unsupported dtype"),
+            (lambda: ac.attncache_rotate(X[:, :, :7 * 64], i32(2, 3), freq, kv), "must hold 4"),
+            (lambda: ac.attncache_rotate(X[:, :, :4 * 64], i32(2, 3), freq, kv), "must hold 4"),
+            (lambda: ac.attncache_rotate(X, i32(2, 3), freq, kv, kv[:, :2]), "K and V must be given both"),
+            (lambda: ac.attncache_rotate(X, i32(2, 3), freq, kv), "need a place"),
+            (lambda: ac.attncache_rotate(X, i32(2, 3), freq, kv, slot=i32(2, 3)), "given all, or none"),
+            (lambda: ac.attncache_page_fork(i32(2), i32(2), i32(2), i32(5), i32(2), i32(2, 3), i32(2), i32(2), pages, pages, i32(99)), "page_table must be"),
+            (lambda: ac.attncache_page_fork(i32(2), i32(2), i32(2), i32(5), i32(2, 3), i32(2, 3), i32(2), i32(2), pages.half(), pages, i32(99)), "unsupported"),
+            (lambda: ac.attncache_page_fork(i32(2), i32(2), i32(2), i32(5), i32(2, 3), i32(2, 3), i32(2), i32(2), pages, pages, i32(99)), "k_pages must be a CUDA"),
+            (lambda: ac.attention_paged_shared(q, pages, pages, i32(2, 3), i32(2), i32(2), i32(1), q, q), "Q must be a CUDA tensor"),
+            (lambda: ac.attention_paged_shared(q, pages, pages, i32(2, 3), i32(2), i32(2), i32(1, 1), q, q), "share_len"),
+            (lambda: ac.attention_paged_shared(q.half(), pages, pages, i32(2, 3), i32(2), i32(2), i32(1), q, q), "unsupported dtype"),
+            (lambda: ac.attention_window(kv, kv, kv, kv, window=3), "Q must be a CUDA tensor"),
+            (lambda: ac.attention_window(kv[0], kv, kv, kv, window=3), "Q must be"),
+            (lambda: ac.attention_window(kv.half(), kv, kv, kv, window=3), "unsupported dtype"),
+            (lambda: ac.attention_paged_window(q, pages, pages, i32(2, 3), i32(2), q, q, window=3), "Q must be a CUDA tensor"),
+            (lambda: ac.attention_paged_window(q[0], pages, pages, i32(2, 3), i32(2), q, q, window=3), "Q must be")):
+        with pytest.raises(ValueError, match=what):
+            call()
+
+
+def test_host_memory_is_refused_where_there_is_a_gpu(L):
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU to tell memory apart")
+    host = (ctypes.c_char * 4096)()
+    at = ctypes.addressof(host) + 15 & ~15
+    for call, name in ((_rotate, "pos"), (_fork, "source"), (_shared, "first"), (_window, "O"), (_step, "O")):
+        assert call(L, **{name: at}) == MEMSPACE
+
+
+def _frequencies(L, rot=64, base=10000.0, scaling=0, factor=8.0, original=4096.0, low=1.0, high=4.0, out=True):
+    freq = (ctypes.c_double * max(rot // 2, 1))()
+    return L.attncache_rotary_frequencies(freq if out else None, rot, base, scaling, factor, original, low, high), list(freq)
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(rot=0), SHAPE), (dict(rot=3), SHAPE), (dict(rot=-4), SHAPE), (dict(base=0.0), SHAPE), (dict(base=-1.0), SHAPE), (dict(base=float("inf")), SHAPE),
+    (dict(base=float("nan")), SHAPE), (dict(scaling=4), DTYPE), (dict(scaling=-1), DTYPE), (dict(scaling=1, factor=0.0), SHAPE), (dict(scaling=1, factor=float("inf")), SHAPE),
+    (dict(scaling=0, factor=0.0), OK), (dict(scaling=2, rot=2), SHAPE), (dict(scaling=3, original=0.0), SHAPE), (dict(scaling=3, low=4.0), SHAPE),
+    (dict(scaling=3, high=float("nan")), SHAPE), (dict(out=False), NULL), (dict(rot=2), OK)])
+def test_frequencies_that_are_refused(L, change, status):
+    assert _frequencies(L, **change)[0] == status
+
+
+@pytest.mark.parametrize("rot,base", [(2, 10000.0), (64, 10000.0), (128, 500000.0), (10, 7.0)])
+def test_frequencies(L, rot, base):
+    """The formulas, by logarithms: a power is off by a few units in its last place, 2^-48 is far beyond."""
+    i = range(rot // 2)
+    plain = [math.exp(-2.0 * k / rot * math.log(base)) for k in i]
+    near = lambda got, want: got[0] == OK and all(math.isclose(a, b, rel_tol=2.0 ** -46) for a, b in zip(got[1], want))  # noqa: E731
+    assert near(_frequencies(L, rot, base), plain)
+    assert near(_frequencies(L, rot, base, 1, 8.0), [f / 8 for f in plain])
+    if rot >= 4:
+        wide = base * 8.0 ** (rot / (rot - 2))
+        got = _frequencies(L, rot, base, 2, 8.0)
+        assert near(got, [math.exp(-2.0 * k / rot * math.log(wide)) for k in i])
+        assert got[1][0] == 1.0 and math.isclose(got[1][-1], plain[-1] / 8, rel_tol=1e-12)    # the fastest stays, the slowest is stretched
+    turns = [4096 * f / (2 * math.pi) for f in plain]
+    got = _frequencies(L, rot, base, 3, 8.0)
+    assert got[0] == OK
+    for f, p, t in zip(got[1], plain, turns):
+        want = p if t >= 4 else p / 8 if t <= 1 else p * ((t - 1) / 3 + (4 - t) / 3 / 8)
+        assert math.isclose(f, want, rel_tol=2.0 ** -44)
+    from paper_2510_25979_amd import binding as ac
+    assert ac.attncache_rotary_frequencies(rot, base=base).tolist() == _frequencies(L, rot, base)[1]
+    with pytest.raises(ac.AttnCacheError):
+        ac.attncache_rotary_frequencies(rot + 1)

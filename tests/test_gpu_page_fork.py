@@ -101,9 +101,15 @@ def cache(rng, B, p, hi, share=0.5, spare=20):
     return table, seq, ring, first, len(pages)
 
 
+# rows, page size, most tokens: one workgroup's work, and more rows, entries or pages than that
+PLACES = [(1, 16, 40), (2, 1, 9), (7, 4, 50), (33, 16, 300), (64, 10, 1000), (300, 16, 100), (1024, 8, 100), (1500, 8, 40), (5, 128, 2000), (4, 1, 5000)]
+TYPES = [(1, 64, "bf16", 0), (8, 128, "bf16", 64), (128, 64, "bf16", 0), (3, 33, "f32", 0), (2, 199, "f32", 5), (5, 256, "f32", 4), (1, 1, "f32", 0)]
+# rows, page size, pages of a row, pages
+LARGE = [(3000, 4, 3, 4000), (9, 16, 2000, 20000), (5, 4, 10, 70000)]
+
+
 @pytest.mark.parametrize("in_place", [False, True])
-@pytest.mark.parametrize("B,p,hi", [(1, 16, 40), (2, 1, 9), (7, 4, 50), (33, 16, 300), (64, 10, 1000), (300, 16, 100), (1500, 8, 40), (5, 128, 2000),
-                                    (4, 1, 5000)])
+@pytest.mark.parametrize("B,p,hi", PLACES)
 def test_rows_change_places(ac, B, p, hi, in_place):  # noqa: F811
     for seed in range(3):
         rng = random.Random(B + seed)
@@ -112,8 +118,7 @@ def test_rows_change_places(ac, B, p, hi, in_place):  # noqa: F811
         check(ac, table, seq, from_, ring, first, count, 2, p, 4, "f32", in_place)
 
 
-@pytest.mark.parametrize("H,D,dt,apart", [(1, 64, "bf16", 0), (8, 128, "bf16", 64), (128, 64, "bf16", 0), (3, 33, "f32", 0), (2, 199, "f32", 5), (5, 256, "f32", 4),
-                                          (1, 1, "f32", 0)])
+@pytest.mark.parametrize("H,D,dt,apart", TYPES)
 def test_types_and_strides(ac, H, D, dt, apart):  # noqa: F811
     rng = random.Random(D)
     table, seq, ring, first, count = cache(rng, 12, 16, 100)
@@ -146,6 +151,23 @@ def test_a_ring_that_runs_out(ac, in_place):  # noqa: F811
         got = check(ac, table, seq, [0, 0, 0, 0, -1], ring, 0, count, 1, p, 4, "f32", in_place)
         assert got[1] == [6] + [6 if i < count else -1 for i in range(3)] + [0]
         assert got[3] == [min(3, count), count - min(3, count) + 2]
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("B,p,width,n", LARGE)
+@pytest.mark.parametrize("dt,D", [("bf16", 64), ("f32", 33)])
+def test_more_than_a_workgroup_plans(ac, B, p, width, n, dt, D, in_place):  # noqa: F811
+    rng = random.Random(B)
+    pages = list(range(n))
+    rng.shuffle(pages)
+    seq = [rng.choice([0, 3, width * p, rng.randint(0, width * p)]) if b < 7 else rng.randint(0, 3) for b in range(B)]
+    table = [[pages.pop() for _ in range(-(-m // p))] for m in seq]
+    table = [t + [-1] * (width - len(t)) for t in table]
+    ring = [-1] * n
+    for i, q in enumerate(pages):
+        ring[(n - 5 + i) % n] = q
+    from_ = [rng.choice([b, rng.randrange(min(B, 7)), -1]) for b in range(B)]
+    check(ac, table, seq, from_, ring, n - 5, len(pages), 1, p, D, dt, in_place)
 
 
 def test_one_row_or_page_more_than_a_workgroup_and_a_word(ac):  # noqa: F811

@@ -67,7 +67,39 @@ CASES = [([(3000, [1] * 64)], [], 32, 8, 128, "bf16", 16), ([(16000, [5, 300] * 
          ([(640, [7] * 8)] * 40, [], 16, 2, 128, "bf16", 10), ([(9, [1] * 150)], [], 3, 3, 64, "bf16", 1), ([(700, [1] * 5)] * 2, [3], 40, 1, 64, "bf16", 16),
          ([(1500, [3, 900])] * 6, [20] * 9, 6, 2, 80, "f32", 10), ([(2000, [1] * 40)], [5], 4, 2, 128, "f32", 16), ([(300, [2] * 17)] * 5, [], 3, 1, 199, "f32", 7),
          ([(1030, [9] * 3)] * 3, [], 33, 1, 256, "f32", 32), ([(100, [1] * 4)] * 50, [7] * 30, 2, 2, 33, "f32", 16), ([(5000, [1, 2])], [], 4, 4, 64, "f32", 16),
-         ([(2000, [30] * 600)], [], 8, 8, 64, "bf16", 16), ([(512, [64] * 4)] * 300, [], 4, 1, 128, "bf16", 16)]
+         ([(2000, [30] * 600)], [], 8, 8, 64, "bf16", 16), ([(512, [64] * 4)] * 300, [], 4, 1, 128, "bf16", 16),
+         ([(100, [1, 2, 3])], [], 4, 1, 64, "bf16", 16), ([(3000, [1, 200])], [77], 10, 2, 128, "bf16", 16)]
+
+
+# more than 256 requests: the list is made before; few rows of a group, and many
+MANY = [([(50, [3] * 8)] * 40, [9] * 20, Hq, 1, D, dt, 16) for D, dt in TYPES for Hq in (1, 4)]
+MANY += [([(300, [5] * 20)] * 15, [700], 4, 2, D, "bf16", 16) for D in (64, 128)] + [([(40, [1])] * 300 + [(90, [2, 3] * 20)], [], 1, 1, 64, "bf16", 16)]
+MANY += [([(40, [1])] * 1100, [], 1, 1, D, dt, 16) for D, dt in ((64, "bf16"), (64, "f32"))]
+MANY += [([(40, [1, 2])] * 150, [], 1, 1, 64, "bf16", 16), ([(3000, [2] * 3)] * 3, [5], 32, 1, 128, "bf16", 16)]
+# caches of more than 4 GiB
+FAR, FAR_MANY, FAR_HEADS = [(400, [20] * 9), (90, [1, 2])], [(400, [20] * 130), (90, [1, 2] * 70)], [(4, 1, 64), (8, 2, 128)]
+
+
+@pytest.mark.parametrize("c", MANY, ids=lambda c: f"{len(c[0])}x{c[0][0][0]}x{len(c[0][0][1])}-{len(c[1])}-" + "-".join(map(str, c[2:])))
+def test_more_requests_than_a_workgroup_lists(ac, c):  # noqa: F811
+    case(ac, *c)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D", FAR_HEADS)
+@pytest.mark.parametrize("groups,stride", [(FAR, 1 << 24), (FAR_MANY, 1 << 20)], ids=["few", "many"])
+def test_a_cache_of_more_than_four_gib(ac, groups, stride, Hq, Hkv, D):  # noqa: F811
+    """Pages far apart: places beyond 2^32 bytes."""
+    c, first, share = build(groups, [3], Hkv, D, "bf16", 16)
+    n, at = c.k.shape[0], {}
+    for name in "kv":
+        old = getattr(c, name)
+        at[name] = torch.empty((n - 1) * stride + old[0].numel(), dtype=torch.bfloat16, device="cuda")
+        new = at[name].as_strided(old.shape, (stride, *old.stride()[1:]))
+        new.copy_(old)
+        setattr(c, name, new)
+    assert 2 ** 32 < n * stride * 2 < 2 ** 34
+    Q = torch.randn(len(c.rows), Hq, D, generator=c.gen, device="cuda").bfloat16()
+    c.check(call(ac, c, Q, first, share), Q, sorted(random.Random(1).sample(range(len(c.rows)), 8)))
 
 
 @pytest.mark.parametrize("page", [1, 7, 16, 48, 128])
@@ -103,13 +135,13 @@ def test_pages_that_lie_apart(ac, dt, more):  # noqa: F811
     case(ac, EDGES, [5], 4, 2, 128, dt, 16, more=more)
 
 
-@pytest.mark.parametrize("dt", ["bf16", "f32"])
-def test_it_is_attention_over_pages(ac, dt):  # noqa: F811
+@pytest.mark.parametrize("D,dt", TYPES)
+def test_it_is_attention_over_pages(ac, D, dt):  # noqa: F811
     """Whatever is said to be shared: groups out of order and range, of one or none, prefixes longer than the requests or negative."""
     lens = [100, 90, 200, 90, 5, 0, 300, 100]
-    c, first, share = build([(80, [20, 10, 120, 10])], [5, 0, 300, 100], 2, 64, dt, 16, blank=False)
+    c, first, share = build([(80, [20, 10, 120, 10])], [5, 0, 300, 100], 2, D, dt, 16, blank=False)
     assert c.len.tolist() == lens
-    Q = torch.randn(8, 4, 64, generator=c.gen, device="cuda").to(DT[dt])
+    Q = torch.randn(8, 4, D, generator=c.gen, device="cuda").to(DT[dt])
     i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
     for first, share in (([0, 4], [80]), ([0, 4], [50]), ([0, 4], [81 - 1]), ([0, 4, 4, 5, 8], [64, 9, 70, 0]), ([0, 8], [2 ** 31 - 1]), ([0, 8], [-7]),
                          ([-5, 4, 2, 4], [80, 80, 3]), ([0, 2, 1, 4], [80, 90, 80]), ([2, 4, 99], [80, 300]), ([8, 8], [80]), ([99, -1], [80]), ([0], []),

@@ -70,6 +70,8 @@ RUNS = [([70, 0, 4000, 31, 0, 0, 1, 5500], 40, 2, 64, "bf16", 16, 3000, 40), ([9
         ([1500] * 300, 2, 2, 40, "f32", 16, 1200, 4), ([1500] * 150, 2, 2, 40, "f32", 16, 1200, 4), ([1500, 9] * 20, 2, 2, 40, "f32", 16, 1200, 4),
         ([1500] * 150, 2, 2, 199, "f32", 16, 1200, 4), ([1500, 2] * 9, 2, 2, 199, "f32", 16, 1200, 4), ([3000] * 3, 64, 2, 128, "f32", 16, 1200, 4),
         ([4000] * 20, 4, 4, 64, "bf16", 16, 3000, 4), ([4000] * 9, 8, 8, 128, "bf16", 16, 3000, 4), ([4000] * 90, 16, 2, 128, "bf16", 16, 3000, 4)]
+RUNS += [([40] * 600 + [5000], 2, 1, 64, "bf16", 16, 3000, 4)] + [([40] * 600 + [3000], 2, 1, D, "f32", 16, 1500, 4) for D in (64, 33, 80, 199)]
+RUNS += [([100] * 150, 2, 2, D, dt, 16, 50, 4) for D, dt in ((128, "bf16"), (64, "f32"), (40, "f32"), (80, "f32"))]
 
 
 @pytest.mark.parametrize("c", RUNS, ids=lambda c: f"{len(c[0])}x{max(c[0])}-" + "-".join(map(str, c[1:])))
