@@ -215,25 +215,27 @@ __global__ __launch_bounds__(kThreads, 2) void window_bf16_kernel(const WindowAr
   }
 }
 
-// Binary32 (the layout of f32_tile.hpp): four waves share stages of 32 keys, the next stage's rows are in registers while this one is multiplied.
-template <int DB, int COLS>
-__global__ __launch_bounds__(kThreads, DB <= 2 ? 2 : 1) void window_f32_kernel(const WindowArgs a) {
-  constexpr int KC = 32, NB = KC / kF32Rows;
+// Binary32 (the layout of f32_tile.hpp): four waves share stages of 16 keys for each wave of a row, the next stage's rows are in registers while this
+// one is multiplied.  With 32 keys a wave the window's edges cost more than the barriers saved (24 heads, 16 items of up to 333 tokens, window 100:
+// 78 us against 75), and a wave that loads its keys for itself, without stages or barriers, reads them four times (96).
+template <int DB, int COLS, int SPLIT>   // SPLIT: waves that share 16 rows, each with 16 keys of every stage
+__global__ __launch_bounds__(kThreads, 2) void window_f32_kernel(const WindowArgs a) {
+  constexpr int KC = kF32Rows * SPLIT, UNITS = 4 / SPLIT;   // keys of a stage; units of a workgroup
   typedef F32Stage<DB, KC, COLS> Stage;
   const int D = COLS == kAllCols ? 64 * DB : a.D;
   __shared__ __attribute__((aligned(16))) float kl[KC * Stage::LD];
   __shared__ __attribute__((aligned(16))) float vl[KC * Stage::LD];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int i = lane & 15, kq = lane >> 4;
+  const int i = lane & 15, kq = lane >> 4, part = wave / UNITS, key0 = part * kF32Rows;
   const int slot = blockIdx.x >> 3, group = a.by_per.div(slot), u = a.first + group * 8 + (blockIdx.x & 7);
   if (u >= a.tiles) return;
   const int b = u / a.Hkv, hk = u - b * a.Hkv;
   if (a.row_sel && a.row_sel[b] >= 0) return;
   const int keys = a.len ? min(max(a.len[b], 0), a.S) : a.S;
-  const int unit0 = 4 * (slot - group * a.per), last = min(unit0 + 3, a.units - 1);
-  const int unit = min(unit0 + wave, last), tb = a.by_g.div(unit), t0 = kF32Rows * tb;
-  const bool live = unit0 + wave <= last;
+  const int unit0 = UNITS * (slot - group * a.per), last = min(unit0 + UNITS - 1, a.units - 1);
+  const int unit = min(unit0 + wave % UNITS, last), tb = a.by_g.div(unit), t0 = kF32Rows * tb;
+  const bool live = unit0 + wave % UNITS <= last;
   const size_t row0 = ((size_t)(b * a.Hkv + hk) * a.g + (unit - tb * a.g)) * a.S;
   const WindowBlocks<KC> chunks(a, kF32Rows * a.by_g.div(unit0), min(a.S, kF32Rows * (a.by_g.div(last) + 1)), keys);
   const float* K = reinterpret_cast<const float*>(a.K) + (size_t)u * a.S * D;
@@ -277,52 +279,68 @@ __global__ __launch_bounds__(kThreads, DB <= 2 ? 2 : 1) void window_f32_kernel(c
       vs.load(V, KC * chunks.at(n + 1), keys, D, tid);
     }
     if (!live) continue;
+    const int k0 = j0 + key0;
+    const WindowBlock bl = window_block<kF32Rows, kF32Rows>(a, t0, k0, keys);
+    if (bl == kNone) continue;   // uniform
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    const float* row = kl + (key0 + i) * Stage::LD + 4 * kq;
+    f32x4 k = *reinterpret_cast<const f32x4*>(row);
 #pragma unroll
-    for (int bk = 0; bk < NB; ++bk) {
-      const int k0 = j0 + kF32Rows * bk;
-      const WindowBlock bl = window_block<kF32Rows, kF32Rows>(a, t0, k0, keys);
-      if (bl == kNone) continue;   // uniform
-      f32x4 s = {0.f, 0.f, 0.f, 0.f};
-      const float* row = kl + (kF32Rows * bk + i) * Stage::LD + 4 * kq;
-      f32x4 k = *reinterpret_cast<const f32x4*>(row);
+    for (int kk = 0; kk < 4 * DB; ++kk)
+      if (COLS == kAllCols || 16 * kk < D) {   // uniform
+        const f32x4 next = *reinterpret_cast<const f32x4*>(row + 16 * ((kk + 1) & (4 * DB - 1)));
 #pragma unroll
-      for (int kk = 0; kk < 4 * DB; ++kk)
-        if (COLS == kAllCols || 16 * kk < D) {   // uniform
-          const f32x4 next = *reinterpret_cast<const f32x4*>(row + 16 * ((kk + 1) & (4 * DB - 1)));
-#pragma unroll
-          for (int x = 0; x < 4; ++x) s = mfma_f32(k[x], q[kk][x], s);
-          k = next;
-          __builtin_amdgcn_sched_barrier(0);
-        }
-      if (bl == kSome) {
-#pragma unroll
-        for (int x = 0; x < 4; ++x)
-          if (window_hides(a, t0 + i, k0 + 4 * kq + x, keys)) s[x] = -INFINITY;
+        for (int x = 0; x < 4; ++x) s = mfma_f32(k[x], q[kk][x], s);
+        k = next;
+        __builtin_amdgcn_sched_barrier(0);
       }
-      float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
-      mx = fmaxf(mx, __shfl_xor(mx, 16));
-      mx = fmaxf(mx, __shfl_xor(mx, 32));
-      const float m_new = fmaxf(m, mx * a.scale_log2e);
-      if (__any(m_new > m)) {
-        const float alpha = m_new > m ? __builtin_amdgcn_exp2f(m - m_new) : 1.f;
-        l *= alpha;
+    if (bl == kSome) {
 #pragma unroll
-        for (int x = 0; x < 4 * DB; ++x) acc[x] *= alpha;
-        m = m_new;
-      }
-      const float ref = m == -INFINITY ? 0.f : m;   // no finite score so far: all weights are zero
-      f32x4 p;
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        p[x] = __builtin_amdgcn_exp2f(fmaf(s[x], a.scale_log2e, -ref));
-        l += p[x];
-      }
-      f32_weights_v<DB>(acc, vl + kF32Rows * bk * Stage::LD, p, i, kq);
+      for (int x = 0; x < 4; ++x)
+        if (window_hides(a, t0 + i, k0 + 4 * kq + x, keys)) s[x] = -INFINITY;
     }
+    float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+    mx = fmaxf(mx, __shfl_xor(mx, 16));
+    mx = fmaxf(mx, __shfl_xor(mx, 32));
+    const float m_new = fmaxf(m, mx * a.scale_log2e);
+    if (__any(m_new > m)) {
+      const float alpha = m_new > m ? __builtin_amdgcn_exp2f(m - m_new) : 1.f;
+      l *= alpha;
+#pragma unroll
+      for (int x = 0; x < 4 * DB; ++x) acc[x] *= alpha;
+      m = m_new;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;   // no finite score so far: all weights are zero
+    f32x4 p;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      p[x] = __builtin_amdgcn_exp2f(fmaf(s[x], a.scale_log2e, -ref));
+      l += p[x];
+    }
+    f32_weights_v<DB>(acc, vl + key0 * Stage::LD, p, i, kq);
   }
-  if (!live) return;
   float sum = l + __shfl_xor(l, 16);
   sum += __shfl_xor(sum, 32);
+  if constexpr (SPLIT == 2) {   // the second wave's sums through the stages, which nobody reads any more
+    static_assert(4 * DB * kWave * 4 * UNITS <= KC * Stage::LD, "sums of two waves");
+    f32x4* sums = reinterpret_cast<f32x4*>(kl) + wave % UNITS * 4 * DB * kWave + lane;
+    float* stats = vl + wave % UNITS * 2 * kWave + lane;
+    __syncthreads();
+    if (part > 0) {
+#pragma unroll
+      for (int x = 0; x < 4 * DB; ++x) sums[x * kWave] = acc[x];
+      stats[0] = m;
+      stats[kWave] = sum;
+    }
+    __syncthreads();
+    if (part > 0) return;
+    const float m1 = stats[0], top = fmaxf(m, m1);
+    const float f0 = m < top ? __builtin_amdgcn_exp2f(m - top) : 1.f, f1 = m1 < top ? __builtin_amdgcn_exp2f(m1 - top) : 1.f;
+    sum = sum * f0 + stats[kWave] * f1;
+#pragma unroll
+    for (int x = 0; x < 4 * DB; ++x) acc[x] = acc[x] * f0 + sums[x * kWave] * f1;
+  }
+  if (!live) return;
   const int rows = min(kF32Rows, a.S - t0);
   bool odd = !(sum < INFINITY);
 #pragma unroll
@@ -336,9 +354,9 @@ __global__ __launch_bounds__(kThreads, DB <= 2 ? 2 : 1) void window_f32_kernel(c
 
 // All tiles, in launches of at most 2^23 workgroups (a multiple of eight tiles each).
 template <typename Kernel>
-static hipError_t window_tiles(Kernel kernel, WindowArgs a, int rows, hipStream_t stream) {
+static hipError_t window_tiles(Kernel kernel, WindowArgs a, int rows, int units, hipStream_t stream) {   // rows of a unit, units of a workgroup
   a.units = (a.S + rows - 1) / rows * a.g;
-  a.per = (a.units + 3) / 4;
+  a.per = (a.units + units - 1) / units;
   a.by_per = Divider((uint32_t)a.per);
   const int64_t most = ((1 << 23) / a.per > 8 ? (1 << 23) / a.per : 8) & ~7LL;
   for (int64_t first = 0; first < a.tiles; first += most) {
@@ -351,6 +369,18 @@ static hipError_t window_tiles(Kernel kernel, WindowArgs a, int rows, hipStream_
   return hipSuccess;
 }
 
+// Two waves a row where workgroups of 64 rows would not give every CU one: a wave's chain of keys is what such a call takes (24 heads on 8 of K and
+// V, 333 tokens, 128 workgroups: 20 -> 15 us; 8 heads, 1,000 tokens, all seen, 256: 61 -> 49).  With more, half as many rows a workgroup read every
+// key twice as often and nothing is gained (576 workgroups: 24 -> 25; 2,688: 79 -> 89).
+constexpr int64_t kWindowSplit = 256;
+
+template <int DB, int COLS>
+static hipError_t launch_window_f32(const WindowArgs& a, hipStream_t stream) {
+  const int64_t workgroups = ((int64_t)((a.S + kF32Rows - 1) / kF32Rows) * a.g + 3) / 4 * a.tiles;
+  return workgroups <= kWindowSplit ? window_tiles(&window_f32_kernel<DB, COLS, 2>, a, kF32Rows, 2, stream)
+                                    : window_tiles(&window_f32_kernel<DB, COLS, 1>, a, kF32Rows, 4, stream);
+}
+
 hipError_t launch_window(const WindowLaunch& p, hipStream_t stream) {
   WindowArgs a;
   a.Q = p.Q; a.K = p.K; a.V = p.V; a.O = p.O; a.len = p.key_len; a.row_sel = p.row_sel;
@@ -361,13 +391,13 @@ hipError_t launch_window(const WindowLaunch& p, hipStream_t stream) {
   a.by_g = Divider((uint32_t)a.g);
   const float scale = p.scale == 0.f ? 1.0f / sqrtf((float)p.D) : p.scale;
   a.scale_log2e = scale * 1.44269504088896340736f;
-  if (!p.is_f32) return p.D == 64 ? window_tiles(&window_bf16_kernel<64>, a, 32, stream) : window_tiles(&window_bf16_kernel<128>, a, 32, stream);
-  if (p.D == 64) return window_tiles(&window_f32_kernel<1, kAllCols>, a, kF32Rows, stream);
-  if (p.D == 128) return window_tiles(&window_f32_kernel<2, kAllCols>, a, kF32Rows, stream);
-  if (p.D < 4) return window_tiles(&window_f32_kernel<1, kFewCols>, a, kF32Rows, stream);
-  if (p.D < 64) return p.D % 4 ? window_tiles(&window_f32_kernel<1, kAnyCols>, a, kF32Rows, stream) : window_tiles(&window_f32_kernel<1, kVecCols>, a, kF32Rows, stream);
-  if (p.D < 128) return p.D % 4 ? window_tiles(&window_f32_kernel<2, kAnyCols>, a, kF32Rows, stream) : window_tiles(&window_f32_kernel<2, kVecCols>, a, kF32Rows, stream);
-  return p.D % 4 ? window_tiles(&window_f32_kernel<4, kAnyCols>, a, kF32Rows, stream) : window_tiles(&window_f32_kernel<4, kVecCols>, a, kF32Rows, stream);
+  if (!p.is_f32) return p.D == 64 ? window_tiles(&window_bf16_kernel<64>, a, 32, 4, stream) : window_tiles(&window_bf16_kernel<128>, a, 32, 4, stream);
+  if (p.D == 64) return launch_window_f32<1, kAllCols>(a, stream);
+  if (p.D == 128) return launch_window_f32<2, kAllCols>(a, stream);
+  if (p.D < 4) return launch_window_f32<1, kFewCols>(a, stream);
+  if (p.D < 64) return p.D % 4 ? launch_window_f32<1, kAnyCols>(a, stream) : launch_window_f32<1, kVecCols>(a, stream);
+  if (p.D < 128) return p.D % 4 ? launch_window_f32<2, kAnyCols>(a, stream) : launch_window_f32<2, kVecCols>(a, stream);
+  return p.D % 4 ? launch_window_f32<4, kAnyCols>(a, stream) : launch_window_f32<4, kVecCols>(a, stream);
 }
 
 }  // namespace ac

@@ -31,7 +31,7 @@ def test_every_kernel_is_reached(tmp_path):
     calls += [("shared", 8, 4, 2, D, 2002, 100, 16, 30, None, dt) for D, dt in shared.TYPES]
     calls += [_shared(shared.FAR, [], Hq, Hkv, D, "bf16", 16, 300, 1 << 24) for Hq, Hkv, D in shared.FAR_HEADS]
     calls += [_shared(shared.FAR_MANY, [], Hq, Hkv, D, "bf16", 16, 4400, 1 << 20) for Hq, Hkv, D in shared.FAR_HEADS]
-    calls += [("window", *size, D, 7, 3, dt) for size in window.SIZES for D, dt in window.TYPES]
+    calls += [("window", *size, D, 7, 3, dt) for size in window.SIZES + window.MANY for D, dt in window.TYPES]
     calls += [("window_step", len(step.EDGES), 6, 2, D, 100, 16, _pages(step.EDGES, 16), 50, 9, dt) for D, dt in step.TYPES]
     calls += [("window_step", 5, 6, 2, D, 400, 16, _pages([2500], 16), 1000, 9, dt) for D, dt in step.TYPES]
     calls += [("window_step", len(c[0]), c[1], c[2], c[3], 100, c[5], _pages(c[0], c[5]), c[6], c[7], c[4]) for c in step.RUNS]
