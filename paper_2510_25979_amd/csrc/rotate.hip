@@ -144,8 +144,8 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a) {
     }
   }
   const int64_t head = (int64_t)a.S * D, page_head = (int64_t)a.ps * D;   // elements from head to head
-  T* Q = static_cast<T*>(a.Q) + b * a.Hq * head + (int64_t)s * D;
-  const int64_t kv = b * a.Hkv * head + (int64_t)s * D;
+  T* Q = static_cast<T*>(a.Q) + (int64_t)b * a.Hq * head + (int64_t)s * D;
+  const int64_t kv = (int64_t)b * a.Hkv * head + (int64_t)s * D;
   auto finish = [&](int u, int h) {   // (h, and which kind it is of, is the wave's)
     const int kind = h < a.Hq ? 0 : h < rotated ? 1 : 2, hk = h - a.Hq - (kind == 2 ? a.Hkv : 0);
     const bool weight = NORM && (kind == 0 ? a.qw : kind == 1 ? a.kw : nullptr) != nullptr;

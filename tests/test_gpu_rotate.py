@@ -138,6 +138,16 @@ def test_many_tokens(ac):  # noqa: F811
     case(ac, 5000, 1, 2, 1, 128, "bf16", 128, page=16, pads=False)
 
 
+def test_more_rows_than_31_bits_count(ac):  # noqa: F811
+    B, Hq = 1 << 20, 2049
+    X = torch.randn(B, 1, Hq + 2, device="cuda")
+    Q, K, V = torch.zeros(B, Hq, 1, 1, device="cuda"), torch.zeros(B, 1, 1, 1, device="cuda"), torch.zeros(B, 1, 1, 1, device="cuda")
+    ac.attncache_rotate(X, torch.zeros(B, 1, dtype=torch.int32, device="cuda"), None, Q, K, V)
+    for b in (0, (1 << 19) - 50, B - 600):      # one number a head, nothing to normalise or rotate
+        assert torch.equal(Q[b:b + 600].view(-1, Hq), X[b:b + 600, 0, :Hq])
+    assert torch.equal(K.view(B), X[:, 0, Hq]) and torch.equal(V.view(B), X[:, 0, Hq + 1])
+
+
 def test_an_infinity_stays_in_its_head_and_nothing_to_do_is_done(ac):  # noqa: F811
     B, S, D = 2, 3, 64
     X = torch.randn(B, S, 4 * D, device="cuda")
