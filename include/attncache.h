@@ -661,7 +661,9 @@ int32_t attncache_rotary_frequencies(double *freq, int32_t rot, double base,
  * share pages, or have lost some to a window, end here.
  * The outputs may be the inputs of the same meaning, or not overlap them.
  * workspace: DEVICE, attncache_page_fork_workspace_bytes(...) bytes, 16-byte
- * aligned; scratch.  Three launches.  B <= 2^22, B * max_pages below
+ * aligned; scratch, and written by a call before it is read.  Two launches up
+ * to 1,024 rows, 16,384 entries of page_table and 65,536 pages, otherwise three.
+ * Results do not depend on the order of threads.  B <= 2^22, B * max_pages below
  * 2^31 - 4096, page_size * D <= 2^30, otherwise as in attncache_page_plan.
  */
 size_t attncache_page_fork_workspace_bytes(int32_t B, int32_t max_pages,
@@ -701,10 +703,11 @@ int32_t attncache_page_fork(const int32_t *from, const int32_t *seq_len,
  *              16-byte aligned; scratch, and written by a call before it is
  *              read.  Calls that may overlap in time need one each.
  *
- * G >= 0, and 0 groups need no share_len.  B and G at most 2^20; three or four
- * launches; deterministic.  Hkv * (B * ceil(g / 16) + B * g / 16 + G) *
- * (ceil(max_pages * page_size / 16) + 2) and B * Hq below 2^31 - 65536, with
- * g = Hq / Hkv.  One workgroup looks through the requests, 1,024 a step.
+ * G >= 0, and 0 groups need no share_len.  B and G at most 2^20, B * Hq at most
+ * 2^25, Hkv * (B * ceil(g / 16) + B * g / 16 + G) * (ceil(max_pages * page_size /
+ * 16) + 2) below 2^31 - 65536, with g = Hq / Hkv.  Two launches up to 256
+ * requests and 255 groups, otherwise three, the first of which is one workgroup
+ * that looks through the requests, 1,024 a step.  Deterministic.
  */
 size_t attention_paged_shared_workspace_bytes(int32_t B, int32_t Hq,
                                               int32_t Hkv, int32_t D,
@@ -739,8 +742,8 @@ int32_t attention_paged_shared(const void *Q, const void *k_pages,
  *
  * Arithmetic as in attention_paged.  Keys that are hidden from a row do not
  * touch it, whatever K and V hold there (rows among 32, binary32 16, that meet
- * an infinity or a NaN take a slower way).  Hq / Hkv * S <= 2^24, B * Hkv <=
- * 2^28, B * Hq below 2^31.
+ * an infinity or a NaN take a slower way).  Hq / Hkv * S <= 2^24, also with S
+ * rounded up to a multiple of 16; B * Hkv <= 2^28, B * Hq below 2^31.
  */
 int32_t attention_window(const void *Q, const void *K, const void *V, void *O,
                          const int32_t *row_sel, const int32_t *key_len,

@@ -878,7 +878,7 @@ int32_t attention_window(const void* Q, const void* K, const void* V, void* O, c
   int32_t rc = check_head(D, dtype);
   if (rc != AC_OK) return rc;
   // units of a K/V head, and tiles, are counted in 31 bits; so are the elements of an item's heads, 32 rows at a time
-  if ((int64_t)(Hq / Hkv) * S > (1 << 24) || (int64_t)B * Hkv > (1 << 28) || (int64_t)B * Hq > 0x7fffffffLL) return AC_ERR_SHAPE;
+  if ((int64_t)(Hq / Hkv) * S > (1 << 24) || (S + 15LL) / 16 * (Hq / Hkv) > (1 << 20) || (int64_t)B * Hkv > (1 << 28) || (int64_t)B * Hq > 0x7fffffffLL) return AC_ERR_SHAPE;
   if (!(scale >= 0.f)) return AC_ERR_SHAPE;
   if (B == 0) return AC_OK;
   if (!Q || !K || !V || !O) return AC_ERR_NULL;

@@ -860,7 +860,7 @@ size_t shared_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int
 bool shared_fits(int64_t B, int64_t Hkv, int64_t g, int64_t G, int64_t keys) {
   // own items' blocks and prefixes' (a group's last row block may be a single row)
   const double units = (double)Hkv * (B * (double)((g + kDecodeRows - 1) / kDecodeRows) + (double)B * g / kDecodeRows + G);
-  return units * ((keys + 15) / 16 + kUnitCost) < 2147483648.0 - 65536 && (double)B * Hkv * g < 2147483648.0 - 65536;
+  return units * ((keys + 15) / 16 + kUnitCost) < 2147483648.0 - 65536 && (double)B * Hkv * g <= 33554432.0;   // (the join's grid)
 }
 
 template <class Core>

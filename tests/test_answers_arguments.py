@@ -70,12 +70,12 @@ def _step(L, **change):
     (_shared, dict(Hq=9), SHAPE), (_shared, dict(B=-1), SHAPE), (_shared, dict(G=-1), SHAPE), (_shared, dict(G=(1 << 20) + 1), SHAPE), (_shared, dict(B=(1 << 20) + 1), SHAPE),
     (_shared, dict(D=32), SHAPE), (_shared, dict(dtype=F16), DTYPE), (_shared, dict(scale=-1.0), SHAPE), (_shared, dict(scale=float("nan")), SHAPE), (_shared, dict(ws_bytes=1000), WORKSPACE),
     (_shared, dict(max_pages=1 << 27), SHAPE), (_shared, dict(max_pages=(1 << 26) + 1, B=1, Hq=1, Hkv=1), SHAPE), (_shared, dict(B=1 << 16, max_pages=1 << 20), SHAPE),
-    (_shared, dict(G=1 << 16, max_pages=1 << 20), SHAPE), (_shared, dict(stride=2 * 16 * 64 - 8), SHAPE), (_shared, dict(stride=2 * 16 * 64 + 4), ALIGN), (_shared, dict(B=0), OK),
+    (_shared, dict(G=1 << 16, max_pages=1 << 20), SHAPE), (_shared, dict(B=1 << 20, Hq=33, Hkv=1, max_pages=1), SHAPE), (_shared, dict(stride=2 * 16 * 64 - 8), SHAPE), (_shared, dict(stride=2 * 16 * 64 + 4), ALIGN), (_shared, dict(B=0), OK),
     *[(_window, {n: None}, NULL) for n in "Q K V O".split()], *[(_window, {n: P + 8}, ALIGN) for n in "Q K V O".split()],
     *[(_window, {n: 0}, SHAPE) for n in "Hq Hkv S D window".split()],
     (_window, dict(Hq=9), SHAPE), (_window, dict(B=-1), SHAPE), (_window, dict(D=96), SHAPE), (_window, dict(dtype=F32, D=257), SHAPE), (_window, dict(dtype=F16), DTYPE),
     (_window, dict(window=-1), SHAPE), (_window, dict(sinks=-1), SHAPE), (_window, dict(scale=-1.0), SHAPE), (_window, dict(S=1 << 23), SHAPE), (_window, dict(B=1 << 28, Hq=2, Hkv=2), SHAPE),
-    (_window, dict(B=1 << 28, Hq=8, Hkv=1), SHAPE), (_window, dict(B=0), OK),
+    (_window, dict(B=1 << 28, Hq=8, Hkv=1), SHAPE), (_window, dict(B=0), OK), (_window, dict(B=1, S=1, Hq=(1 << 20) + 1, Hkv=1), SHAPE), (_window, dict(B=1, S=17, Hq=(1 << 19) + 1, Hkv=1), SHAPE),
     *[(_step, {n: None}, NULL) for n in "Q kp vp table len O ws".split()], *[(_step, {n: P + 8}, ALIGN) for n in "Q kp vp O ws".split()],
     *[(_step, {n: 0}, SHAPE) for n in "Hq Hkv D n page max_pages window".split()],
     (_step, dict(Hq=9), SHAPE), (_step, dict(B=-1), SHAPE), (_step, dict(sinks=-1), SHAPE), (_step, dict(window=-5), SHAPE), (_step, dict(D=32), SHAPE), (_step, dict(dtype=F16), DTYPE),

@@ -66,9 +66,16 @@ def test_the_kernels_that_measured_best_serve_the_call(tmp_path, call, kernels):
     (("rotate", 1 << 20, 1 << 10, 2, 1, 128, 128, 0, 0, 512, "bf16"), "rotate_kernel", 1 << 28),
     (("window", 1 << 18, 64, 64, 200, 64, 10, 0, "bf16"), "window_bf16_kernel", (1 << 24) * 2),
     (("window", 1 << 18, 64, 64, 40, 64, 10, 0, "f32"), "window_f32_kernel", 1 << 24),
+    (("window", 1, 1 << 20, 1, 1, 64, 10, 0, "bf16"), "window_bf16_kernel", 1 << 18),
+    (("window", 9, 1 << 20, 1, 1, 64, 10, 0, "f32"), "window_f32_kernel", 9 << 18),
     (("window", 64, 64, 1, 1 << 18, 64, 10, 0, "bf16"), "window_bf16_kernel", 64 << 17),
 ], ids=lambda x: "-".join(map(str, x)) if isinstance(x, tuple) else None)
 def test_a_grid_that_does_not_fit_is_split(tmp_path, call, kernel, covered):
     (status, ls), = al.record([call], tmp_path)
     assert status == 0 and all(la[0].startswith(kernel) for la in ls)
     assert sum(la[1] * la[2] for la in ls) >= covered and all(la[1] * la[4] < 2**32 for la in ls)
+
+
+def test_the_most_rows_of_shared_prefixes_fit_a_launch(tmp_path):
+    (status, ls), = al.record([("shared", 1 << 20, 32, 1, 64, 1, 10, 16, 1, None, "bf16")], tmp_path)
+    assert status == 0 and all(la[1] * la[4] < 2**32 for la in ls)
