@@ -107,10 +107,9 @@ struct F32Stage {
 
 // acc += W V for one 16-key block: `v` is the block's first row in LDS, w[x] the lane's weight of
 // key 4 kq + x (zero where the key is hidden from its row).
-template <int DB>
+template <int DB, int LD = F32Stage<DB, 64, kAllCols>::LD>
 __device__ __forceinline__ void f32_weights_v(f32x4 (&acc)[4 * DB], const float* __restrict__ v,
                                               const f32x4 w, int i, int kq) {
-  constexpr int LD = F32Stage<DB, 64, kAllCols>::LD;
   struct Rows { f32x4 b[DB]; };   // this lane's part of key 4 kq + x
   auto read = [&](int x) {
     Rows r;

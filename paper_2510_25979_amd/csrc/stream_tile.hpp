@@ -15,7 +15,7 @@ struct StreamSource {
   __amdgpu_buffer_rsrc_t rsrc;
   __device__ __forceinline__ StreamSource(const void* from, uint32_t bytes)   // uniform; bytes behind the last read as zeros
       : rsrc(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(from), 0, bytes, 0x00020000)) {}
-  __device__ __forceinline__ void copy(bf16_t* lds, uint32_t offset) const {   // 16 bytes of each lane, side by side in LDS
+  __device__ __forceinline__ void copy(void* lds, uint32_t offset) const {   // 16 bytes of each lane, side by side in LDS
     __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)lds, 16, offset, 0, 0, 0);
   }
 };
@@ -79,10 +79,11 @@ struct StreamTile {
     const float m05 = fmaxf(fmaxf(s[12], s[13]), s[14]);
     return fmaxf(fmaxf(fmaxf(m01, m02), m03), fmaxf(fmaxf(m04, m05), s[15]));
   }
-  // The reference points of rows whose largest score, `top` of both lanes that share a row, has outgrown them.
+  // The reference points of rows whose largest score has outgrown them; `largest`: of the lane's half of its row.
   __device__ __forceinline__ void follow(float largest) {
-    const float cand = fmaxf(m, max_with_other_half(largest) * scale_log2e);
-    if (__any(cand > m + kStreamSlack)) {
+    largest *= scale_log2e;
+    if (__any(largest > m + kStreamSlack)) {
+      const float cand = fmaxf(m, max_with_other_half(largest));
       const float alpha = cand > m ? __builtin_amdgcn_exp2f(m - cand) : 1.f;
       l *= alpha;
 #pragma unroll

@@ -215,16 +215,22 @@ __global__ __launch_bounds__(kThreads, 2) void window_bf16_kernel(const WindowAr
   }
 }
 
-// Binary32 (the layout of f32_tile.hpp): four waves share stages of 16 keys for each wave of a row, the next stage's rows are in registers while this
-// one is multiplied.  With 32 keys a wave the window's edges cost more than the barriers saved (24 heads, 16 items of up to 333 tokens, window 100:
-// 78 us against 75), and a wave that loads its keys for itself, without stages or barriers, reads them four times (96).
+// Binary32 (the layout of f32_tile.hpp): four waves share stages of 16 keys for each wave of a row.  Heads of 64 and 128 columns go straight from memory
+// into two stages in turn (K's pieces swizzled, V's not: both are then read without bank conflicts); others through registers, in which the next stage is while
+// this one is multiplied.  The vector units form these products themselves, so that what the softmax takes comes on top of them, and its reference
+// points move only when a score has outgrown them by 2^8.  us, 24 heads of 128, 16 items of up to 333 tokens, window 100: 78 with stages of 32 keys
+// a wave, 75 of 16, 74 straight into LDS, 72 with reference points that stay; waves that load their keys for themselves, without stages or barriers, read
+// them four times: 96; eight waves, two for each row: 82.  Bound by products and softmax (47 us of it; four times the items take 216) and, where a
+// chip's few rounds of workgroups end unevenly, by the last ones.
 template <int DB, int COLS, int SPLIT>   // SPLIT: waves that share 16 rows, each with 16 keys of every stage
 __global__ __launch_bounds__(kThreads, 2) void window_f32_kernel(const WindowArgs a) {
   constexpr int KC = kF32Rows * SPLIT, UNITS = 4 / SPLIT;   // keys of a stage; units of a workgroup
+  constexpr bool DIRECT = COLS == kAllCols;   // rows go straight to LDS, into two stages in turn
   typedef F32Stage<DB, KC, COLS> Stage;
   const int D = COLS == kAllCols ? 64 * DB : a.D;
-  __shared__ __attribute__((aligned(16))) float kl[KC * Stage::LD];
-  __shared__ __attribute__((aligned(16))) float vl[KC * Stage::LD];
+  constexpr int LD = DIRECT ? 64 * DB : Stage::LD;
+  __shared__ __attribute__((aligned(16))) float kl[KC * LD];
+  __shared__ __attribute__((aligned(16))) float vl[KC * LD];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int i = lane & 15, kq = lane >> 4, part = wave / UNITS, key0 = part * kF32Rows;
@@ -260,35 +266,18 @@ __global__ __launch_bounds__(kThreads, 2) void window_f32_kernel(const WindowArg
   }
 #pragma unroll
   for (int x = 0; x < 4 * DB; ++x) acc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m = -INFINITY, l = 0.f;
-  Stage ks, vs;
-  if (chunks.count > 0) {
-    ks.load(K, KC * chunks.at(0), keys, D, tid);
-    vs.load(V, KC * chunks.at(0), keys, D, tid);
-  }
-  for (int n = 0; n < chunks.count; ++n) {
-    const int j0 = KC * chunks.at(n);
-    ks.template mask<false>(j0, keys, D, tid);   // (scores of keys that are not there are replaced)
-    vs.template mask<true>(j0, keys, D, tid);
-    __syncthreads();   // the previous stage has been read by everybody
-    ks.commit(kl, tid);
-    vs.commit(vl, tid);
-    __syncthreads();
-    if (n + 1 < chunks.count) {
-      ks.load(K, KC * chunks.at(n + 1), keys, D, tid);
-      vs.load(V, KC * chunks.at(n + 1), keys, D, tid);
-    }
-    if (!live) continue;
+  float m = -INFINITY, ref = 0.f, l = 0.f;
+  auto block = [&](const float* kl, const float* vl, int j0) __attribute__((always_inline)) {
     const int k0 = j0 + key0;
     const WindowBlock bl = window_block<kF32Rows, kF32Rows>(a, t0, k0, keys);
-    if (bl == kNone) continue;   // uniform
+    if (bl == kNone) return;   // uniform
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
-    const float* row = kl + (key0 + i) * Stage::LD + 4 * kq;
-    f32x4 k = *reinterpret_cast<const f32x4*>(row);
+    auto piece = [&](int kk) { return *reinterpret_cast<const f32x4*>(kl + (key0 + i) * LD + (DIRECT ? 4 * ((4 * kk + kq) ^ i) : 16 * kk + 4 * kq)); };
+    f32x4 k = piece(0);
 #pragma unroll
     for (int kk = 0; kk < 4 * DB; ++kk)
       if (COLS == kAllCols || 16 * kk < D) {   // uniform
-        const f32x4 next = *reinterpret_cast<const f32x4*>(row + 16 * ((kk + 1) & (4 * DB - 1)));
+        const f32x4 next = piece((kk + 1) & (4 * DB - 1));
 #pragma unroll
         for (int x = 0; x < 4; ++x) s = mfma_f32(k[x], q[kk][x], s);
         k = next;
@@ -299,30 +288,87 @@ __global__ __launch_bounds__(kThreads, 2) void window_f32_kernel(const WindowArg
       for (int x = 0; x < 4; ++x)
         if (window_hides(a, t0 + i, k0 + 4 * kq + x, keys)) s[x] = -INFINITY;
     }
-    float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
-    mx = fmaxf(mx, __shfl_xor(mx, 16));
-    mx = fmaxf(mx, __shfl_xor(mx, 32));
-    const float m_new = fmaxf(m, mx * a.scale_log2e);
-    if (__any(m_new > m)) {
-      const float alpha = m_new > m ? __builtin_amdgcn_exp2f(m - m_new) : 1.f;
+    const float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])) * a.scale_log2e;
+    if (__any(mx > m + kStreamSlack)) {
+      float top = fmaxf(mx, __shfl_xor(mx, 16));
+      top = fmaxf(fmaxf(top, __shfl_xor(top, 32)), m);
+      const float alpha = top > m ? __builtin_amdgcn_exp2f(m - top) : 1.f;
       l *= alpha;
 #pragma unroll
       for (int x = 0; x < 4 * DB; ++x) acc[x] *= alpha;
-      m = m_new;
+      m = top;
+      ref = m == -INFINITY ? 0.f : m;   // no finite score so far: all weights are zero
     }
-    const float ref = m == -INFINITY ? 0.f : m;   // no finite score so far: all weights are zero
     f32x4 p;
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
       p[x] = __builtin_amdgcn_exp2f(fmaf(s[x], a.scale_log2e, -ref));
       l += p[x];
     }
-    f32_weights_v<DB>(acc, vl + key0 * Stage::LD, p, i, kq);
+    f32_weights_v<DB, LD>(acc, vl + key0 * LD, p, i, kq);
+  };
+  if constexpr (DIRECT) {
+    __shared__ __attribute__((aligned(16))) float kl1[KC * LD];
+    __shared__ __attribute__((aligned(16))) float vl1[KC * LD];
+    constexpr int PPR = 16 * DB, NCOPY = KC * PPR / kThreads;   // 16-byte pieces of a row, of a thread
+    uint32_t kfrom[NCOPY], vfrom[NCOPY];   // bytes from a stage's first row; piece p of K's row r lies at p ^ r % 16
+#pragma unroll
+    for (int n = 0; n < NCOPY; ++n) {
+      const int r = tid / PPR + n * (kThreads / PPR), p = tid % PPR;
+      kfrom[n] = 16 * (r * PPR + (p ^ (r & 15)));
+      vfrom[n] = 16 * (r * PPR + p);
+    }
+    auto copy = [&](float* kl, float* vl, int n) {   // (rows behind the keys: zeros)
+      const int j0 = KC * chunks.at(n);
+      const uint32_t bytes = min(keys - j0, KC) * LD * 4;
+      const StreamSource ks(K + (size_t)j0 * LD, bytes), vs(V + (size_t)j0 * LD, bytes);
+#pragma unroll
+      for (int x = 0; x < NCOPY; ++x) {
+        ks.copy(kl + 4 * kWave * (wave + 4 * x), kfrom[x]);
+        vs.copy(vl + 4 * kWave * (wave + 4 * x), vfrom[x]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    auto publish = [&]() {   // this wave's copies have landed, then everybody's; the other stage is no longer read
+      __builtin_amdgcn_s_waitcnt(0);
+      __syncthreads();
+    };
+    if (chunks.count > 0) copy(kl, vl, 0);
+#pragma unroll 1
+    for (int n = 0; n < chunks.count; n += 2) {
+      publish();
+      if (n + 1 < chunks.count) copy(kl1, vl1, n + 1);
+      if (live) block(kl, vl, KC * chunks.at(n));
+      if (n + 1 >= chunks.count) break;
+      publish();
+      if (n + 2 < chunks.count) copy(kl, vl, n + 2);
+      if (live) block(kl1, vl1, KC * chunks.at(n + 1));
+    }
+  } else {
+    Stage ks, vs;
+    if (chunks.count > 0) {
+      ks.load(K, KC * chunks.at(0), keys, D, tid);
+      vs.load(V, KC * chunks.at(0), keys, D, tid);
+    }
+    for (int n = 0; n < chunks.count; ++n) {
+      const int j0 = KC * chunks.at(n);
+      ks.template mask<false>(j0, keys, D, tid);   // (scores of keys that are not there are replaced)
+      vs.template mask<true>(j0, keys, D, tid);
+      __syncthreads();   // the previous stage has been read by everybody
+      ks.commit(kl, tid);
+      vs.commit(vl, tid);
+      __syncthreads();
+      if (n + 1 < chunks.count) {
+        ks.load(K, KC * chunks.at(n + 1), keys, D, tid);
+        vs.load(V, KC * chunks.at(n + 1), keys, D, tid);
+      }
+      if (live) block(kl, vl, j0);
+    }
   }
   float sum = l + __shfl_xor(l, 16);
   sum += __shfl_xor(sum, 32);
   if constexpr (SPLIT == 2) {   // the second wave's sums through the stages, which nobody reads any more
-    static_assert(4 * DB * kWave * 4 * UNITS <= KC * Stage::LD, "sums of two waves");
+    static_assert(4 * DB * kWave * 4 * UNITS <= KC * LD, "sums of two waves");
     f32x4* sums = reinterpret_cast<f32x4*>(kl) + wave % UNITS * 4 * DB * kWave + lane;
     float* stats = vl + wave % UNITS * 2 * kWave + lane;
     __syncthreads();
