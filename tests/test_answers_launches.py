@@ -17,7 +17,7 @@ def _pages(lens, page):
 
 def _shared(groups, alone, Hq, Hkv, D, dt, page, n=100, stride=None):
     lens = [p + (n_ or 0) for p, rows in groups for n_ in rows] + list(alone)
-    return ("shared", len(lens), Hq, Hkv, D, len(groups), n, page, _pages(lens, page), stride, dt)
+    return ("shared", len(lens), Hq, Hkv, D, len(groups), n, page, max(_pages(lens, page), shared.width(len(lens), Hkv, D, dt, page)), stride, dt)
 
 
 def test_every_kernel_is_reached(tmp_path):
@@ -28,7 +28,7 @@ def test_every_kernel_is_reached(tmp_path):
     calls += [_shared(shared.EDGES, [0, 1, 50], 6, 2, D, dt, 16) for D, dt in shared.TYPES]
     calls += [_shared(*c) for c in shared.CASES]
     calls += [_shared(*c) for c in shared.MANY]
-    calls += [("shared", 8, 4, 2, D, 2002, 100, 16, 30, None, dt) for D, dt in shared.TYPES]
+    calls += [("shared", 8, 4, 2, D, 2002, 100, 16, shared.width(8, 2, D, dt, 16), None, dt) for D, dt in shared.TYPES]
     calls += [_shared(shared.FAR, [], Hq, Hkv, D, "bf16", 16, 300, 1 << 24) for Hq, Hkv, D in shared.FAR_HEADS]
     calls += [_shared(shared.FAR_MANY, [], Hq, Hkv, D, "bf16", 16, 4400, 1 << 20) for Hq, Hkv, D in shared.FAR_HEADS]
     calls += [("window", *size, D, 7, 3, dt) for size in window.SIZES + window.MANY for D, dt in window.TYPES]
@@ -53,6 +53,9 @@ def test_every_kernel_is_reached(tmp_path):
     (("shared", 300, 32, 8, 128, 1, 1100, 16, 1100, None, "bf16"), ["shared_plan_kernel<32, 32, 1024, true>", "shared_both_kernel<128, false, false>", "shared_join_kernel<false, 32, 1>"]),
     (("shared", 64, 32, 8, 64, 1, 1100, 16, 1100, 1 << 22, "bf16"), ["shared_both_kernel<64, true, true>", "shared_join_kernel<false, 16, 1>"]),
     (("shared", 17, 24, 8, 128, 4, 1100, 10, 200, None, "f32"), ["shared_run_kernel<SharedF32<2, true>, true>", "shared_join_kernel<true, 32, 4>"]),
+    (("shared", 61, 8, 8, 128, 1, 1100, 16, 16, None, "bf16"), ["decode_unit_kernel"]),
+    (("shared", 8, 8, 1, 128, 1, 1100, 16, 900, None, "bf16"), ["decode_run_kernel", "decode_join_kernel"]),
+    (("shared", 64, 32, 8, 128, 0, 1100, 16, 1100, None, "bf16"), ["decode_run_kernel", "decode_join_kernel"]),
     (("window", 4, 32, 8, 4096, 128, 1024, 4, "bf16"), ["window_bf16_kernel<128>"]),
     (("window_step", 4, 32, 8, 64, 300, 16, 600, 500, 16, "bf16"), ["window_step_unit_kernel"]),
     (("window_step", 128, 32, 8, 128, 300, 16, 12500, 4096, 4, "bf16"), ["window_step_run_kernel", "window_step_join_kernel"]),

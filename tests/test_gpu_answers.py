@@ -5,6 +5,7 @@ import torch
 
 from tests import generation as gen
 from tests.test_gpu_parity_small import ac  # noqa: F401
+from tests.test_gpu_shared_attention import width as wide
 from tests.test_gpu_rotate import expect
 from tests.test_gpu_window_attention import attend, seen_by
 
@@ -65,7 +66,8 @@ def test_answers_to_one_prompt(ac, dt, D, page, window, sinks):  # noqa: F811
         if window:
             ac.attention_paged_window(q.view(B, Hq, D), k, v, table, seq, O, ws, window=window, sinks=sinks)
         else:
-            ac.attention_paged_shared(q.view(B, Hq, D), k, v, table, seq, i32([0, B]), i32([S]), O, ws)
+            long = torch.full((B, wide(B, Hkv, D, dt, page)), -1, dtype=torch.int32, device="cuda")      # of which a prefix is read once
+            ac.attention_paged_shared(q.view(B, Hq, D), k, v, torch.cat([table, long], 1) if step % 2 else table, seq, i32([0, B]), i32([S]), O, ws)
         t, s = table.tolist(), seq.tolist()
         for b in range(B):
             if not alive[b]:

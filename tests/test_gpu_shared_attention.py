@@ -11,8 +11,14 @@ from tests.test_gpu_parity_small import ac  # noqa: F401
 pytestmark = pytest.mark.gpu
 
 
-def build(groups, alone, Hkv, D, dt, page, seed=0, more=0, blank=True):
-    """groups: (prefix, [tokens behind it, or None: a request of half the prefix]); alone: lengths of requests at the end."""
+def width(B, Hkv, D, dt, page):
+    """Entries of a row from which on K and V of all rows' tokens are more than 64 MiB: prefixes are then read once."""
+    return 2 ** 26 // (B * Hkv * D * (4 if dt == "bf16" else 8) * page) + 1
+
+
+def build(groups, alone, Hkv, D, dt, page, seed=0, more=0, blank=True, wide=True):
+    """groups: (prefix, [tokens behind it, or None: a request of half the prefix]); alone: lengths of requests at the end.  wide: rows of the
+    table are at least as long as that a prefix is read once; entries behind the tokens' are no pages."""
     lens = [p // 2 if n is None else p + n for p, rows in groups for n in rows] + list(alone)
     c = Cache(lens, Hkv, D, dt, page, seed + sum(lens), more=more)
     first, share = [0], []
@@ -34,6 +40,10 @@ def build(groups, alone, Hkv, D, dt, page, seed=0, more=0, blank=True):
                     to[q, :, :p % page] = float("nan") if blank else rows_[:, full * page:p]
         first.append(f + len(rows))
         share.append(p)
+    if wide:
+        B, n = c.table.shape
+        far = torch.full((B, max(width(B, Hkv, D, dt, page) - n, 0)), 2 ** 31 - 1, dtype=torch.int32, device="cuda")
+        c.table = torch.cat([c.table, far], 1).contiguous()
     i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
     return c, i32(first), i32(share)
 
@@ -221,6 +231,17 @@ def test_a_captured_call_two_streams_and_the_same_result_every_time(ac):  # noqa
             ac.attention_paged_shared(Q, c.k, c.v, c.table, c.len, first, share, O[x], ws[x], stream=s[x])
         torch.cuda.synchronize()
         assert torch.equal(O[0], want) and torch.equal(O[1], want)
+
+
+@pytest.mark.parametrize("c", [(EDGES, [0, 1, 50], 6, 2, D, dt, page) for D, dt in TYPES for page in (7, 16)]
+                         + [([(70, [3] * 20)] * 3, [1, 2], 40, 2, 64, "bf16", 7), ([(2000, [1] * 4)], [5], 4, 1, 128, "bf16", 16), ([(300, [2] * 17)], [], 3, 1, 199, "f32", 7)],
+                         ids=lambda c: f"{len(c[0])}x{c[0][0][0]}x{len(c[0][0][1])}-{len(c[1])}-" + "-".join(map(str, c[2:])))
+def test_little_to_read(ac, c):  # noqa: F811
+    """K and V of all rows' tokens are no more than 64 MiB: every request by itself, as with no groups at all."""
+    c, Q, O, first, share = case(ac, *c, wide=False, blank=False)
+    B, Hkv, D = Q.shape[0], c.k.shape[1], Q.shape[2]
+    assert 2 * B * c.table.shape[1] * c.k[0].numel() * Q.element_size() <= 2 ** 26
+    assert torch.equal(O, c.call(ac, Q)) and torch.equal(O, call(ac, c, Q, first[:1], share[:0]))
 
 
 def test_an_empty_batch(ac):  # noqa: F811
