@@ -10,6 +10,7 @@ without a GPU tensor, the calls raise.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional
 
@@ -136,6 +137,7 @@ def lib():
         L.attncache_set_pointer_checks.argtypes = [i32]
         L.attncache_version.restype = i32
         L.attncache_version.argtypes = []
+        L.calls = {}
         _lib = L
     return _lib
 
@@ -152,6 +154,23 @@ try:
 except ImportError:
     def _address(t, dtype, shape):
         return None
+
+try:
+    from . import _tensor_arg as _native
+except ImportError:
+    _native = None
+
+
+def _call(name: str):
+    """An entry point of many arguments, by the native module where it is built: ctypes takes 1.6 to 2.4 us to convert them (0.6 so)."""
+    calls = lib().calls
+    f = calls.get(name)
+    if f is None:
+        f = getattr(lib(), name)
+        if hasattr(_native, name):
+            f = functools.partial(getattr(_native, name), ctypes.cast(f, ctypes.c_void_p).value)
+        calls[name] = f
+    return f
 
 
 def _dev(t: torch.Tensor, name: str, dtype=None, shape=None) -> int:
@@ -614,9 +633,9 @@ def attncache_rotate(X: torch.Tensor, pos: torch.Tensor, freq: Optional[torch.Te
     if slot is not None:
         sp = _dev(slot, "slot", i32, (B, S))
         kc, vc, n, page, stride = _pages(k_pages, v_pages, dtype, Hkv, D)
-    _check(lib().attncache_rotate(xp, qw, kw, pp, fp, sp, qp, kp, vp, kc, vc, B, S, Hq, Hkv, D, rot, batch_stride, row_stride,
-                                  n, page, stride, _DTYPE_CODE[dtype], int(interleaved), float(eps), float(amplitude),
-                                  _stream(stream)), "attncache_rotate")
+    _check(_call("attncache_rotate")(xp, qw, kw, pp, fp, sp, qp, kp, vp, kc, vc, B, S, Hq, Hkv, D, rot, batch_stride, row_stride,
+                                     n, page, stride, _DTYPE_CODE[dtype], int(interleaved), float(eps), float(amplitude),
+                                     _stream(stream)), "attncache_rotate")
 
 
 def attncache_page_fork_workspace_bytes(B: int, max_pages: int, n_pages: int) -> int:
@@ -645,9 +664,9 @@ def attncache_page_fork(from_row: torch.Tensor, seq_len: torch.Tensor, free_stat
     lo = _dev(seq_len_out, "seq_len_out", i32, (B,))
     fo = _dev(free_state_out, "free_state_out", i32, (2,))
     wp = _dev(workspace, "workspace")
-    _check(lib().attncache_page_fork(rp, lp, fs, fp, tp, to, lo, fo, kc, vc, B, H, D, max_pages, n, page, stride, sinks, window,
-                                     _DTYPE_CODE[k_pages.dtype], wp, workspace.numel() * workspace.element_size(),
-                                     _stream(stream)), "attncache_page_fork")
+    _check(_call("attncache_page_fork")(rp, lp, fs, fp, tp, to, lo, fo, kc, vc, B, H, D, max_pages, n, page, stride, sinks, window,
+                                        _DTYPE_CODE[k_pages.dtype], wp, workspace.numel() * workspace.element_size(),
+                                        _stream(stream)), "attncache_page_fork")
 
 
 def attention_paged_shared_workspace_bytes(B: int, Hq: int, Hkv: int, D: int, G: int) -> int:
@@ -673,9 +692,9 @@ def attention_paged_shared(Q: torch.Tensor, k_pages: torch.Tensor, v_pages: torc
     sp = _dev(share_len, "share_len", torch.int32)
     kc, vc, n, page, stride = _pages(k_pages, v_pages, Q.dtype, Hkv, D)
     wp = _dev(workspace, "workspace")
-    _check(lib().attention_paged_shared(qp, kc, vc, tp, lp, fp, sp, op, B, Hq, Hkv, D, G, n, page, max_pages, stride,
-                                        _DTYPE_CODE[Q.dtype], float(scale), wp,
-                                        workspace.numel() * workspace.element_size(), _stream(stream)), "attention_paged_shared")
+    _check(_call("attention_paged_shared")(qp, kc, vc, tp, lp, fp, sp, op, B, Hq, Hkv, D, G, n, page, max_pages, stride,
+                                           _DTYPE_CODE[Q.dtype], float(scale), wp,
+                                           workspace.numel() * workspace.element_size(), _stream(stream)), "attention_paged_shared")
 
 
 def attention_window(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, O: torch.Tensor, *, window: int, sinks: int = 0,
@@ -694,8 +713,8 @@ def attention_window(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, O: torch
     op = _dev(O, "O", Q.dtype, (B, Hq, S, D))
     rp = None if row_sel is None else _dev(row_sel, "row_sel", torch.int32, (B,))
     lp = None if key_len is None else _dev(key_len, "key_len", torch.int32, (B,))
-    _check(lib().attention_window(qp, kp, vp, op, rp, lp, B, Hq, Hkv, S, D, _DTYPE_CODE[Q.dtype], window, sinks, float(scale),
-                                  _stream(stream)), "attention_window")
+    _check(_call("attention_window")(qp, kp, vp, op, rp, lp, B, Hq, Hkv, S, D, _DTYPE_CODE[Q.dtype], window, sinks, float(scale),
+                                     _stream(stream)), "attention_window")
 
 
 def attention_paged_window(Q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor,
@@ -714,6 +733,6 @@ def attention_paged_window(Q: torch.Tensor, k_pages: torch.Tensor, v_pages: torc
     lp = _dev(seq_len, "seq_len", torch.int32, (B,))
     kc, vc, n, page, stride = _pages(k_pages, v_pages, Q.dtype, Hkv, D)
     wp = _dev(workspace, "workspace")
-    _check(lib().attention_paged_window(qp, kc, vc, tp, lp, op, B, Hq, Hkv, D, n, page, max_pages, stride,
-                                        _DTYPE_CODE[Q.dtype], window, sinks, float(scale), wp,
-                                        workspace.numel() * workspace.element_size(), _stream(stream)), "attention_paged_window")
+    _check(_call("attention_paged_window")(qp, kc, vc, tp, lp, op, B, Hq, Hkv, D, n, page, max_pages, stride,
+                                           _DTYPE_CODE[Q.dtype], window, sinks, float(scale), wp,
+                                           workspace.numel() * workspace.element_size(), _stream(stream)), "attention_paged_window")

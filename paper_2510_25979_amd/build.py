@@ -24,7 +24,7 @@ def _older(out, sources) -> bool:
 
 
 def stale() -> bool:
-    return _older(LIB, SOURCES + HEADERS) or _older(ARG, [ARG_SOURCE])
+    return _older(LIB, SOURCES + HEADERS) or _older(ARG, [ARG_SOURCE, HEADERS[-1]])
 
 
 def _lib_command():
@@ -63,7 +63,7 @@ def build(force: bool = True, verbose: bool = False) -> str:
             print(" ".join(cmd))
         lib = subprocess.Popen(cmd)
     try:
-        if force or _older(ARG, [ARG_SOURCE]):
+        if force or _older(ARG, [ARG_SOURCE, HEADERS[-1]]):
             _build_arg(verbose)
     finally:
         code = lib.wait() if lib else 0
