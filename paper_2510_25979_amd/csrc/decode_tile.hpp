@@ -302,27 +302,51 @@ struct DecodeF32 {
     m = -INFINITY;
     l = 0.f;
   }
-  __device__ __forceinline__ f32x4 four(const float* row, int c) const {   // columns c ... c + 3, zeros behind the row's end
-    if (FULL) return *reinterpret_cast<const f32x4*>(row + c);
+  // Columns c ... c + 3, where a row of at least four ends the last four: no load sits behind a test.  What is then in Q and K twice is taken out (once());
+  // columns of V that were read too early are the results' columns, which decode_piece shifts back.  (us, a test a piece / so: runs of
+  // 42 requests on two heads of 100 112 / 75, 64 on four of 33 52 / 29, 24 on 12 of 199 109 / 109.)
+  __device__ __forceinline__ f32x4 four(const float* row, int c) const {
+    return *reinterpret_cast<const f32x4_dw*>(row + (FULL ? c : min(c, D - 4)));
+  }
+  // First column of piece s of K and Q: a row's last piece, where it is no whole one, is piece 0, the others follow.
+  __device__ __forceinline__ int first_of(int s) const { return FULL ? 16 * s : s == 0 ? D & ~15 : 16 * s - 16; }
+  __device__ __forceinline__ f32x4 once(f32x4 r) const {   // of piece 0
+    const int twice = D < 4 ? 0 : 4 * kq + 4 - (D & 15);
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+      if (t < twice) r[t] = 0.f;
+    return r;
+  }
+  __device__ __forceinline__ f32x4 few(const float* row, bool mine) const {   // a row of fewer
     f32x4 r = {0.f, 0.f, 0.f, 0.f};
-    if (c + 4 <= D) {
-      r = *reinterpret_cast<const f32x4_dw*>(row + c);
-    } else {
+    if (mine)
 #pragma unroll
       for (int t = 0; t < 3; ++t)
-        if (c + t < D) r[t] = row[c + t];
-    }
+        if (t < D) r[t] = row[t];
     return r;
   }
   __device__ __forceinline__ void load_row(Query& q, const Elt* row) const {
+    if (!FULL && D < 4) {
+      q.r[0] = few(row, kq == 0);
 #pragma unroll
-    for (int s = 0; s < 4 * DB; ++s) q.r[s] = four(row, 16 * s + 4 * kq);
+      for (int s = 1; s < 4 * DB; ++s) q.r[s] = f32x4{0.f, 0.f, 0.f, 0.f};
+      return;
+    }
+#pragma unroll
+    for (int s = 0; s < 4 * DB; ++s) {
+      q.r[s] = four(row, first_of(s) + 4 * kq);
+      if (!FULL && s == 0) q.r[s] = once(q.r[s]);
+    }
   }
   __device__ __forceinline__ void load_q(Query& q, const Elt* rows, int n_rows) const { load_row(q, rows + (size_t)min(i, n_rows - 1) * dim()); }
   __device__ __forceinline__ void load_k(const Elt* base, const int64_t (&at)[1]) {
     const float* src = base + (at[0] < 0 ? 0 : at[0]);
+    if (!FULL && D < 4) {
+      k[0] = few(src, kq == 0);   // (no other is multiplied)
+      return;
+    }
 #pragma unroll
-    for (int s = 0; s < 4 * DB; ++s) k[s] = four(src, 16 * s + 4 * kq);
+    for (int s = 0; s < 4 * DB; ++s) k[s] = four(src, first_of(s) + 4 * kq);
   }
   // columns 64 b + 4 i and three more of keys 4 kq ... 4 kq + 3; zeros if they are not there
   __device__ __forceinline__ void load_v(const Elt* base, const int64_t (&at)[1]) {
@@ -332,7 +356,7 @@ struct DecodeF32 {
       const float* src = base + (from < 0 ? 0 : from);
 #pragma unroll
       for (int b = 0; b < DB; ++b) {
-        v[t][b] = four(src, 64 * b + 4 * i);
+        v[t][b] = !FULL && D < 4 ? few(src, i == 0) : four(src, 64 * b + 4 * i);
         if (from < 0) v[t][b] = f32x4{0.f, 0.f, 0.f, 0.f};
       }
     }
@@ -341,10 +365,15 @@ struct DecodeF32 {
   __device__ __forceinline__ void scores(Scores& s, const Query& q) const {
     s[0] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int c = 0; c < 4 * DB; ++c)
-      if (FULL || 16 * c < D)
+    for (int c = FULL ? 0 : 1; c < 4 * DB; ++c)
+      if (FULL || 16 * c <= D)
 #pragma unroll
         for (int t = 0; t < 4; ++t) s[0] = mfma_f32(k[c][t], q.r[c][t], s[0]);
+    if (!FULL && (D & 15)) {
+      const f32x4 part = once(k[0]);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) s[0] = mfma_f32(part[t], q.r[0][t], s[0]);
+    }
   }
   __device__ __forceinline__ void hide(Scores& s, const int64_t (&at)[1]) {
     const uint32_t seen = (uint32_t)__ballot(at[0] >= 0) >> (4 * kq);
@@ -395,7 +424,14 @@ __device__ __forceinline__ f32x4 decode_piece(const DecodeBf16<D>& c, int n) { r
 template <int DB, bool FULL>
 __device__ __forceinline__ f32x4 decode_piece(const DecodeF32<DB, FULL>& c, int n) {
   const int b = n >> 2, x = n & 3;
-  return f32x4{c.acc[4 * b][x], c.acc[4 * b + 1][x], c.acc[4 * b + 2][x], c.acc[4 * b + 3][x]};
+  f32x4 r = {c.acc[4 * b][x], c.acc[4 * b + 1][x], c.acc[4 * b + 2][x], c.acc[4 * b + 3][x]};
+  if (!FULL && c.D >= 4) {   // columns that were read too early
+    const int by = c.col(n) - (c.D - 4);
+    if (by == 1) r = f32x4{r[1], r[2], r[3], 0.f};
+    if (by == 2) r = f32x4{r[2], r[3], 0.f, 0.f};
+    if (by == 3) r = f32x4{r[3], 0.f, 0.f, 0.f};
+  }
+  return r;
 }
 __device__ __forceinline__ void store_partial(float* to, const f32x4 r, int d, int D) {
   if (d + 4 <= D) *reinterpret_cast<f32x4_dw*>(to) = r;
@@ -830,6 +866,7 @@ inline hipError_t launch_decode_as(const DecodeLaunch& p, DecodeArgs& a, hipStre
   if (p.D == 128) return launch_decode_core<DecodeF32<2, true>, Kernels>(a, stream);
   if (p.D < 64) return launch_decode_core<DecodeF32<1, false>, Kernels>(a, stream);
   if (p.D < 128) return launch_decode_core<DecodeF32<2, false>, Kernels>(a, stream);
+  if (p.D == 256) return launch_decode_core<DecodeF32<4, true>, Kernels>(a, stream);
   return launch_decode_core<DecodeF32<4, false>, Kernels>(a, stream);
 }
 

@@ -233,7 +233,7 @@ __global__ __launch_bounds__(kForkRows) void fork_small_kernel(const ForkArgs a)
     while (free[w]) {
       const int bit = __ffs(free[w]) - 1;
       free[w] &= free[w] - 1;
-      a.ring[(end + at % (unsigned)a.n) % (unsigned)a.n] = 32 * (tid * NW + w) + bit;
+      a.ring[end + at < (unsigned)a.n ? end + at : end + at - a.n] = 32 * (tid * NW + w) + bit;   // (at < n: each page once)
       ++at;
     }
   if (tid < a.B) a.seq_out[tid] = len;
@@ -311,7 +311,7 @@ __global__ __launch_bounds__(kThreads) void fork_ring_kernel(const ForkArgs a) {
     while (free) {
       const int bit = __ffs(free) - 1;
       free &= free - 1;
-      a.ring[(end + at % (unsigned)a.n) % (unsigned)a.n] = 32 * (c + tid) + bit;
+      a.ring[end + at < (unsigned)a.n ? end + at : end + at - a.n] = 32 * (c + tid) + bit;   // (at < n: each page once)
       ++at;
     }
     before += all;

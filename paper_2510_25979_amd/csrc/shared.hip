@@ -931,6 +931,7 @@ hipError_t launch_shared(const SharedLaunch& p, hipStream_t stream) {
   if (p.d.D == 128) return launch_shared_as<SharedF32<2, true>>(a, big, stream);
   if (p.d.D < 64) return launch_shared_as<SharedF32<1, false>>(a, big, stream);
   if (p.d.D < 128) return launch_shared_as<SharedF32<2, false>>(a, big, stream);
+  if (p.d.D == 256) return launch_shared_as<SharedF32<4, true>>(a, big, stream);
   return launch_shared_as<SharedF32<4, false>>(a, big, stream);
 }
 

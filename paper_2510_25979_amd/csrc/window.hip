@@ -443,6 +443,7 @@ hipError_t launch_window(const WindowLaunch& p, hipStream_t stream) {
   if (p.D < 4) return launch_window_f32<1, kFewCols>(a, stream);
   if (p.D < 64) return p.D % 4 ? launch_window_f32<1, kAnyCols>(a, stream) : launch_window_f32<1, kVecCols>(a, stream);
   if (p.D < 128) return p.D % 4 ? launch_window_f32<2, kAnyCols>(a, stream) : launch_window_f32<2, kVecCols>(a, stream);
+  if (p.D == 256) return launch_window_f32<4, kAllCols>(a, stream);
   return p.D % 4 ? launch_window_f32<4, kAnyCols>(a, stream) : launch_window_f32<4, kVecCols>(a, stream);
 }
 

@@ -65,7 +65,7 @@ def some_heads(B, Hq, most=12):
 # B, Hq, Hkv, S: one token, block borders and beside them, heads alone and many on a K and V
 SIZES = [(1, 1, 1, 1), (2, 4, 2, 2), (3, 3, 1, 15), (2, 6, 2, 17), (1, 5, 1, 31), (2, 4, 4, 32), (2, 8, 1, 33), (9, 3, 3, 64), (2, 7, 1, 65), (4, 12, 12, 96),
          (2, 8, 2, 127), (1, 40, 2, 130), (17, 4, 2, 200), (1, 2, 2, 513), (1, 8, 2, 1100)]
-TYPES = [(64, "bf16"), (128, "bf16"), (64, "f32"), (128, "f32"), (3, "f32"), (33, "f32"), (36, "f32"), (80, "f32"), (101, "f32"), (199, "f32"), (256, "f32")]
+TYPES = [(64, "bf16"), (128, "bf16"), (64, "f32"), (128, "f32"), (3, "f32"), (33, "f32"), (36, "f32"), (80, "f32"), (101, "f32"), (199, "f32"), (200, "f32"), (256, "f32")]
 MANY = [(33, 12, 4, 100), (20, 24, 2, 50)]      # (binary32: more than 256 workgroups of 64 rows)
 WINDOWS = [(1, 0), (1, 1), (7, 3), (32, 0), (33, 70), (64, 4), (100, 16), (300, 64), (10 ** 9, 0), (5, 10 ** 9), (2 ** 31 - 1, 2 ** 31 - 1)]
 

@@ -125,3 +125,30 @@ def test_a_captured_step_goes_on_by_itself(ac):  # noqa: F811
                 gen.check(O[b, h], *gen.attend(Q[b, h], kk, vv))
         held = sum(len({j // p for j in range(len(past)) if j >= (len(past) - window) // p * p or j < -(-sinks // p) * p}) for _ in range(B))
         assert n - state[1].item() == held
+
+
+@pytest.mark.parametrize("D", [1, 2, 3, 4, 5, 15, 17, 33, 36, 65, 100, 101, 127, 129, 199, 200, 255])
+def test_infinities_in_single_columns(ac, D):  # noqa: F811
+    """Binary32 rows of any length: a key of which one column is -inf weighs nothing, a value of which one is infinite fills that column and no other."""
+    lens, cols = [60, 3000], sorted({0, max(D - 18, 0), *range(max(D - 5, 0), D)})
+    c = Cache(lens, 2, D, "f32", 16, D)
+    Q = torch.randn(2, 6, D, generator=c.gen, device="cuda").abs() + 0.1
+    for b, n in enumerate(lens):
+        for j, col in enumerate(cols):
+            if 17 * j < n:
+                c.k[c.table[b, j], :, j, col] = -float("inf")       # key 17 j
+        c.v[c.table[b, 1], :, 2, D - 1] = float("inf")
+    keep = [[j for j in range(n) if j % 17 or j >= 17 * len(cols)] for n in lens]
+    ws = torch.empty(ac.attention_paged_workspace_bytes(2, 6, 2, D), dtype=torch.uint8, device="cuda")
+    O = [torch.empty_like(Q) for _ in range(2)]
+    ac.attention_paged(Q, c.k, c.v, c.table, c.len, O[0], ws)
+    ac.attention_paged_window(Q, c.k, c.v, c.table, c.len, O[1], ws, window=4000)
+    for b in range(2):
+        c.rows[b] = [r[:, keep[b]] for r in c.rows[b]]
+    for o in O:
+        assert (o[:, :, D - 1] == float("inf")).all()
+        for b in range(2):
+            for h in range(2):
+                want, terms, bound = gen.attend(Q[b, 3 * h:3 * h + 3], c.rows[b][0][h], c.rows[b][1][h])
+                if D > 1:
+                    gen.check(o[b, 3 * h:3 * h + 3, :D - 1], want[:, :D - 1], terms[:, :D - 1], bound)
