@@ -707,9 +707,10 @@ int32_t attncache_page_fork(const int32_t *from, const int32_t *seq_len,
  * 2^25, Hkv * (B * ceil(g / 16) + B * g / 16 + G) * (ceil(max_pages * page_size /
  * 16) + 2) below 2^31 - 65536, with g = Hq / Hkv.  Two launches up to 256
  * requests and 255 groups, otherwise three, the first of which is one workgroup
- * that looks through the requests, 1,024 a step.  Without groups, and where K and
- * V of B * max_pages * page_size tokens are at most 64 MiB, the launches of
- * attention_paged, and each request's own row of the table is followed.
+ * that looks through the requests, 1,024 a step.  Without groups, where max_pages
+ * * page_size is at most 128, and where K and V of B times as many tokens are at
+ * most 64 MiB, the launches of attention_paged, and each request's own row of the
+ * table is followed.
  * Deterministic.
  */
 size_t attention_paged_shared_workspace_bytes(int32_t B, int32_t Hq,

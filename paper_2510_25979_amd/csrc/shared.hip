@@ -901,12 +901,14 @@ static hipError_t launch_shared_as(SharedArgs& a, bool big, hipStream_t stream) 
 // Where K and V of the most tokens that all requests can have are at most 64 MiB, reading them for each request by itself (mostly from the caches) takes
 // less time than finding out what is shared and adding up its parts.  us, shared / by itself: two answers to 16 tokens 10.9 / 4.8, 60 to 200 (61 MiB) 23.2 / 10.0,
 // 240 requests on eight heads to 16 tokens 27.1 / 6.5, 64 to 910 tokens (60 MiB) 21.2 / 18.8, 8 to 15,000 (60 MiB) 18.7 / 22.0, 17 in binary32 on eight heads of
-// 128 to 1,270 (169 MiB) 21.6 / 26.9, 141 of 64 columns to 1,168 (80 MiB) 15.5 / 20.6, 23 on 12 heads to 768 (104 MiB) 23.3 / 16.5.  The host knows how many
-// tokens requests can have, not how many they have or share.
+// 128 to 1,270 (169 MiB) 21.6 / 26.9, 141 of 64 columns to 1,168 (80 MiB) 15.5 / 20.6, 23 on 12 heads to 768 (104 MiB) 23.3 / 16.5.  Up to 128 tokens that holds for
+// any number of requests: 748 on 12 heads of 64, prefixes of 12 tokens 67 / 44, of 102 46 / 43; 256 on eight of 128 38 / 20, 33 / 21; to 256 tokens, prefixes of
+// 25 99 / 70 and 49 / 33, of 204 51 / 68 and 36 / 36.  The host knows how many tokens requests can have, not how many they have or share.
 constexpr int64_t kSharedWorth = 64LL << 20;
+constexpr int kSharedTokens = 128;
 
 hipError_t launch_shared(const SharedLaunch& p, hipStream_t stream) {
-  if (p.G == 0 || (double)p.d.B * p.d.Hkv * p.d.Sk * p.d.D * (p.d.is_f32 ? 8 : 4) <= (double)kSharedWorth) return launch_decode(p.d, stream);
+  if (p.G == 0 || p.d.Sk <= kSharedTokens || (double)p.d.B * p.d.Hkv * p.d.Sk * p.d.D * (p.d.is_f32 ? 8 : 4) <= (double)kSharedWorth) return launch_decode(p.d, stream);
   SharedArgs a;
   a.d = decode_args(p.d);
   a.g = p.d.R; a.G = p.G;

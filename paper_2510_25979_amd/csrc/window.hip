@@ -223,7 +223,7 @@ __global__ __launch_bounds__(kThreads, 2) void window_bf16_kernel(const WindowAr
 // them four times: 96; eight waves, two for each row: 82.  Bound by products and softmax (47 us of it; four times the items take 216) and, where a
 // chip's few rounds of workgroups end unevenly, by the last ones.
 template <int DB, int COLS, int SPLIT>   // SPLIT: waves that share 16 rows, each with 16 keys of every stage
-__global__ __launch_bounds__(kThreads, 2) void window_f32_kernel(const WindowArgs a) {
+__global__ __launch_bounds__(kThreads, DB == 4 && COLS == kAllCols && SPLIT == 2 ? 1 : 2) void window_f32_kernel(const WindowArgs a) {
   constexpr int KC = kF32Rows * SPLIT, UNITS = 4 / SPLIT;   // keys of a stage; units of a workgroup
   constexpr bool DIRECT = COLS == kAllCols;   // rows go straight to LDS, into two stages in turn
   typedef F32Stage<DB, KC, COLS> Stage;

@@ -54,6 +54,7 @@ def test_every_kernel_is_reached(tmp_path):
     (("shared", 64, 32, 8, 64, 1, 1100, 16, 1100, 1 << 22, "bf16"), ["shared_both_kernel<64, true, true>", "shared_join_kernel<false, 16, 1>"]),
     (("shared", 17, 24, 8, 128, 4, 1100, 10, 200, None, "f32"), ["shared_run_kernel<SharedF32<2, true>, true>", "shared_join_kernel<true, 32, 4>"]),
     (("shared", 61, 8, 8, 128, 1, 1100, 16, 16, None, "bf16"), ["decode_unit_kernel"]),
+    (("shared", 10000, 8, 8, 128, 1, 1100, 16, 8, None, "bf16"), ["decode_unit_kernel"]),
     (("shared", 8, 8, 1, 128, 1, 1100, 16, 900, None, "bf16"), ["decode_run_kernel", "decode_join_kernel"]),
     (("shared", 64, 32, 8, 128, 0, 1100, 16, 1100, None, "bf16"), ["decode_run_kernel", "decode_join_kernel"]),
     (("window", 4, 32, 8, 4096, 128, 1024, 4, "bf16"), ["window_bf16_kernel<128>"]),

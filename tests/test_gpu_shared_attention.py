@@ -12,8 +12,8 @@ pytestmark = pytest.mark.gpu
 
 
 def width(B, Hkv, D, dt, page):
-    """Entries of a row from which on K and V of all rows' tokens are more than 64 MiB: prefixes are then read once."""
-    return 2 ** 26 // (B * Hkv * D * (4 if dt == "bf16" else 8) * page) + 1
+    """Entries of a row from which on it has room for more than 128 tokens, and K and V of all rows' are more than 64 MiB: prefixes are then read once."""
+    return max(2 ** 26 // (B * Hkv * D * (4 if dt == "bf16" else 8)), 128) // page + 1
 
 
 def build(groups, alone, Hkv, D, dt, page, seed=0, more=0, blank=True, wide=True):
