@@ -662,7 +662,7 @@ int32_t attncache_rotary_frequencies(double *freq, int32_t rot, double base,
  * The outputs may be the inputs of the same meaning, or not overlap them.
  * workspace: DEVICE, attncache_page_fork_workspace_bytes(...) bytes, 16-byte
  * aligned; scratch, and written by a call before it is read.  Two launches up
- * to 1,024 rows, 16,384 entries of page_table and 65,536 pages, otherwise three.
+ * to 1,024 rows, 8,192 entries of page_table and 65,536 pages, otherwise three.
  * Results do not depend on the order of threads.  B <= 2^22, B * max_pages below
  * 2^31 - 4096, page_size * D <= 2^30, otherwise as in attncache_page_plan.
  */

@@ -5,7 +5,7 @@
 // one row keeps it (the row itself if it goes on, otherwise the first that takes it) and each other takes a page from the ring and copies its
 // tokens.  A page is free when some row had it and no row has it: two bitmaps of the pages, before and after, say so without a count a page.
 //
-// Bookkeeping of up to 1,024 rows, 16,384 entries and 65,536 pages is one workgroup's work, in LDS; then the tokens are copied by the whole chip.
+// Bookkeeping of up to 1,024 rows, 8,192 entries and 65,536 pages is one workgroup's work, in LDS; then the tokens are copied by the whole chip.
 // Otherwise three launches, since each needs all of the one before: the rows (who keeps, who copies, which of the ring's pages; one workgroup,
 // which looks at 1,024 rows a step, while others clear the bitmaps), tables and bitmaps, then the ring (one workgroup, pages in order of their
 // number) beside the copies and the way back of tables that are replaced in place.
@@ -24,13 +24,14 @@ struct ForkArgs {
   int32_t *src, *len, *take, *keeper, *sums, *staged;
   int4* copy;
   uint32_t *had, *has;
-  int32_t B, H, max_pages, n, ps, sinks, window, words, segs, row_pieces, wgs;   // wgs: workgroups that copy
+  int32_t B, H, max_pages, n, ps, sinks, window, words, segs, row_pieces, wgs, flat;   // wgs: workgroups that copy; flat: entries of one of fork_flat_kernel
   int64_t page_stride;   // pieces
   Divider by_ps, by_segs, by_max_pages;
 };
 
 constexpr int kForkRows = 1024;   // threads of the workgroup that plans
 constexpr int kForkEntries = 4 * kThreads;   // entries of a table that a workgroup deals with
+constexpr int kForkSmallWords = 2048;        // most of a bitmap in LDS
 
 __device__ __forceinline__ int fork_pages_of(const ForkArgs& a, int tokens) { return tokens > 0 ? a.by_ps.div(tokens - 1) + 1 : 0; }
 __device__ __forceinline__ int fork_tokens(const ForkArgs& a, int b) { return min(max(a.seq_len[b], 0), a.max_pages * a.ps); }
@@ -71,17 +72,23 @@ __global__ __launch_bounds__(kForkRows) void fork_rows_kernel(const ForkArgs a) 
     return;
   }
   __shared__ int part[kForkRows / kWave];
+  __shared__ int s_keeper[kForkRows];
   __shared__ int s_taken;
   const int first = ring_first(a.state[0], a.n), count = min(max(a.state[1], 0), a.n);
-  for (int b = tid; b < a.B; b += kForkRows) a.keeper[b] = a.B;
+  const bool few = a.B <= kForkRows;   // keepers in LDS: no fences (100 rows 10.4 us with them, 3.4 so)
   if (tid == 0) s_taken = 0;
-  __threadfence();
+  if (few) {
+    s_keeper[tid] = a.B;
+  } else {
+    for (int b = tid; b < a.B; b += kForkRows) a.keeper[b] = a.B;
+    __threadfence();
+  }
   __syncthreads();
   for (int b = tid; b < a.B; b += kForkRows) {
     const int f = a.from[b];
-    if ((unsigned)f < (unsigned)a.B) atomicMin(&a.keeper[f], f == b ? -1 : b);
+    if ((unsigned)f < (unsigned)a.B) atomicMin(few ? &s_keeper[f] : &a.keeper[f], f == b ? -1 : b);
   }
-  __threadfence();
+  if (!few) __threadfence();
   __syncthreads();
   int before = 0;
   for (int c = 0; c < a.B; c += kForkRows) {
@@ -94,7 +101,7 @@ __global__ __launch_bounds__(kForkRows) void fork_rows_kernel(const ForkArgs a) 
       if (f >= 0) {
         len = fork_tokens(a, f);
         // (as the atomics left it, past the first-level cache)
-        const int k = __hip_atomic_load(&a.keeper[f], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const int k = few ? s_keeper[f] : __hip_atomic_load(&a.keeper[f], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         copies = len - a.by_ps.div(len) * a.ps > 0 && (k == -1 ? f : k) != b;
       }
     }
@@ -151,8 +158,46 @@ __global__ __launch_bounds__(kThreads) void fork_tables_kernel(const ForkArgs a)
   }
 }
 
+// The same where the bitmaps fit LDS: workgroups mark a.flat entries each there, and then words at a time in the workspace, where atomics on a few lines
+// take turns (24,000 entries 16 us one by one, 5 so).
+__global__ __launch_bounds__(kThreads) void fork_flat_kernel(const ForkArgs a) {
+  __shared__ uint32_t s_had[kForkSmallWords], s_has[kForkSmallWords];
+  const int tid = threadIdx.x;
+  for (int w = tid; w < a.words; w += kThreads) s_had[w] = s_has[w] = 0;
+  __syncthreads();
+  auto mark = [&](uint32_t* bits, int page) {
+    if ((unsigned)page < (unsigned)a.n) atomicOr(&bits[page >> 5], 1u << (page & 31));
+  };
+  int32_t* out = a.table_out == a.table ? a.staged : a.table_out;
+  const int e0 = blockIdx.x * a.flat, e1 = e0 + min(a.flat, a.B * a.max_pages - e0);
+#pragma unroll 4
+  for (int e = e0 + tid; e < e1; e += kThreads) {
+    const int b = a.by_max_pages.div(e), j = e - b * a.max_pages, src = a.src[b], len = a.len[b];
+    const int now = src >= 0 ? fork_pages_of(a, len) : 0;
+    if (j < fork_pages_of(a, fork_tokens(a, b))) mark(s_had, a.table[e]);
+    if (j < now) {
+      int page = a.table[(size_t)src * a.max_pages + j];
+      if (j == now - 1 && a.take[b] >= 0) {
+        const int fresh = fork_ring_page(a, a.sums[0], a.take[b]);
+        a.copy[a.take[b]] = make_int4(page, fresh, len - j * a.ps, 0);
+        page = fresh;
+      }
+      if (fork_gone(a, len, j)) page = -1;
+      out[e] = page;
+      mark(s_has, page);
+    }
+  }
+  __syncthreads();
+  for (int w = tid; w < a.words; w += kThreads) {
+    if (s_had[w]) atomicOr(&a.had[w], s_had[w]);
+    if (s_has[w]) atomicOr(&a.has[w], s_has[w]);
+  }
+}
+
 // The whole plan by one workgroup.  Everything is read before anything is written, since outputs may be inputs.
-constexpr int kForkSmallEntries = 16384, kForkSmallWords = 2048;
+// us, one workgroup / three launches, replayed and called: 8,000 entries of 16 rows 11.2 / 11.2, 12.2 / 13.9, of 128 rows 12.7 / 12.4, 13.3 / 14.8; 9,600 of 320
+// rows 15.3 / 12.9, 15.8 / 14.7; 16,000 of 32 rows 14.1 / 10.9, 14.7 / 13.8; 4,000 of 32 9.9 / 11.3, 11.5 / 14.3.
+constexpr int kForkSmallEntries = 8192;
 __global__ __launch_bounds__(kForkRows) void fork_small_kernel(const ForkArgs a) {
   constexpr int N = kForkSmallEntries / kForkRows, NW = kForkSmallWords / kForkRows;
   __shared__ int s_keeper[kForkRows], s_src[kForkRows], s_len[kForkRows], s_take[kForkRows], s_held[kForkRows];
@@ -342,7 +387,8 @@ static hipError_t launch_fork_as(const ForkArgs& a, hipStream_t stream) {
   hipLaunchKernelGGL(fork_rows_kernel, dim3((unsigned)(1 + (clear < 1024 ? clear : 1024))), dim3(kForkRows), 0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(fork_tables_kernel, dim3((unsigned)(a.B * a.segs)), dim3(kThreads), 0, stream, a);
+  if (a.words <= kForkSmallWords) hipLaunchKernelGGL(fork_flat_kernel, dim3((unsigned)((entries - 1) / a.flat + 1)), dim3(kThreads), 0, stream, a);
+  else hipLaunchKernelGGL(fork_tables_kernel, dim3((unsigned)(a.B * a.segs)), dim3(kThreads), 0, stream, a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int back = a.table_out == a.table ? (a.B < 1024 ? a.B : 1024) : 0;
@@ -358,6 +404,7 @@ hipError_t launch_fork(const ForkLaunch& p, hipStream_t stream) {
   a.B = p.B; a.H = p.H; a.max_pages = p.max_pages; a.n = p.n_pages; a.ps = p.page_size;
   a.sinks = p.sinks; a.window = p.window;
   a.words = (int)fork_words(p.n_pages);
+  a.flat = a.words > 256 ? 4 * a.words : 1024;   // (several entries for each word that is written)
   a.copy = static_cast<int4*>(p.ws);
   a.sums = static_cast<int32_t*>(p.ws) + 4 * (size_t)p.B;
   a.had = reinterpret_cast<uint32_t*>(a.sums + 4);

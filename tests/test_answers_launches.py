@@ -45,8 +45,8 @@ def test_every_kernel_is_reached(tmp_path):
 
 @pytest.mark.parametrize("call,kernels", [
     (("fork", 32, 8, 128, 127, 16, 5000, False, "bf16"), ["fork_small_kernel", "fork_copy_kernel"]),
-    (("fork", 1025, 8, 128, 10, 16, 5000, False, "bf16"), ["fork_rows_kernel", "fork_tables_kernel", "fork_ring_kernel"]),
-    (("fork", 16, 8, 128, 1025, 16, 5000, False, "bf16"), ["fork_rows_kernel", "fork_tables_kernel", "fork_ring_kernel"]),
+    (("fork", 1025, 8, 128, 10, 16, 5000, False, "bf16"), ["fork_rows_kernel", "fork_flat_kernel", "fork_ring_kernel"]),
+    (("fork", 16, 8, 128, 1025, 16, 5000, False, "bf16"), ["fork_rows_kernel", "fork_flat_kernel", "fork_ring_kernel"]),
     (("fork", 16, 8, 128, 10, 16, 65537, False, "bf16"), ["fork_rows_kernel", "fork_tables_kernel", "fork_ring_kernel"]),
     (("shared", 64, 32, 8, 128, 1, 1100, 16, 1100, None, "bf16"), ["shared_both_kernel<128, false, true>", "shared_join_kernel<false, 32, 1>"]),
     (("shared", 4, 32, 8, 128, 1, 1100, 16, 1100, None, "bf16"), ["shared_run_kernel<SharedBf16<128>, true>", "shared_join_kernel<false, 32, 4>"]),
