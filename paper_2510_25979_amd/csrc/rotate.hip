@@ -4,7 +4,7 @@
 //   (a, b) -> amp (a cos t - b sin t, b cos t + a sin t)    of its first `rot` columns in pairs, t = position * freq[pair]
 //
 // Bound by memory: every element is read once from HBM and written once (K and V twice where they go to the cache, too): 32 prompts of up to 1,024 tokens,
-// 48 heads of 64 (232 MB) 50 us = 4.7 TB/s, 4,000 tokens of 48 heads of 128 25.  A workgroup takes a few tokens and some or all of their heads.  It forms
+// 48 heads of 64 (232 MB) 50 to 57 us = 4.1 to 4.7 TB/s, 4,000 tokens of 48 heads of 128 25.  A workgroup takes a few tokens and some or all of their heads.  It forms
 // the sines and cosines of its tokens once, through LDS; the other half of a pair that is not in a lane's own piece is loaded a second time (from L1).
 // Few tokens are bound by latency, position -> angle -> store, 128 of one token each 5.2 us.
 //

@@ -7,12 +7,14 @@
 //
 // The list says who is in which group, what each item has and where its blocks are numbered.  Up to 256 requests and 255 groups each workgroup makes it
 // for itself, in LDS; otherwise shared_plan_kernel writes it before.
-// shared_prefix (bf16) forms prefixes of many rows: workgroups of 128 rows that share chunks of 64 keys in LDS, as cross.hip has them, each an equal
+// shared_prefix (bf16) forms prefixes of many rows: workgroups of 128 rows that share chunks of 64 keys in LDS (stream_tile.hpp), each an equal
 //   run of all such chunks, so that few groups fill the chip and many short ones do, too.
-// shared_run forms everything else in units of 16 rows of one (item, K/V head), cut into equal runs of blocks by wave, as decode.hip.
+// shared_run forms everything else in units of 32 rows (binary32 16) of one (item, K/V head), cut into equal runs of blocks by wave, as decode.hip.
 // shared_join_kernel adds up an output row's parts.
 //
-// Bound by memory where own keys prevail, by the prefixes' products and the partial results' way through memory otherwise.
+// 64 requests of 32 heads on 8 of 128 that share 16,000 tokens 45 us, of which the list takes 5, the prefix 31 -- 16 chunks of some 1.3 us one after another in each
+// workgroup: products, page numbers and copies each need about as long, and neither without the others' wait is much faster (36 without the copies, 33 without
+// the products) --, the join 7.  134 requests that share little: bound by memory, 44 of 50 us in the runs.
 #include <type_traits>
 
 #include "decode_tile.hpp"
