@@ -33,6 +33,7 @@ __global__ __launch_bounds__(NW == 1 ? kThreads : NW * kWave) void decode_join_k
 
 template <DecodeKeys KEYS>
 struct DecodeKernels {
+  static constexpr bool kWave = false;
   template <class Core> static constexpr auto run() { return &decode_run_kernel<Core, KEYS>; }
   template <class Core, int NW> static constexpr auto unit() { return &decode_unit_kernel<Core, KEYS, NW>; }
   template <bool F32, int G, int NW> static constexpr auto join() { return &decode_join_kernel<F32, G, NW>; }

@@ -587,6 +587,76 @@ __device__ __forceinline__ void decode_run(const DecodeArgs& a) {
   }
 }
 
+// A wave per unit, where units are many and small: four of them start with one workgroup, and nothing is added up.  us, four waves a unit / one, bf16 heads of
+// 64: 2,048 units of 12 keys 8.1 / 4.9, of 64 11.7 / 9.0, of 128 15.5 / 13.5, of 254 30.2 / 29.3; 8,192 of 12 24.1 / 10.3; 1,536 of 128 13.0 / 12.3 (of 128
+// columns 21.7 / 23.1); 512 of 12 4.3 / 3.7, of 64 5.2 / 6.0; binary32 of 128: 2,048 of 12 16.2 / 11.2, of 64 33.7 / 31.5; of 100 22.6 / 11.1, 37.2 / 27.8.
+template <class Core>
+inline bool decode_by_wave(const DecodeArgs& a) {
+  const int64_t units = (int64_t)a.B * a.Hkv * a.rbs;
+  return units <= (1 << 25) && (a.Sk <= 2 * Core::BK ? units >= 1024 : units >= 2048 && a.Sk <= 4 * Core::BK);
+}
+template <class Core, DecodeKeys KEYS>
+__device__ __forceinline__ void decode_wave(const DecodeArgs& a) {
+  typedef typename Core::Elt Elt;
+  constexpr int BK = Core::BK, KPL = Core::KPL;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[Core::LDS ? 4 * Core::LDS : 16];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int unit = 4 * blockIdx.x + wave, head = a.by_rbs.div(unit), rb = unit - head * a.rbs;
+  if (head >= a.B * a.Hkv) return;
+  const int b = head / a.Hkv, hk = head - b * a.Hkv;
+  int skip;
+  const int keys = decode_keys_of<KEYS>(a, b, skip), nb = (keys + BK - 1) / BK;
+  Core core(a, lds + (Core::LDS ? wave * Core::LDS : 0), lane);
+  const int D = core.dim(), rows = min(kDecodeRows, a.R - kDecodeRows * rb);
+  const size_t row0 = (size_t)head * a.R + kDecodeRows * rb;
+  const Elt* K = static_cast<const Elt*>(a.K) + (size_t)hk * a.head_stride;
+  const Elt* V = static_cast<const Elt*>(a.V) + (size_t)hk * a.head_stride;
+  typename Core::Query q;
+  int page[KPL];
+  int64_t at[KPL], at_then[KPL];
+  auto ask = [&](int blk) {
+#pragma unroll
+    for (int t = 0; t < KPL; ++t) page[t] = decode_ask<KEYS>(a, b, keys, skip, BK * blk + core.key(t));
+  };
+  auto place = [&](int blk, int64_t(&to)[KPL]) {
+#pragma unroll
+    for (int t = 0; t < KPL; ++t) to[t] = decode_at<KEYS>(a, keys, skip, BK * blk + core.key(t), page[t], D);
+  };
+  core.reset();
+  if (nb > 0) {
+    ask(0);
+    core.load_q(q, static_cast<const Elt*>(a.Q) + row0 * D, rows);
+    place(0, at);
+    core.load_k(K, at);
+    core.load_v(V, at);
+    if (nb > 1) ask(1);
+  }
+  for (int blk = 0; blk < nb; ++blk) {
+    typename Core::Scores s;
+    core.scores(s, q);
+    const bool more = blk + 1 < nb;
+    if (more) {
+      place(blk + 1, at_then);
+      core.load_k(K, at_then);
+      if (blk + 2 < nb) ask(blk + 2);
+    }
+    core.hide(s, at);
+    core.stage_v();
+    if (Core::LDS && more) core.load_v(V, at_then);
+    if (Core::LDS) wave_fence();
+    core.add(s, a.scale_log2e);
+    if (Core::LDS) wave_fence();
+    if (!Core::LDS && more) core.load_v(V, at_then);
+#pragma unroll
+    for (int t = 0; t < KPL; ++t) at[t] = at_then[t];
+  }
+  const float l = sum_of_four(core.l), inv = l == 0.f ? 0.f : 1.f / l;   // no key at all: zeros
+  if (core.i >= rows) return;
+  Elt* o = static_cast<Elt*>(a.O) + (row0 + core.i) * D;
+#pragma unroll
+  for (int n = 0; n < Core::NP; ++n) Core::store(o + core.col(n), decode_piece(core, n), inv, core.col(n), D);
+}
+
 // A workgroup per unit, its waves deal out the blocks.
 template <class Core, DecodeKeys KEYS, int NW>
 __device__ __forceinline__ void decode_unit(const DecodeArgs& a) {
@@ -795,6 +865,11 @@ template <class Core, class Kernels>
 inline hipError_t launch_decode_core(DecodeArgs& a, hipStream_t stream) {
   constexpr bool F32 = Core::BK == 16;
   const int64_t units = (int64_t)a.B * a.Hkv * a.rbs, rows = (int64_t)a.B * a.Hkv * a.R;
+  if constexpr (Kernels::kWave)
+    if (decode_by_wave<Core>(a)) {
+      hipLaunchKernelGGL((Kernels::template wave<Core>()), dim3((unsigned)((units + 3) / 4)), dim3(kThreads), 0, stream, a);
+      return hipGetLastError();
+    }
   const int blocks = (int)(((int64_t)a.Sk + Core::BK - 1) / Core::BK);   // the most of a unit
   // One launch where no unit can be large: it is then over before a second launch would be.  Up to 256 KB of K and V, what one compute unit
   // reads in the time of that launch, 512 KB where there are 128 units, 64 blocks where there are units for the whole chip.  us, runs and
@@ -858,16 +933,21 @@ inline DecodeArgs decode_args(const DecodeLaunch& p) {
 }
 
 // The kernels of a call's type and head dimension.
+template <class C>
+struct DecodeCoreIs {
+  typedef C Core;
+};
+template <typename F>
+inline hipError_t decode_with_core(const DecodeLaunch& p, F f) {   // the core for its type and columns
+  if (!p.is_f32) return p.D == 64 ? f(DecodeCoreIs<DecodeBf16<64>>()) : f(DecodeCoreIs<DecodeBf16<128>>());
+  if (p.D == 64) return f(DecodeCoreIs<DecodeF32<1, true>>());
+  if (p.D == 128) return f(DecodeCoreIs<DecodeF32<2, true>>());
+  if (p.D == 256) return f(DecodeCoreIs<DecodeF32<4, true>>());
+  return p.D < 64 ? f(DecodeCoreIs<DecodeF32<1, false>>()) : p.D < 128 ? f(DecodeCoreIs<DecodeF32<2, false>>()) : f(DecodeCoreIs<DecodeF32<4, false>>());
+}
 template <class Kernels>
 inline hipError_t launch_decode_as(const DecodeLaunch& p, DecodeArgs& a, hipStream_t stream) {
-  if (!p.is_f32)
-    return p.D == 64 ? launch_decode_core<DecodeBf16<64>, Kernels>(a, stream) : launch_decode_core<DecodeBf16<128>, Kernels>(a, stream);
-  if (p.D == 64) return launch_decode_core<DecodeF32<1, true>, Kernels>(a, stream);
-  if (p.D == 128) return launch_decode_core<DecodeF32<2, true>, Kernels>(a, stream);
-  if (p.D < 64) return launch_decode_core<DecodeF32<1, false>, Kernels>(a, stream);
-  if (p.D < 128) return launch_decode_core<DecodeF32<2, false>, Kernels>(a, stream);
-  if (p.D == 256) return launch_decode_core<DecodeF32<4, true>, Kernels>(a, stream);
-  return launch_decode_core<DecodeF32<4, false>, Kernels>(a, stream);
+  return decode_with_core(p, [&](auto c) { return launch_decode_core<typename decltype(c)::Core, Kernels>(a, stream); });
 }
 
 }  // namespace ac

@@ -848,6 +848,10 @@ __global__ __launch_bounds__(NW == 1 ? kThreads : NW * kWave) void shared_join_k
   }
 }
 
+// ---- nothing shared, little of it
+template <class Core>
+__global__ __launch_bounds__(kThreads, Core::OCC) void shared_wave_kernel(const DecodeArgs a) { decode_wave<Core, kPages>(a); }
+
 // ---- launches
 static size_t shared_ints(int64_t B, int64_t G) {   // sums, first, leader, count, start, start1, items; in whole pieces of 16 bytes
   return (size_t)((4 + (G + 1) + G + G + (G + B) + G + 3) / 4 * 4 + (G + B) * (int64_t)(sizeof(SharedItem) / 4));
@@ -910,7 +914,15 @@ constexpr int64_t kSharedWorth = 64LL << 20;
 constexpr int kSharedTokens = 128;
 
 hipError_t launch_shared(const SharedLaunch& p, hipStream_t stream) {
-  if (p.G == 0 || p.d.Sk <= kSharedTokens || (double)p.d.B * p.d.Hkv * p.d.Sk * p.d.D * (p.d.is_f32 ? 8 : 4) <= (double)kSharedWorth) return launch_decode(p.d, stream);
+  if (p.G == 0 || p.d.Sk <= kSharedTokens || (double)p.d.B * p.d.Hkv * p.d.Sk * p.d.D * (p.d.is_f32 ? 8 : 4) <= (double)kSharedWorth) {
+    const DecodeArgs d = decode_args(p.d);
+    return decode_with_core(p.d, [&](auto c) {
+      typedef typename decltype(c)::Core Core;
+      if (!decode_by_wave<Core>(d)) return launch_decode(p.d, stream);
+      hipLaunchKernelGGL((shared_wave_kernel<Core>), dim3((unsigned)(((int64_t)d.B * d.Hkv * d.rbs + 3) / 4)), dim3(kThreads), 0, stream, d);
+      return hipGetLastError();
+    });
+  }
   SharedArgs a;
   a.d = decode_args(p.d);
   a.g = p.d.R; a.G = p.G;

@@ -9,12 +9,16 @@ template <class Core>
 __global__ __launch_bounds__(kThreads, Core::WGS) void window_step_run_kernel(const DecodeArgs a) { decode_run<Core, kWindow>(a); }
 template <class Core, int NW>
 __global__ __launch_bounds__(NW* kWave, Core::OCC) void window_step_unit_kernel(const DecodeArgs a) { decode_unit<Core, kWindow, NW>(a); }
+template <class Core>
+__global__ __launch_bounds__(kThreads, Core::OCC) void window_step_wave_kernel(const DecodeArgs a) { decode_wave<Core, kWindow>(a); }
 template <bool F32, int G, int NW>
 __global__ __launch_bounds__(NW == 1 ? kThreads : NW * kWave) void window_step_join_kernel(const DecodeArgs a) { decode_join<F32, kWindow, G, NW>(a); }
 
 struct WindowStepKernels {
+  static constexpr bool kWave = true;
   template <class Core> static constexpr auto run() { return &window_step_run_kernel<Core>; }
   template <class Core, int NW> static constexpr auto unit() { return &window_step_unit_kernel<Core, NW>; }
+  template <class Core> static constexpr auto wave() { return &window_step_wave_kernel<Core>; }
   template <bool F32, int G, int NW> static constexpr auto join() { return &window_step_join_kernel<F32, G, NW>; }
 };
 

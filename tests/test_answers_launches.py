@@ -35,6 +35,9 @@ def test_every_kernel_is_reached(tmp_path):
     calls += [("window_step", len(step.EDGES), 6, 2, D, 100, 16, _pages(step.EDGES, 16), 50, 9, dt) for D, dt in step.TYPES]
     calls += [("window_step", 5, 6, 2, D, 400, 16, _pages([2500], 16), 1000, 9, dt) for D, dt in step.TYPES]
     calls += [("window_step", len(c[0]), c[1], c[2], c[3], 100, c[5], _pages(c[0], c[5]), c[6], c[7], c[4]) for c in step.RUNS]
+    calls += [("window_step", len(step.LENS), 32, 16, D, 100, 16, _pages(step.LENS, 16), 20, 5, dt) for D, dt in step.TYPES]
+    calls += [("window_step", len(step.LENS), 8, 4, D, 100, 16, _pages(step.LENS, 16), 200, 5, dt) for D, dt in step.TYPES]
+    calls += [("shared", 1203, 4, 1, D, 100, 100, 16, 2, None, dt) for D, dt in shared.TYPES]
     seen = set()
     for call, (status, ls) in zip(calls, al.record(calls, tmp_path)):
         assert status == 0, call
@@ -54,7 +57,9 @@ def test_every_kernel_is_reached(tmp_path):
     (("shared", 64, 32, 8, 64, 1, 1100, 16, 1100, 1 << 22, "bf16"), ["shared_both_kernel<64, true, true>", "shared_join_kernel<false, 16, 1>"]),
     (("shared", 17, 24, 8, 128, 4, 1100, 10, 200, None, "f32"), ["shared_run_kernel<SharedF32<2, true>, true>", "shared_join_kernel<true, 32, 4>"]),
     (("shared", 61, 8, 8, 128, 1, 1100, 16, 16, None, "bf16"), ["decode_unit_kernel"]),
-    (("shared", 10000, 8, 8, 128, 1, 1100, 16, 8, None, "bf16"), ["decode_unit_kernel"]),
+    (("shared", 10000, 8, 8, 128, 1, 1100, 16, 8, None, "bf16"), ["shared_wave_kernel"]),
+    (("shared", 100, 8, 8, 128, 1, 1100, 16, 8, None, "bf16"), ["decode_unit_kernel"]),
+    (("window_step", 256, 32, 8, 64, 300, 16, 600, 100, 16, "bf16"), ["window_step_wave_kernel"]),
     (("shared", 8, 8, 1, 128, 1, 1100, 16, 900, None, "bf16"), ["decode_run_kernel", "decode_join_kernel"]),
     (("shared", 64, 32, 8, 128, 0, 1100, 16, 1100, None, "bf16"), ["decode_run_kernel", "decode_join_kernel"]),
     (("window", 4, 32, 8, 4096, 128, 1024, 4, "bf16"), ["window_bf16_kernel<128>"]),

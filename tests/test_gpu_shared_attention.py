@@ -244,6 +244,15 @@ def test_little_to_read(ac, c):  # noqa: F811
     assert torch.equal(O, c.call(ac, Q)) and torch.equal(O, call(ac, c, Q, first[:1], share[:0]))
 
 
+SHORT = ([(20, [3, 0, 7] * 4)] * 100, [1, 0, 30], 4, 1)
+
+
+@pytest.mark.parametrize("D,dt", TYPES)
+def test_many_requests_with_little_to_read(ac, D, dt):  # noqa: F811
+    case(ac, *SHORT, D, dt, 16, wide=False, blank=False)
+    case(ac, [(50, [0, 2] * 4)], [9] * 22, 48, 48, D, dt, 10, [0, 3, 7, 8, 29], wide=False, blank=False)
+
+
 def test_an_empty_batch(ac):  # noqa: F811
     c, first, share = build([(20, [1, 2])], [], 2, 64, "bf16", 16)
     none = torch.empty(0, 4, 64, dtype=torch.bfloat16, device="cuda")

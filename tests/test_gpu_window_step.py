@@ -127,6 +127,17 @@ def test_a_captured_step_goes_on_by_itself(ac):  # noqa: F811
         assert n - state[1].item() == held
 
 
+LENS, SOME = [300, 0, 1, 19, 20, 21, 24, 25, 26, 33] * 7, [0, 1, 2, 3, 5, 7, 11, 36, 60, 69]      # (of 70: more than 1,024 units of 16 heads)
+
+
+@pytest.mark.parametrize("D,dt", TYPES)
+def test_many_requests_with_short_windows(ac, D, dt):  # noqa: F811
+    case(ac, LENS, 32, 16, D, dt, 16, 20, 5, SOME)
+    case(ac, LENS, 20, 1, D, dt, 7, 30, 0, SOME)
+    case(ac, LENS[:35] * 16, 4, 2, D, dt, 16, 1, 1, SOME)
+    case(ac, LENS, 8, 4, D, dt, 16, 200, 5, SOME)      # (fewer and larger units)
+
+
 @pytest.mark.parametrize("D", [1, 2, 3, 4, 5, 15, 17, 33, 36, 65, 100, 101, 127, 129, 199, 200, 255])
 def test_infinities_in_single_columns(ac, D):  # noqa: F811
     """Binary32 rows of any length: a key of which one column is -inf weighs nothing, a value of which one is infinite fills that column and no other."""
