@@ -718,6 +718,7 @@ __global__ __launch_bounds__(kThreads, 2) void shared_both_kernel(const SharedAr
 }
 
 // ---- parts of an output row
+constexpr int kSharedManyRows = 6144;   // from here on shared_rows_kernel
 // NW waves add up one row (or, NW 1, a wave each): a lane holds four columns, G lanes a partial result; a wave knows the weights of 64 at once.
 template <bool F32, int G, int NW>
 __global__ __launch_bounds__(NW == 1 ? kThreads : NW * kWave) void shared_join_kernel(const SharedArgs a) {
@@ -848,6 +849,75 @@ __global__ __launch_bounds__(NW == 1 ? kThreads : NW * kWave) void shared_join_k
   }
 }
 
+// Many rows: G lanes have one, and look at its parts one after another.
+template <bool F32, int G>
+__global__ __launch_bounds__(kThreads) void shared_rows_kernel(const SharedArgs a) {
+  typedef typename std::conditional<F32, float, bf16_t>::type Elt;
+  constexpr int BK = F32 ? 16 : 32, UNIT = F32 ? 16 : 32, AT_ONCE = 4;
+  const DecodeArgs& d = a.d;
+  const int col = 4 * (threadIdx.x % G), D = d.D;
+  const size_t rows = shared_rows(a), row = (size_t)blockIdx.x * (kThreads / G) + threadIdx.x / G;
+  if (row >= rows) return;
+  const int per = run_length(a.sums[0], a.sums[3]), per1 = a.sums[2];
+  const Divider by_per((uint32_t)max(per, 1)), by_per1((uint32_t)max(per1, 1)), by_heads((uint32_t)d.Hkv);
+  const int head = a.by_g.div((int)row), x = (int)row - head * a.g, b = by_heads.div(head), hk = head - b * d.Hkv;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  float top = -INFINITY, total = 0.f;
+  auto item = [&](const SharedItem& it, int r, bool big, size_t whole) {
+    const int br = big ? kSharedRows : UNIT, blocks = big ? (it.keys + kSharedChunk - 1) / kSharedChunk : (it.keys + BK - 1) / BK;
+    if (blocks == 0) return;
+    const int p = big ? per1 : per, from = it.start + (hk * it.rbs + r / br) * (blocks + (big ? kSharedUnitCost : kUnitCost));
+    const int w0 = big ? by_per1.div(from) : by_per.div(from), n = (big ? by_per1.div(from + blocks - 1) : by_per.div(from + blocks - 1)) - w0 + 1;
+    const size_t base = 2 * rows + (big ? (size_t)2 * d.waves * UNIT : 0) + r % br;
+    for (int e0 = 0; e0 < n; e0 += AT_ONCE) {
+      f32x4 y[AT_ONCE];
+      float m[AT_ONCE], l[AT_ONCE], t = top;
+#pragma unroll
+      for (int e = 0; e < AT_ONCE; ++e) {
+        m[e] = -INFINITY;
+        l[e] = 0.f;
+        y[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (e0 + e < n) {
+          const size_t rec = n == 1 ? whole : base + (size_t)partial_of(w0 + e0 + e, p, from) * br;
+          const float* src = a.part + rec * D + col;
+          m[e] = a.stat[2 * rec];
+          l[e] = a.stat[2 * rec + 1];
+          if (!F32 || col + 4 <= D) {
+            y[e] = *reinterpret_cast<const f32x4_dw*>(src);
+          } else {
+#pragma unroll
+            for (int c = 0; c < 3; ++c)
+              if (col + c < D) y[e][c] = src[c];
+          }
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < AT_ONCE; ++e) t = fmaxf(t, m[e]);
+      const float old = top < t ? __builtin_amdgcn_exp2f(top - t) : 1.f;
+      top = t;
+      total *= old;
+      o *= old;
+#pragma unroll
+      for (int e = 0; e < AT_ONCE; ++e) {
+        const float f = m[e] < t ? __builtin_amdgcn_exp2f(m[e] - t) : 1.f;
+        total = fmaf(l[e], f, total);
+        o += y[e] * f;
+      }
+    }
+  };
+  const SharedItem own = a.item[a.G + b];
+  item(own, x, false, row);
+  if (own.key0 > 0) {
+    const SharedItem pre = a.item[own.group];
+    item(pre, (b - pre.b0) * a.g + x, pre.group != 0, rows + row);
+  }
+  if (col >= D) return;
+  const float inv = total == 0.f ? 0.f : 1.f / total;   // no key at all: zeros
+  Elt* to = static_cast<Elt*>(d.O) + row * D + col;
+  if constexpr (F32) store_partial(to, o * inv, col, D);
+  else DecodeBf16<64>::store(to, o, inv, col, D);
+}
+
 // ---- nothing shared, little of it
 template <class Core>
 __global__ __launch_bounds__(kThreads, Core::OCC) void shared_wave_kernel(const DecodeArgs a) { decode_wave<Core, kPages>(a); }
@@ -898,9 +968,11 @@ static hipError_t launch_shared_as(SharedArgs& a, bool big, hipStream_t stream) 
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int64_t rows = (int64_t)a.d.B * a.d.Hkv * a.g;
-  // us, four waves a row / one: 408 rows of 30 parts 24.7 / 24.9, 2,048 of 17 52.5 / 50.8 (the chip starts some 420 workgroups a us), 4,288 of few 63.8 / 55.1
+  // us, four waves a row / one: 408 rows of 30 parts 24.7 / 24.9, 2,048 of 17 52.5 / 50.8 (the chip starts some 420 workgroups a us), 4,288 of few 63.8 / 55.1;
+  // one / G lanes: 2,048 49.6 / 52.3, 4,288 51.0 / 54.0, 4,816 51.4 / 51.8, 7,056 32.6 / 29.9, 8,736 36.1 / 34.0, 16,384 65.0 / 58.2, 41,280 71.4 / 52.4
   if (rows <= 1024) hipLaunchKernelGGL((shared_join_kernel<F32, G, 4>), dim3((unsigned)rows), dim3(4 * kWave), 0, stream, a);
-  else hipLaunchKernelGGL((shared_join_kernel<F32, G, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(kThreads), 0, stream, a);
+  else if (rows < kSharedManyRows) hipLaunchKernelGGL((shared_join_kernel<F32, G, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(kThreads), 0, stream, a);
+  else hipLaunchKernelGGL((shared_rows_kernel<F32, G>), dim3((unsigned)((rows * G + kThreads - 1) / kThreads)), dim3(kThreads), 0, stream, a);
   return hipGetLastError();
 }
 

@@ -53,7 +53,7 @@ def test_every_kernel_is_reached(tmp_path):
     (("fork", 16, 8, 128, 10, 16, 65537, False, "bf16"), ["fork_rows_kernel", "fork_tables_kernel", "fork_ring_kernel"]),
     (("shared", 64, 32, 8, 128, 1, 1100, 16, 1100, None, "bf16"), ["shared_both_kernel<128, false, true>", "shared_join_kernel<false, 32, 1>"]),
     (("shared", 4, 32, 8, 128, 1, 1100, 16, 1100, None, "bf16"), ["shared_run_kernel<SharedBf16<128>, true>", "shared_join_kernel<false, 32, 4>"]),
-    (("shared", 300, 32, 8, 128, 1, 1100, 16, 1100, None, "bf16"), ["shared_plan_kernel<32, 32, 1024, true>", "shared_both_kernel<128, false, false>", "shared_join_kernel<false, 32, 1>"]),
+    (("shared", 300, 32, 8, 128, 1, 1100, 16, 1100, None, "bf16"), ["shared_plan_kernel<32, 32, 1024, true>", "shared_both_kernel<128, false, false>", "shared_rows_kernel<false, 32>"]),
     (("shared", 64, 32, 8, 64, 1, 1100, 16, 1100, 1 << 22, "bf16"), ["shared_both_kernel<64, true, true>", "shared_join_kernel<false, 16, 1>"]),
     (("shared", 17, 24, 8, 128, 4, 1100, 10, 200, None, "f32"), ["shared_run_kernel<SharedF32<2, true>, true>", "shared_join_kernel<true, 32, 4>"]),
     (("shared", 61, 8, 8, 128, 1, 1100, 16, 16, None, "bf16"), ["decode_unit_kernel"]),

@@ -86,6 +86,8 @@ MANY = [([(50, [3] * 8)] * 40, [9] * 20, Hq, 1, D, dt, 16) for D, dt in TYPES fo
 MANY += [([(300, [5] * 20)] * 15, [700], 4, 2, D, "bf16", 16) for D in (64, 128)] + [([(40, [1])] * 300 + [(90, [2, 3] * 20)], [], 1, 1, 64, "bf16", 16)]
 MANY += [([(40, [1])] * 1100, [], 1, 1, D, dt, 16) for D, dt in ((64, "bf16"), (64, "f32"))]
 MANY += [([(40, [1, 2])] * 150, [], 1, 1, 64, "bf16", 16), ([(3000, [2] * 3)] * 3, [5], 32, 1, 128, "bf16", 16)]
+# more than 6,144 rows, of few parts and of many
+MANY += [([(50, [3] * 8)] * 40, [9, 0] * 10, 20, 1, D, dt, 16) for D, dt in TYPES] + [([(3000, [2] * 199 + [0])], [0, 5], 32, 1, D, dt, 16) for D, dt in TYPES[:3]]
 # caches of more than 4 GiB
 FAR, FAR_MANY, FAR_HEADS = [(400, [20] * 9), (90, [1, 2])], [(400, [20] * 130), (90, [1, 2] * 70)], [(4, 1, 64), (8, 2, 128)]
 
