@@ -182,6 +182,8 @@ __device__ __forceinline__ void f32_store_row(float* __restrict__ o, const f32x4
         for (int t = 0; t < 4; ++t) w[t] = f32_divide(w[t], by, inv);
       if constexpr (COLS == kVecCols || COLS == kAllCols) {
         if (COLS == kAllCols || d < D) *reinterpret_cast<f32x4*>(o + d) = w;
+      } else if (COLS == kAnyCols && d + 4 <= D) {
+        *reinterpret_cast<f32x4_dw*>(o + d) = w;
       } else {
 #pragma unroll
         for (int t = 0; t < 4; ++t)
