@@ -29,7 +29,7 @@ struct RotateArgs {
   int32_t interleaved;
 };
 
-// VEC columns of a row as they lie in memory: 16 bytes, or 1 column where a row or a pair's other half is no whole number of those.
+// VEC columns of a row as they lie in memory: 16 bytes, or 1 column where a row is no whole number of those.
 template <typename T, int VEC>
 struct RotatePiece {
   T v[VEC];
@@ -50,7 +50,9 @@ struct RotatePiece {
 // G lanes a row, NP pieces a lane: a wave has 64 / G tokens, and a lane keeps its token and its columns, so that addresses, sines, cosines and weights are the
 // lane's for all heads, of which the wave takes every fourth, U at a time.  (With heads dealt to threads and tables of tokens in LDS the vector work of
 // addresses took longer than the memory: 59 us and 87 where it is 50 and 25 now.)
-template <typename T, int VEC, int G, int NP, int U, bool NORM>
+// ODD: pairs lie apart and no whole pieces, so that their other halves are loaded one by one (of few columns, in most such models: 40 heads of 128 of which
+// 20 columns turn, 2,400 tokens, 25 us; 38 with all columns one by one, 16 where pieces are whole).
+template <typename T, int VEC, int G, int NP, int U, bool NORM, bool ODD>
 __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a) {
   typedef RotatePiece<T, VEC> Piece;
   constexpr int TOKENS = kWave / G, CS = VEC > 1 ? VEC : 1;
@@ -71,7 +73,12 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a) {
       const int c = VEC * (lane + G * i);
       if (c < D) {
         y[u][i].load(x + (int64_t)h * D + c);
-        if (apart && h < rotated && c < 2 * half) z[u][i].load(x + (int64_t)h * D + other(c));
+        if (ODD) {
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) z[u][i].v[e] = h < rotated && c + e < 2 * half ? x[(int64_t)h * D + other(c + e)] : (T)0.f;
+        } else if (apart && h < rotated && c < 2 * half) {
+          z[u][i].load(x + (int64_t)h * D + other(c));
+        }
       }
     }
   };
@@ -93,7 +100,12 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a) {
       const int c = VEC * (lane + G * i);
       if (c < D) {
         wy[i].load(w + c);
-        if (apart && c < 2 * half) wz[i].load(w + other(c));
+        if (ODD) {
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) wz[i].v[e] = c + e < 2 * half ? w[other(c + e)] : 0.f;
+        } else if (apart && c < 2 * half) {
+          wz[i].load(w + other(c));
+        }
       }
     }
   };
@@ -121,7 +133,15 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a) {
   for (int i = 0; i < NP; ++i) {
     const int c = VEC * (lane + G * i);
     if (c < 2 * half) {
-      if (apart) {
+      if (ODD) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          const int o = other(c + e);
+          cs[i][e] = make_float2(1.f, 0.f);   // (a column that does not turn)
+          if (c + e < 2 * half) cs[i][e] = turn[sub * half + min(c + e, o)];
+          if (c + e < o) cs[i][e].y = -cs[i][e].y;
+        }
+      } else if (apart) {
         const int o = other(c), pair = a.interleaved ? c >> 1 : min(c, o);
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
@@ -230,8 +250,12 @@ static hipError_t launch_rotate_as(RotateArgs a, hipStream_t stream) {
   for (int64_t begin = 0; begin < blocks; begin += most) {
     a.begin = (int)begin;
     const int64_t wgs = blocks - begin < most ? blocks - begin : most;
-    if (a.qw || a.kw) hipLaunchKernelGGL((rotate_kernel<T, VEC, G, NP, U, true>), dim3((unsigned)wgs, gy), dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL((rotate_kernel<T, VEC, G, NP, UN, false>), dim3((unsigned)wgs, gy), dim3(kThreads), 0, stream, a);
+    const bool norm = a.qw || a.kw, odd = !a.interleaved && a.half % VEC != 0;   // (VEC 1: never)
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)wgs, gy), dim3(kThreads), 0, stream, a); };
+    if constexpr (VEC > 1) {
+      if (odd) norm ? go(&rotate_kernel<T, VEC, G, NP, U, true, true>) : go(&rotate_kernel<T, VEC, G, NP, UN, false, true>);
+    }
+    if (!odd) norm ? go(&rotate_kernel<T, VEC, G, NP, U, true, false>) : go(&rotate_kernel<T, VEC, G, NP, UN, false, false>);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -252,14 +276,8 @@ hipError_t launch_rotate(const RotateLaunch& p, hipStream_t stream) {
   a.by_ps = Divider((uint32_t)a.ps);
   a.by_half = Divider((uint32_t)(a.half ? a.half : 1));
   a.eps = p.eps; a.amp = p.amplitude; a.interleaved = p.interleaved;
-  const int vec = p.is_f32 ? 4 : 8;
-  const bool whole = p.D % vec == 0 && p.row_stride % vec == 0 && p.batch_stride % vec == 0 &&
-                     (p.interleaved || a.half % vec == 0);
-  if (!p.is_f32) {
-    if (whole) return p.D == 64 ? launch_rotate_as<bf16_t, 8, 8, 1, 2, 3>(a, stream) : launch_rotate_as<bf16_t, 8, 16, 1, 3>(a, stream);
-    return p.D == 64 ? launch_rotate_as<bf16_t, 1, 64, 1, 4>(a, stream) : launch_rotate_as<bf16_t, 1, 64, 2, 4>(a, stream);
-  }
-  if (whole) {
+  if (!p.is_f32) return p.D == 64 ? launch_rotate_as<bf16_t, 8, 8, 1, 2, 3>(a, stream) : launch_rotate_as<bf16_t, 8, 16, 1, 3>(a, stream);
+  if (p.D % 4 == 0) {   // (the strides are whole pieces, too)
     if (p.D <= 64) return launch_rotate_as<float, 4, 16, 1, 3>(a, stream);
     if (p.D <= 128) return launch_rotate_as<float, 4, 32, 1, 3>(a, stream);
     return launch_rotate_as<float, 4, 64, 1, 3>(a, stream);

@@ -89,7 +89,8 @@ SIZES = [(1, 1, 1, 1, 64, "bf16", 64), (128, 1, 32, 8, 128, "bf16", 128), (3, 7,
          (2, 300, 8, 2, 128, "bf16", 128), (5, 9, 3, 3, 64, "bf16", 20), (5, 9, 3, 3, 128, "bf16", 2), (2, 5, 4, 2, 64, "bf16", 0),
          (3, 7, 5, 1, 80, "f32", 40), (2, 94, 24, 8, 128, "f32", 128), (2, 5, 2, 2, 33, "f32", 32), (2, 5, 2, 1, 199, "f32", 198),
          (2, 5, 2, 1, 256, "f32", 256), (1, 3, 1, 1, 1, "f32", 0), (4, 3, 2, 1, 2, "f32", 2), (2, 6, 3, 1, 100, "f32", 50), (2, 6, 3, 1, 64, "f32", 8),
-         (2, 6, 3, 1, 200, "f32", 64), (1, 2, 40, 1, 64, "bf16", 64), (3, 2, 1, 1, 128, "f32", 6)]
+         (2, 6, 3, 1, 200, "f32", 64), (1, 2, 40, 1, 64, "bf16", 64), (3, 2, 1, 1, 128, "f32", 6),
+         (2, 6, 3, 1, 36, "f32", 10), (2, 6, 3, 1, 200, "f32", 30), (2, 40, 6, 2, 128, "bf16", 94), (2, 40, 6, 2, 64, "bf16", 62), (2, 9, 3, 1, 64, "f32", 62), (2, 6, 3, 1, 101, "f32", 100)]
 
 
 @pytest.mark.parametrize("interleaved", [False, True])
