@@ -122,8 +122,12 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a) {
     f -= floor(f);
     const uint64_t step = (uint64_t)(f * 18446744073709551616.0);
     const int32_t frac = (int32_t)((step * (uint64_t)(uint32_t)max(a.pos[min(first + t, a.n_tokens - 1)], 0)) >> 32);   // of a turn, from -1/2 on
-    float sn, cn;
-    sincospif((float)frac * 4.656612873077392578125e-10f, &sn, &cn);   // 2^-31: half turns
+    // the nearest quarter turn is taken off while the fraction is a whole number: an eighth of a turn at most is then rounded to binary32
+    const uint32_t quarter = ((uint32_t)frac + 0x20000000u) >> 30;
+    float s0, c0;
+    sincospif((float)(int32_t)((uint32_t)frac - (quarter << 30)) * 4.656612873077392578125e-10f, &s0, &c0);   // 2^-31: half turns
+    const float sn = quarter == 0 ? s0 : quarter == 1 ? c0 : quarter == 2 ? -s0 : -c0;
+    const float cn = quarter == 0 ? c0 : quarter == 1 ? -s0 : quarter == 2 ? -c0 : s0;
     turn[tid] = make_float2(cn * a.amp, sn * a.amp);
   }
   __syncthreads();
