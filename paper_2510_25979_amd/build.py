@@ -9,7 +9,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libattncache.so")
 SOURCES = ["api.hip", "apply.hip", "cross.hip", "decode.hip", "exact.hip", "fork.hip", "insert.hip", "page.hip", "project.hip", "rotate.hip",
            "search.hip", "shared.hip", "window.hip", "window_step.hip"]
-HEADERS = ["common.hpp", "decode_tile.hpp", "f32_tile.hpp", "launch.hpp", "row_stream.hpp", "serve.h", "serve_index.h", "short_tile.hpp", "split_tile.hpp", "stream_tile.hpp", os.path.join("..", "..", "include", "attncache.h")]
+HEADERS = ["common.hpp", "decode_tile.h", "f32_tile.hpp", "launch.hpp", "row_stream.hpp", "serve.h", "serve_index.h", "short_tile.hpp", "split_tile.hpp", "stream_tile.h", os.path.join("..", "..", "include", "attncache.h")]
 ARG = os.path.join(HERE, "_tensor_arg.so")
 ARG_SOURCE = "tensor_arg.cpp"
 

@@ -20,7 +20,7 @@
 // through a wave-private LDS tile where the transposing read wants them (O^T = V^T P^T; binary32: straight from memory).  A lane
 // deals with one row of Q, so maximum and sum are in-lane but for the four lanes that share it, and the weights are where the
 // second product takes them.  Pages may end anywhere inside a block: each lane follows its own keys' pages.
-#include "decode_tile.hpp"
+#include "decode_tile.h"
 
 namespace ac {
 

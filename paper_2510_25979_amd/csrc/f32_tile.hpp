@@ -107,9 +107,10 @@ struct F32Stage {
 
 // acc += W V for one 16-key block: `v` is the block's first row in LDS, w[x] the lane's weight of
 // key 4 kq + x (zero where the key is hidden from its row).
-template <int DB, int LD = F32Stage<DB, 64, kAllCols>::LD>
+template <int DB>
 __device__ __forceinline__ void f32_weights_v(f32x4 (&acc)[4 * DB], const float* __restrict__ v,
                                               const f32x4 w, int i, int kq) {
+  constexpr int LD = F32Stage<DB, 64, kAllCols>::LD;
   struct Rows { f32x4 b[DB]; };   // this lane's part of key 4 kq + x
   auto read = [&](int x) {
     Rows r;
@@ -182,8 +183,6 @@ __device__ __forceinline__ void f32_store_row(float* __restrict__ o, const f32x4
         for (int t = 0; t < 4; ++t) w[t] = f32_divide(w[t], by, inv);
       if constexpr (COLS == kVecCols || COLS == kAllCols) {
         if (COLS == kAllCols || d < D) *reinterpret_cast<f32x4*>(o + d) = w;
-      } else if (COLS == kAnyCols && d + 4 <= D) {
-        *reinterpret_cast<f32x4_dw*>(o + d) = w;
       } else {
 #pragma unroll
         for (int t = 0; t < 4; ++t)

@@ -7,7 +7,7 @@
 //
 // The list says who is in which group, what each item has and where its blocks are numbered.  Up to 256 requests and 255 groups each workgroup makes it
 // for itself, in LDS; otherwise shared_plan_kernel writes it before.
-// shared_prefix (bf16) forms prefixes of many rows: workgroups of 128 rows that share chunks of 64 keys in LDS (stream_tile.hpp), each an equal
+// shared_prefix (bf16) forms prefixes of many rows: workgroups of 128 rows that share chunks of 64 keys in LDS (stream_tile.h), each an equal
 //   run of all such chunks, so that few groups fill the chip and many short ones do, too.
 // shared_run forms everything else in units of 32 rows (binary32 16) of one (item, K/V head), cut into equal runs of blocks by wave, as decode.hip.
 // shared_join_kernel adds up an output row's parts.
@@ -17,8 +17,8 @@
 // the products) --, the join 7.  134 requests that share little: bound by memory, 44 of 50 us in the runs.
 #include <type_traits>
 
-#include "decode_tile.hpp"
-#include "stream_tile.hpp"
+#include "decode_tile.h"
+#include "stream_tile.h"
 
 namespace ac {
 

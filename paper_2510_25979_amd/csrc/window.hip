@@ -5,7 +5,7 @@
 // workgroup reads no key that only some of its waves need.  It walks the blocks of 32 keys (16) that hold a first token or lie in the window of one
 // of its rows, and compares keys with rows only where some see them and some do not.
 //
-// bf16: two blocks at a time straight into one of two LDS stages, by buffer loads whose bounds are the item's last key; both products of stream_tile.hpp.
+// bf16: two blocks at a time straight into one of two LDS stages, by buffer loads whose bounds are the item's last key; both products of stream_tile.h.
 // Bound by the softmax's vector work and the matrix pipe at the clock that the chip grants them: 128 heads of 128, 4,096 tokens, window 1,024, 276 us (0.88
 // PFLOP/s; 309 to 370 where nothing else runs between), the pipe busy in 48 % of the cycles.  Blocks of 32 keys and not chunks of 64 spare 5 % at a window's two
 // edges.  Passing over pairs that a wave does not see takes 6 % off rows of one head a workgroup and a window of 64 (66 / 62), and adds 1 to 2 %
@@ -16,7 +16,7 @@
 #include "common.hpp"
 #include "f32_tile.hpp"
 #include "serve.h"
-#include "stream_tile.hpp"
+#include "stream_tile.h"
 
 namespace ac {
 
@@ -218,6 +218,30 @@ __global__ __launch_bounds__(kThreads, 2) void window_bf16_kernel(const WindowAr
   }
 }
 
+// acc += W V for a block of 16 keys whose rows lie LD floats apart, as f32_weights_v.
+template <int DB, int LD>
+__device__ __forceinline__ void window_weights_v(f32x4 (&acc)[4 * DB], const float* __restrict__ v, const f32x4 w, int i, int kq) {
+  struct Rows { f32x4 b[DB]; };   // this lane's part of key 4 kq + x
+  auto read = [&](int x) {
+    Rows r;
+#pragma unroll
+    for (int b = 0; b < DB; ++b) r.b[b] = *reinterpret_cast<const f32x4*>(v + (4 * kq + x) * LD + 64 * b + 4 * i);
+    return r;
+  };
+  Rows now = read(0);
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    Rows next = now;
+    if (x < 3) next = read(x + 1);
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) acc[4 * b + t] = mfma_f32(now.b[b][t], w[x], acc[4 * b + t]);
+    now = next;
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
 // Binary32 (the layout of f32_tile.hpp): four waves share stages of 16 keys for each wave of a row.  Heads of 64 and 128 columns go straight from memory
 // into two stages in turn (K's pieces swizzled, V's not: both are then read without bank conflicts); others through registers, in which the next stage is while
 // this one is multiplied.  The vector units form these products themselves, so that what the softmax takes comes on top of them, and its reference
@@ -308,7 +332,7 @@ __global__ __launch_bounds__(kThreads, DB == 4 && COLS == kAllCols && SPLIT == 2
       p[x] = __builtin_amdgcn_exp2f(fmaf(s[x], a.scale_log2e, -ref));
       l += p[x];
     }
-    f32_weights_v<DB, LD>(acc, vl + key0 * LD, p, i, kq);
+    window_weights_v<DB, LD>(acc, vl + key0 * LD, p, i, kq);
   };
   if constexpr (DIRECT) {
     __shared__ __attribute__((aligned(16))) float kl1[KC * LD];
@@ -398,7 +422,27 @@ __global__ __launch_bounds__(kThreads, DB == 4 && COLS == kAllCols && SPLIT == 2
     window_rows_again<float, DB>(a, Q, K, V, O, t0, rows, keys, lane);
     return;
   }
-  if (i < rows) f32_store_row<DB, COLS, true>(O + (size_t)(t0 + i) * D, acc, sum == 0.f ? 1.f : sum, kq, D);
+  if (i >= rows) return;
+  float* o = O + (size_t)(t0 + i) * D;
+  if constexpr (COLS == kAnyCols) {   // (in pieces, at any address: of 199 columns 57 us where single floats took 98)
+    const float by = sum == 0.f ? 1.f : sum, inv = 1.f / by;
+#pragma unroll
+    for (int n = 0; n < 4 * DB; ++n) {
+      const int b = n >> 2, x = n & 3, d = 64 * b + 16 * kq + 4 * x;
+      f32x4 w = {acc[4 * b][x], acc[4 * b + 1][x], acc[4 * b + 2][x], acc[4 * b + 3][x]};
+#pragma unroll
+      for (int t = 0; t < 4; ++t) w[t] = f32_divide(w[t], by, inv);
+      if (d + 4 <= D) {
+        *reinterpret_cast<f32x4_dw*>(o + d) = w;
+      } else {
+#pragma unroll
+        for (int t = 0; t < 3; ++t)
+          if (d + t < D) o[d + t] = w[t];
+      }
+    }
+  } else {
+    f32_store_row<DB, COLS, true>(o, acc, sum == 0.f ? 1.f : sum, kq, D);
+  }
 }
 
 // All tiles, in launches of at most 2^23 workgroups (a multiple of eight tiles each).

@@ -1,7 +1,7 @@
 // Attention of one new token of each request within a window, with a few first tokens that stay visible: of n tokens, j < sinks and
 // j >= n - window are seen.  They are numbered one after the other, and the rest is attention over pages (decode.hip): the same units, runs and
 // partial results over at most window + sinks keys, whatever the lengths.  Pages in the gap are not looked at, nor their entries.
-#include "decode_tile.hpp"
+#include "decode_tile.h"
 
 namespace ac {
 
