@@ -13,8 +13,8 @@ HEADERS = ["common.hpp", "decode_tile.h", "f32_tile.hpp", "launch.hpp", "row_str
 ARG = os.path.join(HERE, "_tensor_arg.so")
 ARG_SOURCE = "tensor_arg.cpp"
 
-# -packed-fp32-ops is switched off: the compiler must not form packed fp32 instructions
-FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-fno-gpu-rdc",
+# -packed-fp32-ops is switched off: the compiler must not form packed fp32 instructions.  Eight sources at a time: 68 s, 182 one by one.
+FLAGS = ["-parallel-jobs=8", "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-fno-gpu-rdc",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wall",
          "-Wno-unused-command-line-argument", "-Wl,-z,defs"]
 
