@@ -119,8 +119,8 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a) {
   if (blockIdx.y * a.heads < rotated && tid < TOKENS * half) {
     const int t = a.by_half.div(tid);
     double f = a.freq[tid - t * half] * 0.15915494309189533577;
-    f -= floor(f);
-    const uint64_t step = (uint64_t)(f * 18446744073709551616.0);
+    f -= rint(f);   // (nearest: no digit of a small negative frequency is lost to the whole turn beside it)
+    const uint64_t size = (uint64_t)(fabs(f) * 18446744073709551616.0), step = f < 0 ? 0 - size : size;   // (size: up to 2^63)
     const int32_t frac = (int32_t)((step * (uint64_t)(uint32_t)max(a.pos[min(first + t, a.n_tokens - 1)], 0)) >> 32);   // of a turn, from -1/2 on
     // the nearest quarter turn is taken off while the fraction is a whole number: an eighth of a turn at most is then rounded to binary32
     const uint32_t quarter = ((uint32_t)frac + 0x20000000u) >> 30;
