@@ -745,9 +745,10 @@ int32_t attention_paged_shared(const void *Q, const void *k_pages,
  *   scale      0 selects 1/sqrt(D).
  *
  * Arithmetic as in attention_paged.  Keys that are hidden from a row do not
- * touch it, whatever K and V hold there (rows among 32, binary32 16, that meet
- * an infinity or a NaN take a slower way).  Hq / Hkv * S <= 2^24, also with S
- * rounded up to a multiple of 16; B * Hkv <= 2^28, B * Hq below 2^31.
+ * touch it, whatever K and V hold there: workgroups whose blocks of keys hold
+ * an infinity or a NaN of V walk their keys four times, which takes up to ten
+ * times as long; in Q or K they cost nothing.  Hq / Hkv * S <= 2^24, also with
+ * S rounded up to a multiple of 16; B * Hkv <= 2^28, B * Hq below 2^31.
  */
 int32_t attention_window(const void *Q, const void *K, const void *V, void *O,
                          const int32_t *row_sel, const int32_t *key_len,

@@ -20,6 +20,20 @@ struct StreamSource {
   }
 };
 
+enum StreamValues { kFinite, kUp, kDown };   // of chunk_of
+// 2^(score - ref).  A reference point of 2^30 and more may be off by more than 2^6 from the score that it was rounded from: its rows subtract rounded scores.
+__device__ __forceinline__ float stream_weight(float s, float scale_log2e, float ref) {
+#pragma clang fp contract(off)
+  const float scaled = s * scale_log2e;
+  return __builtin_amdgcn_exp2f(fabsf(ref) < 0x1p30f ? fmaf(s, scale_log2e, -ref) : scaled - ref);
+}
+
+// x for kFinite, y for the others, without a branch for each of many values.
+__device__ __forceinline__ float stream_one_of(StreamValues which, float x, float y) {
+  const uint32_t first = which == kFinite ? ~0u : 0u;
+  return __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, x) & first) | (__builtin_bit_cast(uint32_t, y) & ~first));
+}
+
 template <int D>
 struct StreamTile {
   static constexpr int KS = D / 16, DB = D / 32;   // products of a block of 32 keys, first and second (twice DB)
@@ -93,19 +107,22 @@ struct StreamTile {
       m = cand;
     }
   }
-  // A chunk of 64 keys; hide(s0, s1) puts -inf in the places of keys that a row does not see.  The order is given, a product and what stands beside it at a time: LDS reads run four operands ahead of
-  // the products that take them, and the weights of a block are formed between products that do not wait for them.  (In the compiler's own
-  // order a product waited for each pair of reads.)
-  template <typename Hide>
-  __device__ __forceinline__ void chunk(const bf16_t* kb, const bf16_t* vb, Hide hide) {
-    constexpr int AHEAD = 4;
-    // offsets that the compiler does not know to be the same in every chunk: otherwise it keeps an address register for each of them and each stage
+  // Offsets that the compiler does not know to be the same in every chunk: otherwise it keeps an address register for each of them and each stage.
+  __device__ __forceinline__ void new_offsets() {
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(koff[ks]));
 #pragma unroll
     for (int half = 0; half < 2; ++half)
 #pragma unroll
       for (int db = 0; db < DB; ++db) asm volatile("" : "+v"(voff[half][db]));
+  }
+  // A chunk of 64 keys; hide(s0, s1) puts -inf in the places of keys that a row does not see.  The order is given, a product and what stands beside it at a time: LDS reads run four operands ahead of
+  // the products that take them, and the weights of a block are formed between products that do not wait for them.  (In the compiler's own
+  // order a product waited for each pair of reads.)
+  template <typename Hide>
+  __device__ __forceinline__ void chunk(const bf16_t* kb, const bf16_t* vb, Hide hide) {
+    constexpr int AHEAD = 4;
+    new_offsets();
     f32x16 s0 = zeros(), s1 = zeros();
     {
       bf16x8 k[2 * KS];
@@ -153,6 +170,68 @@ struct StreamTile {
     }
   }
   __device__ __forceinline__ float sum() const { return l + __shfl_xor(l, 32); }   // of the lane's row
+
+  // A chunk where V may hold infinities and NaN that some rows see and others do not: a weight of zero does not make them vanish.  kFinite forms the sums without
+  // them, by the same operations in the same order as above; kUp and kDown then count, in a row's columns, the +inf (or NaN) and the -inf (or NaN) of keys that it sees.
+  template <typename Hide>
+  __device__ __forceinline__ void chunk_of(StreamValues which, const bf16_t* kb, const bf16_t* vb, Hide hide) {
+    new_offsets();
+    // bits 15 and 31: which of two values is not finite (an exponent of ones carries)
+    auto odd = [](uint32_t w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; };
+    if (which != kFinite) {   // nothing to count: most chunks
+      uint32_t any = 0;
+#pragma unroll
+      for (int f = 0; f < 4 * DB; ++f) {
+        const u32x4 v = __builtin_bit_cast(u32x4, vop(vb, f / (2 * DB), f / DB % 2, f % DB));
+        any |= odd(v[0]) | odd(v[1]) | odd(v[2]) | odd(v[3]);
+        if (f % 2) __builtin_amdgcn_sched_barrier(0);
+      }
+      if (!__any(any)) return;
+    }
+    constexpr int AHEAD = D == 128 ? 4 : 1;   // reads at once: more would take more registers than the kernels have
+    f32x16 s0 = zeros(), s1 = zeros();
+#pragma unroll
+    for (int f = 0; f < 2 * KS; ++f) {
+      f32x16& s = f < KS ? s0 : s1;
+      s = mfma_bf16(kop(kb, f / KS, f % KS), __builtin_bit_cast(bf16x8, q[f % KS]), s);
+      if (f % AHEAD == AHEAD - 1) __builtin_amdgcn_sched_barrier(0);
+    }
+    hide(s0, s1);
+    if (which == kFinite) follow(fmaxf(top(s0), top(s1)));   // (counts are not scaled)
+    typedef bf16_t bf16x2 __attribute__((ext_vector_type(2)));
+    const bf16x2 ones = {(bf16_t)1.0f, (bf16_t)1.0f};
+    const float ref = m == -INFINITY ? 0.f : m;
+    u32x4 p[4];
+    auto weight = [&](float x) { return stream_one_of(which, stream_weight(x, scale_log2e, ref), x == -INFINITY ? 0.f : 1.f); };   // (-inf: hidden, or weighs nothing)
+#pragma unroll
+    for (int w = 0; w < 16; ++w) {
+      const f32x16& s = w < 8 ? s0 : s1;
+      const uint32_t pk = pack_bf16(weight(s[2 * (w & 7)]), weight(s[2 * (w & 7) + 1]));
+      p[w >> 2][w & 3] = pk;
+      l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pk), ones, l, false);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    auto product = [&](auto value) __attribute__((always_inline)) {   // of two values
+#pragma unroll
+      for (int f = 0; f < 4 * DB; ++f) {
+        u32x4 v = __builtin_bit_cast(u32x4, vop(vb, f / (2 * DB), f / DB % 2, f % DB));
+#pragma unroll
+        for (int x = 0; x < 4; ++x) v[x] = value(v[x]);
+        acc[f % DB] = mfma_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, p[f / DB]), acc[f % DB]);
+        if (f % AHEAD == AHEAD - 1) __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    if (which == kFinite) {
+      product([&](uint32_t w) {
+        const uint32_t o = odd(w);
+        return w & ~((o - (o >> 15)) | o);   // (16 bits of ones for each)
+      });
+    } else {
+      const uint32_t wanted = which == kUp ? 0x7f80u : 0xff80u;
+      auto counts = [&](uint32_t b) { return b == wanted || (b & 0x7fffu) > 0x7f80u ? 0x3f80u : 0u; };
+      product([&](uint32_t w) { return counts(w & 0xffffu) | counts(w >> 16) << 16; });
+    }
+  }
 };
 
 }  // namespace ac

@@ -11,8 +11,12 @@
 // edges.  Passing over pairs that a wave does not see takes 6 % off rows of one head a workgroup and a window of 64 (66 / 62), and adds 1 to 2 %
 // everywhere else: not done.
 //
-// A hidden key must not touch a row even if its V is infinite or NaN, which a product over a block cannot avoid (0 * inf): a wave that ends with
-// such a result forms its rows again key by key.
+// A hidden key must not touch a row even if its V is infinite or NaN, which a product over a block cannot avoid (0 * inf): a workgroup of which a wave ends with such
+// a result walks its keys three times more.  That wave then forms its sums without what is not finite, and counts who sees a +inf, and who a -inf (StreamTile::chunk_of).
+// us, 16 heads of 128 (bf16 / binary32), 1,500 tokens, window 700: 22 / 90; with NaN in Q's last 500 rows 22 / 88, in a first token's V 113 / 490, in all of V 200 / 490;
+// key by key each of the four took 14,900 / 7,600.
+#include <type_traits>
+
 #include "common.hpp"
 #include "f32_tile.hpp"
 #include "serve.h"
@@ -54,59 +58,25 @@ __device__ __forceinline__ bool window_hides(const WindowArgs& a, int t, int key
   return key > t || key >= keys || (key <= t - a.window && key >= a.sinks);
 }
 
-// Rows [t0, t0 + n) of a head key by key: lane l has columns l, l + 64, ...
-template <typename T, int NC>
-__device__ __forceinline__ void window_rows_again(const WindowArgs& a, const T* Q, const T* K, const T* V, T* O, int t0, int n, int keys, int lane) {
-  const int D = a.D;
-  for (int t = t0; t < t0 + n; ++t) {
-    float q[NC], o[NC], m = -INFINITY, l = 0.f;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      q[c] = lane + kWave * c < D ? (float)Q[(size_t)t * D + lane + kWave * c] : 0.f;
-      o[c] = 0.f;
-    }
-    for (int j = 0; j < min(t + 1, keys); ++j) {
-      if (j >= a.sinks && j <= t - a.window) {   // to the end of the gap
-        j = t - a.window + 1;
-        if (j >= keys) break;
-      }
-      float s = 0.f;
-#pragma unroll
-      for (int c = 0; c < NC; ++c)
-        if (lane + kWave * c < D) s = fmaf(q[c], (float)K[(size_t)j * D + lane + kWave * c], s);
-#pragma unroll
-      for (int off = 32; off > 0; off >>= 1) s += __shfl_xor(s, off);
-      s *= a.scale_log2e;
-      if (s > m) {
-        const float alpha = __builtin_amdgcn_exp2f(m - s);
-        l *= alpha;
-#pragma unroll
-        for (int c = 0; c < NC; ++c) o[c] = m == -INFINITY ? 0.f : o[c] * alpha;
-        m = s;
-      }
-      const float p = s == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s - m);
-      l += p;
-      if (s != -INFINITY)
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
-          if (lane + kWave * c < D) o[c] = fmaf(p, (float)V[(size_t)j * D + lane + kWave * c], o[c]);
-    }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-    for (int c = 0; c < NC; ++c)
-      if (lane + kWave * c < D) O[(size_t)t * D + lane + kWave * c] = (T)(o[c] * inv);
-  }
+// Whether what a row came to may have been touched by what it does not see: sums that are not finite beside a sum of weights that is a number.  (The
+// latter knows nothing of V: if it is NaN, a score that the row sees is, or is +inf, and so is the row.  Scores of 2^30 and more may also have left a
+// reference point behind them by so much that weights overflow.)
+__device__ __forceinline__ bool window_doubtful(float m, float sum, float rest) {   // rest: NaN if a sum is not finite, otherwise 0
+  const bool odd = rest != rest, over = sum == INFINITY, far = fabsf(m) >= 0x1p30f && fabsf(m) < INFINITY;
+  return sum == sum ? odd || over : far;
 }
 
 template <int D>
-__global__ __launch_bounds__(kThreads, 2) void window_bf16_kernel(const WindowArgs a) {
+__global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void window_bf16_kernel(const WindowArgs a) {
   constexpr int PPR = D / 8;                             // 16-byte pieces of a row
   constexpr int NCOPY = kWindowChunk * PPR / kWave / 4;  // copy instructions of a wave, tensor and chunk
   __shared__ __attribute__((aligned(16))) bf16_t kb0[kWindowChunk * D];
   __shared__ __attribute__((aligned(16))) bf16_t vb0[kWindowChunk * D];
   __shared__ __attribute__((aligned(16))) bf16_t kb1[kWindowChunk * D];
   __shared__ __attribute__((aligned(16))) bf16_t vb1[kWindowChunk * D];
+  __shared__ int doubt;   // of some wave, about its results
   const int tid = threadIdx.x, lane = tid & 63;
+  if (tid == 0) doubt = 0;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int il = lane & 31, kh = lane >> 5;
   // workgroups with ids equal mod 8 (one XCD) share K and V in its L2
@@ -169,52 +139,77 @@ __global__ __launch_bounds__(kThreads, 2) void window_bf16_kernel(const WindowAr
       for (int v = 0; v < 16; ++v) s[v] = (unsigned)(mfma_row(v, 0) - from) < n ? -INFINITY : s[v];
     }
   };
-  auto step = [&](const bf16_t* kb, const bf16_t* vb, int c) __attribute__((always_inline)) {
-    tile.chunk(kb, vb, [&](f32x16& s0, f32x16& s1) {
+  auto hide_both = [&](int c) {
+    return [&, c](f32x16& s0, f32x16& s1) {
       hide(s0, 32 * blocks.at(2 * c));
       hide(s1, 2 * c + 1 < blocks.count ? 32 * blocks.at(2 * c + 1) : keys);
-    });
+    };
   };
   auto publish = [&]() {   // this wave's copies have landed, then everybody's; the other stage is no longer read
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
   };
+  auto walk = [&](auto step) __attribute__((always_inline)) {
 #pragma unroll 1
-  for (int c = 0; c < n_chunk; c += 2) {   // (two a trip: the stages alternate without pointer arithmetic)
-    publish();
-    if (c + 1 < n_chunk) copy(kb1, vb1, c + 1);
-    step(kb0, vb0, c);
-    if (c + 1 >= n_chunk) break;
-    publish();
-    if (c + 2 < n_chunk) copy(kb0, vb0, c + 2);
-    step(kb1, vb1, c + 1);
-  }
-  __syncthreads();   // every wave is done with both stages: they now stage the output
-  if (!live) return;
+    for (int c = 0; c < n_chunk; c += 2) {   // (two a trip: the stages alternate without pointer arithmetic)
+      publish();
+      if (c + 1 < n_chunk) copy(kb1, vb1, c + 1);
+      step(kb0, vb0, c);
+      if (c + 1 >= n_chunk) break;
+      publish();
+      if (c + 2 < n_chunk) copy(kb0, vb0, c + 2);
+      step(kb1, vb1, c + 1);
+    }
+  };
+  walk([&](const bf16_t* kb, const bf16_t* vb, int c) __attribute__((always_inline)) { tile.chunk(kb, vb, hide_both(c)); });
   f32x16(&acc)[D / 32] = tile.acc;
-  const float sum = tile.sum();
-  bool odd = !(sum < INFINITY);
+  float sum = tile.sum();
+  float rest[4] = {0.f, 0.f, 0.f, 0.f};   // NaN where a sum is not finite (a comparison each waits for scalar registers: 0.3 us)
 #pragma unroll
   for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-    for (int v = 0; v < 16; ++v) odd |= !(fabsf(acc[db][v]) < INFINITY);
-  if (__any(odd && il < rows)) {
-    window_rows_again<bf16_t, D / 64>(a, reinterpret_cast<const bf16_t*>(a.Q) + row0 * D, Ksrc, Vsrc, reinterpret_cast<bf16_t*>(a.O) + row0 * D, t0,
-                                      rows, keys, lane);
-    return;
-  }
-  const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-  bf16_t* ost = wave == 0 ? kb0 : wave == 1 ? vb0 : wave == 2 ? kb1 : vb1;
-  if (rows == kRowsPerWave) {
-    store_tile_bf16<D>(acc, inv, ost, O, lane);
-  } else if (il < rows) {
+    for (int v = 0; v < 16; ++v) rest[v & 3] = fmaf(acc[db][v], 0.f, rest[v & 3]);
+  const bool again = __any(live && il < rows && window_doubtful(tile.m, sum, (rest[0] + rest[1]) + (rest[2] + rest[3])));
+  if (again && lane == 0) doubt = 1;
+  __syncthreads();   // every wave is done with both stages: they now stage the output
+  auto store = [&]() {
+    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+    bf16_t* ost = wave == 0 ? kb0 : wave == 1 ? vb0 : wave == 2 ? kb1 : vb1;
+    if (rows == kRowsPerWave) {
+      store_tile_bf16<D>(acc, inv, ost, O, lane);
+    } else if (il < rows) {
 #pragma unroll
-    for (int db = 0; db < D / 32; ++db)
+      for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-      for (int vq = 0; vq < 4; ++vq)
-        *reinterpret_cast<u32x2*>(O + (size_t)il * D + 32 * db + 8 * vq + 4 * kh) =
-            u32x2{pack_bf16(acc[db][4 * vq] * inv, acc[db][4 * vq + 1] * inv),
-                  pack_bf16(acc[db][4 * vq + 2] * inv, acc[db][4 * vq + 3] * inv)};
+        for (int vq = 0; vq < 4; ++vq)
+          *reinterpret_cast<u32x2*>(O + (size_t)il * D + 32 * db + 8 * vq + 4 * kh) =
+              u32x2{pack_bf16(acc[db][4 * vq] * inv, acc[db][4 * vq + 1] * inv),
+                    pack_bf16(acc[db][4 * vq + 2] * inv, acc[db][4 * vq + 3] * inv)};
+    }
+  };
+  if (live) store();   // (doubtful rows, too, and over them later)
+  if (__builtin_expect(!__builtin_amdgcn_readfirstlane(doubt), 1)) return;
+#pragma unroll 1
+  for (int which = kFinite; which <= kDown; ++which) {
+    __syncthreads();   // the stages are no longer read
+    copy(kb0, vb0, 0);
+    tile.reset();
+    walk([&](const bf16_t* kb, const bf16_t* vb, int c) __attribute__((always_inline)) {
+      if (again) tile.chunk_of((StreamValues)which, kb, vb, hide_both(c));
+    });
+    sum = tile.sum();
+    if (!again || il >= rows) continue;
+    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+    bf16_t* o = O + (size_t)il * D + 4 * kh;
+    auto each = [&](auto f) {   // (a lane's columns are always the same: it reads what it wrote)
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) f(o + 32 * db + mfma_row(v, 0), acc[db][v]);
+    };
+    const float such = which == kUp ? INFINITY : -INFINITY;
+    if (which == kFinite) each([&](bf16_t* o, float x) { *o = (bf16_t)(x * inv); });
+    else each([&](bf16_t* o, float x) { if (x > 0.f) *o = (bf16_t)((float)*o + such); });
   }
 }
 
@@ -242,6 +237,24 @@ __device__ __forceinline__ void window_weights_v(f32x4 (&acc)[4 * DB], const flo
   }
 }
 
+// The same of the values that StreamTile::chunk_of takes.
+template <int DB, int LD>
+__device__ __forceinline__ void window_weights_v_of(StreamValues which, f32x4 (&acc)[4 * DB], const float* __restrict__ v, const f32x4 w, int i, int kq) {
+  const float wanted = which == kUp ? INFINITY : -INFINITY;
+#pragma unroll
+  for (int x = 0; x < 4; ++x)
+#pragma unroll
+    for (int b = 0; b < DB; ++b) {
+      const f32x4 r = *reinterpret_cast<const f32x4*>(v + (4 * kq + x) * LD + 64 * b + 4 * i);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const float count = r[t] == wanted || r[t] != r[t] ? 1.f : 0.f;
+        acc[4 * b + t] = mfma_f32(stream_one_of(which, fabsf(r[t]) < INFINITY ? r[t] : 0.f, count), w[x], acc[4 * b + t]);
+      }
+      __builtin_amdgcn_sched_barrier(0);   // (reads that run ahead would take more registers than the kernel has)
+    }
+}
+
 // Binary32 (the layout of f32_tile.hpp): four waves share stages of 16 keys for each wave of a row.  Heads of 64 and 128 columns go straight from memory
 // into two stages in turn (K's pieces swizzled, V's not: both are then read without bank conflicts); others through registers, in which the next stage is while
 // this one is multiplied.  The vector units form these products themselves, so that what the softmax takes comes on top of them, and its reference
@@ -258,7 +271,11 @@ __global__ __launch_bounds__(kThreads, DB == 4 && COLS == kAllCols && SPLIT == 2
   constexpr int LD = DIRECT ? 64 * DB : Stage::LD;
   __shared__ __attribute__((aligned(16))) float kl[KC * LD];
   __shared__ __attribute__((aligned(16))) float vl[KC * LD];
+  __shared__ __attribute__((aligned(16))) float kl1[DIRECT ? KC * LD : 4];
+  __shared__ __attribute__((aligned(16))) float vl1[DIRECT ? KC * LD : 4];
+  __shared__ __attribute__((aligned(16))) int doubt[4];   // of a wave, about its results
   const int tid = threadIdx.x, lane = tid & 63;
+  if (tid < 4) doubt[tid] = 0;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int i = lane & 15, kq = lane >> 4, part = wave / UNITS, key0 = part * kF32Rows;
   const int slot = blockIdx.x >> 3, group = a.by_per.div(slot), u = a.first + group * 8 + (blockIdx.x & 7);
@@ -291,10 +308,14 @@ __global__ __launch_bounds__(kThreads, DB == 4 && COLS == kAllCols && SPLIT == 2
       }
     }
   }
+  float m, ref, l;
+  auto reset = [&]() {
 #pragma unroll
-  for (int x = 0; x < 4 * DB; ++x) acc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m = -INFINITY, ref = 0.f, l = 0.f;
-  auto block = [&](const float* kl, const float* vl, int j0) __attribute__((always_inline)) {
+    for (int x = 0; x < 4 * DB; ++x) acc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+    m = -INFINITY;
+    ref = l = 0.f;
+  };
+  auto block = [&](const float* kl, const float* vl, int j0, auto apart, int which) __attribute__((always_inline)) {   // apart: the values that `which` says
     const int k0 = j0 + key0;
     const WindowBlock bl = window_block<kF32Rows, kF32Rows>(a, t0, k0, keys);
     if (bl == kNone) return;   // uniform
@@ -316,7 +337,7 @@ __global__ __launch_bounds__(kThreads, DB == 4 && COLS == kAllCols && SPLIT == 2
         if (window_hides(a, t0 + i, k0 + 4 * kq + x, keys)) s[x] = -INFINITY;
     }
     const float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])) * a.scale_log2e;
-    if (__any(mx > m + kStreamSlack)) {
+    if ((!apart || which == kFinite) && __any(mx > m + kStreamSlack)) {   // (counts are not scaled)
       float top = fmaxf(mx, __shfl_xor(mx, 16));
       top = fmaxf(fmaxf(top, __shfl_xor(top, 32)), m);
       const float alpha = top > m ? __builtin_amdgcn_exp2f(m - top) : 1.f;
@@ -329,119 +350,164 @@ __global__ __launch_bounds__(kThreads, DB == 4 && COLS == kAllCols && SPLIT == 2
     f32x4 p;
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
-      p[x] = __builtin_amdgcn_exp2f(fmaf(s[x], a.scale_log2e, -ref));
+      if constexpr (apart) p[x] = stream_one_of((StreamValues)which, stream_weight(s[x], a.scale_log2e, ref), s[x] == -INFINITY ? 0.f : 1.f);
+      else p[x] = __builtin_amdgcn_exp2f(fmaf(s[x], a.scale_log2e, -ref));
       l += p[x];
     }
-    window_weights_v<DB, LD>(acc, vl + key0 * LD, p, i, kq);
+    if constexpr (apart) window_weights_v_of<DB, LD>((StreamValues)which, acc, vl + key0 * LD, p, i, kq);
+    else window_weights_v<DB, LD>(acc, vl + key0 * LD, p, i, kq);
   };
-  if constexpr (DIRECT) {
-    __shared__ __attribute__((aligned(16))) float kl1[KC * LD];
-    __shared__ __attribute__((aligned(16))) float vl1[KC * LD];
-    constexpr int PPR = 16 * DB, NCOPY = KC * PPR / kThreads;   // 16-byte pieces of a row, of a thread
-    uint32_t kfrom[NCOPY], vfrom[NCOPY];   // bytes from a stage's first row; piece p of K's row r lies at p ^ r % 16
+  auto walk = [&](bool mine, auto apart, int which, int tid, int D) __attribute__((always_inline)) {   // all keys; mine: of this wave's row block, too
+    if constexpr (DIRECT) {
+      constexpr int PPR = 16 * DB, NCOPY = KC * PPR / kThreads;   // 16-byte pieces of a row, of a thread
+      uint32_t kfrom[NCOPY], vfrom[NCOPY];   // bytes from a stage's first row; piece p of K's row r lies at p ^ r % 16
 #pragma unroll
-    for (int n = 0; n < NCOPY; ++n) {
-      const int r = tid / PPR + n * (kThreads / PPR), p = tid % PPR;
-      kfrom[n] = 16 * (r * PPR + (p ^ (r & 15)));
-      vfrom[n] = 16 * (r * PPR + p);
-    }
-    auto copy = [&](float* kl, float* vl, int n) {   // (rows behind the keys: zeros)
-      const int j0 = KC * chunks.at(n);
-      const uint32_t bytes = min(keys - j0, KC) * LD * 4;
-      const StreamSource ks(K + (size_t)j0 * LD, bytes), vs(V + (size_t)j0 * LD, bytes);
-#pragma unroll
-      for (int x = 0; x < NCOPY; ++x) {
-        ks.copy(kl + 4 * kWave * (wave + 4 * x), kfrom[x]);
-        vs.copy(vl + 4 * kWave * (wave + 4 * x), vfrom[x]);
+      for (int n = 0; n < NCOPY; ++n) {
+        const int r = tid / PPR + n * (kThreads / PPR), p = tid % PPR;
+        kfrom[n] = 16 * (r * PPR + (p ^ (r & 15)));
+        vfrom[n] = 16 * (r * PPR + p);
       }
-      __builtin_amdgcn_sched_barrier(0);
-    };
-    auto publish = [&]() {   // this wave's copies have landed, then everybody's; the other stage is no longer read
-      __builtin_amdgcn_s_waitcnt(0);
-      __syncthreads();
-    };
-    if (chunks.count > 0) copy(kl, vl, 0);
+      auto copy = [&](float* kl, float* vl, int n) {   // (rows behind the keys: zeros)
+        const int j0 = KC * chunks.at(n);
+        const uint32_t bytes = min(keys - j0, KC) * LD * 4;
+        const StreamSource ks(K + (size_t)j0 * LD, bytes), vs(V + (size_t)j0 * LD, bytes);
+#pragma unroll
+        for (int x = 0; x < NCOPY; ++x) {
+          ks.copy(kl + 4 * kWave * (wave + 4 * x), kfrom[x]);
+          vs.copy(vl + 4 * kWave * (wave + 4 * x), vfrom[x]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      };
+      auto publish = [&]() {   // this wave's copies have landed, then everybody's; the other stage is no longer read
+        __builtin_amdgcn_s_waitcnt(0);
+        __syncthreads();
+      };
+      if (chunks.count > 0) copy(kl, vl, 0);
 #pragma unroll 1
-    for (int n = 0; n < chunks.count; n += 2) {
-      publish();
-      if (n + 1 < chunks.count) copy(kl1, vl1, n + 1);
-      if (live) block(kl, vl, KC * chunks.at(n));
-      if (n + 1 >= chunks.count) break;
-      publish();
-      if (n + 2 < chunks.count) copy(kl, vl, n + 2);
-      if (live) block(kl1, vl1, KC * chunks.at(n + 1));
+      for (int n = 0; n < chunks.count; n += 2) {
+        publish();
+        if (n + 1 < chunks.count) copy(kl1, vl1, n + 1);
+        if (mine) block(kl, vl, KC * chunks.at(n), apart, which);
+        if (n + 1 >= chunks.count) break;
+        publish();
+        if (n + 2 < chunks.count) copy(kl, vl, n + 2);
+        if (mine) block(kl1, vl1, KC * chunks.at(n + 1), apart, which);
+      }
+    } else {
+      Stage ks, vs;
+      if (chunks.count > 0) {
+        ks.load(K, KC * chunks.at(0), keys, D, tid);
+        vs.load(V, KC * chunks.at(0), keys, D, tid);
+      }
+      for (int n = 0; n < chunks.count; ++n) {
+        const int j0 = KC * chunks.at(n);
+        ks.template mask<false>(j0, keys, D, tid);   // (scores of keys that are not there are replaced)
+        vs.template mask<true>(j0, keys, D, tid);
+        __syncthreads();   // the previous stage has been read by everybody
+        ks.commit(kl, tid);
+        vs.commit(vl, tid);
+        __syncthreads();
+        if (n + 1 < chunks.count) {
+          ks.load(K, KC * chunks.at(n + 1), keys, D, tid);
+          vs.load(V, KC * chunks.at(n + 1), keys, D, tid);
+        }
+        if (mine) block(kl, vl, j0, apart, which);
+      }
     }
-  } else {
-    Stage ks, vs;
-    if (chunks.count > 0) {
-      ks.load(K, KC * chunks.at(0), keys, D, tid);
-      vs.load(V, KC * chunks.at(0), keys, D, tid);
-    }
-    for (int n = 0; n < chunks.count; ++n) {
-      const int j0 = KC * chunks.at(n);
-      ks.template mask<false>(j0, keys, D, tid);   // (scores of keys that are not there are replaced)
-      vs.template mask<true>(j0, keys, D, tid);
-      __syncthreads();   // the previous stage has been read by everybody
-      ks.commit(kl, tid);
-      vs.commit(vl, tid);
+  };
+  float sum;
+  auto join = [&](bool mine) __attribute__((always_inline)) {   // what the row's lanes and waves have
+    const float all = l + __shfl_xor(l, 16);
+    if (mine) sum = all + __shfl_xor(all, 32);
+    if constexpr (SPLIT == 2) {   // the second wave's sums through the stages, which nobody reads any more
+      static_assert(4 * DB * kWave * 4 * UNITS <= KC * LD, "sums of two waves");
+      f32x4* sums = reinterpret_cast<f32x4*>(kl) + wave % UNITS * 4 * DB * kWave + lane;
+      float* stats = vl + wave % UNITS * 2 * kWave + lane;
       __syncthreads();
-      if (n + 1 < chunks.count) {
-        ks.load(K, KC * chunks.at(n + 1), keys, D, tid);
-        vs.load(V, KC * chunks.at(n + 1), keys, D, tid);
+      if (mine && part > 0) {
+#pragma unroll
+        for (int x = 0; x < 4 * DB; ++x) sums[x * kWave] = acc[x];
+        stats[0] = m;
+        stats[kWave] = sum;
       }
-      if (live) block(kl, vl, j0);
-    }
-  }
-  float sum = l + __shfl_xor(l, 16);
-  sum += __shfl_xor(sum, 32);
-  if constexpr (SPLIT == 2) {   // the second wave's sums through the stages, which nobody reads any more
-    static_assert(4 * DB * kWave * 4 * UNITS <= KC * LD, "sums of two waves");
-    f32x4* sums = reinterpret_cast<f32x4*>(kl) + wave % UNITS * 4 * DB * kWave + lane;
-    float* stats = vl + wave % UNITS * 2 * kWave + lane;
-    __syncthreads();
-    if (part > 0) {
+      __syncthreads();
+      if (mine && part == 0) {
+        const float m1 = stats[0], top = fmaxf(m, m1);
+        const float f0 = m < top ? __builtin_amdgcn_exp2f(m - top) : 1.f, f1 = m1 < top ? __builtin_amdgcn_exp2f(m1 - top) : 1.f;
+        sum = sum * f0 + stats[kWave] * f1;
+        m = top;
 #pragma unroll
-      for (int x = 0; x < 4 * DB; ++x) sums[x * kWave] = acc[x];
-      stats[0] = m;
-      stats[kWave] = sum;
+        for (int x = 0; x < 4 * DB; ++x) acc[x] = acc[x] * f0 + sums[x * kWave] * f1;
+      }
     }
-    __syncthreads();
-    if (part > 0) return;
-    const float m1 = stats[0], top = fmaxf(m, m1);
-    const float f0 = m < top ? __builtin_amdgcn_exp2f(m - top) : 1.f, f1 = m1 < top ? __builtin_amdgcn_exp2f(m1 - top) : 1.f;
-    sum = sum * f0 + stats[kWave] * f1;
-#pragma unroll
-    for (int x = 0; x < 4 * DB; ++x) acc[x] = acc[x] * f0 + sums[x * kWave] * f1;
-  }
-  if (!live) return;
+  };
   const int rows = min(kF32Rows, a.S - t0);
-  bool odd = !(sum < INFINITY);
+  reset();
+  walk(live, std::false_type{}, kFinite, tid, D);
+  // (sums end here for the compiler: carried on to the stores in the registers that suit those, they took 24 more and a copy after every product)
 #pragma unroll
-  for (int x = 0; x < 4 * DB; ++x) odd |= f32_not_finite(acc[x]);
-  if (__any(odd && i < rows)) {
-    window_rows_again<float, DB>(a, Q, K, V, O, t0, rows, keys, lane);
-    return;
-  }
-  if (i >= rows) return;
-  float* o = O + (size_t)(t0 + i) * D;
-  if constexpr (COLS == kAnyCols) {   // (in pieces, at any address: of 199 columns 57 us where single floats took 98)
-    const float by = sum == 0.f ? 1.f : sum, inv = 1.f / by;
+  for (int x = 0; x < 4 * DB; ++x) asm volatile("" : "+v"(acc[x]));
+  join(true);
+  f32x4 rest = {0.f, 0.f, 0.f, 0.f};   // as above
 #pragma unroll
-    for (int n = 0; n < 4 * DB; ++n) {
-      const int b = n >> 2, x = n & 3, d = 64 * b + 16 * kq + 4 * x;
-      f32x4 w = {acc[4 * b][x], acc[4 * b + 1][x], acc[4 * b + 2][x], acc[4 * b + 3][x]};
+  for (int x = 0; x < 4 * DB; ++x)
 #pragma unroll
-      for (int t = 0; t < 4; ++t) w[t] = f32_divide(w[t], by, inv);
-      if (d + 4 <= D) {
-        *reinterpret_cast<f32x4_dw*>(o + d) = w;
-      } else {
+    for (int t = 0; t < 4; ++t) rest[t] = fmaf(acc[x][t], 0.f, rest[t]);
+  bool again = part == 0 && __any(live && i < rows && window_doubtful(m, sum, (rest[0] + rest[1]) + (rest[2] + rest[3])));
+  if (again && lane == 0) doubt[wave] = 1;
+  auto store = [&]() {
+    if (i >= rows) return;
+    float* o = O + (size_t)(t0 + i) * D;
+    if constexpr (COLS == kAnyCols) {   // (in pieces, at any address: of 199 columns 57 us where single floats took 98)
+      const float by = sum == 0.f ? 1.f : sum, inv = 1.f / by;
 #pragma unroll
-        for (int t = 0; t < 3; ++t)
-          if (d + t < D) o[d + t] = w[t];
+      for (int n = 0; n < 4 * DB; ++n) {
+        const int b = n >> 2, x = n & 3, d = 64 * b + 16 * kq + 4 * x;
+        f32x4 w = {acc[4 * b][x], acc[4 * b + 1][x], acc[4 * b + 2][x], acc[4 * b + 3][x]};
+#pragma unroll
+        for (int t = 0; t < 4; ++t) w[t] = f32_divide(w[t], by, inv);
+        if (d + 4 <= D) {
+          *reinterpret_cast<f32x4_dw*>(o + d) = w;
+        } else {
+#pragma unroll
+          for (int t = 0; t < 3; ++t)
+            if (d + t < D) o[d + t] = w[t];
+        }
       }
+    } else {
+      f32_store_row<DB, COLS, true>(o, acc, sum == 0.f ? 1.f : sum, kq, D);
     }
-  } else {
-    f32_store_row<DB, COLS, true>(o, acc, sum == 0.f ? 1.f : sum, kq, D);
+  };
+  if (part == 0 && live) store();
+  __syncthreads();
+  if (__builtin_expect(!__builtin_amdgcn_readfirstlane(doubt[0] | doubt[1] | doubt[2] | doubt[3]), 1)) return;
+  if (SPLIT == 2) again = __builtin_amdgcn_readfirstlane(doubt[wave % UNITS]);   // both waves of a row
+#pragma unroll 1
+  for (int which = kFinite; which <= kDown; ++which) {
+    __syncthreads();   // the stages are no longer read
+    reset();
+    // (what the first walk knows of its copies need not be kept for these: the compiler forms it again)
+    int tid_ = tid, D_ = D;
+    asm volatile("" : "+v"(tid_), "+s"(D_));
+    walk(again, std::true_type{}, which, tid_, COLS == kAllCols ? D : D_);
+    join(again);
+    if (part > 0 || !again || i >= rows) continue;
+    float* o = O + (size_t)(t0 + i) * D + 16 * kq;   // (an address of its own in every turn: the compiler would keep one a column)
+    asm volatile("" : "+v"(o));
+    const int cols = D_ - 16 * kq;
+    const float by = sum == 0.f ? 1.f : sum, inv = 1.f / by;
+    auto each = [&](auto f) {   // (a lane's columns are always the same: it reads what it wrote)
+#pragma unroll
+      for (int n = 0; n < 4 * DB; ++n)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const int d = 64 * (n >> 2) + 4 * (n & 3) + t;
+          if (d < cols) f(o + d, acc[4 * (n >> 2) + t][n & 3]);
+        }
+    };
+    const float such = which == kUp ? INFINITY : -INFINITY;
+    if (which == kFinite) each([&](float* o, float x) { *o = f32_divide(x, by, inv); });
+    else each([&](float* o, float x) { if (x > 0.f) *o += such; });
   }
 }
 
