@@ -21,7 +21,8 @@ struct StreamSource {
 };
 
 enum StreamValues { kFinite, kUp, kDown };   // of chunk_of
-// 2^(score - ref).  A reference point of 2^30 and more may be off by more than 2^6 from the score that it was rounded from: its rows subtract rounded scores.
+// 2^(score - ref).  A reference point of 2^30 and more may be off by more than 2^6 from the score that it was rounded from, and a weight formed from both then by as
+// many powers of two, up to an infinity or nothing at all: its rows subtract rounded scores.
 __device__ __forceinline__ float stream_weight(float s, float scale_log2e, float ref) {
 #pragma clang fp contract(off)
   const float scaled = s * scale_log2e;

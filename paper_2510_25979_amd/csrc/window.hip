@@ -59,11 +59,10 @@ __device__ __forceinline__ bool window_hides(const WindowArgs& a, int t, int key
 }
 
 // Whether what a row came to may have been touched by what it does not see: sums that are not finite beside a sum of weights that is a number.  (The
-// latter knows nothing of V: if it is NaN, a score that the row sees is, or is +inf, and so is the row.  Scores of 2^30 and more may also have left a
-// reference point behind them by so much that weights overflow.)
+// latter knows nothing of V: if it is NaN, a score that the row sees is, or is +inf, and so is the row.)  Or its scores are of 2^30 and more: stream_weight.
 __device__ __forceinline__ bool window_doubtful(float m, float sum, float rest) {   // rest: NaN if a sum is not finite, otherwise 0
-  const bool odd = rest != rest, over = sum == INFINITY, far = fabsf(m) >= 0x1p30f && fabsf(m) < INFINITY;
-  return sum == sum ? odd || over : far;
+  const bool odd = rest != rest && sum == sum, far = fabsf(m) >= 0x1p30f && fabsf(m) < INFINITY;
+  return odd || far;
 }
 
 template <int D>
