@@ -709,8 +709,10 @@ int32_t attncache_page_fork(const int32_t *from, const int32_t *seq_len,
  * requests and 255 groups, otherwise three, the first of which is one workgroup
  * that looks through the requests, 1,024 a step.  Without groups, where max_pages
  * * page_size is at most 128, and where K and V of B times as many tokens are at
- * most 64 MiB, the launches of attention_paged, and each request's own row of the
- * table is followed.
+ * most 64 MiB, each request is looked at by itself, as attention_paged does, and
+ * its own row of the table is followed: by the launches of attention_paged, or,
+ * where thousands of requests and heads have little each, by one launch that
+ * gives each of them to a wave.
  * Deterministic.
  */
 size_t attention_paged_shared_workspace_bytes(int32_t B, int32_t Hq,

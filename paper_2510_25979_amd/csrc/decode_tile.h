@@ -590,6 +590,7 @@ __device__ __forceinline__ void decode_run(const DecodeArgs& a) {
 // A wave per unit, where units are many and small: four of them start with one workgroup, and nothing is added up.  us, four waves a unit / one, bf16 heads of
 // 64: 2,048 units of 12 keys 8.1 / 4.9, of 64 11.7 / 9.0, of 128 15.5 / 13.5, of 254 30.2 / 29.3; 8,192 of 12 24.1 / 10.3; 1,536 of 128 13.0 / 12.3 (of 128
 // columns 21.7 / 23.1); 512 of 12 4.3 / 3.7, of 64 5.2 / 6.0; binary32 of 128: 2,048 of 12 16.2 / 11.2, of 64 33.7 / 31.5; of 100 22.6 / 11.1, 37.2 / 27.8.
+// (attention_paged and attention_cross go without: a wave's order of sums is another than a workgroup's, and their results are to stay what they were.)
 template <class Core>
 inline bool decode_by_wave(const DecodeArgs& a) {
   const int64_t units = (int64_t)a.B * a.Hkv * a.rbs;
