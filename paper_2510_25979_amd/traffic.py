@@ -5,9 +5,9 @@ through HBM as read from two ``rocprofv3 --pmc`` runs (``FETCH_SIZE``, then ``WR
 per dispatch), each scaled by what the same counter reads for a plain device copy of 2^30 bytes
 issued by ``bench.py --copy-probe`` in the same run.  Every entry carries the revision of the
 kernel source it was measured on (a hash of the ``.hip`` file that defines the kernel and of
-the shared headers); ``lookup`` returns nothing for an entry of another revision, so a changed
-kernel never inherits an old reading, and a change to another kernel's file does not discard
-this one's.
+the headers that it includes); ``lookup`` returns nothing for an entry of another revision, so a
+changed kernel never inherits an old reading, and a change to a file that it does not include
+does not discard its own.
 
 Regenerate (from the repo root, on a GPU box; ``cd /tmp && export TMPDIR=/tmp`` first)::
 
@@ -34,6 +34,7 @@ import glob
 import hashlib
 import json
 import os
+import re
 import statistics
 from typing import Optional
 
@@ -53,15 +54,22 @@ def source_file(kernel: str) -> str:
     return name
 
 
+def sources_of(kernel: str) -> list:
+    """The kernel's source file and every header of csrc/ that it includes, itself or through others."""
+    csrc, names = os.path.join(HERE, "csrc"), [source_file(kernel)]
+    for name in names:      # (grows)
+        text = open(os.path.join(csrc, name)).read()
+        names += [n for n in dict.fromkeys(re.findall(r'^[ \t]*#[ \t]*include[ \t]*"([^"]+)"', text, re.M))
+                  if n not in names and os.path.exists(os.path.join(csrc, n))]
+    return names[:1] + sorted(names[1:])
+
+
 def source_revision(kernel: str) -> str:
-    """Hash of the kernel's source file and of the shared headers: the revision a reading of
-    that kernel belongs to."""
+    """Hash of those files: the revision a reading of that kernel belongs to."""
     h = hashlib.sha256()
-    csrc = os.path.join(HERE, "csrc")
-    names = [source_file(kernel)] + sorted(n for n in os.listdir(csrc) if n.endswith(".hpp"))
-    for name in names:
+    for name in sources_of(kernel):
         h.update(name.encode())
-        h.update(open(os.path.join(csrc, name), "rb").read())
+        h.update(open(os.path.join(HERE, "csrc", name), "rb").read())
     return h.hexdigest()[:16]
 
 
