@@ -27,7 +27,7 @@ __device__ __forceinline__ f32x4 mfma_f32(float a, float b, f32x4 c) {
 // What is known of the head dimension when a kernel is compiled.  With all forms in one kernel every piece
 // of a row was a load behind tests of its own (16 x 24 heads on 8 K and V, 94 x 128 causal: 24.0 us exact, 21.7 so;
 // 16 x 8 heads of 333 x 128 61 / 54).  Rows of any length in single floats behind tests took, exact / reuse, 35.0 / 26.8 us at
-// 333 x 33 and 144 / 89 at 333 x 199; in pieces of four that may overlap 31.9 / 21.5 and 128 / 77.
+// 333 x 33 and 144 / 89 at 333 x 199; in pieces of four that may overlap 31.9 / 21.5 and 128 / 77, with results stored in pieces, too, 32.1 / 19.1 and 105 / 51.
 enum F32Cols {
   kAnyCols = 0,   // any D >= 4: rows may start at any 4-byte address
   kVecCols = 1,   // D % 4 == 0: whole 16-byte pieces
@@ -107,10 +107,9 @@ struct F32Stage {
 
 // acc += W V for one 16-key block: `v` is the block's first row in LDS, w[x] the lane's weight of
 // key 4 kq + x (zero where the key is hidden from its row).
-template <int DB>
+template <int DB, int LD = F32Stage<DB, 64, kAllCols>::LD>   // LD: floats from row to row
 __device__ __forceinline__ void f32_weights_v(f32x4 (&acc)[4 * DB], const float* __restrict__ v,
                                               const f32x4 w, int i, int kq) {
-  constexpr int LD = F32Stage<DB, 64, kAllCols>::LD;
   struct Rows { f32x4 b[DB]; };   // this lane's part of key 4 kq + x
   auto read = [&](int x) {
     Rows r;
@@ -183,6 +182,8 @@ __device__ __forceinline__ void f32_store_row(float* __restrict__ o, const f32x4
         for (int t = 0; t < 4; ++t) w[t] = f32_divide(w[t], by, inv);
       if constexpr (COLS == kVecCols || COLS == kAllCols) {
         if (COLS == kAllCols || d < D) *reinterpret_cast<f32x4*>(o + d) = w;
+      } else if (COLS == kAnyCols && d + 4 <= D) {   // (at any address)
+        *reinterpret_cast<f32x4_dw*>(o + d) = w;
       } else {
 #pragma unroll
         for (int t = 0; t < 4; ++t)

@@ -212,31 +212,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void window_bf16_kernel(
   }
 }
 
-// acc += W V for a block of 16 keys whose rows lie LD floats apart, as f32_weights_v.
-template <int DB, int LD>
-__device__ __forceinline__ void window_weights_v(f32x4 (&acc)[4 * DB], const float* __restrict__ v, const f32x4 w, int i, int kq) {
-  struct Rows { f32x4 b[DB]; };   // this lane's part of key 4 kq + x
-  auto read = [&](int x) {
-    Rows r;
-#pragma unroll
-    for (int b = 0; b < DB; ++b) r.b[b] = *reinterpret_cast<const f32x4*>(v + (4 * kq + x) * LD + 64 * b + 4 * i);
-    return r;
-  };
-  Rows now = read(0);
-#pragma unroll
-  for (int x = 0; x < 4; ++x) {
-    Rows next = now;
-    if (x < 3) next = read(x + 1);
-#pragma unroll
-    for (int b = 0; b < DB; ++b)
-#pragma unroll
-      for (int t = 0; t < 4; ++t) acc[4 * b + t] = mfma_f32(now.b[b][t], w[x], acc[4 * b + t]);
-    now = next;
-    __builtin_amdgcn_sched_barrier(0);
-  }
-}
-
-// The same of the values that StreamTile::chunk_of takes.
+// f32_weights_v of the values that StreamTile::chunk_of takes.
 template <int DB, int LD>
 __device__ __forceinline__ void window_weights_v_of(StreamValues which, f32x4 (&acc)[4 * DB], const float* __restrict__ v, const f32x4 w, int i, int kq) {
   const float wanted = which == kUp ? INFINITY : -INFINITY;
@@ -354,7 +330,7 @@ __global__ __launch_bounds__(kThreads, DB == 4 && COLS == kAllCols && SPLIT == 2
       l += p[x];
     }
     if constexpr (apart) window_weights_v_of<DB, LD>((StreamValues)which, acc, vl + key0 * LD, p, i, kq);
-    else window_weights_v<DB, LD>(acc, vl + key0 * LD, p, i, kq);
+    else f32_weights_v<DB, LD>(acc, vl + key0 * LD, p, i, kq);
   };
   auto walk = [&](bool mine, auto apart, int which, int tid, int D) __attribute__((always_inline)) {   // all keys; mine: of this wave's row block, too
     if constexpr (DIRECT) {
@@ -454,30 +430,7 @@ __global__ __launch_bounds__(kThreads, DB == 4 && COLS == kAllCols && SPLIT == 2
     for (int t = 0; t < 4; ++t) rest[t] = fmaf(acc[x][t], 0.f, rest[t]);
   bool again = part == 0 && __any(live && i < rows && window_doubtful(m, sum, (rest[0] + rest[1]) + (rest[2] + rest[3])));
   if (again && lane == 0) doubt[wave] = 1;
-  auto store = [&]() {
-    if (i >= rows) return;
-    float* o = O + (size_t)(t0 + i) * D;
-    if constexpr (COLS == kAnyCols) {   // (in pieces, at any address: of 199 columns 57 us where single floats took 98)
-      const float by = sum == 0.f ? 1.f : sum, inv = 1.f / by;
-#pragma unroll
-      for (int n = 0; n < 4 * DB; ++n) {
-        const int b = n >> 2, x = n & 3, d = 64 * b + 16 * kq + 4 * x;
-        f32x4 w = {acc[4 * b][x], acc[4 * b + 1][x], acc[4 * b + 2][x], acc[4 * b + 3][x]};
-#pragma unroll
-        for (int t = 0; t < 4; ++t) w[t] = f32_divide(w[t], by, inv);
-        if (d + 4 <= D) {
-          *reinterpret_cast<f32x4_dw*>(o + d) = w;
-        } else {
-#pragma unroll
-          for (int t = 0; t < 3; ++t)
-            if (d + t < D) o[d + t] = w[t];
-        }
-      }
-    } else {
-      f32_store_row<DB, COLS, true>(o, acc, sum == 0.f ? 1.f : sum, kq, D);
-    }
-  };
-  if (part == 0 && live) store();
+  if (part == 0 && live && i < rows) f32_store_row<DB, COLS, true>(O + (size_t)(t0 + i) * D, acc, sum == 0.f ? 1.f : sum, kq, D);
   __syncthreads();
   if (__builtin_expect(!__builtin_amdgcn_readfirstlane(doubt[0] | doubt[1] | doubt[2] | doubt[3]), 1)) return;
   if (SPLIT == 2) again = __builtin_amdgcn_readfirstlane(doubt[wave % UNITS]);   // both waves of a row
