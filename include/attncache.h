@@ -655,6 +655,13 @@ int32_t attncache_rotary_frequencies(double *freq, int32_t rot, double base,
  * nothing.  Pages that some row held and none holds afterwards go behind the
  * ring's last one, in order of their number, for the next call.
  *
+ * Where the ring may run out, a call before, with from[b] = b for each row that
+ * some row will come from and -1 for the others, gives back what nobody goes on
+ * with; it takes no page.  Or give the call outputs of its own: it then leaves
+ * the tables, lengths and states that it reads, the ring's entries in use and
+ * the pages that rows hold as they were, so that a caller who finds a -1 can go
+ * on from them in another way.
+ *
  * All rows of the cache belong into one call: a page that a row outside it
  * holds would be given back.  attncache_page_plan goes on from the result (a
  * page it writes to is one row's), but does not know about sharing: rows that
