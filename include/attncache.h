@@ -744,7 +744,10 @@ int32_t attention_paged_shared(const void *Q, const void *k_pages,
  *              (AC_BF16: D 64 or 128; AC_F32: D <= 256), any S.
  *   row_sel    NULL or DEVICE [B] int32: items with row_sel[b] >= 0 are
  *              skipped and their rows of O not written (attncache_search's
- *              hits: only misses are computed).
+ *              hits: only misses are computed.  The maps that hits reuse have
+ *              to be of the same window; attncache_insert forms maps of causal
+ *              or full attention, which serve a layer with a window only where
+ *              this covers all S tokens).
  *   key_len    NULL or DEVICE [B] int32: tokens of item b that are real,
  *              clamped to [0, S]; the other keys are hidden and may hold
  *              anything.  Rows of padding are computed by the same rule; those
