@@ -4,7 +4,8 @@
 //   (a, b) -> amp (a cos t - b sin t, b cos t + a sin t)    of its first `rot` columns in pairs, t = position * freq[pair]
 //
 // Bound by memory: every element is read once from HBM and written once (K and V twice where they go to the cache, too): 32 prompts of up to 1,024 tokens,
-// 48 heads of 64 (232 MB) 50 to 57 us = 4.1 to 4.7 TB/s, 4,000 tokens of 48 heads of 128 25.  A workgroup takes a few tokens and some or all of their heads.  It forms
+// 48 heads of 64 (232 MB) 57 us = 4.1 TB/s on new inputs each time (38 where the same ones lie in the last-level cache), 4,000 tokens of 48 heads of 128 19.5.
+// A workgroup takes a few tokens and some or all of their heads.  It forms
 // the sines and cosines of its tokens once, through LDS; the other half of a pair that is not in a lane's own piece is loaded a second time (from L1).
 // Few tokens are bound by latency, position -> angle -> store, 128 of one token each 5.2 us.
 //
@@ -48,8 +49,8 @@ struct RotatePiece {
 };
 
 // G lanes a row, NP pieces a lane: a wave has 64 / G tokens, and a lane keeps its token and its columns, so that addresses, sines, cosines and weights are the
-// lane's for all heads, of which the wave takes every fourth, U at a time.  (With heads dealt to threads and tables of tokens in LDS the vector work of
-// addresses took longer than the memory: 59 us and 87 where it is 50 and 25 now.)
+// lane's for all heads, of which the wave takes every fourth, U at a time.  (us, heads dealt to threads and tables of tokens in LDS / so: those prompts
+// 58.2 / 57.2, from the cache 44 / 38, normalised 145 / 58; 4,000 tokens of 128 23.1 / 19.5; single tokens of 128 requests 6.2 / 5.1.)
 // ODD: pairs lie apart and no whole pieces, so that their other halves are loaded one by one (of few columns, in most such models: 40 heads of 128 of which
 // 20 columns turn, 2,400 tokens, 25 us; 38 with all columns one by one, 16 where pieces are whole).
 template <typename T, int VEC, int G, int NP, int U, bool NORM, bool ODD>
