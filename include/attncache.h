@@ -512,7 +512,8 @@ int32_t attncache_page_append(const void *K, const void *V,
  *              the lengths.  Calls that may overlap in time need one each.
  *
  * fp32 statistics and sums; bf16 weights are rounded once before the product
- * with V and the result once.  One launch, or two; deterministic.
+ * with V and the result once; scores (scale * Q K^T) up to 2^30 in size, rows
+ * with larger ones may be lost.  One launch, or two; deterministic.
  * B * Hkv * ceil(Hq / Hkv / 16) * (ceil(max_pages * page_size / 16) + 2) and
  * B * Hq below 2^31 - 65536.  Where the tables are wide, the lengths are looked
  * through by all workgroups: 16,384 requests of 16 tokens on one head take some
@@ -756,11 +757,12 @@ int32_t attention_paged_shared(const void *Q, const void *k_pages,
  *   sinks      0 or more.
  *   scale      0 selects 1/sqrt(D).
  *
- * Arithmetic as in attention_paged.  Keys that are hidden from a row do not
- * touch it, whatever K and V hold there: workgroups whose blocks of keys hold
- * an infinity or a NaN of V walk their keys four times, which takes up to ten
- * times as long; in Q or K they cost nothing.  Hq / Hkv * S <= 2^24, also with
- * S rounded up to a multiple of 16; B * Hkv <= 2^28, B * Hq below 2^31.
+ * Arithmetic as in attention_paged, at scores of any size.  Keys that are hidden
+ * from a row do not touch it, whatever K and V hold there: workgroups whose
+ * blocks of keys hold an infinity or a NaN of V walk their keys four times,
+ * which takes up to ten times as long; in Q or K they cost nothing.
+ * Hq / Hkv * S <= 2^24, also with S rounded up to a multiple of 16;
+ * B * Hkv <= 2^28, B * Hq below 2^31.
  */
 int32_t attention_window(const void *Q, const void *K, const void *V, void *O,
                          const int32_t *row_sel, const int32_t *key_len,
